@@ -363,6 +363,212 @@ size_t fff_backward_workspace_bytes(int64_t n_tokens, int32_t depth, int32_t n_t
 /* fff_describe for a stack. */
 int fff_describe_stack(const fff_args* a, const fff_layer* layers, int32_t n_layers, char* buf, size_t len);
 
+/* ---------------------------------------------------------------------------
+ * Operators around the layer: what a transformer block needs next to the FFF
+ * forward and backward to be trained (LayerNorm with its gradients, dropout)
+ * and to have dense networks at the leaves of a routing tree (the tokens of
+ * every leaf grouped, the leaves' matrix products and their gradients).  The
+ * conventions above hold: contiguous row-major device buffers, 16-byte aligned
+ * bases (index and statistics arrays 4-byte aligned), fp32 arithmetic, all
+ * checks before any HIP call, work enqueued on hip_stream.  Outputs overlap no
+ * input and no other output unless stated.  Zero tokens or entries are allowed.
+ * ------------------------------------------------------------------------- */
+
+/* Dropout of element (row, col) of an [n_tokens, hidden] matrix:
+ *   drop(v) = v / (1 - p) where r >= floor(p 2^32), else 0 (whatever v is),
+ *   r = word col % 4 of Philox4x32-10 (Salmon, Moraes, Dror and Shaw, "Parallel
+ *       random numbers: as easy as 1, 2, 3", 2011) with key `seed` (low word
+ *       first) and counter (col / 4, row, offset low, offset high).
+ * The mask is never stored: the backward draws it again from the same seed and
+ * offset.  Calls with one seed need different offsets to draw different masks.
+ * rng_offset, when set, points to a device int64 (8-byte aligned) that is read
+ * when the work runs and added to offset, so that the replays of a captured
+ * graph can draw new masks.  0 <= p < 1; p = 0 drops nothing and reads no
+ * generator. */
+typedef struct {
+    double p;
+    uint64_t seed;
+    uint64_t offset;
+    const int64_t* rng_offset; /* device, or NULL */
+} fff_dropout_rng;
+
+/*
+ * fff_layer_norm -- s = residual + drop(x) (either part optional), then
+ *   y = (s - mean(s)) / sqrt(var(s) + eps) * gamma + beta
+ * per row, with the biased variance over the hidden dimension: the step
+ * between two pre-norm blocks in one pass.  y, mean and rstd come from the
+ * fp32 s, before it is rounded to s_dtype for the stream.  Any hidden >= 1;
+ * n_tokens < 2^32.
+ */
+typedef struct {
+    const void* x;         /* [n_tokens, hidden] (x_dtype) */
+    const void* residual;  /* [n_tokens, hidden] (s_dtype), or NULL */
+    const float* gamma;    /* [hidden], or NULL for ones */
+    const float* beta;     /* [hidden], or NULL for zeros */
+    void* y;               /* [n_tokens, hidden] (y_dtype) */
+    void* s;               /* [n_tokens, hidden] (s_dtype), or NULL; may be the buffer residual */
+    float* mean;           /* [n_tokens], or NULL */
+    float* rstd;           /* [n_tokens] 1 / sqrt(var + eps), or NULL */
+    int64_t n_tokens;
+    int32_t hidden;
+    int32_t x_dtype, s_dtype, y_dtype; /* fff_dtype */
+    float eps;             /* >= 0 and finite */
+    fff_dropout_rng drop;
+    void* hip_stream;
+} fff_layer_norm_args;
+
+int fff_layer_norm(const fff_layer_norm_args* a);
+
+/*
+ * fff_layer_norm_backward -- with xh = (s - mean) rstd and g = dy gamma,
+ *   ds     = rstd (g - mean(g) - xh mean(g xh)) + ds_in
+ *   dx     = drop(ds), the gradient of the branch that went through dropout
+ *   dgamma = sum over rows of dy xh,   dbeta = sum over rows of dy
+ * where ds_in is the gradient that reaches s past the norm (the residual
+ * stream's).  ds is also the gradient of residual.  dx is formed from the fp32
+ * ds.  The sums over rows run in a fixed order: the same bits on every run.
+ */
+typedef struct {
+    const void* dy;        /* [n_tokens, hidden] (y_dtype) */
+    const void* s;         /* [n_tokens, hidden] (s_dtype): the forward's s, or its x if it had neither part */
+    const float* mean;     /* [n_tokens], from the forward */
+    const float* rstd;
+    const float* gamma;    /* [hidden], or NULL for ones */
+    const void* ds_in;     /* [n_tokens, hidden] (s_dtype), or NULL */
+    void* ds;              /* [n_tokens, hidden] (s_dtype), or NULL to skip; may be the buffer ds_in */
+    void* dx;              /* [n_tokens, hidden] (x_dtype), or NULL to skip */
+    float* dgamma;         /* [hidden], or NULL to skip */
+    float* dbeta;          /* [hidden], or NULL to skip */
+    int64_t n_tokens;
+    int32_t hidden;
+    int32_t x_dtype, s_dtype, y_dtype;
+    int32_t accumulate;    /* 0: dgamma and dbeta overwritten; 1: added to */
+    fff_dropout_rng drop;  /* the forward's */
+    void* workspace;       /* with dgamma or dbeta: device scratch of the size below, 256-byte aligned */
+    size_t workspace_bytes;
+    void* hip_stream;
+} fff_layer_norm_backward_args;
+
+int fff_layer_norm_backward(const fff_layer_norm_backward_args* a);
+
+/* Scratch of fff_layer_norm_backward: partial sums of dgamma and dbeta.  0 for invalid shapes. */
+size_t fff_layer_norm_backward_workspace_bytes(int64_t n_tokens, int32_t hidden);
+
+/* fff_dropout -- y = residual + drop(x) (residual optional).  The gradient of x is the same call
+ * on dy without a residual.  y may be the buffer x or residual when the types agree.  n_tokens < 2^32. */
+typedef struct {
+    const void* x;         /* [n_tokens, hidden] (x_dtype) */
+    const void* residual;  /* [n_tokens, hidden] (r_dtype), or NULL */
+    void* y;               /* [n_tokens, hidden] (y_dtype) */
+    int64_t n_tokens;
+    int32_t hidden;
+    int32_t x_dtype, r_dtype, y_dtype;
+    fff_dropout_rng drop;
+    void* hip_stream;
+} fff_dropout_args;
+
+int fff_dropout(const fff_dropout_args* a);
+
+/*
+ * fff_group_rows -- a stable counting sort of entries by group: which rows go
+ * to which leaf expert.  Entry e (of n_entries = tokens x trees, tree fastest)
+ * belongs to group (e % n_trees) n_ids + ids[e] - first.  Written: offsets
+ * [n_trees n_ids + 1], where group g's entries stand, and order, the entry
+ * indices group by group, in entry order within a group.  Entries whose id is
+ * outside [first, first + n_ids) are in no group: they are counted in bad_ids
+ * and the tail of order behind offsets' last value is left as it was.  With
+ * the forward's nodes_out[..., depth] as ids, first = 2^depth - 1 and
+ * n_ids = 2^depth.  n_entries < 2^31; at most FFF_MAX_GROUPS groups
+ * (FFF_ERR_UNSUPPORTED above).
+ */
+#define FFF_MAX_GROUPS 32768
+typedef struct {
+    const int32_t* ids;    /* [n_entries] */
+    int32_t* order;        /* [n_entries] */
+    int32_t* offsets;      /* [n_trees n_ids + 1] */
+    int32_t* bad_ids;      /* optional device int32, incremented once per entry without a group */
+    int64_t n_entries;
+    int32_t n_ids, n_trees, first;
+    void* workspace;       /* device scratch of the size below, 256-byte aligned */
+    size_t workspace_bytes;
+    void* hip_stream;
+} fff_group_rows_args;
+
+int fff_group_rows(const fff_group_rows_args* a);
+
+/* Scratch of fff_group_rows: entries per (chunk, group).  0 for invalid shapes. */
+size_t fff_group_rows_workspace_bytes(int64_t n_entries, int32_t n_ids, int32_t n_trees);
+
+/*
+ * fff_grouped_matmul -- every entry's row times its group's matrix:
+ *   z_i = x_src(i) W_g^T  (W_g [n, k]), or with w_transposed  z_i = x_src(i) W_g  (W_g [k, n]),
+ * for the entries i in [offsets[g], offsets[g+1]) of each group g, with
+ * src(i) = x_index[i] / x_div (i / x_div without x_index); then
+ *   y_dst(i) = act(z_i), z_i itself kept in z_out when set, or
+ *   y_dst(i) = z_i act'(z_in_i) when z_in is set (a data gradient through the
+ *              activation: x is dL/dy, W the forward's matrix read transposed),
+ * with dst(i) = y_index[i], or i.  x_index with x_div = n_trees takes
+ * fff_group_rows' order straight to the tokens' rows; y_index puts results
+ * back in entry order (its values must differ from each other).  z rows are in
+ * grouped order.  Rows of y and z that no entry names are left as they were.
+ * Bad device values stay in bounds: offsets are clamped to [0, n_entries] and
+ * taken as empty where they fall, an x_index outside x reads a row of zeros,
+ * and a y_index outside y stores nothing.  x and W are both bf16 (MFMA on
+ * bf16, fp32 sums) or both fp32; anything else is FFF_ERR_UNSUPPORTED.  Any
+ * k >= 1 and n >= 1.
+ */
+typedef struct {
+    const void* x;          /* [x_rows, k] (x_dtype) */
+    const void* w;          /* [n_groups, n, k], or [n_groups, k, n] with w_transposed (w_dtype) */
+    const int32_t* offsets; /* [n_groups + 1] */
+    const int32_t* x_index; /* [n_entries], or NULL */
+    const int32_t* y_index; /* [n_entries], or NULL */
+    void* y;                /* [y_rows, n] (y_dtype) */
+    void* z_out;            /* [n_entries, n] (z_dtype), or NULL */
+    const void* z_in;       /* [n_entries, n] (z_dtype), or NULL; not with z_out */
+    int64_t n_entries, x_rows, y_rows; /* below 2^31; without an index at least n_entries rows */
+    int32_t n_groups, k, n;
+    int32_t x_div;          /* >= 1 */
+    int32_t w_transposed;
+    int32_t x_dtype, w_dtype, y_dtype, z_dtype;
+    int32_t act;            /* fff_act */
+    void* hip_stream;
+} fff_grouped_matmul_args;
+
+int fff_grouped_matmul(const fff_grouped_matmul_args* a);
+
+/*
+ * fff_grouped_weight_grad -- dW_g = sum over the entries i of group g of
+ *   dy_dst(i)^T x_src(i),   [n, k] per group, fp32,
+ * the gradient of fff_grouped_matmul's W (with w_transposed: swap dy and x).
+ * dst(i) = dy_index[i], or i; src(i) as above.  Groups
+ * without entries get zeros (with accumulate: stay).  Offsets and indices out
+ * of range as above.  dy and x are both bf16 or both fp32.  The sums run in a
+ * fixed order: the same bits on every run.
+ */
+typedef struct {
+    const void* dy;          /* [dy_rows, n] (dtype) */
+    const void* x;           /* [x_rows, k] (dtype) */
+    const int32_t* offsets;  /* [n_groups + 1] */
+    const int32_t* dy_index; /* [n_entries], or NULL */
+    const int32_t* x_index;  /* [n_entries], or NULL */
+    float* dw;               /* [n_groups, n, k] */
+    int64_t n_entries, dy_rows, x_rows;
+    int32_t n_groups, k, n;
+    int32_t x_div;
+    int32_t dy_dtype, x_dtype;
+    int32_t accumulate;      /* 0: dw overwritten; 1: added to */
+    void* workspace;         /* device scratch of the size below, 256-byte aligned (NULL when that is 0) */
+    size_t workspace_bytes;
+    void* hip_stream;
+} fff_grouped_weight_grad_args;
+
+int fff_grouped_weight_grad(const fff_grouped_weight_grad_args* a);
+
+/* Scratch of fff_grouped_weight_grad: partial sums where few groups have many entries (0 when
+ * there are enough groups, and for invalid shapes). */
+size_t fff_grouped_weight_grad_workspace_bytes(int64_t n_entries, int32_t n_groups, int32_t k, int32_t n);
+
 const char* fff_status_str(int status);
 int fff_last_hip_error(void); /* raw hipError_t behind the calling thread's last FFF_ERR_HIP */
 int fff_version(void);

@@ -574,6 +574,369 @@ FFF_EXPORT int fff_describe_stack(const fff_args* a, const fff_layer* layers, in
     return FFF_OK;
 }
 
+// ---- operators around the layer -------------------------------------------
+
+namespace {
+
+bool dtype_ok(int32_t dt) { return dt == FFF_F32 || dt == FFF_BF16; }
+int64_t dtype_bytes(int32_t dt) { return dt == FFF_BF16 ? 2 : 4; }
+
+// Bytes of a [rows, cols] matrix (or [a, rows, cols]); false where they pass 63 bits.
+bool matrix_bytes(int64_t a, int64_t rows, int64_t cols, int64_t elem, int64_t* out) {
+    return mul_ok(a, rows, out) && mul_ok(*out, cols, out) && mul_ok(*out, elem, out);
+}
+
+// No output overlaps another output or an input, but that output 0 may be the very buffer
+// in_place (an input of its size and type).
+bool disjoint(const Span* outs, int n_outs, const Span* ins, int n_ins, const void* in_place, const void* in_place2) {
+    for (int i = 0; i < n_outs; ++i) {
+        if (!outs[i].ptr) continue;
+        for (int j = i + 1; j < n_outs; ++j)
+            if (overlap(outs[i].ptr, outs[i].bytes, outs[j].ptr, outs[j].bytes)) return false;
+        for (int j = 0; j < n_ins; ++j) {
+            const bool same = i == 0 && ins[j].ptr == outs[0].ptr && (ins[j].ptr == in_place || ins[j].ptr == in_place2);
+            if (!same && overlap(outs[i].ptr, outs[i].bytes, ins[j].ptr, ins[j].bytes)) return false;
+        }
+    }
+    return true;
+}
+
+bool drop_ok(const fff_dropout_rng& d) {
+    return d.p >= 0.0 && d.p < 1.0 && (reinterpret_cast<uintptr_t>(d.rng_offset) & 7u) == 0;
+}
+
+fff::DropRng drop_rng(const fff_dropout_rng& d) {
+    fff::DropRng r;
+    r.on = d.p > 0.0;
+    r.threshold = uint32_t(d.p * 4294967296.0);
+    r.scale = float(1.0 / (1.0 - d.p));
+    r.k0 = uint32_t(d.seed);
+    r.k1 = uint32_t(d.seed >> 32);
+    r.offset = d.offset;
+    r.offset_dev = d.rng_offset;
+    return r;
+}
+
+constexpr int64_t kMaxRows = int64_t(1) << 32;     // dropout's counter holds 32 bits of the row
+constexpr int64_t kMaxEntries = int64_t(1) << 31;  // entries and indices are int32
+
+hipStream_t stream_of(void* s) { return reinterpret_cast<hipStream_t>(s); }
+
+}  // namespace
+
+FFF_EXPORT int fff_layer_norm(const fff_layer_norm_args* a) {
+    if (!a || a->n_tokens < 0 || a->n_tokens >= kMaxRows || a->hidden < 1) return FFF_ERR_INVALID_ARG;
+    if (!dtype_ok(a->x_dtype) || !dtype_ok(a->s_dtype) || !dtype_ok(a->y_dtype)) return FFF_ERR_INVALID_ARG;
+    if (!(a->eps >= 0.0f && a->eps <= 3.4028234663852886e38f) || !drop_ok(a->drop)) return FFF_ERR_INVALID_ARG;
+    if (a->n_tokens == 0) return FFF_OK;
+    if (!a->x || !a->y) return FFF_ERR_INVALID_ARG;
+    for (const void* q : {a->x, a->residual, static_cast<const void*>(a->gamma), static_cast<const void*>(a->beta),
+                          static_cast<const void*>(a->y), static_cast<const void*>(a->s)})
+        if (!aligned16(q)) return FFF_ERR_INVALID_ARG;
+    if (!aligned4(a->mean) || !aligned4(a->rstd)) return FFF_ERR_INVALID_ARG;
+    const int64_t B = a->n_tokens, H = a->hidden;
+    int64_t xb, sb, yb;
+    if (!matrix_bytes(1, B, H, dtype_bytes(a->x_dtype), &xb) || !matrix_bytes(1, B, H, dtype_bytes(a->s_dtype), &sb) ||
+        !matrix_bytes(1, B, H, dtype_bytes(a->y_dtype), &yb))
+        return FFF_ERR_INVALID_ARG;
+    const Span outs[] = {{a->s, sb}, {a->y, yb}, {a->mean, 4 * B}, {a->rstd, 4 * B}};
+    const Span ins[] = {{a->x, xb}, {a->residual, sb}, {a->gamma, 4 * H}, {a->beta, 4 * H}, {a->drop.rng_offset, 8}};
+    if (!disjoint(outs, 4, ins, 5, a->residual, nullptr)) return FFF_ERR_INVALID_ARG;
+    fff::DeviceInfo dev;
+    const int rc = current_device_info(&dev);
+    if (rc != FFF_OK) return rc;
+    fff::NormParams p;
+    p.x = a->x;
+    p.residual = a->residual;
+    p.gamma = a->gamma;
+    p.beta = a->beta;
+    p.y = a->y;
+    p.s = a->s;
+    p.mean = a->mean;
+    p.rstd = a->rstd;
+    p.n_tokens = B;
+    p.hidden = a->hidden;
+    p.x_bf16 = a->x_dtype == FFF_BF16;
+    p.s_bf16 = a->s_dtype == FFF_BF16;
+    p.y_bf16 = a->y_dtype == FFF_BF16;
+    p.eps = a->eps;
+    p.drop = drop_rng(a->drop);
+    const hipError_t e = fff::run_layer_norm(p, dev, stream_of(a->hip_stream));
+    return e == hipSuccess ? FFF_OK : hip_fail(e);
+}
+
+FFF_EXPORT size_t fff_layer_norm_backward_workspace_bytes(int64_t n_tokens, int32_t hidden) {
+    if (n_tokens < 0 || n_tokens >= kMaxRows || hidden < 1) return 0;
+    return fff::norm_bwd_workspace_bytes(n_tokens, hidden);
+}
+
+FFF_EXPORT int fff_layer_norm_backward(const fff_layer_norm_backward_args* a) {
+    if (!a || a->n_tokens < 0 || a->n_tokens >= kMaxRows || a->hidden < 1) return FFF_ERR_INVALID_ARG;
+    if (!dtype_ok(a->x_dtype) || !dtype_ok(a->s_dtype) || !dtype_ok(a->y_dtype)) return FFF_ERR_INVALID_ARG;
+    if ((a->accumulate != 0 && a->accumulate != 1) || !drop_ok(a->drop)) return FFF_ERR_INVALID_ARG;
+    const int64_t B = a->n_tokens, H = a->hidden;
+    const bool sums = a->dgamma || a->dbeta;
+    if (!a->ds && !a->dx && !sums) return FFF_OK;
+    if (B == 0 && (!sums || a->accumulate)) return FFF_OK;
+    if (B > 0 && (!a->dy || !a->s || !a->mean || !a->rstd)) return FFF_ERR_INVALID_ARG;
+    for (const void* q : {a->dy, a->s, static_cast<const void*>(a->gamma), a->ds_in, static_cast<const void*>(a->ds),
+                          static_cast<const void*>(a->dx), static_cast<const void*>(a->dgamma),
+                          static_cast<const void*>(a->dbeta)})
+        if (!aligned16(q)) return FFF_ERR_INVALID_ARG;
+    if (!aligned4(a->mean) || !aligned4(a->rstd)) return FFF_ERR_INVALID_ARG;
+    int64_t xb, sb, yb;
+    if (!matrix_bytes(1, B, H, dtype_bytes(a->x_dtype), &xb) || !matrix_bytes(1, B, H, dtype_bytes(a->s_dtype), &sb) ||
+        !matrix_bytes(1, B, H, dtype_bytes(a->y_dtype), &yb))
+        return FFF_ERR_INVALID_ARG;
+    int64_t need = 0;
+    if (sums) {
+        need = int64_t(fff::norm_bwd_workspace_bytes(B, a->hidden));
+        if (need > 0 && (!a->workspace || a->workspace_bytes < size_t(need))) return FFF_ERR_WORKSPACE;
+        if (reinterpret_cast<uintptr_t>(a->workspace) & 255u) return FFF_ERR_INVALID_ARG;
+    }
+    const Span outs[] = {{a->ds, sb}, {a->dx, xb}, {a->dgamma, 4 * H}, {a->dbeta, 4 * H},
+                         {need ? a->workspace : nullptr, need}};
+    const Span ins[] = {{a->dy, yb},        {a->s, sb},     {a->mean, 4 * B}, {a->rstd, 4 * B},
+                        {a->gamma, 4 * H}, {a->ds_in, sb}, {a->drop.rng_offset, 8}};
+    if (!disjoint(outs, 5, ins, 7, a->ds_in, nullptr)) return FFF_ERR_INVALID_ARG;
+    fff::DeviceInfo dev;
+    const int rc = current_device_info(&dev);
+    if (rc != FFF_OK) return rc;
+    fff::NormBwdParams p;
+    p.dy = a->dy;
+    p.s = a->s;
+    p.mean = a->mean;
+    p.rstd = a->rstd;
+    p.gamma = a->gamma;
+    p.ds_in = a->ds_in;
+    p.ds = a->ds;
+    p.dx = a->dx;
+    p.dgamma = a->dgamma;
+    p.dbeta = a->dbeta;
+    p.part = static_cast<float*>(a->workspace);
+    p.n_tokens = B;
+    p.hidden = a->hidden;
+    p.x_bf16 = a->x_dtype == FFF_BF16;
+    p.s_bf16 = a->s_dtype == FFF_BF16;
+    p.y_bf16 = a->y_dtype == FFF_BF16;
+    p.accumulate = a->accumulate;
+    p.drop = drop_rng(a->drop);
+    const hipError_t e = fff::run_layer_norm_backward(p, dev, stream_of(a->hip_stream));
+    return e == hipSuccess ? FFF_OK : hip_fail(e);
+}
+
+FFF_EXPORT int fff_dropout(const fff_dropout_args* a) {
+    if (!a || a->n_tokens < 0 || a->n_tokens >= kMaxRows || a->hidden < 1) return FFF_ERR_INVALID_ARG;
+    if (!dtype_ok(a->x_dtype) || !dtype_ok(a->r_dtype) || !dtype_ok(a->y_dtype)) return FFF_ERR_INVALID_ARG;
+    if (!drop_ok(a->drop)) return FFF_ERR_INVALID_ARG;
+    if (a->n_tokens == 0) return FFF_OK;
+    if (!a->x || !a->y) return FFF_ERR_INVALID_ARG;
+    for (const void* q : {a->x, a->residual, static_cast<const void*>(a->y)})
+        if (!aligned16(q)) return FFF_ERR_INVALID_ARG;
+    const int64_t B = a->n_tokens, H = a->hidden;
+    int64_t xb, rb, yb;
+    if (!matrix_bytes(1, B, H, dtype_bytes(a->x_dtype), &xb) || !matrix_bytes(1, B, H, dtype_bytes(a->r_dtype), &rb) ||
+        !matrix_bytes(1, B, H, dtype_bytes(a->y_dtype), &yb))
+        return FFF_ERR_INVALID_ARG;
+    const Span outs[] = {{a->y, yb}};
+    const Span ins[] = {{a->x, xb}, {a->residual, rb}, {a->drop.rng_offset, 8}};
+    if (!disjoint(outs, 1, ins, 3, a->x_dtype == a->y_dtype ? a->x : nullptr,
+                  a->r_dtype == a->y_dtype ? a->residual : nullptr))
+        return FFF_ERR_INVALID_ARG;
+    fff::DeviceInfo dev;
+    const int rc = current_device_info(&dev);
+    if (rc != FFF_OK) return rc;
+    fff::DropoutParams p;
+    p.x = a->x;
+    p.residual = a->residual;
+    p.y = a->y;
+    p.n_tokens = B;
+    p.hidden = a->hidden;
+    p.x_bf16 = a->x_dtype == FFF_BF16;
+    p.r_bf16 = a->r_dtype == FFF_BF16;
+    p.y_bf16 = a->y_dtype == FFF_BF16;
+    p.drop = drop_rng(a->drop);
+    const hipError_t e = fff::run_dropout(p, dev, stream_of(a->hip_stream));
+    return e == hipSuccess ? FFF_OK : hip_fail(e);
+}
+
+namespace {
+// FFF_OK, or why the group count of fff_group_rows is refused.
+int check_groups(int64_t n_entries, int32_t n_ids, int32_t n_trees) {
+    if (n_entries < 0 || n_entries >= kMaxEntries || n_ids < 1 || n_trees < 1) return FFF_ERR_INVALID_ARG;
+    return int64_t(n_ids) * n_trees > FFF_MAX_GROUPS ? FFF_ERR_UNSUPPORTED : FFF_OK;
+}
+}  // namespace
+
+FFF_EXPORT size_t fff_group_rows_workspace_bytes(int64_t n_entries, int32_t n_ids, int32_t n_trees) {
+    return check_groups(n_entries, n_ids, n_trees) == FFF_OK ? fff::group_workspace_bytes(n_entries, n_ids * n_trees) : 0;
+}
+
+FFF_EXPORT int fff_group_rows(const fff_group_rows_args* a) {
+    static_assert(FFF_MAX_GROUPS == fff::MAX_GROUPS, "one limit");
+    if (!a) return FFF_ERR_INVALID_ARG;
+    int rc = check_groups(a->n_entries, a->n_ids, a->n_trees);
+    if (rc != FFF_OK) return rc;
+    const int64_t E = a->n_entries, G = int64_t(a->n_ids) * a->n_trees;
+    if (!a->offsets || (E > 0 && (!a->ids || !a->order))) return FFF_ERR_INVALID_ARG;
+    for (const void* q : {static_cast<const void*>(a->ids), static_cast<const void*>(a->order),
+                          static_cast<const void*>(a->offsets), static_cast<const void*>(a->bad_ids)})
+        if (!aligned4(q)) return FFF_ERR_INVALID_ARG;
+    const int64_t need = int64_t(fff::group_workspace_bytes(E, int32_t(G)));
+    if (need > 0) {
+        if (!a->workspace || a->workspace_bytes < size_t(need)) return FFF_ERR_WORKSPACE;
+        if (reinterpret_cast<uintptr_t>(a->workspace) & 255u) return FFF_ERR_INVALID_ARG;
+    }
+    const Span outs[] = {{a->order, 4 * E}, {a->offsets, 4 * (G + 1)}, {a->bad_ids, 4}, {need ? a->workspace : nullptr, need}};
+    const Span ins[] = {{a->ids, 4 * E}};
+    if (!disjoint(outs, 4, ins, 1, nullptr, nullptr)) return FFF_ERR_INVALID_ARG;
+    fff::DeviceInfo dev;
+    rc = current_device_info(&dev);
+    if (rc != FFF_OK) return rc;
+    fff::GroupParams p;
+    p.ids = a->ids;
+    p.order = a->order;
+    p.offsets = a->offsets;
+    p.bad = a->bad_ids;
+    p.n_entries = E;
+    p.n_ids = a->n_ids;
+    p.n_trees = a->n_trees;
+    p.first = a->first;
+    p.n_groups = int32_t(G);
+    p.workspace = a->workspace;
+    const hipError_t e = fff::run_group_rows(p, stream_of(a->hip_stream));
+    return e == hipSuccess ? FFF_OK : hip_fail(e);
+}
+
+namespace {
+// Sizes common to the grouped products.
+bool grouped_sizes_ok(int64_t n_entries, int32_t n_groups, int32_t k, int32_t n, int32_t x_div) {
+    return n_entries >= 0 && n_entries < kMaxEntries && n_groups >= 1 && k >= 1 && n >= 1 && x_div >= 1;
+}
+// Rows of a matrix that entries read or write, directly or through an index.
+bool rows_ok(int64_t rows, int64_t n_entries, const int32_t* index) {
+    return rows >= 0 && rows < kMaxEntries && (index || rows >= n_entries) && aligned4(index);
+}
+}  // namespace
+
+FFF_EXPORT int fff_grouped_matmul(const fff_grouped_matmul_args* a) {
+    if (!a || !grouped_sizes_ok(a->n_entries, a->n_groups, a->k, a->n, a->x_div)) return FFF_ERR_INVALID_ARG;
+    for (int32_t dt : {a->x_dtype, a->w_dtype, a->y_dtype, a->z_dtype})
+        if (!dtype_ok(dt)) return FFF_ERR_INVALID_ARG;
+    if (a->act < FFF_ACT_GELU_ERF || a->act > FFF_ACT_IDENTITY) return FFF_ERR_INVALID_ARG;
+    if (a->w_transposed != 0 && a->w_transposed != 1) return FFF_ERR_INVALID_ARG;
+    const int64_t E = a->n_entries;
+    if (E == 0) return FFF_OK;
+    // without an index entry i reads row i / x_div of x
+    const int64_t x_direct = (E - 1) / a->x_div + 1;
+    if (!rows_ok(a->x_rows, x_direct, a->x_index) || !rows_ok(a->y_rows, E, a->y_index)) return FFF_ERR_INVALID_ARG;
+    if (!a->x || !a->w || !a->offsets || !a->y || (a->z_in && a->z_out)) return FFF_ERR_INVALID_ARG;
+    for (const void* q : {a->x, a->w, static_cast<const void*>(a->y), static_cast<const void*>(a->z_out), a->z_in})
+        if (!aligned16(q)) return FFF_ERR_INVALID_ARG;
+    if (!aligned4(a->offsets)) return FFF_ERR_INVALID_ARG;
+    int64_t xb, wb, yb, zb;
+    if (!matrix_bytes(1, a->x_rows, a->k, dtype_bytes(a->x_dtype), &xb) ||
+        !matrix_bytes(a->n_groups, a->k, a->n, dtype_bytes(a->w_dtype), &wb) ||
+        !matrix_bytes(1, a->y_rows, a->n, dtype_bytes(a->y_dtype), &yb) ||
+        !matrix_bytes(1, E, a->n, dtype_bytes(a->z_dtype), &zb))
+        return FFF_ERR_INVALID_ARG;
+    const Span outs[] = {{a->y, yb}, {a->z_out, zb}};
+    const Span ins[] = {{a->x, xb}, {a->w, wb}, {a->offsets, 4 * (int64_t(a->n_groups) + 1)},
+                        {a->x_index, 4 * E}, {a->y_index, 4 * E}, {a->z_in, zb}};
+    if (!disjoint(outs, 2, ins, 6, nullptr, nullptr)) return FFF_ERR_INVALID_ARG;
+    if (a->x_dtype != a->w_dtype) return FFF_ERR_UNSUPPORTED;
+    fff::DeviceInfo dev;
+    const int rc = current_device_info(&dev);
+    if (rc != FFF_OK) return rc;
+    fff::GroupedParams p;
+    p.x = a->x;
+    p.w = a->w;
+    p.offsets = a->offsets;
+    p.x_index = a->x_index;
+    p.y_index = a->y_index;
+    p.y = a->y;
+    p.z_out = a->z_out;
+    p.z_in = a->z_in;
+    p.n_entries = E;
+    p.x_rows = a->x_rows;
+    p.y_rows = a->y_rows;
+    p.n_groups = a->n_groups;
+    p.k = a->k;
+    p.n = a->n;
+    p.x_div = a->x_div;
+    p.w_transposed = a->w_transposed;
+    p.bf16 = a->x_dtype == FFF_BF16;
+    p.y_bf16 = a->y_dtype == FFF_BF16;
+    p.z_bf16 = a->z_dtype == FFF_BF16;
+    p.act = a->act;
+    int status = FFF_OK;
+    const hipError_t e = fff::run_grouped_matmul(p, dev, stream_of(a->hip_stream), &status);
+    if (status != FFF_OK) return status;
+    return e == hipSuccess ? FFF_OK : hip_fail(e);
+}
+
+FFF_EXPORT size_t fff_grouped_weight_grad_workspace_bytes(int64_t n_entries, int32_t n_groups, int32_t k, int32_t n) {
+    if (!grouped_sizes_ok(n_entries, n_groups, k, n, 1)) return 0;
+    return fff::grouped_grad_workspace_bytes(n_entries, n_groups, k, n);
+}
+
+FFF_EXPORT int fff_grouped_weight_grad(const fff_grouped_weight_grad_args* a) {
+    if (!a || !grouped_sizes_ok(a->n_entries, a->n_groups, a->k, a->n, a->x_div)) return FFF_ERR_INVALID_ARG;
+    if (!dtype_ok(a->dy_dtype) || !dtype_ok(a->x_dtype)) return FFF_ERR_INVALID_ARG;
+    if (a->accumulate != 0 && a->accumulate != 1) return FFF_ERR_INVALID_ARG;
+    const int64_t E = a->n_entries;
+    if (E == 0 && a->accumulate) return FFF_OK;
+    if (!a->dw || !a->offsets) return FFF_ERR_INVALID_ARG;
+    if (E > 0) {
+        const int64_t x_direct = (E - 1) / a->x_div + 1;
+        if (!rows_ok(a->x_rows, x_direct, a->x_index) || !rows_ok(a->dy_rows, E, a->dy_index))
+            return FFF_ERR_INVALID_ARG;
+        if (!a->dy || !a->x) return FFF_ERR_INVALID_ARG;
+    }
+    for (const void* q : {a->dy, a->x, static_cast<const void*>(a->dw)})
+        if (!aligned16(q)) return FFF_ERR_INVALID_ARG;
+    if (!aligned4(a->offsets)) return FFF_ERR_INVALID_ARG;
+    int64_t xb = 0, yb = 0, wb;
+    if ((E > 0 && (!matrix_bytes(1, a->x_rows, a->k, dtype_bytes(a->x_dtype), &xb) ||
+                   !matrix_bytes(1, a->dy_rows, a->n, dtype_bytes(a->dy_dtype), &yb))) ||
+        !matrix_bytes(a->n_groups, a->k, a->n, 4, &wb))
+        return FFF_ERR_INVALID_ARG;
+    const int64_t need = int64_t(fff::grouped_grad_workspace_bytes(E, a->n_groups, a->k, a->n));
+    if (need > 0) {
+        if (!a->workspace || a->workspace_bytes < size_t(need)) return FFF_ERR_WORKSPACE;
+        if (reinterpret_cast<uintptr_t>(a->workspace) & 255u) return FFF_ERR_INVALID_ARG;
+    }
+    const Span outs[] = {{a->dw, wb}, {need ? a->workspace : nullptr, need}};
+    const Span ins[] = {{a->dy, yb}, {a->x, xb}, {a->offsets, 4 * (int64_t(a->n_groups) + 1)},
+                        {a->dy_index, 4 * E}, {a->x_index, 4 * E}};
+    if (!disjoint(outs, 2, ins, 5, nullptr, nullptr)) return FFF_ERR_INVALID_ARG;
+    if (a->dy_dtype != a->x_dtype) return FFF_ERR_UNSUPPORTED;
+    fff::DeviceInfo dev;
+    const int rc = current_device_info(&dev);
+    if (rc != FFF_OK) return rc;
+    fff::GroupedGradParams p;
+    p.dy = a->dy;
+    p.x = a->x;
+    p.offsets = a->offsets;
+    p.dy_index = a->dy_index;
+    p.x_index = a->x_index;
+    p.dw = a->dw;
+    p.n_entries = E;
+    p.dy_rows = a->dy_rows;
+    p.x_rows = a->x_rows;
+    p.n_groups = a->n_groups;
+    p.k = a->k;
+    p.n = a->n;
+    p.x_div = a->x_div;
+    p.bf16 = a->x_dtype == FFF_BF16;
+    p.accumulate = a->accumulate;
+    p.part = static_cast<float*>(a->workspace);
+    int status = FFF_OK;
+    const hipError_t e = fff::run_grouped_weight_grad(p, dev, stream_of(a->hip_stream), &status);
+    if (status != FFF_OK) return status;
+    return e == hipSuccess ? FFF_OK : hip_fail(e);
+}
+
 FFF_EXPORT const char* fff_status_str(int status) {
     switch (status) {
         case FFF_OK: return "FFF_OK";

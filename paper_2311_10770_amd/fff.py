@@ -70,7 +70,9 @@ _lib = None
 
 EXPORTS = ("fff_forward", "fff_forward_ex", "fff_forward_static", "fff_workspace_bytes", "fff_describe", "fff_forward_stack",
            "fff_describe_stack", "fff_backward", "fff_backward_workspace_bytes", "fff_status_str",
-           "fff_last_hip_error", "fff_version")
+           "fff_last_hip_error", "fff_version", "fff_layer_norm", "fff_layer_norm_backward",
+           "fff_layer_norm_backward_workspace_bytes", "fff_dropout", "fff_group_rows", "fff_group_rows_workspace_bytes",
+           "fff_grouped_matmul", "fff_grouped_weight_grad", "fff_grouped_weight_grad_workspace_bytes")
 
 
 def load_library(path: Path | str | None = None):
@@ -102,6 +104,16 @@ def load_library(path: Path | str | None = None):
     lib.fff_backward.restype = c_int
     lib.fff_backward_workspace_bytes.argtypes = [c_int64, c_int32, c_int32, c_int32]
     lib.fff_backward_workspace_bytes.restype = c_size_t
+    for name in ("fff_layer_norm", "fff_layer_norm_backward", "fff_dropout", "fff_group_rows", "fff_grouped_matmul",
+                 "fff_grouped_weight_grad"):
+        getattr(lib, name).argtypes = [c_void_p]  # the struct's address
+        getattr(lib, name).restype = c_int
+    lib.fff_layer_norm_backward_workspace_bytes.argtypes = [c_int64, c_int32]
+    lib.fff_group_rows_workspace_bytes.argtypes = [c_int64, c_int32, c_int32]
+    lib.fff_grouped_weight_grad_workspace_bytes.argtypes = [c_int64, c_int32, c_int32, c_int32]
+    for name in ("fff_layer_norm_backward_workspace_bytes", "fff_group_rows_workspace_bytes",
+                 "fff_grouped_weight_grad_workspace_bytes"):
+        getattr(lib, name).restype = c_size_t
     lib.fff_status_str.argtypes = [c_int]
     lib.fff_status_str.restype = c_char_p
     lib.fff_last_hip_error.argtypes = []
