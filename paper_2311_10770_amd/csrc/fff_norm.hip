@@ -498,45 +498,52 @@ __global__ __launch_bounds__(1024) void norm_bwd_sum_kernel(NormBwdParams p, int
 }
 
 // A thread takes DU generator blocks, 256 apart; a workgroup's blocks are consecutive, rows being
-// `vecs` blocks long.
-constexpr int DU = 8;
+// `vecs` blocks long (step_q and step_v: 256 / vecs and 256 % vecs, so only the first place of a
+// thread is divided for).  Threads behind the last block load it again and store nothing: loads
+// without a branch stay in flight together.
+constexpr int DU = 4;
 template <bool DROP, bool FULL>
-__global__ __launch_bounds__(256) void dropout_kernel(DropoutParams p, int vecs, int64_t all) {
+__global__ __launch_bounds__(256) void dropout_kernel(DropoutParams p, int vecs, int64_t all, uint32_t step_q,
+                                                      uint32_t step_v) {
     const uint64_t off = DROP ? rng_offset(p.drop) : 0;
-    const int64_t H = p.hidden;
+    const int H = p.hidden;
     for (int64_t i0 = int64_t(blockIdx.x) * (256 * DU); i0 < all; i0 += int64_t(gridDim.x) * (256 * DU)) {
         const int64_t row0 = i0 / vecs;
-        const uint32_t v0 = uint32_t(i0 - row0 * vecs);
+        const uint32_t at = uint32_t(i0 - row0 * vecs) + threadIdx.x;
         const int count = int(all - i0 < 256 * DU ? all - i0 : 256 * DU);
+        uint32_t q = at / uint32_t(vecs), v = at - q * uint32_t(vecs);
+        int64_t e[DU];
+        uint32_t qs[DU], vs[DU];
         Raw4 rx[DU], rr[DU];
-        uint32_t q[DU], v[DU];
 #pragma unroll
         for (int u = 0; u < DU; ++u) {
-            const uint32_t at = v0 + u * 256 + threadIdx.x;
-            q[u] = at / uint32_t(vecs);
-            v[u] = at - q[u] * uint32_t(vecs);
-            if (u * 256 + int(threadIdx.x) < count)
-                rx[u] = load4<FULL>(p.x, p.x_bf16, (row0 + q[u]) * H + 4 * int64_t(v[u]), int(H - 4 * int64_t(v[u])));
+            const bool in = u * 256 + int(threadIdx.x) < count;
+            qs[u] = in ? q : 0;
+            vs[u] = in ? v : uint32_t(vecs - 1);
+            e[u] = in ? (row0 + q) * H + 4 * int64_t(v) : (p.n_tokens - 1) * H + 4 * int64_t(vecs - 1);
+            rx[u] = load4<FULL>(p.x, p.x_bf16, e[u], H - 4 * int(vs[u]));
+            q += step_q;
+            v += step_v;
+            if (v >= uint32_t(vecs)) {
+                v -= uint32_t(vecs);
+                ++q;
+            }
         }
         if (p.residual) {
 #pragma unroll
-            for (int u = 0; u < DU; ++u)
-                if (u * 256 + int(threadIdx.x) < count)
-                    rr[u] = load4<FULL>(p.residual, p.r_bf16, (row0 + q[u]) * H + 4 * int64_t(v[u]),
-                                        int(H - 4 * int64_t(v[u])));
+            for (int u = 0; u < DU; ++u) rr[u] = load4<FULL>(p.residual, p.r_bf16, e[u], H - 4 * int(vs[u]));
         }
 #pragma unroll
         for (int u = 0; u < DU; ++u) {
-            if (u * 256 + int(threadIdx.x) >= count) break;
             float f[4], g[4];
             unpack4(f, rx[u], p.x_bf16);
-            if (DROP) drop4(f, p.drop, off, v[u], uint32_t(row0 + q[u]));
+            if (DROP) drop4(f, p.drop, off, vs[u], uint32_t(row0 + qs[u]));
             if (p.residual) {
                 unpack4(g, rr[u], p.r_bf16);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) f[j] += g[j];
             }
-            store4<FULL>(p.y, p.y_bf16, (row0 + q[u]) * H + 4 * int64_t(v[u]), int(H - 4 * int64_t(v[u])), f);
+            if (u * 256 + int(threadIdx.x) < count) store4<FULL>(p.y, p.y_bf16, e[u], H - 4 * int(vs[u]), f);
         }
     }
 }
@@ -625,7 +632,7 @@ hipError_t run_dropout(const DropoutParams& p, const DeviceInfo& dev, hipStream_
     const int vecs = int((int64_t(p.hidden) + 3) / 4);
     const int64_t all = p.n_tokens * vecs;
     const unsigned grid = unsigned(std::min<int64_t>((all + 256 * DU - 1) / (256 * DU), 64 * std::max(dev.cu_count, 1)));
-    auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, stream, p, vecs, all); };
+    auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, stream, p, vecs, all, 256u / unsigned(vecs), 256u % unsigned(vecs)); };
     const bool full = p.hidden % 4 == 0;
     if (p.drop.on) full ? launch(dropout_kernel<true, true>) : launch(dropout_kernel<true, false>);
     else full ? launch(dropout_kernel<false, true>) : launch(dropout_kernel<false, false>);
