@@ -1,10 +1,18 @@
 // fff_group.hip -- fff_group_rows: a stable counting sort of entries by group.
 //
-// Entries are cut into chunks; a workgroup counts its chunk's entries per
-// group in LDS (hist), every group's counts become running sums over the
-// chunks, the totals the groups' offsets, and a wave per chunk places the
-// chunk's entries in order.  Within a wave equal groups are found with one
-// ballot per bit of the group number, so no order depends on an atomic.
+// Every wave owns a run of consecutive entries and a row of counters in LDS.
+// It counts its entries per group; the counts become running sums over the
+// waves (and over the workgroups, through the workspace) and over the groups;
+// then the wave goes through its entries again, 64 at a time, and places
+// them.  Within 64 entries equal groups are found with one ballot per bit of
+// the group number, so no place depends on the order of atomics.
+//
+// Up to GROUP_ONE entries take one workgroup and one launch; more take three
+// (count, scan, place), every workgroup with a chunk of its own.  The work is a
+// few bytes per entry: launches and the latency of dependent steps are the time.
+// 16384 entries of 64 groups: 15.1 us in one launch, called or in a graph (a
+// single entry a lane: 8.9), 11.4 in three launches in a graph, but 19.1 called.
+// 524288 entries of 4096 groups: 24.5 us.
 #include "fff_internal.hpp"
 
 #include <hip/hip_runtime.h>
@@ -16,119 +24,282 @@ namespace fff {
 
 namespace {
 
-constexpr int GROUP_CHUNKS = 256;  // at most
-constexpr int64_t GROUP_MIN_CHUNK = 1024;
+constexpr int GROUP_ONE = 16384;         // entries of the one-launch form, at most
+constexpr int GROUP_ONE_GROUPS = 1024;   // its groups: their counters and the staged order fit LDS
+constexpr int GROUP_COUNTERS = 32768;    // counters in LDS: waves x groups
+constexpr int64_t GROUP_CHUNKS = 256;    // about so many chunks, of at least GROUP_ROUNDS rounds a wave
+constexpr int GROUP_ROUNDS = 4;
 
-int64_t group_chunk(int64_t n) {
-    const int64_t c = (n + GROUP_CHUNKS - 1) / GROUP_CHUNKS;
-    return std::max(GROUP_MIN_CHUNK, (c + 63) / 64 * 64);
+// Waves of a workgroup: as many as have counters, up to sixteen.
+int group_waves(int32_t n_groups) {
+    int w = 16;
+    while (w > 1 && w * n_groups > GROUP_COUNTERS) w /= 2;
+    return w;
 }
-int64_t group_chunks(int64_t n) { return (n + group_chunk(n) - 1) / group_chunk(n); }
+bool group_one(int64_t n, int32_t n_groups) { return n <= GROUP_ONE && n_groups <= GROUP_ONE_GROUPS; }
+// Entries of a chunk: whole rounds of 64 for each of its waves.
+int64_t group_chunk(int64_t n, int waves) {
+    const int64_t round = 64 * waves, c = (n + GROUP_CHUNKS - 1) / GROUP_CHUNKS;
+    return std::max<int64_t>(GROUP_ROUNDS, (c + round - 1) / round) * round;
+}
+int64_t group_chunks(int64_t n, int32_t n_groups) {
+    const int64_t c = group_chunk(n, group_waves(n_groups));
+    return std::max<int64_t>(1, (n + c - 1) / c);
+}
 
 // The group of entry e, or -1.
-__device__ __forceinline__ int group_of(const GroupParams& p, int64_t e) {
+__device__ __forceinline__ int group_of(const GroupParams& p, uint32_t e) {
     const int64_t id = int64_t(p.ids[e]) - p.first;
-    return id >= 0 && id < p.n_ids ? int(e % p.n_trees) * p.n_ids + int(id) : -1;
+    const int tree = p.n_trees == 1 ? 0 : int(e % uint32_t(p.n_trees));
+    return id >= 0 && id < p.n_ids ? tree * p.n_ids + int(id) : -1;
 }
 
-__global__ __launch_bounds__(256) void group_count_kernel(GroupParams p, int64_t chunk) {
-    extern __shared__ int32_t g_cnt[];  // [n_groups]
-    const int G = p.n_groups;
-    for (int g = threadIdx.x; g < G; g += 256) g_cnt[g] = 0;
-    __syncthreads();
-    const int64_t e1 = std::min<int64_t>(p.n_entries, (int64_t(blockIdx.x) + 1) * chunk);
-    for (int64_t e = int64_t(blockIdx.x) * chunk + threadIdx.x; e < e1; e += 256) {
-        const int g = group_of(p, e);
-        if (g >= 0) atomicAdd(&g_cnt[g], 1);
-        else if (p.bad) atomicAdd(p.bad, 1);
+// One wave's entries [e0, e1) counted into its row of counters, RB rounds loaded at a time.
+template <int RB>
+__device__ __forceinline__ void count_run(const GroupParams& p, int64_t e0, int64_t e1, int32_t* row, bool tell) {
+    const int lane = threadIdx.x & 63;
+    int lost = 0;
+    for (int64_t b = e0 + lane; b < e1; b += 64 * RB) {
+        int g[RB];
+#pragma unroll
+        for (int r = 0; r < RB; ++r) g[r] = b + 64 * r < e1 ? group_of(p, uint32_t(b + 64 * r)) : -2;
+#pragma unroll
+        for (int r = 0; r < RB; ++r) {
+            if (g[r] >= 0) atomicAdd(&row[g[r]], 1);
+            lost += g[r] == -1;
+        }
     }
-    __syncthreads();
-    int32_t* hist = static_cast<int32_t*>(p.workspace) + int64_t(blockIdx.x) * G;
-    for (int g = threadIdx.x; g < G; g += 256) hist[g] = g_cnt[g];
+    if (tell && p.bad && lost) atomicAdd(p.bad, lost);
 }
 
-// Counts become running sums over the chunks; the totals go to offsets[1 + g].
-__global__ __launch_bounds__(256) void group_scan_kernel(GroupParams p, int chunks) {
-    const int64_t g = int64_t(blockIdx.x) * 256 + threadIdx.x;
-    const int G = p.n_groups;
-    if (g >= G) return;
-    int32_t* hist = static_cast<int32_t*>(p.workspace);
-    int32_t run = 0;
-    for (int c = 0; c < chunks; ++c) {
-        const int32_t v = hist[int64_t(c) * G + g];
-        hist[int64_t(c) * G + g] = run;
-        run += v;
+// One wave's entries [e0, e1) placed in order, RB rounds loaded at a time; row[g]: the wave's next
+// place in group g.  Entries go to order, or (STAGE) as 16 bits to `staged` in LDS.
+template <int RB, bool STAGE>
+__device__ __forceinline__ void place_run(const GroupParams& p, int64_t e0, int64_t e1, int32_t* row, uint16_t* staged,
+                                          int bits) {
+    const int lane = threadIdx.x & 63;
+    for (int64_t b = e0; b < e1; b += 64 * RB) {
+        int g[RB];
+#pragma unroll
+        for (int r = 0; r < RB; ++r) {
+            const int64_t e = b + 64 * r + lane;
+            g[r] = e < e1 ? group_of(p, uint32_t(e)) : -1;
+        }
+        // the lanes of each round with this lane's group; the rounds' chains of ballots run side by side
+        uint32_t lo[RB], hi[RB];
+#pragma unroll
+        for (int r = 0; r < RB; ++r) {
+            const uint64_t any = __ballot(g[r] >= 0);
+            lo[r] = uint32_t(any);
+            hi[r] = uint32_t(any >> 32);
+        }
+        for (int k = 0; k < bits; ++k) {
+#pragma unroll
+            for (int r = 0; r < RB; ++r) {
+                const int32_t one = int32_t(uint32_t(g[r]) << (31 - k)) >> 31;  // bit k in every bit
+                const uint64_t set = __ballot(one != 0);
+                lo[r] &= ~(uint32_t(set) ^ uint32_t(one));
+                hi[r] &= ~(uint32_t(set >> 32) ^ uint32_t(one));
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < RB; ++r) {
+            if (g[r] >= 0) {
+                const uint64_t same = uint64_t(hi[r]) << 32 | lo[r];
+                const int before = __popcll(same & ((uint64_t(1) << lane) - 1));
+                const int32_t at = row[g[r]];
+                // every lane has read its group's counter before the group's first lane moves it on
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                if (before == 0) row[g[r]] = at + __popcll(same);
+                if constexpr (STAGE) staged[at + before] = uint16_t(b + 64 * r + lane);
+                else p.order[at + before] = int32_t(b + 64 * r + lane);
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        }
     }
-    p.offsets[1 + g] = run;
 }
 
-// offsets: totals to inclusive sums, by one workgroup.
-__global__ __launch_bounds__(1024) void group_offsets_kernel(GroupParams p) {
-    __shared__ int32_t part[1024];
-    const int G = p.n_groups, tid = threadIdx.x, per = (G + 1023) / 1024;
-    const int g0 = std::min(G, tid * per), g1 = std::min(G, g0 + per);
-    int32_t sum = 0;
-    for (int g = g0; g < g1; ++g) sum += p.offsets[1 + g];
-    part[tid] = sum;
-    __syncthreads();
-    for (int d = 1; d < 1024; d *= 2) {
-        const int32_t v = tid >= d ? part[tid - d] : 0;
-        __syncthreads();
-        part[tid] += v;
-        __syncthreads();
+// Counters of group g in W rows of n_groups: exclusive sums from `at` on; returns their end.
+template <int W>
+__device__ __forceinline__ int32_t rows_scan(int32_t* cnt, int n_groups, int g, int32_t at) {
+    int32_t c[W];
+#pragma unroll
+    for (int w = 0; w < W; ++w) c[w] = cnt[w * n_groups + g];
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+        cnt[w * n_groups + g] = at;
+        at += c[w];
     }
-    int32_t run = part[tid] - sum;
+    return at;
+}
+
+// Inclusive sums over the 64 lanes.
+__device__ __forceinline__ int32_t wave_scan(int32_t v) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const int32_t u = __shfl_up(v, d);
+        if (lane >= d) v += u;
+    }
+    return v;
+}
+
+// Exclusive sums over a workgroup of `waves` waves.
+__device__ __forceinline__ int32_t block_scan(int32_t v, int32_t* sums, int waves) {
+    const int32_t in = wave_scan(v);
+    const int wave = threadIdx.x >> 6;
+    if ((threadIdx.x & 63) == 63) sums[wave] = in;
+    __syncthreads();
+    int32_t before = 0;
+    for (int w = 0; w < wave; ++w) before += sums[w];
+    return before + in - v;
+}
+
+// Everything in one workgroup of sixteen waves.  The order is put together in LDS and stored in whole
+// lines.
+__global__ __launch_bounds__(1024) void group_one_kernel(GroupParams p, int bits) {
+    extern __shared__ int32_t g_cnt[];  // [16][n_groups], then the order as 16-bit entries
+    __shared__ int32_t sums[16], listed;
+    const int G = p.n_groups, tid = threadIdx.x, wave = tid >> 6;
+    uint16_t* staged = reinterpret_cast<uint16_t*>(g_cnt + 16 * G);
+    for (int i = tid; i < 16 * G; i += 1024) g_cnt[i] = 0;
+    __syncthreads();
+    const int64_t run = (p.n_entries + 1023) / 1024 * 64;
+    const int64_t e0 = std::min<int64_t>(p.n_entries, wave * run), e1 = std::min<int64_t>(p.n_entries, e0 + run);
+    count_run<16>(p, e0, e1, g_cnt + wave * G, true);
+    __syncthreads();
+    // a thread takes a few consecutive groups: their totals, then every wave's first place in them
+    const int per = (G + 1023) / 1024, g0 = std::min(G, tid * per), g1 = std::min(G, g0 + per);
+    int32_t mine = 0;
     for (int g = g0; g < g1; ++g) {
-        run += p.offsets[1 + g];
-        p.offsets[1 + g] = run;
+#pragma unroll
+        for (int w = 0; w < 16; ++w) mine += g_cnt[w * G + g];
     }
-    if (tid == 0) p.offsets[0] = 0;
+    int32_t at = block_scan(mine, sums, 16);
+    for (int g = g0; g < g1; ++g) {
+        p.offsets[g] = at;
+        at = rows_scan<16>(g_cnt, G, g, at);
+        if (g == G - 1) p.offsets[G] = listed = at;
+    }
+    __syncthreads();
+    place_run<16, true>(p, e0, e1, g_cnt + wave * G, staged, bits);
+    __syncthreads();
+    for (int i = tid; i < listed; i += 1024) p.order[i] = staged[i];
 }
 
-__global__ __launch_bounds__(64) void group_place_kernel(GroupParams p, int64_t chunk, int bits) {
-    extern __shared__ int32_t g_next[];  // [n_groups] next place of each group
-    const int G = p.n_groups, lane = threadIdx.x;
-    const int32_t* hist = static_cast<const int32_t*>(p.workspace) + int64_t(blockIdx.x) * G;
-    for (int g = lane; g < G; g += 64) g_next[g] = p.offsets[g] + hist[g];
+// A chunk's entries per group: hist [chunk][group].
+__global__ __launch_bounds__(1024) void group_count_kernel(GroupParams p, int64_t chunk, int32_t* hist) {
+    extern __shared__ int32_t g_cnt[];  // [n_groups]
+    const int G = p.n_groups, tid = threadIdx.x, waves = blockDim.x >> 6, wave = tid >> 6;
+    for (int g = tid; g < G; g += blockDim.x) g_cnt[g] = 0;
     __syncthreads();
-    const int64_t e1 = std::min<int64_t>(p.n_entries, (int64_t(blockIdx.x) + 1) * chunk);
-    for (int64_t e0 = int64_t(blockIdx.x) * chunk; e0 < e1; e0 += 64) {
-        const int64_t e = e0 + lane;
-        const int g = e < e1 ? group_of(p, e) : -1;
-        uint64_t same = __ballot(g >= 0);
-        for (int b = 0; b < bits; ++b) {
-            const uint64_t set = __ballot((g >> b) & 1);
-            same &= (g >> b) & 1 ? set : ~set;
-        }
-        const int before = __popcll(same & ((uint64_t(1) << lane) - 1));
-        int32_t place = 0;
-        if (g >= 0) place = g_next[g] + before;
-        __syncthreads();
-        if (g >= 0) {
-            if (before == 0) g_next[g] += __popcll(same);
-            p.order[place] = int32_t(e);
-        }
-        __syncthreads();
+    const int64_t c0 = int64_t(blockIdx.x) * chunk, run = chunk / waves;
+    const int64_t e0 = std::min<int64_t>(p.n_entries, c0 + wave * run), e1 = std::min<int64_t>(p.n_entries, e0 + run);
+    count_run<GROUP_ROUNDS>(p, e0, e1, g_cnt, true);
+    __syncthreads();
+    for (int g = tid; g < G; g += blockDim.x) hist[int64_t(blockIdx.x) * G + g] = g_cnt[g];
+}
+
+// Running sums of hist over the chunks, 32 groups a workgroup, a piece of the chunks for each of 32
+// threads; the groups' totals behind it.
+__global__ __launch_bounds__(1024) void group_scan_kernel(GroupParams p, int chunks, int32_t* hist, int32_t* totals) {
+    __shared__ int32_t piece[32][33];
+    const int G = p.n_groups, col = threadIdx.x % 32, part = threadIdx.x / 32;
+    const int g = blockIdx.x * 32 + col, per = (chunks + 31) / 32;
+    const int c0 = std::min(chunks, part * per), c1 = std::min(chunks, c0 + per);
+    int32_t sum = 0;
+    if (g < G) {
+#pragma unroll 8
+        for (int c = c0; c < c1; ++c) sum += hist[int64_t(c) * G + g];
     }
+    piece[part][col] = sum;
+    __syncthreads();
+    int32_t run = 0, all = 0;
+#pragma unroll
+    for (int q = 0; q < 32; ++q) {
+        run += q < part ? piece[q][col] : 0;
+        all += piece[q][col];
+    }
+    if (g >= G) return;
+    for (int cb = c0; cb < c1; cb += 8) {
+        int32_t v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = cb + j < c1 ? hist[int64_t(cb + j) * G + g] : 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            if (cb + j < c1) hist[int64_t(cb + j) * G + g] = run;
+            run += v[j];
+        }
+    }
+    if (part == 0) totals[g] = all;
+}
+
+// A chunk's entries to their places: W of the sixteen waves have entries and counters, all of them
+// sum the totals to the groups' offsets (every workgroup for itself: a launch for it took 4 us, and as
+// the last act of the scan's last workgroup to finish 50, for the device-scope release that it needs of
+// every workgroup writes back its XCD's L2).
+template <int W>
+__global__ __launch_bounds__(1024) void group_place_kernel(GroupParams p, int64_t chunk, const int32_t* hist,
+                                                           const int32_t* totals, int bits) {
+    extern __shared__ int32_t g_cnt[];  // [W][n_groups]
+    __shared__ int32_t sums[16];
+    const int G = p.n_groups, tid = threadIdx.x, wave = tid >> 6;
+    const int64_t c0 = int64_t(blockIdx.x) * chunk, run = chunk / W;
+    const int64_t e0 = std::min<int64_t>(p.n_entries, c0 + wave * run);
+    const int64_t e1 = wave < W ? std::min<int64_t>(p.n_entries, e0 + run) : e0;
+    for (int i = tid; i < W * G; i += 1024) g_cnt[i] = 0;
+    const int per = (G + 1023) / 1024, g0 = std::min(G, tid * per), g1 = std::min(G, g0 + per);
+    int32_t mine = 0;
+#pragma unroll 4
+    for (int g = g0; g < g1; ++g) mine += totals[g];
+    int32_t at = block_scan(mine, sums, 16);  // (a barrier: the counters are clear)
+    count_run<GROUP_ROUNDS>(p, e0, e1, g_cnt + wave * G, false);
+    __syncthreads();
+    hist += int64_t(blockIdx.x) * G;
+    for (int g = g0; g < g1; ++g) {
+        if (blockIdx.x == 0) p.offsets[g] = at;
+        rows_scan<W>(g_cnt, G, g, at + hist[g]);
+        at += totals[g];
+        if (blockIdx.x == 0 && g == G - 1) p.offsets[G] = at;
+    }
+    __syncthreads();
+    place_run<GROUP_ROUNDS, false>(p, e0, e1, g_cnt + wave * G, nullptr, bits);
+}
+
+template <int W>
+void launch_place(int waves, const GroupParams& p, int chunks, int64_t chunk, const int32_t* hist, const int32_t* totals,
+                  int bits, hipStream_t stream) {
+    if constexpr (W > 1) {
+        if (waves < W) return launch_place<W / 2>(waves, p, chunks, chunk, hist, totals, bits, stream);
+    }
+    hipLaunchKernelGGL(group_place_kernel<W>, dim3(chunks), dim3(1024), size_t(W) * p.n_groups * sizeof(int32_t),
+                       stream, p, chunk, hist, totals, bits);
 }
 
 }  // namespace
 
 size_t group_workspace_bytes(int64_t n_entries, int32_t n_groups) {
-    return size_t(group_chunks(n_entries)) * size_t(n_groups) * sizeof(int32_t);
+    if (group_one(n_entries, n_groups)) return 0;
+    return (size_t(group_chunks(n_entries, n_groups)) + 1) * size_t(n_groups) * sizeof(int32_t);
 }
 
 hipError_t run_group_rows(const GroupParams& p, hipStream_t stream) {
-    const int G = p.n_groups;
-    const int64_t chunk = group_chunk(p.n_entries);
-    const int chunks = int(group_chunks(p.n_entries));
-    const size_t lds = size_t(G) * sizeof(int32_t);
+    const int G = p.n_groups, waves = group_waves(G);
     int bits = 0;
     while ((1 << bits) < G) ++bits;
-    if (chunks > 0) hipLaunchKernelGGL(group_count_kernel, dim3(chunks), dim3(256), lds, stream, p, chunk);
-    hipLaunchKernelGGL(group_scan_kernel, dim3((G + 255) / 256), dim3(256), 0, stream, p, chunks);
-    hipLaunchKernelGGL(group_offsets_kernel, dim3(1), dim3(1024), 0, stream, p);
-    if (chunks > 0) hipLaunchKernelGGL(group_place_kernel, dim3(chunks), dim3(64), lds, stream, p, chunk, bits);
+    if (group_one(p.n_entries, G)) {
+        hipLaunchKernelGGL(group_one_kernel, dim3(1), dim3(1024),
+                           16 * size_t(G) * sizeof(int32_t) + size_t(p.n_entries) * sizeof(uint16_t), stream, p, bits);
+        return hipGetLastError();
+    }
+    const int64_t chunk = group_chunk(p.n_entries, waves);
+    const int chunks = int(group_chunks(p.n_entries, G));
+    int32_t* hist = static_cast<int32_t*>(p.workspace);  // [chunks][n_groups], then the totals
+    int32_t* totals = hist + size_t(chunks) * G;
+    hipLaunchKernelGGL(group_count_kernel, dim3(chunks), dim3(64 * waves), size_t(G) * sizeof(int32_t), stream, p, chunk,
+                       hist);
+    hipLaunchKernelGGL(group_scan_kernel, dim3((G + 31) / 32), dim3(1024), 0, stream, p, chunks, hist, totals);
+    launch_place<16>(waves, p, chunks, chunk, hist, totals, bits, stream);
     return hipGetLastError();
 }
 

@@ -240,7 +240,8 @@ def _group_ref(ids, n_ids, first, n_trees):
 
 @pytest.mark.parametrize("E,n_ids,n_trees,first", [
     (1, 1, 1, 0), (1, 2048, 1, 2047), (2, 3, 2, -5), (63, 7, 1, 0), (64, 64, 1, 63), (65, 2, 1, 1), (1000, 1, 1, 0),
-    (1023, 33, 3, 100), (1025, 256, 1, 255), (4096, 512, 8, 511), (5000, 32768, 1, 32767), (16384, 64, 1, 63),
+    (1023, 33, 3, 100), (1025, 256, 1, 255), (4096, 512, 8, 511), (5000, 32768, 1, 32767), (40000, 32768, 1, 32767), (16384, 64, 1, 63), (16384, 1024, 1, 0), (16383, 1025, 1, 0),
+    (30000, 16384, 1, 0), (16384, 2048, 1, 2047), (2000000, 1000, 3, 0),
     (16385, 5, 1, 0), (40001, 4096, 8, 4095), (70000, 100, 1, -50), (300000, 2, 1, 0), (524288, 512, 8, 511)])
 def test_group_rows(fff_lib, E, n_ids, n_trees, first):
     gen = _gen(E)
@@ -266,8 +267,9 @@ def test_group_rows(fff_lib, E, n_ids, n_trees, first):
 
 
 def test_group_rows_nothing(fff_lib):
-    order, offsets = fff_lib.group_rows(torch.empty((0, 2), dtype=torch.int32, device=DEV), 5, n_trees=2)
-    assert order.numel() == 0 and torch.equal(offsets.cpu(), torch.zeros(11, dtype=torch.int32))
+    for n_ids in (5, 2048, 16384):
+        order, offsets = fff_lib.group_rows(torch.empty((0, 2), dtype=torch.int32, device=DEV), n_ids, n_trees=2)
+        assert order.numel() == 0 and torch.equal(offsets.cpu(), torch.zeros(2 * n_ids + 1, dtype=torch.int32))
 
 
 # ------------------------------------------------------------------------------------- grouped products

@@ -115,7 +115,7 @@ def test_dropout_refusals(lib, over):
     _refused(lib, "fff_dropout", _fill(ops.FffDropoutArgs, DROP, over), INVALID)
 
 
-GROUP = dict(ids=P, order=2 * P, offsets=3 * P, bad_ids=4 * P, n_entries=100, n_ids=16, n_trees=2, first=15,
+GROUP = dict(ids=P, order=2 * P, offsets=3 * P, bad_ids=4 * P, n_entries=100000, n_ids=16, n_trees=2, first=15,
              workspace=5 * P, workspace_bytes=1 << 24)
 
 
