@@ -526,7 +526,7 @@ typedef struct {
     void* y;                /* [y_rows, n] (y_dtype) */
     void* z_out;            /* [n_entries, n] (z_dtype), or NULL */
     const void* z_in;       /* [n_entries, n] (z_dtype), or NULL; not with z_out */
-    int64_t n_entries, x_rows, y_rows; /* below 2^31; without an index at least n_entries rows */
+    int64_t n_entries, x_rows, y_rows; /* below 2^31; x_rows >= 1; without an index a row for every entry */
     int32_t n_groups, k, n;
     int32_t x_div;          /* >= 1 */
     int32_t w_transposed;

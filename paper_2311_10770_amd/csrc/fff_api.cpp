@@ -829,7 +829,8 @@ FFF_EXPORT int fff_grouped_matmul(const fff_grouped_matmul_args* a) {
     if (E == 0) return FFF_OK;
     // without an index entry i reads row i / x_div of x
     const int64_t x_direct = (E - 1) / a->x_div + 1;
-    if (!rows_ok(a->x_rows, x_direct, a->x_index) || !rows_ok(a->y_rows, E, a->y_index)) return FFF_ERR_INVALID_ARG;
+    if (a->x_rows < 1 || !rows_ok(a->x_rows, x_direct, a->x_index) || !rows_ok(a->y_rows, E, a->y_index))
+        return FFF_ERR_INVALID_ARG;
     if (!a->x || !a->w || !a->offsets || !a->y || (a->z_in && a->z_out)) return FFF_ERR_INVALID_ARG;
     for (const void* q : {a->x, a->w, static_cast<const void*>(a->y), static_cast<const void*>(a->z_out), a->z_in})
         if (!aligned16(q)) return FFF_ERR_INVALID_ARG;
@@ -889,7 +890,8 @@ FFF_EXPORT int fff_grouped_weight_grad(const fff_grouped_weight_grad_args* a) {
     if (!a->dw || !a->offsets) return FFF_ERR_INVALID_ARG;
     if (E > 0) {
         const int64_t x_direct = (E - 1) / a->x_div + 1;
-        if (!rows_ok(a->x_rows, x_direct, a->x_index) || !rows_ok(a->dy_rows, E, a->dy_index))
+        if (a->x_rows < 1 || a->dy_rows < 1 || !rows_ok(a->x_rows, x_direct, a->x_index) ||
+            !rows_ok(a->dy_rows, E, a->dy_index))
             return FFF_ERR_INVALID_ARG;
         if (!a->dy || !a->x) return FFF_ERR_INVALID_ARG;
     }

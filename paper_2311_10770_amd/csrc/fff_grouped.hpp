@@ -1,0 +1,284 @@
+// fff_grouped.hpp -- what the grouped products' kernels share: the tile lookup
+// over ragged groups, operand tiles in LDS and the matrix-core loop.
+//
+// Every product is C[BM, BN] += A[BM, red] B[BN, red]^T over a reduction axis,
+// one step of ROWB bytes of it per row at a time.  An operand whose rows run
+// along the reduction axis ("row" tiles: x, and W as [n, k]) lies in LDS as BM
+// or BN rows of ROWB bytes; one whose rows run across it ("column" tiles: W as
+// [k, n], and both operands of a weight gradient) as steps of reduction rows,
+// read back transposed.  Tiles are staged 16 bytes a lane, straight from
+// global memory (global_load_lds, S - 1 steps ahead) where rows are 16-byte
+// aligned, else through registers, which takes rows at any element.
+#pragma once
+
+#include "fff_device.hpp"
+#include "fff_gemm.hpp"
+#include "fff_internal.hpp"
+#include "fff_rows.hpp"
+
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cstdint>
+
+namespace fff {
+
+// Entries [lo, hi) of group g: within [0, n_entries], empty where the offsets fall.
+__device__ __forceinline__ void group_range(const int32_t* offsets, int64_t n_entries, int g, int64_t* lo, int64_t* hi) {
+    const int64_t a = offsets[g], b = offsets[g + 1];
+    *lo = a < 0 ? 0 : a > n_entries ? n_entries : a;
+    *hi = b < *lo ? *lo : b > n_entries ? n_entries : b;
+}
+
+struct Tile {
+    int g;           // group, or -1: no tile of this number
+    int n0;          // first column
+    int64_t m0, m1;  // its entries
+};
+
+// Tile of workgroup h among row tiles of bm entries (groups in order, each group's last one partly
+// filled) times tn column tiles of bn: every thread sums the row tiles of a few consecutive groups, the
+// workgroup scans the sums, and the thread whose groups hold the row tile finds it.  Workgroup h runs
+// on XCD h % 8: each XCD takes a contiguous range of the tiles, MB row tiles deep before the next
+// column tile, so that a CU's neighbours share rows and columns in their L2.
+template <int THREADS>
+__device__ __forceinline__ Tile find_tile(const int32_t* offsets, int n_groups, int64_t n_entries, int bm, int bn, int tn,
+                                          int64_t h) {
+    constexpr int64_t MB = 8;
+    __shared__ int64_t wave_sum[THREADS / 64];
+    __shared__ Tile found;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int per = (n_groups + THREADS - 1) / THREADS;
+    const int g0 = std::min(n_groups, tid * per), g1 = std::min(n_groups, g0 + per);
+    int64_t mine = 0, lo, hi;
+    for (int g = g0; g < g1; ++g) {
+        group_range(offsets, n_entries, g, &lo, &hi);
+        mine += (hi - lo + bm - 1) / bm;
+    }
+    int64_t run = mine;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const int64_t v = __shfl_up(run, d);
+        if (lane >= d) run += v;
+    }
+    if (lane == 63) wave_sum[wave] = run;
+    if (tid == 0) found.g = -1;
+    __syncthreads();
+    int64_t total = 0;
+    for (int w = 0; w < THREADS / 64; ++w) {
+        if (w < wave) run += wave_sum[w];
+        total += wave_sum[w];
+    }
+    if (h < total * tn) {
+        const int64_t t = xcd_tile(h, total * tn), block = t / (MB * tn), in = t - block * (MB * tn);
+        const int64_t deep = std::min<int64_t>(MB, total - block * MB);
+        const int64_t mt = block * MB + in % deep;
+        int64_t at = run - mine;
+        if (at <= mt && mt < run) {
+            for (int g = g0; g < g1; ++g) {
+                group_range(offsets, n_entries, g, &lo, &hi);
+                const int64_t tiles = (hi - lo + bm - 1) / bm;
+                if (mt < at + tiles) {
+                    found.g = g;
+                    found.n0 = int(in / deep) * bn;
+                    found.m0 = lo + (mt - at) * bm;
+                    found.m1 = hi;
+                    break;
+                }
+                at += tiles;
+            }
+        }
+    }
+    __syncthreads();
+    return found;
+}
+
+// Most row tiles of bm entries that n_entries in n_groups groups can make.
+inline int64_t most_tiles(int64_t n_entries, int32_t n_groups, int bm) {
+    return n_entries / bm + std::min<int64_t>(n_groups, n_entries);
+}
+
+// Row that entry i reads or writes, or -1 where there is none.
+__device__ __forceinline__ int64_t entry_row(const int32_t* index, int div, int64_t rows, int64_t i) {
+    const int64_t v = index ? index[i] : i;
+    if (v < 0) return -1;
+    const int64_t r = div == 1 ? v : uint32_t(v) / uint32_t(div);
+    return r < rows ? r : -1;
+}
+
+// Sixteen zero bytes: what a lane stages for places outside its matrix.
+static __device__ const uint4 g_zero16 = {0, 0, 0, 0};
+
+// Sixteen bytes of a row from element e of `left` (elements behind it zero); rows at any element.
+template <bool BF>
+__device__ __forceinline__ uint4 load16(const char* p, int64_t left) {
+    constexpr int EV = BF ? 8 : 4;
+    typedef uint32_t u4_a2 __attribute__((ext_vector_type(4), aligned(2)));
+    typedef uint32_t u4_a4 __attribute__((ext_vector_type(4), aligned(4)));
+    if (left >= EV) {
+        if constexpr (BF) {
+            const u4_a2 v = *reinterpret_cast<const u4_a2*>(p);
+            return make_uint4(v.x, v.y, v.z, v.w);
+        } else {
+            const u4_a4 v = *reinterpret_cast<const u4_a4*>(p);
+            return make_uint4(v.x, v.y, v.z, v.w);
+        }
+    }
+    uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int j = 0; j < EV - 1; ++j) {
+        if (j >= left) continue;
+        if constexpr (BF) w[j >> 1] |= uint32_t(reinterpret_cast<const uint16_t*>(p)[j]) << (16 * (j & 1));
+        else w[j] = reinterpret_cast<const uint32_t*>(p)[j];
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// Order of the 16-byte vectors in LDS: vector v of row r at v ^ key, so that the lanes of a fragment
+// read fall on different banks.
+// Row tiles: a b128 read serves eight consecutive rows and two adjacent vectors at once.
+template <int ROWB>
+__device__ __forceinline__ int row_key(int r) {
+    static_assert(ROWB == 64 || ROWB == 128, "four or eight vectors a row");
+    return ROWB == 128 ? swz32(r & 15) : ((r >> 2) & 1) * 2;
+}
+// Column tiles of C columns, bf16: a transposing read takes four rows and four adjacent vectors, or
+// eight rows (0..3, 8..11) and two; fp32: 32 columns of rows r and r + 4.
+template <bool BF, int C>
+__device__ __forceinline__ int col_key(int r) {
+    if constexpr (!BF) return ((r >> 2) & 1) * 8;
+    else if constexpr (C >= 128) return (r & 3) * 4 ^ ((r >> 3) & 1) * 2;
+    else return ((r >> 1) & 1) * 4 ^ ((r >> 3) & 1) * 2;
+}
+
+// Fragments of reduction slice kk (32 bytes' worth: 16 bf16 or 8 fp32) of a 32-row MFMA operand, as the
+// sixteen bytes lane l holds: row l % 32, elements 8 (l / 32) on (fp32: 4 (l / 32) on).
+template <int ROWB>
+__device__ __forceinline__ uint4 row_frag(const unsigned char* tile, int row0, int kk, int lane) {
+    const int r = row0 + (lane & 31);
+    return *reinterpret_cast<const uint4*>(tile + r * ROWB + (((2 * kk + (lane >> 5)) ^ row_key<ROWB>(r)) * 16));
+}
+template <bool BF, int C>
+__device__ __forceinline__ uint4 col_frag(const unsigned char* tile, int col0, int kk, int lane) {
+    if constexpr (BF) {
+        // A transposing read hands lane i of sixteen column i of the 4 x 16 block their addresses cover
+        // (lane i: row i / 4, columns 4 (i % 4) .. +3); two of them give eight reduction rows.
+        typedef short s4 __attribute__((ext_vector_type(4)));
+        typedef __attribute__((address_space(3))) s4* lds_s4;
+        const int grp = lane >> 4, i = lane & 15;
+        uint2 u[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int r = 16 * kk + 8 * (grp >> 1) + 4 * h + (i >> 2);
+            const int c = col0 / 8 + 2 * (grp & 1) + ((i & 3) >> 1);
+            u[h] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                                 (lds_s4)(tile + r * (C * 2) + ((c ^ col_key<true, C>(r)) * 16) + (i & 1) * 8)));
+        }
+        return make_uint4(u[0].x, u[0].y, u[1].x, u[1].y);
+    } else {
+        uint32_t w[4];
+        const int c = col0 + (lane & 31);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            const int r = 8 * kk + 4 * (lane >> 5) + t;
+            w[t] = *reinterpret_cast<const uint32_t*>(tile + r * (C * 4) + (((c >> 2) ^ col_key<false, C>(r)) * 16) + (c & 3) * 4);
+        }
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+}
+
+// c += a b over one slice: one 32 x 32 x 16 MFMA in bf16; in fp32 four 32 x 32 x 2, the t-th on
+// element t of both operands' vectors (a permutation of the slice's reduction indices).
+template <bool BF>
+__device__ __forceinline__ void mfma_slice(tile_v16f& c, const uint4& a, const uint4& b) {
+    if constexpr (BF) {
+        c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c,
+                                                    0, 0, 0);
+    } else {
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+            c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(word(a, t)), __uint_as_float(word(b, t)), c, 0, 0, 0);
+    }
+}
+
+// Shape of a workgroup's tile: WGM x WGN waves of TM x TN 32 x 32 blocks, S stages of ROWB bytes a row.
+template <bool BF_, int TM_, int TN_, int WGM_, int WGN_, int S_, int ROWB_>
+struct GCfg {
+    static constexpr bool BF = BF_;
+    static constexpr int TM = TM_, TN = TN_, WGM = WGM_, WGN = WGN_, S = S_, ROWB = ROWB_;
+    static constexpr int BM = 32 * TM * WGM, BN = 32 * TN * WGN;
+    static constexpr int WAVES = WGM * WGN, THREADS = 64 * WAVES;
+    static constexpr int ESZ = BF ? 2 : 4, EV = 16 / ESZ;
+    static constexpr int KS = ROWB / ESZ;      // reduction elements a step
+    static constexpr int SLICES = ROWB / 32;
+    static constexpr int LA = BM * ROWB / 1024 / WAVES, LB = BN * ROWB / 1024 / WAVES;  // wave loads a step
+    static constexpr int LPS = LA + LB;
+    static constexpr int STAGE = (BM + BN) * ROWB;
+    static constexpr size_t LDS = size_t(S) * STAGE;
+    static_assert(BM * ROWB % (1024 * WAVES) == 0 && BN * ROWB % (1024 * WAVES) == 0, "whole wave loads");
+    static_assert(LPS * (S - 2) <= 63, "vmcnt holds 6 bits");
+};
+
+// The matrix-core loop over `steps` steps.  issue(step, stage) starts (DMA) the loads of a step into its
+// stage or, without DMA, reads them into registers, which commit(stage) stores; ACOL, BCOL: column
+// tiles.  The wave's TM x TN blocks are summed into acc.
+template <class G, bool DMA, bool ACOL, bool BCOL, class Issue, class Commit>
+__device__ __forceinline__ void grouped_loop(unsigned char* lds, int64_t steps, tile_v16f (&acc)[G::TM][G::TN],
+                                             Issue issue, Commit commit) {
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave / G::WGN, wn = wave % G::WGN;
+    auto compute = [&](const unsigned char* st) {
+        uint4 fa[2][G::TM], fb[2][G::TN];
+        auto read = [&](int kk, int buf) {
+#pragma unroll
+            for (int j = 0; j < G::TN; ++j) {
+                const int c0 = (wn * G::TN + j) * 32;
+                if constexpr (BCOL) fb[buf][j] = col_frag<G::BF, G::BN>(st + G::BM * G::ROWB, c0, kk, lane);
+                else fb[buf][j] = row_frag<G::ROWB>(st + G::BM * G::ROWB, c0, kk, lane);
+            }
+#pragma unroll
+            for (int i = 0; i < G::TM; ++i) {
+                const int r0 = (wm * G::TM + i) * 32;
+                if constexpr (ACOL) fa[buf][i] = col_frag<G::BF, G::BM>(st, r0, kk, lane);
+                else fa[buf][i] = row_frag<G::ROWB>(st, r0, kk, lane);
+            }
+        };
+        // the fragments of slice kk + 1 are read while slice kk's MFMAs run
+        read(0, 0);
+#pragma unroll
+        for (int kk = 0; kk < G::SLICES; ++kk) {
+            if (kk + 1 < G::SLICES) read(kk + 1, (kk + 1) & 1);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < G::TM; ++i)
+#pragma unroll
+                for (int j = 0; j < G::TN; ++j) mfma_slice<G::BF>(acc[i][j], fa[kk & 1][i], fb[kk & 1][j]);
+        }
+    };
+    if constexpr (DMA) {
+#pragma unroll
+        for (int s = 0; s < G::S - 1; ++s)
+            if (s < steps) issue(s, s);
+        int stage = 0, ahead = G::S - 1;  // stages of step s and of step s + S - 1
+        for (int64_t s = 0; s < steps; ++s) {
+            const int64_t left = steps - 1 - s;
+            wait_steps<G::S - 2, G::LPS>(int(left < G::S - 2 ? left : G::S - 2));
+            __syncthreads();  // step s is in LDS for every wave; every wave is done with step s - 1
+            if (s + G::S - 1 < steps) issue(s + G::S - 1, ahead);
+            compute(lds + stage * G::STAGE);
+            stage = stage + 1 == G::S ? 0 : stage + 1;
+            ahead = ahead + 1 == G::S ? 0 : ahead + 1;
+        }
+    } else {
+        issue(0, 0);
+        for (int64_t s = 0; s < steps; ++s) {
+            commit(int(s & 1));
+            __syncthreads();  // step s is in LDS; step s - 1, two commits back, is done with
+            if (s + 1 < steps) issue(s + 1, 0);
+            compute(lds + (s & 1) * G::STAGE);
+        }
+    }
+}
+
+}  // namespace fff

@@ -138,7 +138,7 @@ PRODUCT = dict(x=P, w=2 * P, offsets=3 * P, x_index=4 * P, y_index=5 * P, y=6 * 
     (dict(n_entries=-1), INVALID), (dict(n_entries=1 << 31), INVALID), (dict(n_groups=0), INVALID), (dict(k=0), INVALID),
     (dict(n=0), INVALID), (dict(x_div=0), INVALID), (dict(x_dtype=2), INVALID), (dict(w_dtype=2), INVALID),
     (dict(y_dtype=2), INVALID), (dict(z_dtype=2), INVALID), (dict(act=3), INVALID), (dict(w_transposed=2), INVALID),
-    (dict(x_rows=-1), INVALID), (dict(x_index=None, x_rows=9), INVALID), (dict(y_index=None, y_rows=9), INVALID),
+    (dict(x_rows=-1), INVALID), (dict(x_rows=0), INVALID), (dict(x_index=None, x_rows=9), INVALID), (dict(y_index=None, y_rows=9), INVALID),
     (dict(x_rows=1 << 31), INVALID), (dict(x=None), INVALID), (dict(w=None), INVALID), (dict(offsets=None), INVALID),
     (dict(y=None), INVALID), (dict(z_in=8 * P), INVALID), (dict(x=P + 4), INVALID), (dict(w=P + 4), INVALID),
     (dict(offsets=P + 2), INVALID), (dict(x_index=P + 2), INVALID), (dict(y=P), INVALID), (dict(y=2 * P + 16), INVALID),
@@ -157,7 +157,7 @@ GRAD = dict(dy=P, x=2 * P, offsets=3 * P, dy_index=4 * P, x_index=5 * P, dw=6 * 
     (dict(n_entries=-1), INVALID), (dict(n_entries=1 << 31), INVALID), (dict(n_groups=0), INVALID), (dict(k=0), INVALID),
     (dict(n=0), INVALID), (dict(x_div=0), INVALID), (dict(dy_dtype=2), INVALID), (dict(x_dtype=2), INVALID),
     (dict(accumulate=2), INVALID), (dict(dy=None), INVALID), (dict(x=None), INVALID), (dict(offsets=None), INVALID),
-    (dict(dw=None), INVALID), (dict(dy=P + 4), INVALID), (dict(dw=P + 4), INVALID), (dict(dy_index=None, dy_rows=9), INVALID),
+    (dict(dw=None), INVALID), (dict(x_rows=0), INVALID), (dict(dy_rows=0), INVALID), (dict(dy=P + 4), INVALID), (dict(dw=P + 4), INVALID), (dict(dy_index=None, dy_rows=9), INVALID),
     (dict(x_index=None, x_rows=9), INVALID), (dict(dw=P), INVALID), (dict(dw=2 * P + 32), INVALID), (dict(dw=4 * P), INVALID),
     (dict(dy_dtype=1), UNSUPPORTED)])
 def test_grouped_weight_grad_refusals(lib, over, code):
