@@ -515,7 +515,7 @@ size_t fff_group_rows_workspace_bytes(int64_t n_entries, int32_t n_ids, int32_t 
  * taken as empty where they fall, an x_index outside x reads a row of zeros,
  * and a y_index outside y stores nothing.  x and W are both bf16 (MFMA on
  * bf16, fp32 sums) or both fp32; anything else is FFF_ERR_UNSUPPORTED.  Any
- * k >= 1 and n >= 1.
+ * k and n from 1 to 2^28 - 1.
  */
 typedef struct {
     const void* x;          /* [x_rows, k] (x_dtype) */

@@ -619,6 +619,7 @@ fff::DropRng drop_rng(const fff_dropout_rng& d) {
 
 constexpr int64_t kMaxRows = int64_t(1) << 32;     // dropout's counter holds 32 bits of the row
 constexpr int64_t kMaxEntries = int64_t(1) << 31;  // entries and indices are int32
+constexpr int32_t kMaxWidth = 1 << 28;              // rows of the grouped products: 31 bits of bytes
 
 hipStream_t stream_of(void* s) { return reinterpret_cast<hipStream_t>(s); }
 
@@ -811,7 +812,8 @@ FFF_EXPORT int fff_group_rows(const fff_group_rows_args* a) {
 namespace {
 // Sizes common to the grouped products.
 bool grouped_sizes_ok(int64_t n_entries, int32_t n_groups, int32_t k, int32_t n, int32_t x_div) {
-    return n_entries >= 0 && n_entries < kMaxEntries && n_groups >= 1 && k >= 1 && n >= 1 && x_div >= 1;
+    return n_entries >= 0 && n_entries < kMaxEntries && n_groups >= 1 && k >= 1 && k < kMaxWidth && n >= 1 &&
+           n < kMaxWidth && x_div >= 1;
 }
 // Rows of a matrix that entries read or write, directly or through an index.
 bool rows_ok(int64_t rows, int64_t n_entries, const int32_t* index) {

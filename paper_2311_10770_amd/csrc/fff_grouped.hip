@@ -6,7 +6,7 @@
 // most row tiles there can be and every workgroup finds its tile from the
 // offsets (find_tile).  The product runs on the matrix cores
 // (fff_grouped.hpp); its 32 x 32 blocks then pass through LDS, so that the
-// epilogue works on four consecutive columns a lane and stores whole lines.
+// epilogue works on eight consecutive columns a lane and stores whole lines.
 #include "fff_grouped.hpp"
 
 namespace fff {
@@ -15,76 +15,132 @@ namespace {
 
 enum { ST_OK_ = 0, ST_UNSUPPORTED_ = -2 };
 
-// Epilogue and store of four columns n .. n + 3 of entry i (left: columns in the row from n on).
-__device__ __forceinline__ void grouped_store4(const GroupedParams& p, int64_t i, int32_t dst, int n, float* z) {
-    const int left = p.n - n;
-    if (p.z_in) {
-        float d[4];
-        unpack4(d, load4<false>(p.z_in, p.z_bf16, i * p.n + n, left), p.z_bf16);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) z[j] *= activation_grad(d[j], p.act);
-    } else {
-        if (p.z_out) store4<false>(p.z_out, p.z_bf16, i * p.n + n, left, z);
-        if (p.act != ACT_IDENTITY) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) z[j] = activation(z[j], p.act);
+// What becomes of z (grouped_rows).
+enum { EPI_STORE = 0, EPI_GELU = 1, EPI_TANH = 2, EPI_GELU_GRAD = 3, EPI_TANH_GRAD = 4 };
+
+// Eight consecutive values of a row; `left` of them in it where not FULL.
+template <bool FULL>
+__device__ __forceinline__ void put8(char* row, int bf, int col, int left, const float* v) {
+    if (bf) {
+        if (FULL || left >= 8) {
+            typedef uint32_t u4_a2 __attribute__((ext_vector_type(4), aligned(2)));
+            *reinterpret_cast<u4_a2*>(row + col * 2) = u4_a2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]),
+                                                             pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
+            return;
         }
+    } else if (FULL || left >= 8) {
+        typedef float f4_a4 __attribute__((ext_vector_type(4), aligned(4)));
+        reinterpret_cast<f4_a4*>(row + col * 4)[0] = f4_a4{v[0], v[1], v[2], v[3]};
+        reinterpret_cast<f4_a4*>(row + col * 4)[1] = f4_a4{v[4], v[5], v[6], v[7]};
+        return;
     }
-    if (dst >= 0) store4<false>(p.y, p.y_bf16, int64_t(dst) * p.n + n, left, z);
+    if constexpr (!FULL) {
+        store4<false>(row, bf, col, left, v);
+        store4<false>(row, bf, col + 4, left - 4, v + 4);
+    }
 }
 
-// A workgroup per tile.  BCOL: W is [k, n].
-template <class G, bool DMA, bool BCOL>
-__global__ __launch_bounds__(G::THREADS, 2 * G::THREADS / 256) void grouped_kernel(GroupedParams p) {
-    extern __shared__ __align__(16) unsigned char glds[];
-    __shared__ int32_t s_dst[G::BM];   // row of y, or -1
-    __shared__ uint8_t s_src[G::BM];   // whether the entry has a row of x
-    const Tile t = find_tile<G::THREADS>(p.offsets, p.n_groups, p.n_entries, G::BM, G::BN, (p.n + G::BN - 1) / G::BN,
-                                         blockIdx.x);
-    if (t.g < 0) return;
-    const int tid = threadIdx.x, lane = tid & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    for (int r = tid; r < G::BM; r += G::THREADS) {
-        const int64_t i = t.m0 + r;
-        s_dst[r] = i < t.m1 ? int32_t(entry_row(p.y_index, 1, p.y_rows, i)) : -1;
-    }
-
-    // this lane's sources: A rows through the index (rows behind the tile and absent ones read row 0),
-    // B rows of [n, k] or reduction rows of [k, n] (columns behind n read the last ones or zeros)
-    const char* x = static_cast<const char*>(p.x);
-    const char* w = static_cast<const char*>(p.w) + int64_t(t.g) * p.n * p.k * G::ESZ;
-    constexpr int RPL = 1024 / G::ROWB, VPR = G::ROWB / 16;  // rows and vectors per row of a wave load
-    const char* pa[G::LA];
-    const char* pb[G::LB];
-    int va[G::LA], vb[G::LB];  // first reduction element of the lane's vector (BCOL's B: its row)
+// Epilogue and store of sixteen rows of a tile from row m0 on, COLS columns from n0 on, out of the
+// wave's LDS: eight columns a lane.  FULL: all these columns are in the matrix.  The instructions of
+// this loop are what the epilogue costs: offsets are one 32 x 32 + 64 bit product, and rows without
+// a row of x are looked for in tiles that have some (bad).
+template <int KIND, bool FULL, int COLS, int PITCH>
+__device__ __forceinline__ void grouped_rows(const GroupedParams& p, const float* blk, int m0, int rows, int64_t e0, int n0,
+                                             const int32_t* s_dst, const uint8_t* s_src, bool bad) {
+    constexpr int LPR = COLS / 8, RPI = 64 / LPR, U = 16 / RPI;
+    const int lane = threadIdx.x & 63, c = lane % LPR * 8, n = n0 + c, left = p.n - n;
+    if (!FULL && left <= 0) return;
+    const uint32_t ypitch = uint32_t(p.n) << (p.y_bf16 ? 1 : 2), zpitch = uint32_t(p.n) << (p.z_bf16 ? 1 : 2);
+    const uint32_t ze = uint32_t(e0);  // entries are below 2^31
+    Raw4 d[U][2];
+    if constexpr (KIND >= EPI_GELU_GRAD) {
 #pragma unroll
-    for (int i = 0; i < G::LA; ++i) {
-        const int r = (wave * G::LA + i) * RPL + lane / VPR, v = (lane % VPR) ^ row_key<G::ROWB>(r);
-        const int64_t e = t.m0 + r;
-        const int64_t src = e < t.m1 ? entry_row(p.x_index, p.x_div, p.x_rows, e) : -1;
-        if (lane % VPR == 0) s_src[r] = src >= 0;
-        va[i] = v * G::EV;
-        pa[i] = x + (src >= 0 ? src : 0) * p.k * G::ESZ + v * 16;
-    }
-    constexpr int CPL = G::BN * G::ESZ / 16;  // vectors of a column tile's row
-#pragma unroll
-    for (int i = 0; i < G::LB; ++i) {
-        if constexpr (BCOL) {
-            const int at = (wave * G::LB + i) * 64 + lane, r = at / CPL, v = (at % CPL) ^ col_key<G::BF, G::BN>(r);
-            vb[i] = r;
-            pb[i] = w + (int64_t(r) * p.n + t.n0 + v * G::EV) * G::ESZ;
-        } else {
-            const int r = (wave * G::LB + i) * RPL + lane / VPR, v = (lane % VPR) ^ row_key<G::ROWB>(r);
-            const int n = t.n0 + r < p.n ? t.n0 + r : p.n - 1;
-            vb[i] = v * G::EV;
-            pb[i] = w + int64_t(n) * p.k * G::ESZ + v * 16;
+        for (int u = 0; u < U; ++u) {
+            const int m = m0 + u * RPI + lane / LPR;
+            if (m >= rows) continue;
+            const char* row = static_cast<const char*>(p.z_in) + uint64_t(ze + m) * zpitch;
+            d[u][0] = load4<FULL>(row, p.z_bf16, n, left);
+            d[u][1] = load4<FULL>(row, p.z_bf16, n + 4, left - 4);
         }
     }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int rr = u * RPI + lane / LPR, m = m0 + rr;
+        const float4 a = *reinterpret_cast<const float4*>(blk + rr * PITCH + c);
+        const float4 b = *reinterpret_cast<const float4*>(blk + rr * PITCH + c + 4);
+        float z[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+        const int32_t dst = s_dst[m];
+        if (bad && !s_src[m]) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) z[j] = 0.0f;
+        }
+        if (m >= rows) continue;
+        if constexpr (KIND >= EPI_GELU_GRAD) {
+            float g[8];
+            unpack4(g, d[u][0], p.z_bf16);
+            unpack4(g + 4, d[u][1], p.z_bf16);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) z[j] *= act_slope<KIND == EPI_GELU_GRAD ? ACT_GELU_ERF : ACT_GELU_TANH>(g[j]);
+        } else {
+            if (p.z_out) put8<FULL>(static_cast<char*>(p.z_out) + uint64_t(ze + m) * zpitch, p.z_bf16, n, left, z);
+            constexpr int ACT = KIND == EPI_GELU ? ACT_GELU_ERF : KIND == EPI_TANH ? ACT_GELU_TANH : ACT_IDENTITY;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) z[j] = act_value<ACT>(z[j]);
+        }
+        if (dst >= 0) put8<FULL>(static_cast<char*>(p.y) + uint64_t(uint32_t(dst)) * ypitch, p.y_bf16, n, left, z);
+    }
+}
+template <int COLS, int PITCH, bool FULL>
+__device__ __forceinline__ void grouped_epilogue(int kind, const GroupedParams& p, const float* blk, int m0, int rows,
+                                                 int64_t e0, int n0, const int32_t* dst, const uint8_t* src, bool bad) {
+    switch (kind) {
+        case EPI_GELU: return grouped_rows<EPI_GELU, FULL, COLS, PITCH>(p, blk, m0, rows, e0, n0, dst, src, bad);
+        case EPI_TANH: return grouped_rows<EPI_TANH, FULL, COLS, PITCH>(p, blk, m0, rows, e0, n0, dst, src, bad);
+        case EPI_GELU_GRAD: return grouped_rows<EPI_GELU_GRAD, FULL, COLS, PITCH>(p, blk, m0, rows, e0, n0, dst, src, bad);
+        case EPI_TANH_GRAD: return grouped_rows<EPI_TANH_GRAD, FULL, COLS, PITCH>(p, blk, m0, rows, e0, n0, dst, src, bad);
+        default: return grouped_rows<EPI_STORE, FULL, COLS, PITCH>(p, blk, m0, rows, e0, n0, dst, src, bad);
+    }
+}
+
+// Workgroups take tiles gridDim.x apart.  BCOL: W is [k, n].  The next tile is looked up while this one
+// is multiplied, and its first step is on its way to LDS (DMA) while this one's results are stored.
+template <class G, bool DMA, bool BCOL>
+__global__ __launch_bounds__(G::THREADS, 2) void grouped_kernel(GroupedParams p) {
+    extern __shared__ __align__(16) unsigned char glds[];
+    __shared__ int32_t s_dst[2][G::BM];   // row of y, or -1
+    __shared__ uint8_t s_src[2][G::BM];   // whether the entry has a row of x
+    __shared__ Tile s_tile[2];
+    __shared__ int s_sum[G::WAVES], s_bad[2];
+    TileMap<G::THREADS> map{p.offsets, p.n_entries, p.n_groups, G::BM, G::BN, (p.n + G::BN - 1) / G::BN};
+    map.init(s_sum);
+    int64_t h = blockIdx.x;
+    map.find(h, &s_tile[0]);
+    if (threadIdx.x == 0) s_bad[0] = 0;
+    __syncthreads();
+
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const char* x = static_cast<const char*>(p.x);
+    constexpr int RPL = 1024 / G::ROWB, VPR = G::ROWB / 16;  // rows and vectors per row of a wave load
+    constexpr int CPL = G::BN * G::ESZ / 16;                 // vectors of a column tile's row
     const int64_t steps = (p.k + G::KS - 1) / G::KS;
     const int64_t bstep = BCOL ? int64_t(G::KS) * p.n * G::ESZ : G::ROWB;
-    uint4 ra[DMA ? 1 : G::LA], rb[DMA ? 1 : G::LB];
     const uint32_t lds0 = uint32_t(uintptr_t((__attribute__((address_space(3))) unsigned char*)glds));
     const char* zero = reinterpret_cast<const char*>(&g_zero16);
+
+    // this lane's sources: A rows through the index (rows behind the tile and absent ones read row 0),
+    // B rows of [n, k] (rows behind n read the last one) or reduction rows of [k, n]
+    const char* pa[G::LA];
+    const char* pb[G::LB];
+    int n0 = 0;
+    // reduction element of a row vector's first element; row and column of a column tile's vector
+    auto row_at = [&](int i) { return (lane % VPR ^ row_key<G::ROWB>(i * RPL + lane / VPR)) * G::EV; };
+    auto col_row = [&](int i) { return (i * 64 + lane) / CPL; };
+    auto col_at = [&](int i) {
+        const int at = i * 64 + lane;
+        return (at % CPL ^ col_key<G::BF, G::BN>(at / CPL)) * G::EV;
+    };
+    uint4 ra[DMA ? 1 : G::LA], rb[DMA ? 1 : G::LB];
     auto issue = [&](int64_t s, int stage) {
         const bool part = s == steps - 1 && p.k % G::KS != 0;
         const int k0 = int(s) * G::KS;
@@ -92,30 +148,28 @@ __global__ __launch_bounds__(G::THREADS, 2 * G::THREADS / 256) void grouped_kern
             const uint32_t st = lds0 + uint32_t(stage) * G::STAGE;
 #pragma unroll
             for (int i = 0; i < G::LA; ++i)
-                lds_dma16(part && k0 + va[i] >= p.k ? zero : pa[i] + s * G::ROWB, st + (wave * G::LA + i) * 1024);
+                lds_dma16(part && k0 + row_at(wave * G::LA + i) >= p.k ? zero : pa[i] + s * G::ROWB,
+                          st + (wave * G::LA + i) * 1024);
 #pragma unroll
             for (int i = 0; i < G::LB; ++i) {
+                const int w = wave * G::LB + i;
                 const char* q = pb[i] + s * bstep;
                 if constexpr (BCOL) {
-                    const int at = (wave * G::LB + i) * 64 + lane, r = at / CPL;
-                    const int n = t.n0 + ((at % CPL) ^ col_key<G::BF, G::BN>(r)) * G::EV;
-                    if (n >= p.n || (part && k0 + vb[i] >= p.k)) q = zero;
+                    if (n0 + col_at(w) >= p.n || (part && k0 + col_row(w) >= p.k)) q = zero;
                 } else {
-                    if (part && k0 + vb[i] >= p.k) q = zero;
+                    if (part && k0 + row_at(w) >= p.k) q = zero;
                 }
-                lds_dma16(q, st + G::BM * G::ROWB + (wave * G::LB + i) * 1024);
+                lds_dma16(q, st + G::BM * G::ROWB + w * 1024);
             }
         } else {
 #pragma unroll
-            for (int i = 0; i < G::LA; ++i) ra[i] = load16<G::BF>(pa[i] + s * G::ROWB, int64_t(p.k) - k0 - va[i]);
+            for (int i = 0; i < G::LA; ++i)
+                ra[i] = load16<G::BF>(pa[i] + s * G::ROWB, int64_t(p.k) - k0 - row_at(wave * G::LA + i));
 #pragma unroll
             for (int i = 0; i < G::LB; ++i) {
-                int64_t left = int64_t(p.k) - k0 - vb[i];
-                if constexpr (BCOL) {
-                    const int at = (wave * G::LB + i) * 64 + lane, r = at / CPL;
-                    const int n = t.n0 + ((at % CPL) ^ col_key<G::BF, G::BN>(r)) * G::EV;
-                    left = left > 0 ? int64_t(p.n) - n : 0;
-                }
+                const int w = wave * G::LB + i;
+                int64_t left = int64_t(p.k) - k0 - (BCOL ? col_row(w) : row_at(w));
+                if constexpr (BCOL) left = left > 0 ? int64_t(p.n) - n0 - col_at(w) : 0;
                 rb[i] = load16<G::BF>(pb[i] + s * bstep, left);
             }
         }
@@ -130,49 +184,99 @@ __global__ __launch_bounds__(G::THREADS, 2 * G::THREADS / 256) void grouped_kern
                 *reinterpret_cast<uint4*>(st + G::BM * G::ROWB + (wave * G::LB + i) * 1024 + lane * 16) = rb[i];
         }
     };
-    tile_v16f acc[G::TM][G::TN];
+    // a tile's sources, its rows' records in buffer `buf`, and the loads of its first step
+    auto begin = [&](const Tile& t, int buf) {
+        n0 = t.n0;
+        const char* w = static_cast<const char*>(p.w) + int64_t(t.g) * p.n * p.k * G::ESZ;
 #pragma unroll
-    for (int i = 0; i < G::TM; ++i)
+        for (int i = 0; i < G::LA; ++i) {
+            const int r = (wave * G::LA + i) * RPL + lane / VPR;
+            const int64_t e = t.m0 + r;
+            const int64_t src = e < t.m1 ? entry_row(p.x_index, p.x_div, p.x_rows, e) : -1;
+            if (lane % VPR == 0) s_src[buf][r] = src >= 0;
+            if (e < t.m1 && src < 0) s_bad[buf] = 1;
+            pa[i] = x + ((src >= 0 ? src : 0) * p.k + row_at(wave * G::LA + i)) * G::ESZ;
+        }
 #pragma unroll
-        for (int j = 0; j < G::TN; ++j)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
-    grouped_loop<G, DMA, false, BCOL>(glds, steps, acc, issue, commit);
+        for (int i = 0; i < G::LB; ++i) {
+            const int at = wave * G::LB + i;
+            if constexpr (BCOL) {
+                pb[i] = w + (int64_t(col_row(at)) * p.n + n0 + col_at(at)) * G::ESZ;
+            } else {
+                const int r = n0 + at * RPL + lane / VPR, n = r < p.n ? r : p.n - 1;
+                pb[i] = w + (int64_t(n) * p.k + row_at(at)) * G::ESZ;
+            }
+        }
+        issue(0, 0);
+        for (int r = tid; r < G::BM; r += G::THREADS) {
+            const int64_t i = t.m0 + r;
+            s_dst[buf][r] = i < t.m1 ? int32_t(entry_row(p.y_index, 1, p.y_rows, i)) : -1;
+        }
+    };
 
-    // a 32 x 32 result: lane l, register r holds row 8 (r / 4) + 4 (l / 32) + r % 4, column l % 32;
-    // blocks pass through the wave's own LDS (rows of 36 floats: the two half-waves, four rows
-    // apart, fall on different banks) and come back four columns a lane, eight lanes a row
-    constexpr int PITCH = 36;
-    static_assert(size_t(G::WAVES) * 32 * PITCH * 4 <= G::LDS, "epilogue blocks fit the stages");
-    __syncthreads();
-    float* blk = reinterpret_cast<float*>(glds) + wave * 32 * PITCH;
+    // Epilogue: a 32 x 32 result holds row 8 (r / 4) + 4 (l / 32) + r % 4, column l % 32 in lane l,
+    // register r.  Half a row of blocks at a time (sixteen rows) passes through the wave's own LDS, behind
+    // the first stage, where the next tile's first step arrives (row pitch 8 floats past the blocks: the
+    // two half-waves, four rows apart, fall on different banks), and comes back eight columns a lane.  Its
+    // code stands once, in a rolled loop: unrolled over the blocks it was 45000 instructions, which
+    // every workgroup fetched anew (65536 entries, 1024 -> 4096, then a workgroup per tile: 888 against 762 us).
+    constexpr int COLS = 32 * G::TN, PITCH = COLS + 8;
+    static_assert(G::STAGE + size_t(G::WAVES) * 16 * PITCH * 4 <= G::LDS, "half rows of blocks fit behind the first stage");
+    float* blk = reinterpret_cast<float*>(glds + G::STAGE) + wave * 16 * PITCH;
     const int wm = wave / G::WGN, wn = wave % G::WGN;
+    const int kind = p.act == ACT_IDENTITY ? EPI_STORE : (p.z_in ? EPI_GELU_GRAD : EPI_GELU) + (p.act == ACT_GELU_TANH);
+
+    Tile t = s_tile[0];
+    if (t.g < 0) return;
+    begin(t, 0);
+    for (int turn = 0;; turn ^= 1) {
+        h += gridDim.x;
+        map.find(h, &s_tile[turn ^ 1]);  // seen behind the loop's barriers
+        if (threadIdx.x == 0) s_bad[turn ^ 1] = 0;
+        tile_v16f acc[G::TM][G::TN];
 #pragma unroll
-    for (int i = 0; i < G::TM; ++i)
+        for (int i = 0; i < G::TM; ++i)
 #pragma unroll
-        for (int j = 0; j < G::TN; ++j) {
+            for (int j = 0; j < G::TN; ++j)
 #pragma unroll
-            for (int r = 0; r < 16; ++r)
-                blk[(8 * (r / 4) + 4 * (lane >> 5) + r % 4) * PITCH + (lane & 31)] = acc[i][j][r];
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            const int n = t.n0 + (wn * G::TN + j) * 32 + (lane & 7) * 4;
+                for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
+        grouped_loop<G, DMA, false, BCOL>(glds, steps, acc, issue, commit);
+        __syncthreads();  // every wave is done with the stages
+        const Tile next = s_tile[turn ^ 1];
+        if (DMA && next.g >= 0) begin(next, turn ^ 1);
+        const int rows = int(t.m1 - t.m0 < G::BM ? t.m1 - t.m0 : G::BM), c0 = t.n0 + wn * COLS;
+        const bool full = c0 + COLS <= p.n, bad = s_bad[turn];
+#pragma unroll 1
+        for (int i = 0; i < 2 * G::TM; ++i) {
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int rr = q * 8 + (lane >> 3), m = (wm * G::TM + i) * 32 + rr;
-                const float4 v = *reinterpret_cast<const float4*>(blk + rr * PITCH + (lane & 7) * 4);
-                float z[4] = {v.x, v.y, v.z, v.w};
-                if (!s_src[m]) z[0] = z[1] = z[2] = z[3] = 0.0f;
-                if (n < p.n && t.m0 + m < t.m1) grouped_store4(p, t.m0 + m, s_dst[m], n, z);
+            for (int u = 0; u < 2 * G::TM; ++u) {
+                if (i != u) continue;
+#pragma unroll
+                for (int j = 0; j < G::TN; ++j)
+#pragma unroll
+                    for (int r = 0; r < 8; ++r)
+                        blk[(8 * (r / 4) + 4 * (lane >> 5) + r % 4) * PITCH + j * 32 + (lane & 31)] =
+                            acc[u / 2][j][u % 2 * 8 + r];
             }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            const int m0 = wm * G::TM * 32 + i * 16;
+            if (full) grouped_epilogue<COLS, PITCH, true>(kind, p, blk, m0, rows, t.m0, c0, s_dst[turn], s_src[turn], bad);
+            else grouped_epilogue<COLS, PITCH, false>(kind, p, blk, m0, rows, t.m0, c0, s_dst[turn], s_src[turn], bad);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         }
+        if (next.g < 0) return;
+        t = next;
+        __syncthreads();  // the blocks' LDS is free, the next tile's records are written
+        if constexpr (!DMA) begin(t, turn ^ 1);
+    }
 }
 
 template <class G>
-hipError_t launch_grouped(const GroupedParams& p, hipStream_t stream, int* status) {
-    const int64_t grid = most_tiles(p.n_entries, p.n_groups, G::BM) * ((int64_t(p.n) + G::BN - 1) / G::BN);
-    *status = grid > INT32_MAX ? ST_UNSUPPORTED_ : ST_OK_;
+hipError_t launch_grouped(const GroupedParams& p, int cus, hipStream_t stream, int* status) {
+    const int64_t tiles = most_tiles(p.n_entries, p.n_groups, G::BM) * ((int64_t(p.n) + G::BN - 1) / G::BN);
+    *status = tiles > INT32_MAX ? ST_UNSUPPORTED_ : ST_OK_;
     if (*status != ST_OK_) return hipSuccess;
+    const int grid = int(std::min<int64_t>(tiles, int64_t(cus) * G::PER_CU));
     auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(unsigned(grid)), dim3(G::THREADS), G::LDS, stream, p); };
     // rows of whole 16-byte vectors go straight to LDS
     const bool dma = p.k % G::EV == 0 && (!p.w_transposed || p.n % G::EV == 0);
@@ -183,14 +287,16 @@ hipError_t launch_grouped(const GroupedParams& p, hipStream_t stream, int* statu
 
 }  // namespace
 
-hipError_t run_grouped_matmul(const GroupedParams& p, const DeviceInfo&, hipStream_t stream, int* status) {
+hipError_t run_grouped_matmul(const GroupedParams& p, const DeviceInfo& dev, hipStream_t stream, int* status) {
     const int64_t mean = p.n_entries / p.n_groups;
+    const int cus = dev.cu_count > 0 ? dev.cu_count : 256;
     if (p.bf16) {
-        if (mean >= 128) return launch_grouped<GCfg<true, 4, 2, 2, 2, 3, 64>>(p, stream, status);
-        return launch_grouped<GCfg<true, 1, 2, 2, 2, 3, 64>>(p, stream, status);
+        if (mean >= 256) return launch_grouped<GCfg<true, 4, 2, 2, 4, 2, 128>>(p, cus, stream, status);
+        if (mean >= 64) return launch_grouped<GCfg<true, 2, 2, 2, 2, 2, 128>>(p, cus, stream, status);
+        return launch_grouped<GCfg<true, 1, 2, 1, 4, 2, 128>>(p, cus, stream, status);
     }
-    if (mean >= 128) return launch_grouped<GCfg<false, 2, 2, 2, 2, 3, 64>>(p, stream, status);
-    return launch_grouped<GCfg<false, 1, 2, 2, 2, 3, 64>>(p, stream, status);
+    if (mean >= 128) return launch_grouped<GCfg<false, 2, 2, 2, 2, 2, 128>>(p, cus, stream, status);
+    return launch_grouped<GCfg<false, 1, 2, 1, 4, 2, 128>>(p, cus, stream, status);
 }
 
 }  // namespace fff

@@ -36,62 +36,71 @@ struct Tile {
     int64_t m0, m1;  // its entries
 };
 
-// Tile of workgroup h among row tiles of bm entries (groups in order, each group's last one partly
-// filled) times tn column tiles of bn: every thread sums the row tiles of a few consecutive groups, the
-// workgroup scans the sums, and the thread whose groups hold the row tile finds it.  Workgroup h runs
+// The row tiles of bm entries of all groups (groups in order, each group's last one partly filled)
+// times tn column tiles of bn.  Every thread keeps the sum over a few consecutive groups and all
+// before them; the thread whose groups hold a tile finds it (find) for the workgroup.  Number h runs
 // on XCD h % 8: each XCD takes a contiguous range of the tiles, MB row tiles deep before the next
-// column tile, so that a CU's neighbours share rows and columns in their L2.
+// column tile, so that neighbours share rows and columns in their L2.
 template <int THREADS>
-__device__ __forceinline__ Tile find_tile(const int32_t* offsets, int n_groups, int64_t n_entries, int bm, int bn, int tn,
-                                          int64_t h) {
-    constexpr int64_t MB = 8;
-    __shared__ int64_t wave_sum[THREADS / 64];
-    __shared__ Tile found;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int per = (n_groups + THREADS - 1) / THREADS;
-    const int g0 = std::min(n_groups, tid * per), g1 = std::min(n_groups, g0 + per);
-    int64_t mine = 0, lo, hi;
-    for (int g = g0; g < g1; ++g) {
-        group_range(offsets, n_entries, g, &lo, &hi);
-        mine += (hi - lo + bm - 1) / bm;
-    }
-    int64_t run = mine;
+struct TileMap {
+    static constexpr int MB = 8;
+    const int32_t* offsets;
+    int64_t n_entries;
+    int n_groups, bm, bn, tn;
+    int before, mine, total;  // row tiles before this thread's groups, in them, and of all groups
+
+    // wave_sum: LDS of THREADS / 64 words.  Every thread of the workgroup calls this (a barrier).
+    __device__ __forceinline__ void init(int* wave_sum) {
+        const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+        int64_t lo, hi;
+        mine = 0;
+        for (int g = first(tid); g < first(tid + 1); ++g) {
+            group_range(offsets, n_entries, g, &lo, &hi);
+            mine += int((hi - lo + bm - 1) / bm);
+        }
+        int run = mine;
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const int64_t v = __shfl_up(run, d);
-        if (lane >= d) run += v;
-    }
-    if (lane == 63) wave_sum[wave] = run;
-    if (tid == 0) found.g = -1;
-    __syncthreads();
-    int64_t total = 0;
-    for (int w = 0; w < THREADS / 64; ++w) {
-        if (w < wave) run += wave_sum[w];
-        total += wave_sum[w];
-    }
-    if (h < total * tn) {
-        const int64_t t = xcd_tile(h, total * tn), block = t / (MB * tn), in = t - block * (MB * tn);
-        const int64_t deep = std::min<int64_t>(MB, total - block * MB);
-        const int64_t mt = block * MB + in % deep;
-        int64_t at = run - mine;
-        if (at <= mt && mt < run) {
-            for (int g = g0; g < g1; ++g) {
-                group_range(offsets, n_entries, g, &lo, &hi);
-                const int64_t tiles = (hi - lo + bm - 1) / bm;
-                if (mt < at + tiles) {
-                    found.g = g;
-                    found.n0 = int(in / deep) * bn;
-                    found.m0 = lo + (mt - at) * bm;
-                    found.m1 = hi;
-                    break;
-                }
-                at += tiles;
-            }
+        for (int d = 1; d < 64; d *= 2) {
+            const int v = __shfl_up(run, d);
+            if (lane >= d) run += v;
+        }
+        if (lane == 63) wave_sum[wave] = run;
+        __syncthreads();
+        before = run - mine;
+        total = 0;
+        for (int w = 0; w < THREADS / 64; ++w) {
+            if (w < wave) before += wave_sum[w];
+            total += wave_sum[w];
         }
     }
-    __syncthreads();
-    return found;
-}
+    __device__ __forceinline__ int first(int tid) const {
+        const int per = (n_groups + THREADS - 1) / THREADS;
+        return std::min(n_groups, tid * per);
+    }
+    // Writes tile h to *out: the owner thread alone, or thread 0 where there is no such tile.
+    __device__ __forceinline__ void find(int64_t h, Tile* out) const {
+        const int64_t all = int64_t(total) * tn;
+        if (h >= all) {
+            if (threadIdx.x == 0) out->g = -1;
+            return;
+        }
+        const int64_t t = xcd_tile(h, all);
+        const int block = int(t / (MB * tn)), in = int(t - int64_t(block) * (MB * tn));
+        const int deep = std::min(MB, total - block * MB), mt = block * MB + in % deep;
+        int at = before;
+        if (mt < at || mt >= at + mine) return;
+        for (int g = first(threadIdx.x);; ++g) {
+            int64_t lo, hi;
+            group_range(offsets, n_entries, g, &lo, &hi);
+            const int tiles = int((hi - lo + bm - 1) / bm);
+            if (mt < at + tiles) {
+                *out = Tile{g, in / deep * bn, lo + int64_t(mt - at) * bm, hi};
+                return;
+            }
+            at += tiles;
+        }
+    }
+};
 
 // Most row tiles of bm entries that n_entries in n_groups groups can make.
 inline int64_t most_tiles(int64_t n_entries, int32_t n_groups, int bm) {
@@ -104,6 +113,54 @@ __device__ __forceinline__ int64_t entry_row(const int32_t* index, int div, int6
     if (v < 0) return -1;
     const int64_t r = div == 1 ? v : uint32_t(v) / uint32_t(div);
     return r < rows ? r : -1;
+}
+
+// Phi(-a) for a = |z|, Phi the standard normal distribution, and e = exp(-a^2 / 2): e t Q(t) with
+// t = 1 / (1 + 0.3 a), Q the polynomial of degree 7 nearest to Phi(-a) / (e t) over a = 0 .. 14 in relative
+// error (1.5e-7, fitted for this kernel; 15 roundings of fp32 to a = 4, 130 at 13, where e carries
+// that of its argument).  Twenty instructions; erfcf's are several times as many, and at 268 M values
+// they took as long as the product.
+__device__ __forceinline__ float normal_tail(float z, float& e) {
+    const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.3f, __builtin_fabsf(z), 1.0f));
+    e = __builtin_amdgcn_exp2f(z * z * -0.72134752044448170368f);
+    float q = 0.03567512333393097f;
+    q = __builtin_fmaf(q, t, -0.15720446407794952f);
+    q = __builtin_fmaf(q, t, 0.2063557654619217f);
+    q = __builtin_fmaf(q, t, -0.05368557944893837f);
+    q = __builtin_fmaf(q, t, 0.1285625696182251f);
+    q = __builtin_fmaf(q, t, 0.09991323202848434f);
+    q = __builtin_fmaf(q, t, 0.12075399607419968f);
+    q = __builtin_fmaf(q, t, 0.11962929368019104f);
+    return e * t * q;
+}
+
+// The activations and their derivatives (fff_device.hpp has their formulas).
+template <int ACT>
+__device__ __forceinline__ float act_value(float z) {
+    if constexpr (ACT == ACT_GELU_ERF) {
+        float e;
+        const float p = normal_tail(z, e);
+        return z * (z > 0.0f ? 1.0f - p : p);
+    } else if constexpr (ACT == ACT_GELU_TANH) {
+        return z * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-2.88539008177792681472f * gelu_tanh_u(z)));
+    } else {
+        return z;
+    }
+}
+template <int ACT>
+__device__ __forceinline__ float act_slope(float z) {
+    if constexpr (ACT == ACT_GELU_ERF) {
+        float e;
+        const float p = normal_tail(z, e);
+        return __builtin_fmaf(z * 0.39894228040143267794f, e, z > 0.0f ? 1.0f - p : p);
+    } else if constexpr (ACT == ACT_GELU_TANH) {
+        const float u = 2.88539008177792681472f * gelu_tanh_u(z);
+        const float up = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-u));
+        const float down = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(u));
+        return __builtin_fmaf(2.0f * z * up * down, 0.79788456080286535588f * __builtin_fmaf(0.134145f * z, z, 1.0f), up);
+    } else {
+        return 1.0f;
+    }
 }
 
 // Sixteen zero bytes: what a lane stages for places outside its matrix.
@@ -136,11 +193,11 @@ __device__ __forceinline__ uint4 load16(const char* p, int64_t left) {
 
 // Order of the 16-byte vectors in LDS: vector v of row r at v ^ key, so that the lanes of a fragment
 // read fall on different banks.
-// Row tiles: a b128 read serves eight consecutive rows and two adjacent vectors at once.
+// Row tiles: the lanes of a b128 read are served eight consecutive rows at a time.
 template <int ROWB>
 __device__ __forceinline__ int row_key(int r) {
     static_assert(ROWB == 64 || ROWB == 128, "four or eight vectors a row");
-    return ROWB == 128 ? swz32(r & 15) : ((r >> 2) & 1) * 2;
+    return ROWB == 128 ? swz32(r & 15) : (r >> 1) & 3;
 }
 // Column tiles of C columns, bf16: a transposing read takes four rows and four adjacent vectors, or
 // eight rows (0..3, 8..11) and two; fp32: 32 columns of rows r and r + 4.
@@ -215,11 +272,13 @@ struct GCfg {
     static constexpr int LPS = LA + LB;
     static constexpr int STAGE = (BM + BN) * ROWB;
     static constexpr size_t LDS = size_t(S) * STAGE;
+    // workgroups a CU holds: 160 KB of LDS (4 KB for the kernels' own arrays), two waves a SIMD
+    static constexpr int PER_CU = int(std::min<size_t>((160 * 1024) / (LDS + 4096), 8 / WAVES));
     static_assert(BM * ROWB % (1024 * WAVES) == 0 && BN * ROWB % (1024 * WAVES) == 0, "whole wave loads");
     static_assert(LPS * (S - 2) <= 63, "vmcnt holds 6 bits");
 };
 
-// The matrix-core loop over `steps` steps.  issue(step, stage) starts (DMA) the loads of a step into its
+// The matrix-core loop over `steps` steps, of which the caller has issued the first.  issue(step, stage) starts (DMA) the loads of a step into its
 // stage or, without DMA, reads them into registers, which commit(stage) stores; ACOL, BCOL: column
 // tiles.  The wave's TM x TN blocks are summed into acc.
 template <class G, bool DMA, bool ACOL, bool BCOL, class Issue, class Commit>
@@ -257,8 +316,9 @@ __device__ __forceinline__ void grouped_loop(unsigned char* lds, int64_t steps, 
         }
     };
     if constexpr (DMA) {
+        // step 0 is on its way already; the first wait below is for all that this wave has in flight
 #pragma unroll
-        for (int s = 0; s < G::S - 1; ++s)
+        for (int s = 1; s < G::S - 1; ++s)
             if (s < steps) issue(s, s);
         int stage = 0, ahead = G::S - 1;  // stages of step s and of step s + S - 1
         for (int64_t s = 0; s < steps; ++s) {
@@ -271,7 +331,6 @@ __device__ __forceinline__ void grouped_loop(unsigned char* lds, int64_t steps, 
             ahead = ahead + 1 == G::S ? 0 : ahead + 1;
         }
     } else {
-        issue(0, 0);
         for (int64_t s = 0; s < steps; ++s) {
             commit(int(s & 1));
             __syncthreads();  // step s is in LDS; step s - 1, two commits back, is done with

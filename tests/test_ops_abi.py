@@ -136,7 +136,8 @@ PRODUCT = dict(x=P, w=2 * P, offsets=3 * P, x_index=4 * P, y_index=5 * P, y=6 * 
 
 @pytest.mark.parametrize("over,code", [
     (dict(n_entries=-1), INVALID), (dict(n_entries=1 << 31), INVALID), (dict(n_groups=0), INVALID), (dict(k=0), INVALID),
-    (dict(n=0), INVALID), (dict(x_div=0), INVALID), (dict(x_dtype=2), INVALID), (dict(w_dtype=2), INVALID),
+    (dict(n=0), INVALID), (dict(n=1 << 28), INVALID), (dict(k=1 << 28), INVALID), (dict(x_div=0), INVALID),
+    (dict(x_dtype=2), INVALID), (dict(w_dtype=2), INVALID),
     (dict(y_dtype=2), INVALID), (dict(z_dtype=2), INVALID), (dict(act=3), INVALID), (dict(w_transposed=2), INVALID),
     (dict(x_rows=-1), INVALID), (dict(x_rows=0), INVALID), (dict(x_index=None, x_rows=9), INVALID), (dict(y_index=None, y_rows=9), INVALID),
     (dict(x_rows=1 << 31), INVALID), (dict(x=None), INVALID), (dict(w=None), INVALID), (dict(offsets=None), INVALID),
