@@ -879,7 +879,8 @@ FFF_EXPORT int fff_grouped_matmul(const fff_grouped_matmul_args* a) {
 }
 
 FFF_EXPORT size_t fff_grouped_weight_grad_workspace_bytes(int64_t n_entries, int32_t n_groups, int32_t k, int32_t n) {
-    if (!grouped_sizes_ok(n_entries, n_groups, k, n, 1)) return 0;
+    int64_t bytes;
+    if (!grouped_sizes_ok(n_entries, n_groups, k, n, 1) || !matrix_bytes(n_groups, k, n, 4, &bytes)) return 0;
     return fff::grouped_grad_workspace_bytes(n_entries, n_groups, k, n);
 }
 

@@ -1,5 +1,11 @@
 // fff_grouped_grad.hip -- weight gradients of the grouped products
 // (fff_grouped_weight_grad): dW_g = sum over group g's entries of dy_i^T x_i.
+//
+// A tile of one group's dW is a product over the group's entries, which both
+// operands hold as rows: column tiles of fff_grouped.hpp, read back transposed.
+// The entries' rows are looked up some steps ahead, into LDS.  Where there are
+// few tiles, a group's entries are cut into pieces (splits) for workgroups of
+// their own; their partial sums are added in order.
 #include "fff_grouped.hpp"
 
 namespace fff {
@@ -8,58 +14,220 @@ namespace {
 
 enum { ST_OK_ = 0, ST_UNSUPPORTED_ = -2 };
 
-// Any sizes and types: a workgroup per 64 x 64 tile of one group's dW, its entries sixteen at a time.
-__global__ __launch_bounds__(256) void grouped_grad_any_kernel(GroupedGradParams p) {
-    __shared__ float sa[16][65], sb[16][65];
-    const int tn = (p.n + 63) / 64, tk = (p.k + 63) / 64;
-    const int64_t b = blockIdx.x;
-    const int g = int(b / (int64_t(tn) * tk)), rest = int(b % (int64_t(tn) * tk));
-    const int n0 = rest / tk * 64, k0 = rest % tk * 64, tid = threadIdx.x;
+using GradBig = GCfg<true, 4, 2, 2, 4, 2, 128>;    // 256 x 256, eight waves
+using GradSmall = GCfg<true, 2, 2, 2, 2, 2, 128>;  // 128 x 128, four waves
+using GradF32 = GCfg<false, 2, 2, 2, 2, 2, 128>;
+
+constexpr size_t GRAD_PART_BYTES = size_t(64) << 20;  // partial sums, at most
+
+struct GradPlan {
+    bool big;
+    int bm, bn, splits;
+    int64_t tiles;
+};
+
+// Tiles of 256 x 256 where a group's matrix has them and there are enough; splits: up to two workgroups
+// a CU, eight steps of the mean group each at least, within GRAD_PART_BYTES.  By the sizes alone, so
+// the workspace's size and the result's bits are too.
+GradPlan grad_plan(int64_t n_entries, int32_t n_groups, int32_t k, int32_t n, bool bf16) {
+    auto cdiv = [](int64_t a, int64_t b) { return (a + b - 1) / b; };
+    GradPlan p;
+    p.big = bf16 && k > 128 && n > 128 && n_groups * cdiv(n, 256) * cdiv(k, 256) >= 64;
+    p.bm = p.bn = p.big ? 256 : 128;
+    p.tiles = n_groups * cdiv(n, p.bm) * cdiv(k, p.bn);
+    const int64_t slots = p.big ? 256 : 512, step = bf16 ? 64 : 32;
+    const int64_t most = int64_t(GRAD_PART_BYTES / (size_t(n_groups) * size_t(n) * size_t(k) * 4 + 1));
+    p.splits = p.tiles >= slots ? 1
+               : int(std::max<int64_t>(1, std::min({cdiv(slots, p.tiles), n_entries / n_groups / (8 * step), most})));
+    return p;
+}
+
+// A workgroup per tile and split.
+template <class G, bool DMA>
+__global__ __launch_bounds__(G::THREADS, 2) void grouped_grad_kernel(GroupedGradParams p, int tk, int tiles, int splits) {
+    constexpr int CH = 8 * G::KS;  // entries whose rows are looked up together
+    extern __shared__ __align__(16) unsigned char glds[];
+    __shared__ int32_t s_row[2][2][CH];  // [buffer][dy, x]: source rows, -1 where there is none
+    const int64_t tile = xcd_tile(blockIdx.x, int64_t(tiles) * splits);
+    const int per = tiles / p.n_groups;  // tiles of a group
+    const int g = int(tile / (int64_t(per) * splits)), in = int(tile - int64_t(g) * per * splits);
+    const int sp = in / per, n0 = in % per / tk * G::BM, k0 = in % per % tk * G::BN;
     int64_t lo = 0, hi = 0;
     if (p.n_entries > 0) group_range(p.offsets, p.n_entries, g, &lo, &hi);
-    float acc[4][4] = {};
-    const int tm = tid / 16, tc = tid % 16;
-    for (int64_t e0 = lo; e0 < hi; e0 += 16) {
-        for (int v = tid; v < 1024; v += 256) {
-            const int c = v % 64, r = v / 64;
-            const int64_t i = e0 + r;
-            const int64_t d = i < hi ? entry_row(p.dy_index, 1, p.dy_rows, i) : -1;
-            const int64_t s = i < hi ? entry_row(p.x_index, p.x_div, p.x_rows, i) : -1;
-            sa[r][c] = d >= 0 && n0 + c < p.n ? load_elem(p.dy, p.bf16, d * p.n + n0 + c) : 0.0f;
-            sb[r][c] = s >= 0 && k0 + c < p.k ? load_elem(p.x, p.bf16, s * p.k + k0 + c) : 0.0f;
+    const int64_t all = (hi - lo + G::KS - 1) / G::KS;  // steps of the group, and this split's
+    const int64_t s0 = all * sp / splits, steps = all * (sp + 1) / splits - s0;
+    lo += s0 * G::KS;
+    const int64_t count = std::min<int64_t>(hi - lo, steps * G::KS);  // entries
+
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const uint32_t lds0 = uint32_t(uintptr_t((__attribute__((address_space(3))) unsigned char*)glds));
+    const char* zero = reinterpret_cast<const char*>(&g_zero16);
+    const uint32_t dypitch = uint32_t(p.n) * G::ESZ, xpitch = uint32_t(p.k) * G::ESZ;
+
+    // rows of entries [c CH, (c + 1) CH): read, and some steps later stored
+    constexpr int PT = (CH + G::THREADS - 1) / G::THREADS;
+    int32_t row_dy[PT], row_x[PT];
+    auto look = [&](int64_t c) {
+#pragma unroll
+        for (int u = 0; u < PT; ++u) {
+            const int e = u * G::THREADS + tid;
+            const int64_t i = c * CH + e;
+            row_dy[u] = row_x[u] = -1;
+            if (e < CH && i < count) {
+                row_dy[u] = int32_t(entry_row(p.dy_index, 1, p.dy_rows, lo + i));
+                row_x[u] = int32_t(entry_row(p.x_index, p.x_div, p.x_rows, lo + i));
+            }
         }
+    };
+    auto note = [&](int64_t c) {
+#pragma unroll
+        for (int u = 0; u < PT; ++u) {
+            const int e = u * G::THREADS + tid;
+            if (e >= CH) continue;
+            s_row[c & 1][0][e] = row_dy[u];
+            s_row[c & 1][1][e] = row_x[u];
+        }
+    };
+
+    constexpr int CPA = G::BM * G::ESZ / 16, CPB = G::BN * G::ESZ / 16;  // vectors of a reduction row
+    auto row_of = [&](int at, int cp) { return (at * 64 + lane) / cp; };
+    auto acol = [&](int at) { return ((at * 64 + lane) % CPA ^ col_key<G::BF, G::BM>(row_of(at, CPA))) * G::EV; };
+    auto bcol = [&](int at) { return ((at * 64 + lane) % CPB ^ col_key<G::BF, G::BN>(row_of(at, CPB))) * G::EV; };
+    uint4 ra[DMA ? 1 : G::LA], rb[DMA ? 1 : G::LB];
+    auto issue = [&](int64_t s, int stage) {
+        const int64_t c = s / 8;
+        const int e0 = int(s % 8) * G::KS;
+        const uint32_t st = lds0 + uint32_t(stage) * G::STAGE;
+#pragma unroll
+        for (int i = 0; i < G::LA; ++i) {
+            const int at = wave * G::LA + i, n = n0 + acol(at);
+            const int32_t r = s_row[c & 1][0][e0 + row_of(at, CPA)];
+            const char* q = static_cast<const char*>(p.dy) + uint64_t(uint32_t(r)) * dypitch + n * G::ESZ;
+            if constexpr (DMA) lds_dma16(r < 0 || n >= p.n ? zero : q, st + at * 1024);
+            else ra[i] = load16<G::BF>(q, r < 0 ? 0 : p.n - n);
+        }
+#pragma unroll
+        for (int i = 0; i < G::LB; ++i) {
+            const int at = wave * G::LB + i, k = k0 + bcol(at);
+            const int32_t r = s_row[c & 1][1][e0 + row_of(at, CPB)];
+            const char* q = static_cast<const char*>(p.x) + uint64_t(uint32_t(r)) * xpitch + k * G::ESZ;
+            if constexpr (DMA) lds_dma16(r < 0 || k >= p.k ? zero : q, st + G::BM * G::ROWB + at * 1024);
+            else rb[i] = load16<G::BF>(q, r < 0 ? 0 : p.k - k);
+        }
+        // the next chunk's rows: read at a chunk's second step, stored at its fifth, used from the eighth on
+        if (s % 8 == 1) look(c + 1);
+        if (s % 8 == 4) note(c + 1);
+    };
+    auto commit = [&](int stage) {
+        if constexpr (!DMA) {
+            unsigned char* st = glds + stage * G::STAGE;
+#pragma unroll
+            for (int i = 0; i < G::LA; ++i) *reinterpret_cast<uint4*>(st + (wave * G::LA + i) * 1024 + lane * 16) = ra[i];
+#pragma unroll
+            for (int i = 0; i < G::LB; ++i)
+                *reinterpret_cast<uint4*>(st + G::BM * G::ROWB + (wave * G::LB + i) * 1024 + lane * 16) = rb[i];
+        }
+    };
+    tile_v16f acc[G::TM][G::TN];
+#pragma unroll
+    for (int i = 0; i < G::TM; ++i)
+#pragma unroll
+        for (int j = 0; j < G::TN; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
+    if (steps > 0) {
+        look(0);
+        note(0);
         __syncthreads();
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-#pragma unroll
-            for (int a = 0; a < 4; ++a)
-#pragma unroll
-                for (int c = 0; c < 4; ++c)
-                    acc[a][c] = __builtin_fmaf(sa[r][tm * 4 + a], sb[r][tc * 4 + c], acc[a][c]);
-        __syncthreads();
+        issue(0, 0);
+        grouped_loop<G, DMA, true, true>(glds, steps, acc, issue, commit);
     }
-    if (hi == lo && p.accumulate) return;
+    // a result's columns are consecutive over 32 lanes: whole 128-byte lines without another pass
+    const bool add = splits == 1 && p.accumulate;
+    if (add && hi == lo) return;
+    float* dw = (splits > 1 ? p.part + int64_t(sp) * p.n_groups * p.n * p.k : p.dw) + int64_t(g) * p.n * p.k;
+    const int wm = wave / G::WGN, wn = wave % G::WGN;
 #pragma unroll
-    for (int a = 0; a < 4; ++a)
+    for (int i = 0; i < G::TM; ++i)
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-            const int n = n0 + tm * 4 + a, k = k0 + tc * 4 + c;
-            if (n >= p.n || k >= p.k) continue;
-            float* d = p.dw + (int64_t(g) * p.n + n) * p.k + k;
-            *d = p.accumulate ? *d + acc[a][c] : acc[a][c];
+        for (int j = 0; j < G::TN; ++j) {
+            const int k = k0 + (wn * G::TN + j) * 32 + (lane & 31), n = n0 + (wm * G::TM + i) * 32 + 4 * (lane >> 5);
+            if (k >= p.k) continue;
+            float* d = dw + int64_t(n) * p.k + k;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int dn = 8 * (r / 4) + r % 4;
+                if (n + dn >= p.n) continue;
+                float* q = d + int64_t(dn) * p.k;
+                *q = add ? *q + acc[i][j][r] : acc[i][j][r];
+            }
         }
+}
+
+// dW: the splits' partial sums in order.
+__global__ __launch_bounds__(256) void grouped_grad_sum_kernel(GroupedGradParams p, int splits, int64_t all) {
+    for (int64_t i = (int64_t(blockIdx.x) * 256 + threadIdx.x) * 4; i < all; i += int64_t(gridDim.x) * 1024) {
+        if (i + 4 <= all && all % 4 == 0) {
+            float4 v = *reinterpret_cast<const float4*>(p.part + i);
+            for (int s = 1; s < splits; ++s) {
+                const float4 w = *reinterpret_cast<const float4*>(p.part + int64_t(s) * all + i);
+                v.x += w.x;
+                v.y += w.y;
+                v.z += w.z;
+                v.w += w.w;
+            }
+            float4* d = reinterpret_cast<float4*>(p.dw + i);
+            if (p.accumulate) {
+                const float4 o = *d;
+                v = make_float4(o.x + v.x, o.y + v.y, o.z + v.z, o.w + v.w);
+            }
+            *d = v;
+        } else {
+            for (int64_t e = i; e < std::min<int64_t>(all, i + 4); ++e) {
+                float v = p.part[e];
+                for (int s = 1; s < splits; ++s) v += p.part[int64_t(s) * all + e];
+                p.dw[e] = p.accumulate ? p.dw[e] + v : v;
+            }
+        }
+    }
+}
+
+template <class G>
+hipError_t launch_grad(const GroupedGradParams& p, const GradPlan& plan, hipStream_t stream) {
+    const int tk = int((int64_t(p.k) + G::BN - 1) / G::BN);
+    auto launch = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, dim3(unsigned(plan.tiles * plan.splits)), dim3(G::THREADS), G::LDS, stream, p, tk,
+                           int(plan.tiles), plan.splits);
+    };
+    p.n % G::EV == 0 && p.k % G::EV == 0 ? launch(grouped_grad_kernel<G, true>) : launch(grouped_grad_kernel<G, false>);
+    if (plan.splits > 1) {
+        const int64_t all = int64_t(p.n_groups) * p.n * p.k;
+        const unsigned blocks = unsigned(std::min<int64_t>((all + 1023) / 1024, 2048));
+        hipLaunchKernelGGL(grouped_grad_sum_kernel, dim3(blocks), dim3(256), 0, stream, p, plan.splits, all);
+    }
+    return hipGetLastError();
 }
 
 }  // namespace
 
-size_t grouped_grad_workspace_bytes(int64_t, int32_t, int32_t, int32_t) { return 0; }
+size_t grouped_grad_workspace_bytes(int64_t n_entries, int32_t n_groups, int32_t k, int32_t n) {
+    // either type's plan: the caller's call names the sizes alone
+    const size_t one = size_t(n_groups) * size_t(n) * size_t(k) * sizeof(float);
+    size_t most = 0;
+    for (bool bf16 : {false, true}) {
+        const int s = grad_plan(n_entries, n_groups, k, n, bf16).splits;
+        most = std::max(most, s > 1 ? s * one : 0);
+    }
+    return most;
+}
 
 hipError_t run_grouped_weight_grad(const GroupedGradParams& p, const DeviceInfo&, hipStream_t stream, int* status) {
-    const int64_t grid = int64_t(p.n_groups) * ((int64_t(p.n) + 63) / 64) * ((int64_t(p.k) + 63) / 64);
-    *status = grid > INT32_MAX ? ST_UNSUPPORTED_ : ST_OK_;
+    const GradPlan plan = grad_plan(p.n_entries, p.n_groups, p.k, p.n, p.bf16);
+    *status = plan.tiles * plan.splits > INT32_MAX ? ST_UNSUPPORTED_ : ST_OK_;
     if (*status != ST_OK_) return hipSuccess;
-    hipLaunchKernelGGL(grouped_grad_any_kernel, dim3(unsigned(grid)), dim3(256), 0, stream, p);
-    return hipGetLastError();
+    if (!p.bf16) return launch_grad<GradF32>(p, plan, stream);
+    return plan.big ? launch_grad<GradBig>(p, plan, stream) : launch_grad<GradSmall>(p, plan, stream);
 }
 
 }  // namespace fff
