@@ -285,11 +285,125 @@ hipError_t launch_grouped(const GroupedParams& p, int cus, hipStream_t stream, i
     return hipGetLastError();
 }
 
+// Few entries a group (decoding): the weights of the groups in use are read once, and that is the time.
+// A workgroup takes sixteen columns of a group's matrix and up to sixteen of its entries; its waves
+// split the reduction axis, whole 128-byte lines of a row at a time, with FEW_U steps (2 FEW_U KB a wave)
+// in flight.  Weights are the MFMA's first operand (sixteen rows of W), the entries its second, straight
+// from global memory in the operands' layout (lane l: row l % 16, the 16 bytes l / 16 of every 64); the
+// waves' sums meet in LDS.
+constexpr int FEW_WAVES = 8, FEW_U = 4;
+constexpr int64_t FEW_MEAN = 8;  // entries a group, at most
+
+// Row tile mt (of sixteen entries) over all groups, found by every wave for itself, 64 groups at a time.
+__device__ __forceinline__ Tile few_tile(const GroupedParams& p, int mt) {
+    const int lane = threadIdx.x & 63;
+    int at = 0;
+    for (int g0 = 0; g0 < p.n_groups; g0 += 64) {
+        int64_t lo = 0, hi = 0;
+        if (g0 + lane < p.n_groups) group_range(p.offsets, p.n_entries, g0 + lane, &lo, &hi);
+        const int mine = int((hi - lo + 15) / 16);
+        int run = mine;
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const int v = __shfl_up(run, d);
+            if (lane >= d) run += v;
+        }
+        const uint64_t has = __ballot(at + run > mt);
+        if (has) {
+            const int l = __builtin_ctzll(has);
+            const int before = at + __builtin_amdgcn_readlane(run - mine, l);
+            const int first = __builtin_amdgcn_readlane(int(lo), l), end = __builtin_amdgcn_readlane(int(hi), l);
+            return Tile{g0 + l, 0, first + int64_t(mt - before) * 16, end};
+        }
+        at += __builtin_amdgcn_readlane(run, 63);
+    }
+    return Tile{-1, 0, 0, 0};
+}
+
+template <bool BF, bool ALIGNED>
+__global__ __launch_bounds__(64 * FEW_WAVES) void grouped_few_kernel(GroupedParams p) {
+    constexpr int ESZ = BF ? 2 : 4, EV = 16 / ESZ, STEP = 128 / ESZ;  // elements of a step
+    __shared__ float s_sum[FEW_WAVES][256];
+    const int tn = (p.n + 15) / 16;
+    const Tile t = few_tile(p, int(blockIdx.x / tn));
+    if (t.g < 0) return;
+    const int n0 = int(blockIdx.x % tn) * 16, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int r16 = lane & 15, q = lane >> 4;
+    const int64_t e = t.m0 + r16;
+    const int64_t src = e < t.m1 ? entry_row(p.x_index, p.x_div, p.x_rows, e) : -1;
+    const int n = n0 + r16 < p.n ? n0 + r16 : p.n - 1;
+    const char* w = static_cast<const char*>(p.w) + (int64_t(t.g) * p.n + n) * p.k * ESZ;
+    const char* x = static_cast<const char*>(p.x) + (src >= 0 ? src : 0) * p.k * ESZ;
+    auto load = [&](const char* row, int64_t k, bool in) {  // sixteen bytes from element k on
+        const int64_t left = in ? int64_t(p.k) - k : 0;
+        if constexpr (ALIGNED) return left > 0 ? *reinterpret_cast<const uint4*>(row + k * ESZ) : make_uint4(0, 0, 0, 0);
+        else return load16<BF>(row + k * ESZ, left);
+    };
+    tile_v4f acc = {0.0f, 0.0f, 0.0f, 0.0f};
+    const int steps = (p.k + STEP - 1) / STEP;
+    for (int s = wave; s < steps; s += FEW_WAVES * FEW_U) {
+        uint4 fw[FEW_U][2], fx[FEW_U][2];
+#pragma unroll
+        for (int u = 0; u < FEW_U; ++u)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int64_t k = int64_t(s + u * FEW_WAVES) * STEP + (h * 4 + q) * EV;
+                fw[u][h] = load(w, k, true);
+                fx[u][h] = load(x, k, src >= 0);
+            }
+#pragma unroll
+        for (int u = 0; u < FEW_U; ++u)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                if constexpr (BF) {
+                    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, fw[u][h]),
+                                                                  __builtin_bit_cast(bf16x8_t, fx[u][h]), acc, 0, 0, 0);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(word(fw[u][h], j)),
+                                                                   __uint_as_float(word(fx[u][h], j)), acc, 0, 0, 0);
+                }
+            }
+    }
+    // lane l, register r: column (entry) l % 16, row (of W) 4 (l / 16) + r
+#pragma unroll
+    for (int r = 0; r < 4; ++r) s_sum[wave][r16 * 16 + 4 * q + r] = acc[r];
+    __syncthreads();
+    if (tid >= 256) return;
+    float z = 0.0f;
+#pragma unroll
+    for (int v = 0; v < FEW_WAVES; ++v) z += s_sum[v][tid];
+    const int64_t i = t.m0 + tid / 16;
+    const int c = n0 + tid % 16;
+    if (i >= t.m1 || c >= p.n) return;
+    if (p.z_in) {
+        const float d = load_elem(p.z_in, p.z_bf16, i * p.n + c);
+        z *= p.act == ACT_GELU_ERF ? act_slope<ACT_GELU_ERF>(d) : p.act == ACT_GELU_TANH ? act_slope<ACT_GELU_TANH>(d) : 1.0f;
+    } else {
+        if (p.z_out) store_elem(p.z_out, p.z_bf16, i * p.n + c, z);
+        z = p.act == ACT_GELU_ERF ? act_value<ACT_GELU_ERF>(z) : p.act == ACT_GELU_TANH ? act_value<ACT_GELU_TANH>(z) : z;
+    }
+    const int64_t dst = entry_row(p.y_index, 1, p.y_rows, i);
+    if (dst >= 0) store_elem(p.y, p.y_bf16, dst * p.n + c, z);
+}
+
+hipError_t launch_few(const GroupedParams& p, hipStream_t stream, int* status) {
+    const int64_t tiles = most_tiles(p.n_entries, p.n_groups, 16) * ((int64_t(p.n) + 15) / 16);
+    *status = tiles > INT32_MAX ? ST_UNSUPPORTED_ : ST_OK_;
+    if (*status != ST_OK_) return hipSuccess;
+    auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(unsigned(tiles)), dim3(64 * FEW_WAVES), 0, stream, p); };
+    if (p.bf16) p.k % 8 == 0 ? launch(grouped_few_kernel<true, true>) : launch(grouped_few_kernel<true, false>);
+    else p.k % 4 == 0 ? launch(grouped_few_kernel<false, true>) : launch(grouped_few_kernel<false, false>);
+    return hipGetLastError();
+}
+
 }  // namespace
 
 hipError_t run_grouped_matmul(const GroupedParams& p, const DeviceInfo& dev, hipStream_t stream, int* status) {
     const int64_t mean = p.n_entries / p.n_groups;
     const int cus = dev.cu_count > 0 ? dev.cu_count : 256;
+    if (!p.w_transposed && mean <= FEW_MEAN) return launch_few(p, stream, status);
     if (p.bf16) {
         if (mean >= 256) return launch_grouped<GCfg<true, 4, 2, 2, 4, 2, 128>>(p, cus, stream, status);
         if (mean >= 64) return launch_grouped<GCfg<true, 2, 2, 2, 2, 2, 128>>(p, cus, stream, status);
