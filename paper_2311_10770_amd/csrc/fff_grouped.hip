@@ -9,6 +9,8 @@
 // epilogue works on eight consecutive columns a lane and stores whole lines.
 #include "fff_grouped.hpp"
 
+#include <cmath>
+
 namespace fff {
 
 namespace {
@@ -292,7 +294,6 @@ hipError_t launch_grouped(const GroupedParams& p, int cus, hipStream_t stream, i
 // from global memory in the operands' layout (lane l: row l % 16, the 16 bytes l / 16 of every 64); the
 // waves' sums meet in LDS.
 constexpr int FEW_WAVES = 8, FEW_U = 4;
-constexpr int64_t FEW_MEAN = 8;  // entries a group, at most
 
 // Row tile mt (of sixteen entries) over all groups, found by every wave for itself, 64 groups at a time.
 __device__ __forceinline__ Tile few_tile(const GroupedParams& p, int mt) {
@@ -398,19 +399,65 @@ hipError_t launch_few(const GroupedParams& p, hipStream_t stream, int* status) {
     return hipGetLastError();
 }
 
+// Which kernel: the one of the least time by what each took (us, measured with 1 to 64 groups, 64 to 16384
+// entries, k and n 128 to 4096): a tile costs `start` and `alone` a 128-byte step of the reduction axis,
+// or `pair` where two workgroups share its CU.  Small tiles lose rate (32 x 128: 0.35 of 256 x 256's, whose
+// two workgroups' worth of tile has a CU to itself) and win where large ones leave CUs idle or rows of
+// the tile empty; sixteen-entry tiles read the weights again for every sixteen entries of a group.  Some
+// of both sides, bf16 (few, 32, 64, 128, 256 rows): 64 entries x 1 group, 4096 -> 1024: 11, 27, 33, 39, 99;
+// 1000 x 16 groups, 768 -> 768: 26, 10, 12, 15, 28; 4000 x 64, 1024 -> 1024: 139, 44, 30, 39, 40;
+// 16000 x 16, 768 -> 768: -, 81, 42, 38, 34; fp32: 500 x 16, 768 -> 768: 28, 25, 35, 57;
+// 16000 x 64, 1024 -> 1024: -, 448, 338, 352.
+struct TileCost {
+    int bm, bn;
+    double start, alone, pair;
+};
+constexpr TileCost COST_BF16[] = {{32, 128, 2, 0.34, 0.70}, {64, 128, 2.5, 0.43, 0.58}, {128, 128, 4, 0.50, 0.95},
+                                  {256, 256, 6, 1.85, 3.70}};
+constexpr TileCost COST_F32[] = {{32, 128, 2, 0.74, 1.60}, {64, 128, 2.5, 1.18, 2.20}, {128, 128, 4, 2.00, 3.60}};
+
+// 0: few entries a group; 1 ..: the tiles of the tables.
+int grouped_variant(const GroupedParams& p, int cus) {
+    const double E = double(p.n_entries), used = double(std::min<int64_t>(p.n_groups, p.n_entries));
+    const int esz = p.bf16 ? 2 : 4;
+    const double steps = (double(p.k) * esz + 127) / 128;
+    auto row_tiles = [&](int bm) { return std::max(used, E / bm + 0.5 * used); };
+    int best = 0;
+    double least = 1e300;
+    if (!p.w_transposed) {
+        // 768 workgroups at once; rows off 16-byte addresses take 2.4 times as long
+        const double rounds = row_tiles(16) * ((p.n + 15) / 16) / (3.0 * cus);
+        const double kb = double(p.k) * esz / 64, slow = p.k % (16 / esz) ? 2.4 : 1.0;
+        least = rounds < 1 ? 2.5 + 0.115 * kb * std::max(rounds, 0.35) * slow : rounds * (2.5 + 0.115 * kb) * slow;
+    }
+    const TileCost* cost = p.bf16 ? COST_BF16 : COST_F32;
+    for (int v = 0; v < (p.bf16 ? 4 : 3); ++v) {
+        const double per_cu = std::ceil(row_tiles(cost[v].bm) * ((p.n + cost[v].bn - 1) / cost[v].bn) / cus);
+        const double pairs = std::floor(per_cu / 2), odd = per_cu - 2 * pairs;
+        const double t = pairs * (cost[v].start * (v == 3 ? 2 : 1) + steps * cost[v].pair) +
+                         odd * (cost[v].start + steps * cost[v].alone);
+        if (t < least) {
+            least = t;
+            best = v + 1;
+        }
+    }
+    return best;
+}
+
 }  // namespace
 
 hipError_t run_grouped_matmul(const GroupedParams& p, const DeviceInfo& dev, hipStream_t stream, int* status) {
-    const int64_t mean = p.n_entries / p.n_groups;
     const int cus = dev.cu_count > 0 ? dev.cu_count : 256;
-    if (!p.w_transposed && mean <= FEW_MEAN) return launch_few(p, stream, status);
-    if (p.bf16) {
-        if (mean >= 256) return launch_grouped<GCfg<true, 4, 2, 2, 4, 2, 128>>(p, cus, stream, status);
-        if (mean >= 64) return launch_grouped<GCfg<true, 2, 2, 2, 2, 2, 128>>(p, cus, stream, status);
-        return launch_grouped<GCfg<true, 1, 2, 1, 4, 2, 128>>(p, cus, stream, status);
+    switch (grouped_variant(p, cus)) {
+        case 0: return launch_few(p, stream, status);
+        case 1: return p.bf16 ? launch_grouped<GCfg<true, 1, 1, 1, 4, 4, 128>>(p, cus, stream, status)
+                              : launch_grouped<GCfg<false, 1, 1, 1, 4, 4, 128>>(p, cus, stream, status);
+        case 2: return p.bf16 ? launch_grouped<GCfg<true, 1, 2, 2, 2, 3, 128>>(p, cus, stream, status)
+                              : launch_grouped<GCfg<false, 1, 2, 2, 2, 3, 128>>(p, cus, stream, status);
+        case 3: return p.bf16 ? launch_grouped<GCfg<true, 2, 2, 2, 2, 2, 128>>(p, cus, stream, status)
+                              : launch_grouped<GCfg<false, 2, 2, 2, 2, 2, 128>>(p, cus, stream, status);
+        default: return launch_grouped<GCfg<true, 4, 2, 2, 4, 2, 128>>(p, cus, stream, status);
     }
-    if (mean >= 128) return launch_grouped<GCfg<false, 2, 2, 2, 2, 2, 128>>(p, cus, stream, status);
-    return launch_grouped<GCfg<false, 1, 2, 1, 4, 2, 128>>(p, cus, stream, status);
 }
 
 }  // namespace fff
