@@ -9,13 +9,14 @@ that graph's own memory), so no two calls and no two graphs share any.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
+import functools
+import inspect
 from ctypes import c_double, c_float, c_int32, c_int64, c_size_t, c_uint64, c_void_p
 
 import torch
 
-from .fff import _TORCH_DT, ACTS, FFF_F32, _check, _dt, _on_device, _raw_stream, load_library
+from .fff import _TORCH_DT, ACTS, FFF_F32, _check, _dt, _raw_stream, load_library
 
 
 class FffDropoutRng(ctypes.Structure):
@@ -92,58 +93,99 @@ class FffGroupedWeightGradArgs(ctypes.Structure):
     ]
 
 
-def _gpu(t, what: str, device=None):
-    """``t`` as a contiguous GPU tensor (on ``device``)."""
+_get_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+_LIB = None
+
+
+def _lib():
+    global _LIB
+    if _LIB is None:
+        _LIB = load_library()
+    return _LIB
+
+
+def _gpu(t, what: str, index=None):
+    """``t`` as a contiguous GPU tensor (on GPU ``index``)."""
     if not isinstance(t, torch.Tensor):
         raise ValueError(f"{what} must be a torch.Tensor")
     if not t.is_cuda:
         raise ValueError(f"{what} must be a GPU tensor")
-    if device is not None and t.device != device:
-        raise ValueError(f"{what} is on {t.device}, expected {device}")
+    if index is not None and t.get_device() != index:
+        raise ValueError(f"{what} is on {t.device}, expected cuda:{index}")
     if not t.is_contiguous():
         raise ValueError(f"{what} must be contiguous")
     return t
 
 
-def _like(t, what, device, shape, dtype=None):
+def _like(t, what, index, shape, dtype=None):
     """Pointer of an optional tensor of exactly ``shape`` (and ``dtype``), or None."""
     if t is None:
         return None
-    _gpu(t, what, device)
-    if tuple(t.shape) != tuple(shape):
+    _gpu(t, what, index)
+    if t.shape != shape:
         raise ValueError(f"{what} must be {list(shape)}, got {tuple(t.shape)}")
     if dtype is not None and t.dtype != dtype:
         raise ValueError(f"{what} must be {dtype}, got {t.dtype}")
     return t.data_ptr()
 
 
-def _index(t, what, device, n):
+def _index(t, what, index, n):
     """Pointer of an optional int32 tensor of n elements, or None."""
     if t is None:
         return None
-    _gpu(t, what, device)
+    _gpu(t, what, index)
     if t.dtype != torch.int32 or t.numel() != n:
         raise ValueError(f"{what} must be int32 with {n} elements")
     return t.data_ptr()
 
 
-def _on_stream(stream):
-    """Allocations of a call on ``stream`` belong to that stream."""
-    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+def _scratch(t, what, index):
+    """Pointer and bytes of an optional workspace."""
+    if t is None:
+        return None, 0
+    _gpu(t, what, index)
+    return t.data_ptr(), t.numel() * t.element_size()
 
 
-def _set_rng(drop, p, seed, offset, rng_offset, device):
+def _on_call(fn):
+    """Runs ``fn`` with its first tensor's GPU current, and ``stream`` too when one is given: allocations then
+    belong to the call's stream."""
+    name = next(iter(inspect.signature(fn).parameters))
+
+    @functools.wraps(fn)
+    def call(*args, stream=None, **kw):
+        t = args[0] if args else kw.get(name)
+        if not (isinstance(t, torch.Tensor) and t.is_cuda):
+            return fn(*args, stream=None, **kw)  # refused there
+        if stream is None:
+            if t.get_device() == _get_device():
+                return fn(*args, stream=None, **kw)
+            with torch.cuda.device(t.device):
+                return fn(*args, stream=None, **kw)
+        if stream.device != t.device:
+            raise ValueError(f"stream is on {stream.device}, the tensors on {t.device}")
+        with torch.cuda.stream(stream):
+            return fn(*args, stream=stream, **kw)
+
+    return call
+
+
+_NO_DROP = FffDropoutRng()
+
+
+def _rng(p, seed, offset, rng_offset, index):
     p = float(p)
     if not 0.0 <= p < 1.0:
         raise ValueError("p must be in [0, 1)")
     if not (0 <= seed < 1 << 64 and 0 <= offset < 1 << 64):
         raise ValueError("seed and offset must fit 64 unsigned bits")
-    drop.p, drop.seed, drop.offset = p, seed, offset
+    at = None
     if rng_offset is not None:
-        _gpu(rng_offset, "rng_offset", device)
+        _gpu(rng_offset, "rng_offset", index)
         if rng_offset.dtype != torch.int64 or rng_offset.numel() != 1:
             raise ValueError("rng_offset must be one int64")
-        drop.rng_offset = rng_offset.data_ptr()
+        at = rng_offset.data_ptr()
+    return FffDropoutRng(p, seed, offset, at)
 
 
 def _rows(x, what: str):
@@ -153,11 +195,13 @@ def _rows(x, what: str):
     return x.shape
 
 
-def _run(fn, args, device):
-    with _on_device(device):
-        _check(getattr(load_library(), fn)(ctypes.addressof(args)))
+def _run(fn, args):
+    rc = fn(ctypes.addressof(args))
+    if rc:
+        _check(rc)
 
 
+@_on_call
 def layer_norm(x, gamma=None, beta=None, *, eps=1e-12, residual=None, p=0.0, seed=0, offset=0, rng_offset=None, y=None,
                s=None, mean=None, rstd=None, y_dtype=None, s_dtype=None, stats=True, stream=None):
     """``s = residual + drop(x)``, then ``y = (s - mean) * rstd * gamma + beta`` per row, through ``fff_layer_norm``.
@@ -165,49 +209,39 @@ def layer_norm(x, gamma=None, beta=None, *, eps=1e-12, residual=None, p=0.0, see
     Returns (y, s, mean, rstd).  Without a residual and with p = 0, s is x itself.  With ``stats``
     false, mean and rstd are None unless passed.  ``s`` may be ``residual`` (the stream updated in
     place).  Types of what is allocated: y as ``y_dtype`` or x; s as ``s_dtype``, residual or x."""
-    B, H = _rows(x, "x")
-    device = x.device
-    a = FffLayerNormArgs()
+    B, H = shape = _rows(x, "x")
+    device, at = x.device, x.get_device()
     summed = residual is not None or p > 0
     if not summed and s is not None:
         raise ValueError("s is x itself without a residual and dropout")
     if residual is not None and s_dtype is not None and s_dtype != residual.dtype:
         raise ValueError("residual and s share a dtype")
     s_dt = residual.dtype if residual is not None else s.dtype if s is not None else s_dtype or x.dtype
-    with _on_device(device), _on_stream(stream):
-        if y is None:
-            y = torch.empty((B, H), dtype=y_dtype or x.dtype, device=device)
-        if summed and s is None:
-            s = torch.empty((B, H), dtype=s_dt, device=device)
-        if stats and mean is None:
-            mean = torch.empty(B, dtype=torch.float32, device=device)
-        if stats and rstd is None:
-            rstd = torch.empty(B, dtype=torch.float32, device=device)
-    a.x = x.data_ptr()
-    a.residual = _like(residual, "residual", device, (B, H))
-    a.gamma = _like(gamma, "gamma", device, (H,), torch.float32)
-    a.beta = _like(beta, "beta", device, (H,), torch.float32)
-    a.y = _like(y, "y", device, (B, H))
-    a.s = _like(s, "s", device, (B, H), s_dt)
-    a.mean = _like(mean, "mean", device, (B,), torch.float32)
-    a.rstd = _like(rstd, "rstd", device, (B,), torch.float32)
-    a.n_tokens, a.hidden = B, H
-    a.x_dtype, a.y_dtype = _dt(x, "x"), _dt(y, "y")
-    a.s_dtype = _TORCH_DT.get(s_dt, -1)
-    if a.s_dtype < 0:
+    if s_dt not in _TORCH_DT:
         raise ValueError(f"s must be float32 or bfloat16, got {s_dt}")
-    a.eps = eps
-    if p or rng_offset is not None:
-        _set_rng(a.drop, p, seed, offset, rng_offset, device)
-    a.hip_stream = _raw_stream(device, stream)
-    _run("fff_layer_norm", a, device)
+    if y is None:
+        y = torch.empty(shape, dtype=y_dtype or x.dtype, device=device)
+    if summed and s is None:
+        s = torch.empty(shape, dtype=s_dt, device=device)
+    if stats and mean is None:
+        mean = torch.empty(B, dtype=torch.float32, device=device)
+    if stats and rstd is None:
+        rstd = torch.empty(B, dtype=torch.float32, device=device)
+    f32 = torch.float32
+    _run(_lib().fff_layer_norm, FffLayerNormArgs(
+        x.data_ptr(), _like(residual, "residual", at, shape), _like(gamma, "gamma", at, (H,), f32),
+        _like(beta, "beta", at, (H,), f32), _like(y, "y", at, shape), _like(s, "s", at, shape, s_dt),
+        _like(mean, "mean", at, (B,), f32), _like(rstd, "rstd", at, (B,), f32), B, H, _dt(x, "x"), _TORCH_DT[s_dt],
+        _dt(y, "y"), eps, _rng(p, seed, offset, rng_offset, at) if p or rng_offset is not None else _NO_DROP,
+        _raw_stream(device, stream)))
     return y, s if summed else x, mean, rstd
 
 
 def layer_norm_backward_workspace_bytes(n_tokens: int, hidden: int) -> int:
-    return int(load_library().fff_layer_norm_backward_workspace_bytes(n_tokens, hidden))
+    return int(_lib().fff_layer_norm_backward_workspace_bytes(n_tokens, hidden))
 
 
+@_on_call
 def layer_norm_backward(dy, s, mean, rstd, gamma=None, *, ds_in=None, p=0.0, seed=0, offset=0, rng_offset=None, ds=None,
                         dx=None, dgamma=None, dbeta=None, accumulate=False, dx_dtype=None, workspace=None,
                         want=("ds", "dx", "dgamma", "dbeta"), stream=None):
@@ -218,78 +252,59 @@ def layer_norm_backward(dy, s, mean, rstd, gamma=None, *, ds_in=None, p=0.0, see
     the gradient of s and of the residual, ``dx`` (``dx_dtype`` or dy's type) that of x behind the
     dropout: ds itself where p = 0, unless a dx is passed.  Gradients named in ``want`` are allocated when
     not given; ``accumulate`` adds to dgamma and dbeta, which must then be given."""
-    B, H = _rows(dy, "dy")
-    device = dy.device
-    a = FffLayerNormBackwardArgs()
-    a.dy = dy.data_ptr()
-    a.s = _like(s, "s", device, (B, H))
-    a.mean = _like(mean, "mean", device, (B,), torch.float32)
-    a.rstd = _like(rstd, "rstd", device, (B,), torch.float32)
+    B, H = shape = _rows(dy, "dy")
+    device, at, f32 = dy.device, dy.get_device(), torch.float32
     if s is None or mean is None or rstd is None:
         raise ValueError("s, mean and rstd are needed")
+    _like(s, "s", at, shape)
     alias = dx is None and p == 0  # dx is ds
     if alias and "dx" in want and "ds" not in want:
         want = tuple(want) + ("ds",)
     if accumulate and (("dgamma" in want and dgamma is None) or ("dbeta" in want and dbeta is None)):
         raise ValueError("accumulate adds to the dgamma and dbeta that are given")
-    with _on_device(device), _on_stream(stream):
-        if ds is None and "ds" in want:
-            ds = torch.empty((B, H), dtype=s.dtype, device=device)
-        if dx is None and not alias and "dx" in want:
-            dx = torch.empty((B, H), dtype=dx_dtype or dy.dtype, device=device)
-        if dgamma is None and "dgamma" in want:
-            dgamma = torch.empty(H, dtype=torch.float32, device=device)
-        if dbeta is None and "dbeta" in want:
-            dbeta = torch.empty(H, dtype=torch.float32, device=device)
-        if workspace is None and (dgamma is not None or dbeta is not None):
-            workspace = torch.empty(max(256, layer_norm_backward_workspace_bytes(B, H)), dtype=torch.uint8, device=device)
-    a.gamma = _like(gamma, "gamma", device, (H,), torch.float32)
-    a.ds_in = _like(ds_in, "ds_in", device, (B, H), s.dtype)
-    a.ds = _like(ds, "ds", device, (B, H), s.dtype)
-    a.dx = _like(dx, "dx", device, (B, H))
-    a.dgamma = _like(dgamma, "dgamma", device, (H,), torch.float32)
-    a.dbeta = _like(dbeta, "dbeta", device, (H,), torch.float32)
-    a.n_tokens, a.hidden = B, H
-    a.y_dtype, a.s_dtype = _dt(dy, "dy"), _dt(s, "s")
-    a.x_dtype = _dt(dx, "dx") if dx is not None else FFF_F32
-    a.accumulate = int(bool(accumulate))
-    if p or rng_offset is not None:
-        _set_rng(a.drop, p, seed, offset, rng_offset, device)
-    if workspace is not None:
-        _gpu(workspace, "workspace", device)
-        a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    a.hip_stream = _raw_stream(device, stream)
-    _run("fff_layer_norm_backward", a, device)
+    if ds is None and "ds" in want:
+        ds = torch.empty(shape, dtype=s.dtype, device=device)
+    if dx is None and not alias and "dx" in want:
+        dx = torch.empty(shape, dtype=dx_dtype or dy.dtype, device=device)
+    if dgamma is None and "dgamma" in want:
+        dgamma = torch.empty(H, dtype=f32, device=device)
+    if dbeta is None and "dbeta" in want:
+        dbeta = torch.empty(H, dtype=f32, device=device)
+    if workspace is None and (dgamma is not None or dbeta is not None):
+        workspace = torch.empty(max(256, layer_norm_backward_workspace_bytes(B, H)), dtype=torch.uint8, device=device)
+    _run(_lib().fff_layer_norm_backward, FffLayerNormBackwardArgs(
+        dy.data_ptr(), s.data_ptr(), _like(mean, "mean", at, (B,), f32), _like(rstd, "rstd", at, (B,), f32),
+        _like(gamma, "gamma", at, (H,), f32), _like(ds_in, "ds_in", at, shape, s.dtype),
+        _like(ds, "ds", at, shape, s.dtype), _like(dx, "dx", at, shape), _like(dgamma, "dgamma", at, (H,), f32),
+        _like(dbeta, "dbeta", at, (H,), f32), B, H, _dt(dx, "dx") if dx is not None else FFF_F32, _dt(s, "s"),
+        _dt(dy, "dy"), int(bool(accumulate)),
+        _rng(p, seed, offset, rng_offset, at) if p or rng_offset is not None else _NO_DROP,
+        *_scratch(workspace, "workspace", at), _raw_stream(device, stream)))
     return ds, (ds if "dx" in want else None) if alias else dx, dgamma, dbeta
 
 
+@_on_call
 def dropout(x, p, seed, offset=0, *, rng_offset=None, residual=None, y=None, y_dtype=None, stream=None):
     """``y = residual + drop(x)`` (residual optional) through ``fff_dropout``; y may be x or residual.
 
     The gradient of x is ``dropout(dy, p, seed, offset)``: the mask is drawn again, never stored.
     Without a y it is allocated, of ``y_dtype`` or x's type."""
-    B, H = _rows(x, "x")
-    device = x.device
-    a = FffDropoutArgs()
+    B, H = shape = _rows(x, "x")
+    device, at = x.device, x.get_device()
     if y is None:
-        with _on_device(device), _on_stream(stream):
-            y = torch.empty((B, H), dtype=y_dtype or x.dtype, device=device)
-    a.x = x.data_ptr()
-    a.residual = _like(residual, "residual", device, (B, H))
-    a.y = _like(y, "y", device, (B, H))
-    a.n_tokens, a.hidden = B, H
-    a.x_dtype, a.y_dtype = _dt(x, "x"), _dt(y, "y")
-    a.r_dtype = _dt(residual, "residual") if residual is not None else FFF_F32
-    _set_rng(a.drop, p, seed, offset, rng_offset, device)
-    a.hip_stream = _raw_stream(device, stream)
-    _run("fff_dropout", a, device)
+        y = torch.empty(shape, dtype=y_dtype or x.dtype, device=device)
+    _run(_lib().fff_dropout, FffDropoutArgs(
+        x.data_ptr(), _like(residual, "residual", at, shape), _like(y, "y", at, shape), B, H, _dt(x, "x"),
+        _dt(residual, "residual") if residual is not None else FFF_F32, _dt(y, "y"), _rng(p, seed, offset, rng_offset, at),
+        _raw_stream(device, stream)))
     return y
 
 
 def group_rows_workspace_bytes(n_entries: int, n_ids: int, n_trees: int = 1) -> int:
-    return int(load_library().fff_group_rows_workspace_bytes(n_entries, n_ids, n_trees))
+    return int(_lib().fff_group_rows_workspace_bytes(n_entries, n_ids, n_trees))
 
 
+@_on_call
 def group_rows(ids, n_ids: int, *, first: int = 0, n_trees: int = 1, order=None, offsets=None, bad_ids=None,
                workspace=None, stream=None):
     """Entries by group through ``fff_group_rows``; returns (order, offsets), int32.
@@ -299,38 +314,27 @@ def group_rows(ids, n_ids: int, *, first: int = 0, n_trees: int = 1, order=None,
     group, ``offsets`` [n_trees * n_ids + 1] where each group's stand.  For the leaves of a forward:
     ``group_rows(nodes_out[..., depth].contiguous(), 2**depth, first=2**depth - 1, n_trees=n_trees)``."""
     _gpu(ids, "ids")
-    device, E = ids.device, ids.numel()
+    device, at, E = ids.device, ids.get_device(), ids.numel()
     if ids.dtype != torch.int32:
         raise ValueError("ids must be int32")
     if n_ids < 1 or n_trees < 1:
         raise ValueError("n_ids and n_trees must be positive")
     G = n_ids * n_trees
-    with _on_device(device), _on_stream(stream):
-        if order is None:
-            order = torch.empty(E, dtype=torch.int32, device=device)
-        if offsets is None:
-            offsets = torch.empty(G + 1, dtype=torch.int32, device=device)
-        if workspace is None:
-            workspace = torch.empty(max(256, group_rows_workspace_bytes(E, n_ids, n_trees)), dtype=torch.uint8,
-                                    device=device)
-    a = FffGroupRowsArgs()
-    a.ids = ids.data_ptr()
-    a.order = _index(order, "order", device, E)
-    a.offsets = _index(offsets, "offsets", device, G + 1)
-    a.bad_ids = _index(bad_ids, "bad_ids", device, 1)
-    a.n_entries, a.n_ids, a.n_trees, a.first = E, n_ids, n_trees, first
-    _gpu(workspace, "workspace", device)
-    a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    a.hip_stream = _raw_stream(device, stream)
-    _run("fff_group_rows", a, device)
+    if order is None:
+        order = torch.empty(E, dtype=torch.int32, device=device)
+    if offsets is None:
+        offsets = torch.empty(G + 1, dtype=torch.int32, device=device)
+    if workspace is None:
+        need = group_rows_workspace_bytes(E, n_ids, n_trees)
+        workspace = torch.empty(need, dtype=torch.uint8, device=device) if need else None
+    _run(_lib().fff_group_rows, FffGroupRowsArgs(
+        ids.data_ptr(), _index(order, "order", at, E), _index(offsets, "offsets", at, G + 1),
+        _index(bad_ids, "bad_ids", at, 1), E, n_ids, n_trees, first, *_scratch(workspace, "workspace", at),
+        _raw_stream(device, stream)))
     return order, offsets
 
 
-def _entries(x, index, x_div, what):
-    """How many entries read x's rows."""
-    return index.numel() if index is not None else x.shape[0] * x_div
-
-
+@_on_call
 def grouped_matmul(x, w, offsets, *, x_index=None, x_div=1, y=None, y_index=None, y_dtype=None, transpose_w=False,
                    act="identity", z_out=None, keep_z=False, z_in=None, stream=None):
     """Every entry's row times its group's matrix, through ``fff_grouped_matmul``.
@@ -343,52 +347,45 @@ def grouped_matmul(x, w, offsets, *, x_index=None, x_div=1, y=None, y_index=None
     Returns y, or (y, z) when z is kept.  y without an argument is allocated with a row per entry;
     its rows that no entry names are not written."""
     _gpu(x, "x")
-    _gpu(w, "w", x.device)
+    device, at = x.device, x.get_device()
+    _gpu(w, "w", at)
     if x.dim() != 2 or w.dim() != 3:
         raise ValueError("x must be [rows, k] and w [n_groups, n, k] ([n_groups, k, n] with transpose_w)")
     if x_div < 1:
         raise ValueError("x_div must be positive")
-    device = x.device
-    G, N, K = (w.shape[0], w.shape[2], w.shape[1]) if transpose_w else w.shape
+    if offsets is None:
+        raise ValueError("offsets are needed")
+    G, N, K = w.shape
+    if transpose_w:
+        N, K = K, N
     if x.shape[1] != K:
         raise ValueError(f"x has rows of {x.shape[1]}, w takes {K}")
-    E = _entries(x, x_index, x_div, "x")
-    a = FffGroupedMatmulArgs()
+    E = x_index.numel() if x_index is not None else x.shape[0] * x_div
     keep_z = keep_z or z_out is not None
     if keep_z and z_in is not None:
         raise ValueError("z_in makes a gradient: no z is kept")
-    if y is None or (keep_z and z_out is None):
-        with _on_device(device), _on_stream(stream):
-            if y is None:
-                y = torch.empty((E, N), dtype=y_dtype or x.dtype, device=device)
-            if keep_z and z_out is None:
-                z_out = torch.empty((E, N), dtype=y.dtype, device=device)
-    _gpu(y, "y", device)
+    if y is None:
+        y = torch.empty((E, N), dtype=y_dtype or x.dtype, device=device)
+    _gpu(y, "y", at)
     if y.dim() != 2 or y.shape[1] != N:
         raise ValueError(f"y must have rows of {N}")
-    a.x, a.w, a.y = x.data_ptr(), w.data_ptr(), y.data_ptr()
-    if offsets is None:
-        raise ValueError("offsets are needed")
-    a.offsets = _index(offsets, "offsets", device, G + 1)
-    a.x_index = _index(x_index, "x_index", device, E)
-    a.y_index = _index(y_index, "y_index", device, E)
-    a.z_out = _like(z_out, "z_out", device, (E, N))
-    a.z_in = _like(z_in, "z_in", device, (E, N))
+    if keep_z and z_out is None:
+        z_out = torch.empty((E, N), dtype=y.dtype, device=device)
     z = z_out if z_out is not None else z_in
-    a.n_entries, a.x_rows, a.y_rows = E, x.shape[0], y.shape[0]
-    a.n_groups, a.k, a.n, a.x_div, a.w_transposed = G, K, N, x_div, int(bool(transpose_w))
-    a.x_dtype, a.w_dtype, a.y_dtype = _dt(x, "x"), _dt(w, "w"), _dt(y, "y")
-    a.z_dtype = _dt(z, "z") if z is not None else FFF_F32
-    a.act = ACTS[act] if isinstance(act, str) else int(act)
-    a.hip_stream = _raw_stream(device, stream)
-    _run("fff_grouped_matmul", a, device)
+    _run(_lib().fff_grouped_matmul, FffGroupedMatmulArgs(
+        x.data_ptr(), w.data_ptr(), _index(offsets, "offsets", at, G + 1), _index(x_index, "x_index", at, E),
+        _index(y_index, "y_index", at, E), y.data_ptr(), _like(z_out, "z_out", at, (E, N)), _like(z_in, "z_in", at, (E, N)),
+        E, x.shape[0], y.shape[0], G, K, N, x_div, int(bool(transpose_w)), _dt(x, "x"), _dt(w, "w"), _dt(y, "y"),
+        _dt(z, "z") if z is not None else FFF_F32, ACTS[act] if isinstance(act, str) else int(act),
+        _raw_stream(device, stream)))
     return (y, z_out) if keep_z else y
 
 
 def grouped_weight_grad_workspace_bytes(n_entries: int, n_groups: int, k: int, n: int) -> int:
-    return int(load_library().fff_grouped_weight_grad_workspace_bytes(n_entries, n_groups, k, n))
+    return int(_lib().fff_grouped_weight_grad_workspace_bytes(n_entries, n_groups, k, n))
 
 
+@_on_call
 def grouped_weight_grad(dy, x, offsets, *, dy_index=None, x_index=None, x_div=1, dw=None, accumulate=False,
                         workspace=None, stream=None):
     """``dW_g = sum dy_i^T x_i`` over every group's entries, through ``fff_grouped_weight_grad``.
@@ -397,38 +394,26 @@ def grouped_weight_grad(dy, x, offsets, *, dy_index=None, x_index=None, x_div=1,
     ``accumulate``.  Entry i reads row ``dy_index[i]`` of dy (i without) and ``x_index[i] // x_div`` of
     x (i // x_div without).  For a W used transposed, pass x as ``dy`` and dy as ``x``."""
     _gpu(dy, "dy")
-    _gpu(x, "x", dy.device)
+    device, at = dy.device, dy.get_device()
+    _gpu(x, "x", at)
     if x.dim() != 2 or dy.dim() != 2:
         raise ValueError("dy must be [rows, n] and x [rows, k]")
     if x_div < 1:
         raise ValueError("x_div must be positive")
     if offsets is None or offsets.numel() < 2:
         raise ValueError("offsets must hold n_groups + 1 values")
-    device = dy.device
     N, K, G = dy.shape[1], x.shape[1], offsets.numel() - 1
     E = dy_index.numel() if dy_index is not None else dy.shape[0]
     if accumulate and dw is None:
         raise ValueError("accumulate adds to the dw that is given")
-    a = FffGroupedWeightGradArgs()
-    need = grouped_weight_grad_workspace_bytes(E, G, K, N)
-    if dw is None or (workspace is None and need):
-        with _on_device(device), _on_stream(stream):
-            if dw is None:
-                dw = torch.empty((G, N, K), dtype=torch.float32, device=device)
-            if workspace is None and need:
-                workspace = torch.empty(need, dtype=torch.uint8, device=device)
-    a.dy, a.x = dy.data_ptr(), x.data_ptr()
-    a.offsets = _index(offsets, "offsets", device, G + 1)
-    a.dy_index = _index(dy_index, "dy_index", device, E)
-    a.x_index = _index(x_index, "x_index", device, E)
-    a.dw = _like(dw, "dw", device, (G, N, K), torch.float32)
-    a.n_entries, a.dy_rows, a.x_rows = E, dy.shape[0], x.shape[0]
-    a.n_groups, a.k, a.n, a.x_div = G, K, N, x_div
-    a.dy_dtype, a.x_dtype = _dt(dy, "dy"), _dt(x, "x")
-    a.accumulate = int(bool(accumulate))
-    if workspace is not None:
-        _gpu(workspace, "workspace", device)
-        a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    a.hip_stream = _raw_stream(device, stream)
-    _run("fff_grouped_weight_grad", a, device)
+    if dw is None:
+        dw = torch.empty((G, N, K), dtype=torch.float32, device=device)
+    if workspace is None:
+        need = grouped_weight_grad_workspace_bytes(E, G, K, N)
+        workspace = torch.empty(need, dtype=torch.uint8, device=device) if need else None
+    _run(_lib().fff_grouped_weight_grad, FffGroupedWeightGradArgs(
+        dy.data_ptr(), x.data_ptr(), _index(offsets, "offsets", at, G + 1), _index(dy_index, "dy_index", at, E),
+        _index(x_index, "x_index", at, E), _like(dw, "dw", at, (G, N, K), torch.float32), E, dy.shape[0], x.shape[0],
+        G, K, N, x_div, _dt(dy, "dy"), _dt(x, "x"), int(bool(accumulate)), *_scratch(workspace, "workspace", at),
+        _raw_stream(device, stream)))
     return dw

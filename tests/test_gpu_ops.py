@@ -205,6 +205,26 @@ def test_dropout_hides_what_it_drops(fff_lib):
         assert torch.equal(got, want)
 
 
+def test_keywords_and_streams_of_the_binding(fff_lib):
+    x = _randn(_gen(3), 8, 64)
+    want = fff_lib.dropout(x, 0.5, 7)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    got = fff_lib.dropout(x=x, p=0.5, seed=7, stream=side)
+    side.synchronize()
+    assert torch.equal(got, want)
+    with pytest.raises(ValueError):
+        fff_lib.dropout(x.t(), 0.5, 7)
+    with pytest.raises(ValueError):
+        fff_lib.dropout(x.half(), 0.5, 7)
+    with pytest.raises(ValueError):
+        fff_lib.dropout(x, 1.0, 7)
+    with pytest.raises(ValueError):
+        fff_lib.layer_norm(x, torch.ones(63, device=DEV))
+    with pytest.raises(fff_lib.FffError):
+        fff_lib.layer_norm(x, eps=-1.0)
+
+
 def test_rows_past_four_billion_elements(fff_lib):
     """65552 rows of 65536: offsets and addresses past 32 bits (checked on sampled rows)."""
     B, H = 65552, 65536
