@@ -4,7 +4,7 @@
 //
 // Only the device knows how many entries a group has, so a launch covers the
 // most row tiles there can be and every workgroup finds its tile from the
-// offsets (find_tile).  The product runs on the matrix cores
+// offsets (TileMap).  The product runs on the matrix cores
 // (fff_grouped.hpp); its 32 x 32 blocks then pass through LDS, so that the
 // epilogue works on eight consecutive columns a lane and stores whole lines.
 #include "fff_grouped.hpp"
@@ -143,36 +143,28 @@ __global__ __launch_bounds__(G::THREADS, 2) void grouped_kernel(GroupedParams p)
         return (at % CPL ^ col_key<G::BF, G::BN>(at / CPL)) * G::EV;
     };
     uint4 ra[DMA ? 1 : G::LA], rb[DMA ? 1 : G::LB];
-    auto issue = [&](int64_t s, int stage) {
+    auto issue = [&](int64_t s, int stage, int l) {
         const bool part = s == steps - 1 && p.k % G::KS != 0;
         const int k0 = int(s) * G::KS;
-        if constexpr (DMA) {
-            const uint32_t st = lds0 + uint32_t(stage) * G::STAGE;
-#pragma unroll
-            for (int i = 0; i < G::LA; ++i)
-                lds_dma16(part && k0 + row_at(wave * G::LA + i) >= p.k ? zero : pa[i] + s * G::ROWB,
-                          st + (wave * G::LA + i) * 1024);
-#pragma unroll
-            for (int i = 0; i < G::LB; ++i) {
-                const int w = wave * G::LB + i;
-                const char* q = pb[i] + s * bstep;
-                if constexpr (BCOL) {
-                    if (n0 + col_at(w) >= p.n || (part && k0 + col_row(w) >= p.k)) q = zero;
-                } else {
-                    if (part && k0 + row_at(w) >= p.k) q = zero;
-                }
-                lds_dma16(q, st + G::BM * G::ROWB + w * 1024);
-            }
+        const uint32_t st = lds0 + uint32_t(stage) * G::STAGE;
+        if (l < G::LA) {
+            const int i = l, at = wave * G::LA + i;
+            if constexpr (DMA) lds_dma16(part && k0 + row_at(at) >= p.k ? zero : pa[i] + s * G::ROWB, st + at * 1024);
+            else ra[i] = load16<G::BF>(pa[i] + s * G::ROWB, int64_t(p.k) - k0 - row_at(at));
         } else {
-#pragma unroll
-            for (int i = 0; i < G::LA; ++i)
-                ra[i] = load16<G::BF>(pa[i] + s * G::ROWB, int64_t(p.k) - k0 - row_at(wave * G::LA + i));
-#pragma unroll
-            for (int i = 0; i < G::LB; ++i) {
-                const int w = wave * G::LB + i;
-                int64_t left = int64_t(p.k) - k0 - (BCOL ? col_row(w) : row_at(w));
-                if constexpr (BCOL) left = left > 0 ? int64_t(p.n) - n0 - col_at(w) : 0;
-                rb[i] = load16<G::BF>(pb[i] + s * bstep, left);
+            const int i = l - G::LA, at = wave * G::LB + i;
+            const char* q = pb[i] + s * bstep;
+            if constexpr (DMA) {
+                if constexpr (BCOL) {
+                    if (n0 + col_at(at) >= p.n || (part && k0 + col_row(at) >= p.k)) q = zero;
+                } else {
+                    if (part && k0 + row_at(at) >= p.k) q = zero;
+                }
+                lds_dma16(q, st + G::BM * G::ROWB + at * 1024);
+            } else {
+                int64_t left = int64_t(p.k) - k0 - (BCOL ? col_row(at) : row_at(at));
+                if constexpr (BCOL) left = left > 0 ? int64_t(p.n) - n0 - col_at(at) : 0;
+                rb[i] = load16<G::BF>(q, left);
             }
         }
     };
@@ -209,7 +201,8 @@ __global__ __launch_bounds__(G::THREADS, 2) void grouped_kernel(GroupedParams p)
                 pb[i] = w + (int64_t(n) * p.k + row_at(at)) * G::ESZ;
             }
         }
-        issue(0, 0);
+#pragma unroll
+        for (int l = 0; l < G::LPS; ++l) issue(0, 0, l);
         for (int r = tid; r < G::BM; r += G::THREADS) {
             const int64_t i = t.m0 + r;
             s_dst[buf][r] = i < t.m1 ? int32_t(entry_row(p.y_index, 1, p.y_rows, i)) : -1;
@@ -242,7 +235,7 @@ __global__ __launch_bounds__(G::THREADS, 2) void grouped_kernel(GroupedParams p)
             for (int j = 0; j < G::TN; ++j)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
-        grouped_loop<G, DMA, false, BCOL>(glds, steps, acc, issue, commit);
+        grouped_loop<G, DMA, false, BCOL>(glds, steps, acc, [](int64_t) {}, issue, commit);
         __syncthreads();  // every wave is done with the stages
         const Tile next = s_tile[turn ^ 1];
         if (DMA && next.g >= 0) begin(next, turn ^ 1);
@@ -432,7 +425,9 @@ int grouped_variant(const GroupedParams& p, int cus) {
     }
     const TileCost* cost = p.bf16 ? COST_BF16 : COST_F32;
     for (int v = 0; v < (p.bf16 ? 4 : 3); ++v) {
-        const double per_cu = std::ceil(row_tiles(cost[v].bm) * ((p.n + cost[v].bn - 1) / cost[v].bn) / cus);
+        // (the half tile a group is an estimate: a tenth of a round does not make one)
+        const double per_cu =
+            std::max(1.0, std::ceil(row_tiles(cost[v].bm) * ((p.n + cost[v].bn - 1) / cost[v].bn) / cus - 0.1));
         const double pairs = std::floor(per_cu / 2), odd = per_cu - 2 * pairs;
         const double t = pairs * (cost[v].start * (v == 3 ? 2 : 1) + steps * cost[v].pair) +
                          odd * (cost[v].start + steps * cost[v].alone);

@@ -275,68 +275,100 @@ struct GCfg {
     // workgroups a CU holds: 160 KB of LDS (4 KB for the kernels' own arrays), two waves a SIMD
     static constexpr int PER_CU = int(std::min<size_t>((160 * 1024) / (LDS + 4096), 8 / WAVES));
     static_assert(BM * ROWB % (1024 * WAVES) == 0 && BN * ROWB % (1024 * WAVES) == 0, "whole wave loads");
-    static_assert(LPS * (S - 2) <= 63, "vmcnt holds 6 bits");
+    static_assert(LPS * (S - 1) <= 63, "vmcnt holds 6 bits");
+    static_assert(SLICES % 2 == 0, "slice 0 of every step reads the same registers");
 };
 
-// The matrix-core loop over `steps` steps, of which the caller has issued the first.  issue(step, stage) starts (DMA) the loads of a step into its
-// stage or, without DMA, reads them into registers, which commit(stage) stores; ACOL, BCOL: column
-// tiles.  The wave's TM x TN blocks are summed into acc.
-template <class G, bool DMA, bool ACOL, bool BCOL, class Issue, class Commit>
+// The matrix-core loop over `steps` steps.  issue(step, stage, l) starts load l of LPS of a step into its
+// stage (DMA) or reads it into registers, which commit(stage) stores; prepare(step) does what the loads
+// of a step need earlier.  The caller has prepared and issued step 0.  ACOL, BCOL:
+// column tiles.
+//
+// The fragments of slice kk + 1 are read while slice kk's MFMAs run, across steps too: the barrier that
+// ends a step stands before its last slice's MFMAs, when all its fragments are in registers, so the next
+// step's first reads, and the loads into the stage just read, run under those MFMAs (with the
+// barrier between the steps the matrix cores waited for a whole LDS read each step).  Those loads start at
+// once behind the barrier, which is soonest, or (SPREAD: two column tiles, whose reads take twice the
+// instructions) between the MFMAs: 65536 entries, 1024 -> 4096, weight gradients 762 us spread, 812 at
+// once; forward 835 and 822.
+template <class G, bool DMA, bool ACOL, bool BCOL, class Prepare, class Issue, class Commit>
 __device__ __forceinline__ void grouped_loop(unsigned char* lds, int64_t steps, tile_v16f (&acc)[G::TM][G::TN],
-                                             Issue issue, Commit commit) {
+                                             Prepare prepare, Issue issue, Commit commit) {
+    constexpr int S = DMA ? G::S : 2;
+    constexpr bool SPREAD = DMA && ACOL;
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / G::WGN, wn = wave % G::WGN;
-    auto compute = [&](const unsigned char* st) {
-        uint4 fa[2][G::TM], fb[2][G::TN];
-        auto read = [&](int kk, int buf) {
+    uint4 fa[2][G::TM], fb[2][G::TN];
+    auto read = [&](const unsigned char* st, int kk) {
 #pragma unroll
-            for (int j = 0; j < G::TN; ++j) {
-                const int c0 = (wn * G::TN + j) * 32;
-                if constexpr (BCOL) fb[buf][j] = col_frag<G::BF, G::BN>(st + G::BM * G::ROWB, c0, kk, lane);
-                else fb[buf][j] = row_frag<G::ROWB>(st + G::BM * G::ROWB, c0, kk, lane);
-            }
+        for (int j = 0; j < G::TN; ++j) {
+            const int c0 = (wn * G::TN + j) * 32;
+            if constexpr (BCOL) fb[kk & 1][j] = col_frag<G::BF, G::BN>(st + G::BM * G::ROWB, c0, kk, lane);
+            else fb[kk & 1][j] = row_frag<G::ROWB>(st + G::BM * G::ROWB, c0, kk, lane);
+        }
 #pragma unroll
-            for (int i = 0; i < G::TM; ++i) {
-                const int r0 = (wm * G::TM + i) * 32;
-                if constexpr (ACOL) fa[buf][i] = col_frag<G::BF, G::BM>(st, r0, kk, lane);
-                else fa[buf][i] = row_frag<G::ROWB>(st, r0, kk, lane);
-            }
-        };
-        // the fragments of slice kk + 1 are read while slice kk's MFMAs run
-        read(0, 0);
-#pragma unroll
-        for (int kk = 0; kk < G::SLICES; ++kk) {
-            if (kk + 1 < G::SLICES) read(kk + 1, (kk + 1) & 1);
-            __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-            for (int i = 0; i < G::TM; ++i)
-#pragma unroll
-                for (int j = 0; j < G::TN; ++j) mfma_slice<G::BF>(acc[i][j], fa[kk & 1][i], fb[kk & 1][j]);
+        for (int i = 0; i < G::TM; ++i) {
+            const int r0 = (wm * G::TM + i) * 32;
+            if constexpr (ACOL) fa[kk & 1][i] = col_frag<G::BF, G::BM>(st, r0, kk, lane);
+            else fa[kk & 1][i] = row_frag<G::ROWB>(st, r0, kk, lane);
         }
     };
-    if constexpr (DMA) {
-        // step 0 is on its way already; the first wait below is for all that this wave has in flight
+    auto issue_all = [&](int64_t s, int stage) {
 #pragma unroll
-        for (int s = 1; s < G::S - 1; ++s)
-            if (s < steps) issue(s, s);
-        int stage = 0, ahead = G::S - 1;  // stages of step s and of step s + S - 1
-        for (int64_t s = 0; s < steps; ++s) {
-            const int64_t left = steps - 1 - s;
-            wait_steps<G::S - 2, G::LPS>(int(left < G::S - 2 ? left : G::S - 2));
-            __syncthreads();  // step s is in LDS for every wave; every wave is done with step s - 1
-            if (s + G::S - 1 < steps) issue(s + G::S - 1, ahead);
-            compute(lds + stage * G::STAGE);
-            stage = stage + 1 == G::S ? 0 : stage + 1;
-            ahead = ahead + 1 == G::S ? 0 : ahead + 1;
-        }
+        for (int l = 0; l < G::LPS; ++l) issue(s, stage, l);
+    };
+    if constexpr (DMA) {
+#pragma unroll
+        for (int s = 1; s < S; ++s)
+            if (s < steps) {
+                prepare(s);
+                issue_all(s, s);
+            }
+        wait_steps<S - 1, G::LPS>(int(steps - 1 < S - 1 ? steps - 1 : S - 1));
     } else {
-        for (int64_t s = 0; s < steps; ++s) {
-            commit(int(s & 1));
-            __syncthreads();  // step s is in LDS; step s - 1, two commits back, is done with
-            if (s + 1 < steps) issue(s + 1, 0);
-            compute(lds + (s & 1) * G::STAGE);
+        commit(0);
+        if (steps > 1) {
+            prepare(1);
+            issue_all(1, 0);
         }
+    }
+    __syncthreads();  // step 0 is in LDS
+    read(lds, 0);
+    int stage = 0;
+    for (int64_t s = 0; s < steps; ++s) {
+        const unsigned char* st = lds + stage * G::STAGE;
+        const int follow = stage + 1 == S ? 0 : stage + 1;
+        const int64_t load = s + S;  // the step whose loads this one starts
+        if (load < steps) prepare(load);
+#pragma unroll
+        for (int kk = 0; kk < G::SLICES; ++kk) {
+            if (kk + 1 < G::SLICES) {
+                read(st, kk + 1);
+            } else if (s + 1 < steps) {
+                if constexpr (DMA) {
+                    const int64_t left = steps - 2 - s;
+                    wait_steps<S - 2, G::LPS>(int(left < S - 2 ? left : S - 2));
+                } else {
+                    commit(follow);
+                }
+                __syncthreads();  // step s + 1 is in LDS; every wave has read all of step s
+                if (!SPREAD && load < steps) issue_all(load, stage);
+                read(lds + follow * G::STAGE, 0);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < G::TM; ++i) {
+                if (SPREAD && kk + 1 == G::SLICES && load < steps) {
+#pragma unroll
+                    for (int l = i * G::LPS / G::TM; l < (i + 1) * G::LPS / G::TM; ++l) issue(load, stage, l);
+                }
+#pragma unroll
+                for (int j = 0; j < G::TN; ++j) mfma_slice<G::BF>(acc[i][j], fa[kk & 1][i], fb[kk & 1][j]);
+                if (SPREAD && kk + 1 == G::SLICES) __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        stage = follow;
     }
 }
 

@@ -95,29 +95,32 @@ __global__ __launch_bounds__(G::THREADS, 2) void grouped_grad_kernel(GroupedGrad
     auto acol = [&](int at) { return ((at * 64 + lane) % CPA ^ col_key<G::BF, G::BM>(row_of(at, CPA))) * G::EV; };
     auto bcol = [&](int at) { return ((at * 64 + lane) % CPB ^ col_key<G::BF, G::BN>(row_of(at, CPB))) * G::EV; };
     uint4 ra[DMA ? 1 : G::LA], rb[DMA ? 1 : G::LB];
-    auto issue = [&](int64_t s, int stage) {
+    // a step's rows, read from LDS ahead of its loads; the next chunk's rows: looked up at a chunk's second
+    // step, stored at its fifth, used from the eighth on (a barrier between any two steps' loads)
+    int32_t da[G::LA], xb[G::LB];
+    auto prepare = [&](int64_t s) {
         const int64_t c = s / 8;
         const int e0 = int(s % 8) * G::KS;
-        const uint32_t st = lds0 + uint32_t(stage) * G::STAGE;
 #pragma unroll
-        for (int i = 0; i < G::LA; ++i) {
-            const int at = wave * G::LA + i, n = n0 + acol(at);
-            const int32_t r = s_row[c & 1][0][e0 + row_of(at, CPA)];
-            const char* q = static_cast<const char*>(p.dy) + uint64_t(uint32_t(r)) * dypitch + n * G::ESZ;
-            if constexpr (DMA) lds_dma16(r < 0 || n >= p.n ? zero : q, st + at * 1024);
-            else ra[i] = load16<G::BF>(q, r < 0 ? 0 : p.n - n);
-        }
+        for (int i = 0; i < G::LA; ++i) da[i] = s_row[c & 1][0][e0 + row_of(wave * G::LA + i, CPA)];
 #pragma unroll
-        for (int i = 0; i < G::LB; ++i) {
-            const int at = wave * G::LB + i, k = k0 + bcol(at);
-            const int32_t r = s_row[c & 1][1][e0 + row_of(at, CPB)];
-            const char* q = static_cast<const char*>(p.x) + uint64_t(uint32_t(r)) * xpitch + k * G::ESZ;
-            if constexpr (DMA) lds_dma16(r < 0 || k >= p.k ? zero : q, st + G::BM * G::ROWB + at * 1024);
-            else rb[i] = load16<G::BF>(q, r < 0 ? 0 : p.k - k);
-        }
-        // the next chunk's rows: read at a chunk's second step, stored at its fifth, used from the eighth on
+        for (int i = 0; i < G::LB; ++i) xb[i] = s_row[c & 1][1][e0 + row_of(wave * G::LB + i, CPB)];
         if (s % 8 == 1) look(c + 1);
         if (s % 8 == 4) note(c + 1);
+    };
+    auto issue = [&](int64_t, int stage, int l) {
+        const uint32_t st = lds0 + uint32_t(stage) * G::STAGE;
+        if (l < G::LA) {
+            const int i = l, at = wave * G::LA + i, n = n0 + acol(at);
+            const char* q = static_cast<const char*>(p.dy) + uint64_t(uint32_t(da[i])) * dypitch + n * G::ESZ;
+            if constexpr (DMA) lds_dma16(da[i] < 0 || n >= p.n ? zero : q, st + at * 1024);
+            else ra[i] = load16<G::BF>(q, da[i] < 0 ? 0 : p.n - n);
+        } else {
+            const int i = l - G::LA, at = wave * G::LB + i, k = k0 + bcol(at);
+            const char* q = static_cast<const char*>(p.x) + uint64_t(uint32_t(xb[i])) * xpitch + k * G::ESZ;
+            if constexpr (DMA) lds_dma16(xb[i] < 0 || k >= p.k ? zero : q, st + G::BM * G::ROWB + at * 1024);
+            else rb[i] = load16<G::BF>(q, xb[i] < 0 ? 0 : p.k - k);
+        }
     };
     auto commit = [&](int stage) {
         if constexpr (!DMA) {
@@ -140,8 +143,10 @@ __global__ __launch_bounds__(G::THREADS, 2) void grouped_grad_kernel(GroupedGrad
         look(0);
         note(0);
         __syncthreads();
-        issue(0, 0);
-        grouped_loop<G, DMA, true, true>(glds, steps, acc, issue, commit);
+        prepare(0);
+#pragma unroll
+        for (int l = 0; l < G::LPS; ++l) issue(0, 0, l);
+        grouped_loop<G, DMA, true, true>(glds, steps, acc, prepare, issue, commit);
     }
     // a result's columns are consecutive over 32 lanes: whole 128-byte lines without another pass
     const bool add = splits == 1 && p.accumulate;
