@@ -143,6 +143,11 @@ __global__ __launch_bounds__(G::THREADS, 2) void grouped_kernel(GroupedParams p)
         return (at % CPL ^ col_key<G::BF, G::BN>(at / CPL)) * G::EV;
     };
     uint4 ra[DMA ? 1 : G::LA], rb[DMA ? 1 : G::LB];
+    [[maybe_unused]] uint64_t offs = 0;  // four bits a load: elements it was read early by
+    [[maybe_unused]] int off;
+    [[maybe_unused]] auto note = [&](int l, const uint4&, int early) {
+        offs = (l == 0 ? 0 : offs) | uint64_t(early) << (4 * l);
+    };
     auto issue = [&](int64_t s, int stage, int l) {
         const bool part = s == steps - 1 && p.k % G::KS != 0;
         const int k0 = int(s) * G::KS;
@@ -150,7 +155,7 @@ __global__ __launch_bounds__(G::THREADS, 2) void grouped_kernel(GroupedParams p)
         if (l < G::LA) {
             const int i = l, at = wave * G::LA + i;
             if constexpr (DMA) lds_dma16(part && k0 + row_at(at) >= p.k ? zero : pa[i] + s * G::ROWB, st + at * 1024);
-            else ra[i] = load16<G::BF>(pa[i] + s * G::ROWB, int64_t(p.k) - k0 - row_at(at));
+            else note(l, ra[i] = load16<G::BF>(pa[i] + s * G::ROWB, int64_t(p.k) - k0 - row_at(at), p.k, off), off);
         } else {
             const int i = l - G::LA, at = wave * G::LB + i;
             const char* q = pb[i] + s * bstep;
@@ -164,13 +169,19 @@ __global__ __launch_bounds__(G::THREADS, 2) void grouped_kernel(GroupedParams p)
             } else {
                 int64_t left = int64_t(p.k) - k0 - (BCOL ? col_row(at) : row_at(at));
                 if constexpr (BCOL) left = left > 0 ? int64_t(p.n) - n0 - col_at(at) : 0;
-                rb[i] = load16<G::BF>(q, left);
+                note(l, rb[i] = load16<G::BF>(q, left, BCOL ? p.n : p.k, off), off);
             }
         }
     };
     auto commit = [&](int stage) {
         if constexpr (!DMA) {
             unsigned char* st = glds + stage * G::STAGE;
+            if (offs) {
+#pragma unroll
+                for (int i = 0; i < G::LA; ++i) ra[i] = shift16<G::BF>(ra[i], int(offs >> (4 * i)) & 15);
+#pragma unroll
+                for (int i = 0; i < G::LB; ++i) rb[i] = shift16<G::BF>(rb[i], int(offs >> (4 * (G::LA + i))) & 15);
+            }
 #pragma unroll
             for (int i = 0; i < G::LA; ++i) *reinterpret_cast<uint4*>(st + (wave * G::LA + i) * 1024 + lane * 16) = ra[i];
 #pragma unroll
@@ -266,6 +277,12 @@ __global__ __launch_bounds__(G::THREADS, 2) void grouped_kernel(GroupedParams p)
     }
 }
 
+// Whether the operands' rows are whole 16-byte vectors.
+bool whole_vectors(const GroupedParams& p) {
+    const int ev = p.bf16 ? 8 : 4;
+    return p.k % ev == 0 && (!p.w_transposed || p.n % ev == 0);
+}
+
 template <class G>
 hipError_t launch_grouped(const GroupedParams& p, int cus, hipStream_t stream, int* status) {
     const int64_t tiles = most_tiles(p.n_entries, p.n_groups, G::BM) * ((int64_t(p.n) + G::BN - 1) / G::BN);
@@ -274,9 +291,9 @@ hipError_t launch_grouped(const GroupedParams& p, int cus, hipStream_t stream, i
     const int grid = int(std::min<int64_t>(tiles, int64_t(cus) * G::PER_CU));
     auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(unsigned(grid)), dim3(G::THREADS), G::LDS, stream, p); };
     // rows of whole 16-byte vectors go straight to LDS
-    const bool dma = p.k % G::EV == 0 && (!p.w_transposed || p.n % G::EV == 0);
-    if (p.w_transposed) dma ? launch(grouped_kernel<G, true, true>) : launch(grouped_kernel<G, false, true>);
-    else dma ? launch(grouped_kernel<G, true, false>) : launch(grouped_kernel<G, false, false>);
+    const bool dma = whole_vectors(p);
+    if (dma) p.w_transposed ? launch(grouped_kernel<G, true, true>) : launch(grouped_kernel<G, true, false>);
+    else if constexpr (G::BM < 256) p.w_transposed ? launch(grouped_kernel<G, false, true>) : launch(grouped_kernel<G, false, false>);
     return hipGetLastError();
 }
 
@@ -331,7 +348,11 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void grouped_few_kernel(GroupedPara
     auto load = [&](const char* row, int64_t k, bool in) {  // sixteen bytes from element k on
         const int64_t left = in ? int64_t(p.k) - k : 0;
         if constexpr (ALIGNED) return left > 0 ? *reinterpret_cast<const uint4*>(row + k * ESZ) : make_uint4(0, 0, 0, 0);
-        else return load16<BF>(row + k * ESZ, left);
+        else {
+            int off;
+            const uint4 v = load16<BF>(row + k * ESZ, left, p.k, off);
+            return off ? shift16<BF>(v, off) : v;
+        }
     };
     tile_v4f acc = {0.0f, 0.0f, 0.0f, 0.0f};
     const int steps = (p.k + STEP - 1) / STEP;
@@ -424,7 +445,8 @@ int grouped_variant(const GroupedParams& p, int cus) {
         least = rounds < 1 ? 2.5 + 0.115 * kb * std::max(rounds, 0.35) * slow : rounds * (2.5 + 0.115 * kb) * slow;
     }
     const TileCost* cost = p.bf16 ? COST_BF16 : COST_F32;
-    for (int v = 0; v < (p.bf16 ? 4 : 3); ++v) {
+    // (256 x 256 tiles through registers spill: 65536 entries, 1023 -> 4095: 1042 us)
+    for (int v = 0; v < (p.bf16 && whole_vectors(p) ? 4 : 3); ++v) {
         // (the half tile a group is an estimate: a tenth of a round does not make one)
         const double per_cu =
             std::max(1.0, std::ceil(row_tiles(cost[v].bm) * ((p.n + cost[v].bn - 1) / cost[v].bn) / cus - 0.1));

@@ -166,20 +166,20 @@ __device__ __forceinline__ float act_slope(float z) {
 // Sixteen zero bytes: what a lane stages for places outside its matrix.
 static __device__ const uint4 g_zero16 = {0, 0, 0, 0};
 
-// Sixteen bytes of a row from element e of `left` (elements behind it zero); rows at any element.
+// Sixteen bytes of a row, `left` of its elements from p on in it (none where left <= 0: zeros); rows of
+// `len` elements at any element.  A vector that ends past the row is read so that it ends with the row,
+// `off` elements early, for shift16 to put right when the load has arrived.  (Element by element, as rows
+// shorter than a vector still are, edge tiles took several times as long as whole ones.)
 template <bool BF>
-__device__ __forceinline__ uint4 load16(const char* p, int64_t left) {
-    constexpr int EV = BF ? 8 : 4;
+__device__ __forceinline__ uint4 load16(const char* p, int64_t left, int len, int& off) {
+    constexpr int EV = BF ? 8 : 4, ESZ = 16 / EV;
     typedef uint32_t u4_a2 __attribute__((ext_vector_type(4), aligned(2)));
-    typedef uint32_t u4_a4 __attribute__((ext_vector_type(4), aligned(4)));
-    if (left >= EV) {
-        if constexpr (BF) {
-            const u4_a2 v = *reinterpret_cast<const u4_a2*>(p);
-            return make_uint4(v.x, v.y, v.z, v.w);
-        } else {
-            const u4_a4 v = *reinterpret_cast<const u4_a4*>(p);
-            return make_uint4(v.x, v.y, v.z, v.w);
-        }
+    off = 0;
+    if (left <= 0) return make_uint4(0, 0, 0, 0);
+    if (len >= EV) {
+        off = left >= EV ? 0 : EV - int(left);
+        const u4_a2 v = *reinterpret_cast<const u4_a2*>(p - off * ESZ);
+        return make_uint4(v.x, v.y, v.z, v.w);
     }
     uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll
@@ -189,6 +189,15 @@ __device__ __forceinline__ uint4 load16(const char* p, int64_t left) {
         else w[j] = reinterpret_cast<const uint32_t*>(p)[j];
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
+}
+// The vector without its first `off` elements, zeros behind (off < 8 bf16 or 4 fp32 elements).
+template <bool BF>
+__device__ __forceinline__ uint4 shift16(const uint4& r, int off) {
+    const int bits = off * (BF ? 16 : 32);
+    const uint64_t lo = uint64_t(r.y) << 32 | r.x, hi = uint64_t(r.w) << 32 | r.z;
+    const uint64_t l = bits == 0 ? lo : bits >= 64 ? hi >> (bits - 64) : lo >> bits | hi << (64 - bits);
+    const uint64_t h = bits >= 64 ? 0 : hi >> bits;
+    return make_uint4(uint32_t(l), uint32_t(l >> 32), uint32_t(h), uint32_t(h >> 32));
 }
 
 // Order of the 16-byte vectors in LDS: vector v of row r at v ^ key, so that the lanes of a fragment

@@ -16,30 +16,36 @@ enum { ST_OK_ = 0, ST_UNSUPPORTED_ = -2 };
 
 using GradBig = GCfg<true, 4, 2, 2, 4, 2, 128>;    // 256 x 256, eight waves
 using GradSmall = GCfg<true, 2, 2, 2, 2, 2, 128>;  // 128 x 128, four waves
-using GradF32 = GCfg<false, 2, 2, 2, 2, 2, 128>;
+using GradTiny = GCfg<true, 1, 1, 2, 2, 3, 128>;   // 64 x 64, four waves
+using GradSmallF32 = GCfg<false, 2, 2, 2, 2, 2, 128>;
+using GradTinyF32 = GCfg<false, 1, 1, 2, 2, 3, 128>;
 
 constexpr size_t GRAD_PART_BYTES = size_t(64) << 20;  // partial sums, at most
 
 struct GradPlan {
-    bool big;
-    int bm, bn, splits;
+    int bm, splits;
     int64_t tiles;
 };
 
-// Tiles of 256 x 256 where a group's matrix has them and there are enough; splits: up to two workgroups
-// a CU, eight steps of the mean group each at least, within GRAD_PART_BYTES.  By the sizes alone, so
-// the workspace's size and the result's bits are too.
+// 256 x 256 tiles where rows are whole 16-byte vectors and there are 64 of them; else 128 x 128, unless
+// they and their splits leave the CUs' 512 places a third empty in their only or second round, where
+// 64 x 64 does better (us, 128 and 64: 5003 fp32 entries, 64 groups of 203 x 300: 39, 30; 8000 x 16 of
+// 768 x 768: 169, 140; where 128 fills them, 16384 x 8 of 1024 x 1024: 444, 511; bf16, 65536 x 1 of
+// 768 x 768: 172, 276).  Splits: up to two workgroups a CU, eight steps of the mean group each at least,
+// within GRAD_PART_BYTES.  By the sizes alone, so the workspace's size and the result's bits are too.
 GradPlan grad_plan(int64_t n_entries, int32_t n_groups, int32_t k, int32_t n, bool bf16) {
     auto cdiv = [](int64_t a, int64_t b) { return (a + b - 1) / b; };
-    GradPlan p;
-    p.big = bf16 && k > 128 && n > 128 && n_groups * cdiv(n, 256) * cdiv(k, 256) >= 64;
-    p.bm = p.bn = p.big ? 256 : 128;
-    p.tiles = n_groups * cdiv(n, p.bm) * cdiv(k, p.bn);
-    const int64_t slots = p.big ? 256 : 512, step = bf16 ? 64 : 32;
+    const int64_t step = bf16 ? 64 : 32;
     const int64_t most = int64_t(GRAD_PART_BYTES / (size_t(n_groups) * size_t(n) * size_t(k) * 4 + 1));
-    p.splits = p.tiles >= slots ? 1
-               : int(std::max<int64_t>(1, std::min({cdiv(slots, p.tiles), n_entries / n_groups / (8 * step), most})));
-    return p;
+    auto plan = [&](int bm) {
+        const int64_t tiles = n_groups * cdiv(n, bm) * cdiv(k, bm), slots = bm == 256 ? 256 : 512;
+        const int64_t splits = tiles >= slots ? 1 : std::min({cdiv(slots, tiles), n_entries / n_groups / (8 * step), most});
+        return GradPlan{bm, int(std::max<int64_t>(1, splits)), tiles};
+    };
+    if (bf16 && k > 128 && n > 128 && k % 8 == 0 && n % 8 == 0 && plan(256).tiles >= 64) return plan(256);
+    const GradPlan p = plan(128);
+    const int64_t groups = p.tiles * p.splits, places = cdiv(groups, 512) * 512;
+    return groups < 1024 && 3 * groups < 2 * places ? plan(64) : p;
 }
 
 // A workgroup per tile and split.
@@ -95,6 +101,11 @@ __global__ __launch_bounds__(G::THREADS, 2) void grouped_grad_kernel(GroupedGrad
     auto acol = [&](int at) { return ((at * 64 + lane) % CPA ^ col_key<G::BF, G::BM>(row_of(at, CPA))) * G::EV; };
     auto bcol = [&](int at) { return ((at * 64 + lane) % CPB ^ col_key<G::BF, G::BN>(row_of(at, CPB))) * G::EV; };
     uint4 ra[DMA ? 1 : G::LA], rb[DMA ? 1 : G::LB];
+    [[maybe_unused]] uint64_t offs = 0;  // four bits a load: elements it was read early by
+    [[maybe_unused]] int off;
+    [[maybe_unused]] auto early = [&](int l, const uint4&, int by) {
+        offs = (l == 0 ? 0 : offs) | uint64_t(by) << (4 * l);
+    };
     // a step's rows, read from LDS ahead of its loads; the next chunk's rows: looked up at a chunk's second
     // step, stored at its fifth, used from the eighth on (a barrier between any two steps' loads)
     int32_t da[G::LA], xb[G::LB];
@@ -114,17 +125,23 @@ __global__ __launch_bounds__(G::THREADS, 2) void grouped_grad_kernel(GroupedGrad
             const int i = l, at = wave * G::LA + i, n = n0 + acol(at);
             const char* q = static_cast<const char*>(p.dy) + uint64_t(uint32_t(da[i])) * dypitch + n * G::ESZ;
             if constexpr (DMA) lds_dma16(da[i] < 0 || n >= p.n ? zero : q, st + at * 1024);
-            else ra[i] = load16<G::BF>(q, da[i] < 0 ? 0 : p.n - n);
+            else early(l, ra[i] = load16<G::BF>(q, da[i] < 0 ? 0 : p.n - n, p.n, off), off);
         } else {
             const int i = l - G::LA, at = wave * G::LB + i, k = k0 + bcol(at);
             const char* q = static_cast<const char*>(p.x) + uint64_t(uint32_t(xb[i])) * xpitch + k * G::ESZ;
             if constexpr (DMA) lds_dma16(xb[i] < 0 || k >= p.k ? zero : q, st + G::BM * G::ROWB + at * 1024);
-            else rb[i] = load16<G::BF>(q, xb[i] < 0 ? 0 : p.k - k);
+            else early(l, rb[i] = load16<G::BF>(q, xb[i] < 0 ? 0 : p.k - k, p.k, off), off);
         }
     };
     auto commit = [&](int stage) {
         if constexpr (!DMA) {
             unsigned char* st = glds + stage * G::STAGE;
+            if (offs) {
+#pragma unroll
+                for (int i = 0; i < G::LA; ++i) ra[i] = shift16<G::BF>(ra[i], int(offs >> (4 * i)) & 15);
+#pragma unroll
+                for (int i = 0; i < G::LB; ++i) rb[i] = shift16<G::BF>(rb[i], int(offs >> (4 * (G::LA + i))) & 15);
+            }
 #pragma unroll
             for (int i = 0; i < G::LA; ++i) *reinterpret_cast<uint4*>(st + (wave * G::LA + i) * 1024 + lane * 16) = ra[i];
 #pragma unroll
@@ -205,7 +222,8 @@ hipError_t launch_grad(const GroupedGradParams& p, const GradPlan& plan, hipStre
         hipLaunchKernelGGL(kernel, dim3(unsigned(plan.tiles * plan.splits)), dim3(G::THREADS), G::LDS, stream, p, tk,
                            int(plan.tiles), plan.splits);
     };
-    p.n % G::EV == 0 && p.k % G::EV == 0 ? launch(grouped_grad_kernel<G, true>) : launch(grouped_grad_kernel<G, false>);
+    if (p.n % G::EV == 0 && p.k % G::EV == 0) launch(grouped_grad_kernel<G, true>);
+    else if constexpr (G::BM < 256) launch(grouped_grad_kernel<G, false>);
     if (plan.splits > 1) {
         const int64_t all = int64_t(p.n_groups) * p.n * p.k;
         const unsigned blocks = unsigned(std::min<int64_t>((all + 1023) / 1024, 2048));
@@ -231,8 +249,9 @@ hipError_t run_grouped_weight_grad(const GroupedGradParams& p, const DeviceInfo&
     const GradPlan plan = grad_plan(p.n_entries, p.n_groups, p.k, p.n, p.bf16);
     *status = plan.tiles * plan.splits > INT32_MAX ? ST_UNSUPPORTED_ : ST_OK_;
     if (*status != ST_OK_) return hipSuccess;
-    if (!p.bf16) return launch_grad<GradF32>(p, plan, stream);
-    return plan.big ? launch_grad<GradBig>(p, plan, stream) : launch_grad<GradSmall>(p, plan, stream);
+    if (plan.bm == 256) return launch_grad<GradBig>(p, plan, stream);
+    if (plan.bm == 128) return p.bf16 ? launch_grad<GradSmall>(p, plan, stream) : launch_grad<GradSmallF32>(p, plan, stream);
+    return p.bf16 ? launch_grad<GradTiny>(p, plan, stream) : launch_grad<GradTinyF32>(p, plan, stream);
 }
 
 }  // namespace fff
