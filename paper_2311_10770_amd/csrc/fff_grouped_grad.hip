@@ -28,7 +28,7 @@ struct GradPlan {
 };
 
 // 256 x 256 tiles where rows are whole 16-byte vectors and there are 64 of them; else 128 x 128, unless
-// they and their splits leave the CUs' 512 places a third empty in their only or second round, where
+// they and their splits leave a fifth of the CUs' 512 places empty in their only or second round, where
 // 64 x 64 does better (us, 128 and 64: 5003 fp32 entries, 64 groups of 203 x 300: 39, 30; 8000 x 16 of
 // 768 x 768: 169, 140; where 128 fills them, 16384 x 8 of 1024 x 1024: 444, 511; bf16, 65536 x 1 of
 // 768 x 768: 172, 276).  Splits: up to two workgroups a CU, eight steps of the mean group each at least,
@@ -39,13 +39,13 @@ GradPlan grad_plan(int64_t n_entries, int32_t n_groups, int32_t k, int32_t n, bo
     const int64_t most = int64_t(GRAD_PART_BYTES / (size_t(n_groups) * size_t(n) * size_t(k) * 4 + 1));
     auto plan = [&](int bm) {
         const int64_t tiles = n_groups * cdiv(n, bm) * cdiv(k, bm), slots = bm == 256 ? 256 : 512;
-        const int64_t splits = tiles >= slots ? 1 : std::min({cdiv(slots, tiles), n_entries / n_groups / (8 * step), most});
+        const int64_t splits = tiles >= slots ? 1 : std::min({slots / tiles, n_entries / n_groups / (8 * step), most});
         return GradPlan{bm, int(std::max<int64_t>(1, splits)), tiles};
     };
     if (bf16 && k > 128 && n > 128 && k % 8 == 0 && n % 8 == 0 && plan(256).tiles >= 64) return plan(256);
     const GradPlan p = plan(128);
     const int64_t groups = p.tiles * p.splits, places = cdiv(groups, 512) * 512;
-    return groups < 1024 && 3 * groups < 2 * places ? plan(64) : p;
+    return groups < 1024 && 5 * groups < 4 * places ? plan(64) : p;
 }
 
 // A workgroup per tile and split.
