@@ -20,7 +20,7 @@ using GradTiny = GCfg<true, 1, 1, 2, 2, 3, 128>;   // 64 x 64, four waves
 using GradSmallF32 = GCfg<false, 2, 2, 2, 2, 2, 128>;
 using GradTinyF32 = GCfg<false, 1, 1, 2, 2, 3, 128>;
 
-constexpr size_t GRAD_PART_BYTES = size_t(64) << 20;  // partial sums, at most
+constexpr size_t GRAD_PART_BYTES = size_t(128) << 20;  // partial sums, at most
 
 struct GradPlan {
     int bm, splits;
@@ -48,14 +48,26 @@ GradPlan grad_plan(int64_t n_entries, int32_t n_groups, int32_t k, int32_t n, bo
     return groups < 1024 && 5 * groups < 4 * places ? plan(64) : p;
 }
 
+// Tiles that one XCD takes in a row (four at least: 32 groups of 16 tiles took 242 us two at a time, 230 four).
+__host__ __device__ __forceinline__ int64_t grad_run(int per, int splits) {
+    const int64_t run = int64_t(per) * splits / XCDS;
+    return run > 4 ? run : 4;
+}
+
 // A workgroup per tile and split.
 template <class G, bool DMA>
 __global__ __launch_bounds__(G::THREADS, 2) void grouped_grad_kernel(GroupedGradParams p, int tk, int tiles, int splits) {
     constexpr int CH = 8 * G::KS;  // entries whose rows are looked up together
     extern __shared__ __align__(16) unsigned char glds[];
     __shared__ int32_t s_row[2][2][CH];  // [buffer][dy, x]: source rows, -1 where there is none
-    const int64_t tile = xcd_tile(blockIdx.x, int64_t(tiles) * splits);
+    // Workgroup h runs on XCD h % 8.  Runs of an eighth of a group's tiles go round the XCDs: neighbours
+    // share rows in their L2, and every XCD has a part of every group, large or small (whole groups an
+    // XCD: 32 uneven groups of 65536 entries, 4096 x 1024: 750 us, 670 so).
     const int per = tiles / p.n_groups;  // tiles of a group
+    const int64_t run = grad_run(per, splits);
+    const int64_t at = blockIdx.x / XCDS;
+    const int64_t tile = (at / run * XCDS + blockIdx.x % XCDS) * run + at % run;
+    if (tile >= int64_t(tiles) * splits) return;
     const int g = int(tile / (int64_t(per) * splits)), in = int(tile - int64_t(g) * per * splits);
     const int sp = in / per, n0 = in % per / tk * G::BM, k0 = in % per % tk * G::BN;
     int64_t lo = 0, hi = 0;
@@ -218,9 +230,11 @@ __global__ __launch_bounds__(256) void grouped_grad_sum_kernel(GroupedGradParams
 template <class G>
 hipError_t launch_grad(const GroupedGradParams& p, const GradPlan& plan, hipStream_t stream) {
     const int tk = int((int64_t(p.k) + G::BN - 1) / G::BN);
+    const int64_t round = XCDS * grad_run(int(plan.tiles / p.n_groups), plan.splits);
+    const int64_t grid = (plan.tiles * plan.splits + round - 1) / round * round;
     auto launch = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, dim3(unsigned(plan.tiles * plan.splits)), dim3(G::THREADS), G::LDS, stream, p, tk,
-                           int(plan.tiles), plan.splits);
+        hipLaunchKernelGGL(kernel, dim3(unsigned(grid)), dim3(G::THREADS), G::LDS, stream, p, tk, int(plan.tiles),
+                           plan.splits);
     };
     if (p.n % G::EV == 0 && p.k % G::EV == 0) launch(grouped_grad_kernel<G, true>);
     else if constexpr (G::BM < 256) launch(grouped_grad_kernel<G, false>);
@@ -247,7 +261,7 @@ size_t grouped_grad_workspace_bytes(int64_t n_entries, int32_t n_groups, int32_t
 
 hipError_t run_grouped_weight_grad(const GroupedGradParams& p, const DeviceInfo&, hipStream_t stream, int* status) {
     const GradPlan plan = grad_plan(p.n_entries, p.n_groups, p.k, p.n, p.bf16);
-    *status = plan.tiles * plan.splits > INT32_MAX ? ST_UNSUPPORTED_ : ST_OK_;
+    *status = plan.tiles * plan.splits > INT32_MAX / 2 ? ST_UNSUPPORTED_ : ST_OK_;  // the grid rounds up
     if (*status != ST_OK_) return hipSuccess;
     if (plan.bm == 256) return launch_grad<GradBig>(p, plan, stream);
     if (plan.bm == 128) return p.bf16 ? launch_grad<GradSmall>(p, plan, stream) : launch_grad<GradSmallF32>(p, plan, stream);
