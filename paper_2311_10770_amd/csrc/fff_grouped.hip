@@ -26,8 +26,8 @@ __device__ __forceinline__ void put8(char* row, int bf, int col, int left, const
     if (bf) {
         if (FULL || left >= 8) {
             typedef uint32_t u4_a2 __attribute__((ext_vector_type(4), aligned(2)));
-            *reinterpret_cast<u4_a2*>(row + col * 2) = u4_a2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]),
-                                                             pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
+            *reinterpret_cast<u4_a2*>(row + col * 2) = u4_a2{pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]),
+                                                             pack2(v[6], v[7])};
             return;
         }
     } else if (FULL || left >= 8) {
@@ -112,7 +112,8 @@ __global__ __launch_bounds__(G::THREADS, 2) void grouped_kernel(GroupedParams p)
     __shared__ int32_t s_dst[2][G::BM];   // row of y, or -1
     __shared__ uint8_t s_src[2][G::BM];   // whether the entry has a row of x
     __shared__ Tile s_tile[2];
-    __shared__ int s_sum[G::WAVES], s_bad[2];
+    __shared__ int64_t s_sum[G::WAVES];
+    __shared__ int s_bad[2];
     TileMap<G::THREADS> map{p.offsets, p.n_entries, p.n_groups, G::BM, G::BN, (p.n + G::BN - 1) / G::BN};
     map.init(s_sum);
     int64_t h = blockIdx.x;
@@ -304,14 +305,15 @@ hipError_t launch_grouped(const GroupedParams& p, int cus, hipStream_t stream, i
 // from global memory in the operands' layout (lane l: row l % 16, the 16 bytes l / 16 of every 64); the
 // waves' sums meet in LDS.
 constexpr int FEW_WAVES = 8, FEW_U = 4;
+constexpr int64_t FEW_ENTRIES = int64_t(1) << 28;  // below: 64 groups' tiles are counted in 32 bits
 
 // Row tile mt (of sixteen entries) over all groups, found by every wave for itself, 64 groups at a time.
 __device__ __forceinline__ Tile few_tile(const GroupedParams& p, int mt) {
     const int lane = threadIdx.x & 63;
-    int at = 0;
-    for (int g0 = 0; g0 < p.n_groups; g0 += 64) {
+    int64_t at = 0;
+    for (int64_t g0 = 0; g0 < p.n_groups; g0 += 64) {
         int64_t lo = 0, hi = 0;
-        if (g0 + lane < p.n_groups) group_range(p.offsets, p.n_entries, g0 + lane, &lo, &hi);
+        if (g0 + lane < p.n_groups) group_range(p.offsets, p.n_entries, int(g0) + lane, &lo, &hi);
         const int mine = int((hi - lo + 15) / 16);
         int run = mine;
 #pragma unroll
@@ -322,9 +324,9 @@ __device__ __forceinline__ Tile few_tile(const GroupedParams& p, int mt) {
         const uint64_t has = __ballot(at + run > mt);
         if (has) {
             const int l = __builtin_ctzll(has);
-            const int before = at + __builtin_amdgcn_readlane(run - mine, l);
+            const int64_t before = at + __builtin_amdgcn_readlane(run - mine, l);
             const int first = __builtin_amdgcn_readlane(int(lo), l), end = __builtin_amdgcn_readlane(int(hi), l);
-            return Tile{g0 + l, 0, first + int64_t(mt - before) * 16, end};
+            return Tile{int(g0) + l, 0, first + (mt - before) * 16, end};
         }
         at += __builtin_amdgcn_readlane(run, 63);
     }
@@ -438,7 +440,7 @@ int grouped_variant(const GroupedParams& p, int cus) {
     auto row_tiles = [&](int bm) { return std::max(used, E / bm + 0.5 * used); };
     int best = 0;
     double least = 1e300;
-    if (!p.w_transposed) {
+    if (!p.w_transposed && p.n_entries < FEW_ENTRIES) {
         // 768 workgroups at once; rows off 16-byte addresses take 2.4 times as long
         const double rounds = row_tiles(16) * ((p.n + 15) / 16) / (3.0 * cus);
         const double kb = double(p.k) * esz / 64, slow = p.k % (16 / esz) ? 2.4 : 1.0;

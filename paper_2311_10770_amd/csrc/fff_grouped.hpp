@@ -47,54 +47,60 @@ struct TileMap {
     const int32_t* offsets;
     int64_t n_entries;
     int n_groups, bm, bn, tn;
-    int before, mine, total;  // row tiles before this thread's groups, in them, and of all groups
+    int64_t before, mine;  // row tiles before this thread's groups, and in them
+    int total;             // of all groups (offsets that name entries twice can make more than a launch holds: those
+                           // past 2^31 / tn are left out)
 
     // wave_sum: LDS of THREADS / 64 words.  Every thread of the workgroup calls this (a barrier).
-    __device__ __forceinline__ void init(int* wave_sum) {
+    __device__ __forceinline__ void init(int64_t* wave_sum) {
         const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
         int64_t lo, hi;
         mine = 0;
         for (int g = first(tid); g < first(tid + 1); ++g) {
             group_range(offsets, n_entries, g, &lo, &hi);
-            mine += int((hi - lo + bm - 1) / bm);
+            mine += (hi - lo + bm - 1) / bm;
         }
-        int run = mine;
+        int64_t run = mine;
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) {
-            const int v = __shfl_up(run, d);
+            const int64_t v = __shfl_up(run, d);
             if (lane >= d) run += v;
         }
         if (lane == 63) wave_sum[wave] = run;
         __syncthreads();
         before = run - mine;
-        total = 0;
+        int64_t all = 0;
         for (int w = 0; w < THREADS / 64; ++w) {
             if (w < wave) before += wave_sum[w];
-            total += wave_sum[w];
+            all += wave_sum[w];
         }
+        total = int(std::min<int64_t>(all, INT32_MAX / tn));
     }
     __device__ __forceinline__ int first(int tid) const {
-        const int per = (n_groups + THREADS - 1) / THREADS;
-        return std::min(n_groups, tid * per);
+        const int64_t per = (int64_t(n_groups) + THREADS - 1) / THREADS;
+        return int(std::min<int64_t>(n_groups, tid * per));
     }
     // Writes tile h to *out: the owner thread alone, or thread 0 where there is no such tile.
-    __device__ __forceinline__ void find(int64_t h, Tile* out) const {
-        const int64_t all = int64_t(total) * tn;
-        if (h >= all) {
+    __device__ __forceinline__ void find(int64_t number, Tile* out) const {
+        // 32-bit arithmetic: the host launches at most 2^31 - 1 tiles
+        const uint32_t all = uint32_t(total) * uint32_t(tn);
+        if (number >= int64_t(all)) {
             if (threadIdx.x == 0) out->g = -1;
             return;
         }
-        const int64_t t = xcd_tile(h, all);
-        const int block = int(t / (MB * tn)), in = int(t - int64_t(block) * (MB * tn));
+        const uint32_t h = uint32_t(number), x = h % XCDS, rem = all % XCDS;
+        const uint32_t t = x * (all / XCDS) + (x < rem ? x : rem) + h / XCDS;
+        const uint32_t wide = uint32_t(MB) * uint32_t(tn);
+        const int block = int(t / wide), in = int(t % wide);
         const int deep = std::min(MB, total - block * MB), mt = block * MB + in % deep;
-        int at = before;
+        int64_t at = before;
         if (mt < at || mt >= at + mine) return;
         for (int g = first(threadIdx.x);; ++g) {
             int64_t lo, hi;
             group_range(offsets, n_entries, g, &lo, &hi);
-            const int tiles = int((hi - lo + bm - 1) / bm);
+            const int64_t tiles = (hi - lo + bm - 1) / bm;
             if (mt < at + tiles) {
-                *out = Tile{g, in / deep * bn, lo + int64_t(mt - at) * bm, hi};
+                *out = Tile{g, in / deep * bn, lo + (mt - at) * bm, hi};
                 return;
             }
             at += tiles;

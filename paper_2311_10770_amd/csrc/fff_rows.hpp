@@ -10,6 +10,12 @@
 
 namespace fff {
 
+// Two values rounded to bf16 by one instruction (pack_bf16x2's separate roundings take four).
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+    typedef float f2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f2{lo, hi}, bf16x2_t));
+}
+
 __device__ __forceinline__ float load_elem(const void* p, bool bf, int64_t i) {
     return bf ? bf16_to_f32(static_cast<const uint16_t*>(p)[i]) : static_cast<const float*>(p)[i];
 }
@@ -62,7 +68,7 @@ __device__ __forceinline__ void store4(void* base, int bf, int64_t e, int left, 
     if (bf) {
         uint16_t* p = static_cast<uint16_t*>(base) + e;
         if (FULL || left >= 4) {
-            *reinterpret_cast<u32x2_a2*>(p) = u32x2_a2{pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3])};
+            *reinterpret_cast<u32x2_a2*>(p) = u32x2_a2{pack2(f[0], f[1]), pack2(f[2], f[3])};
         } else {
             if (left > 0) p[0] = f32_to_bf16(f[0]);
             if (left > 1) p[1] = f32_to_bf16(f[1]);

@@ -420,6 +420,21 @@ def test_grouped_weight_grad(fff_lib, E, G, K, N, t):
         ref.check(got, want + base.cpu().double(), err + ref.U * (want.abs() + base.cpu().double().abs()), "accumulated")
 
 
+def test_grouped_offsets_that_name_entries_again(fff_lib):
+    """Offsets that rise and fall over many groups: more tiles than the launch holds, every access in bounds."""
+    E, G, K, N = 300, 5000, 32, 40
+    x, w = torch.ones((E, K), device=DEV), torch.ones((G, N, K), device=DEV)
+    offsets = torch.tensor([0, E] * (G // 2) + [0], dtype=torch.int32, device=DEV)
+    flush_print("[gpu] grouped_matmul offsets that name entries again")
+    for t in (torch.float32, torch.bfloat16):
+        for transpose in (False, True):
+            wt = w.transpose(1, 2).contiguous() if transpose else w
+            y = fff_lib.grouped_matmul(x.to(t), wt.to(t), offsets, transpose_w=transpose)
+            assert (y == K).all()  # every group gives the same rows
+    dw = fff_lib.grouped_weight_grad(torch.ones((E, N), device=DEV), x, offsets)
+    assert (dw[0::2] == E).all() and (dw[1::2] == 0).all()
+
+
 def test_grouped_no_entries(fff_lib):
     w = torch.ones((3, 4, 8), device=DEV)
     e8, e4, off = torch.empty((0, 8), device=DEV), torch.empty((0, 4), device=DEV), torch.zeros(4, dtype=torch.int32, device=DEV)
