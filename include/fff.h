@@ -512,10 +512,10 @@ size_t fff_group_rows_workspace_bytes(int64_t n_entries, int32_t n_ids, int32_t 
  * back in entry order (its values must differ from each other).  z rows are in
  * grouped order.  Rows of y and z that no entry names are left as they were.
  * Bad device values stay in bounds: offsets are clamped to [0, n_entries] and
- * taken as empty where they fall, an x_index outside x reads a row of zeros,
- * and a y_index outside y stores nothing.  x and W are both bf16 (MFMA on
- * bf16, fp32 sums) or both fp32; anything else is FFF_ERR_UNSUPPORTED.  Any
- * k and n from 1 to 2^28 - 1.
+ * taken as empty where they fall, z is 0 where x_index is outside x (whatever
+ * W holds), and a y_index outside y stores nothing.  x and W are both bf16
+ * (MFMA on bf16, fp32 sums) or both fp32; anything else is
+ * FFF_ERR_UNSUPPORTED.  Any k and n from 1 to 2^28 - 1.
  */
 typedef struct {
     const void* x;          /* [x_rows, k] (x_dtype) */
@@ -542,9 +542,10 @@ int fff_grouped_matmul(const fff_grouped_matmul_args* a);
  *   dy_dst(i)^T x_src(i),   [n, k] per group, fp32,
  * the gradient of fff_grouped_matmul's W (with w_transposed: swap dy and x).
  * dst(i) = dy_index[i], or i; src(i) as above.  Groups
- * without entries get zeros (with accumulate: stay).  Offsets and indices out
- * of range as above.  dy and x are both bf16 or both fp32.  The sums run in a
- * fixed order: the same bits on every run.
+ * without entries get zeros (with accumulate: stay).  Offsets out of range as
+ * above; an entry with an index outside dy or x adds nothing.  dy and x are
+ * both bf16 or both fp32.  The sums run in a fixed order: the same bits on
+ * every run.
  */
 typedef struct {
     const void* dy;          /* [dy_rows, n] (dtype) */

@@ -394,6 +394,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void grouped_few_kernel(GroupedPara
     const int64_t i = t.m0 + tid / 16;
     const int c = n0 + tid % 16;
     if (i >= t.m1 || c >= p.n) return;
+    if (entry_row(p.x_index, p.x_div, p.x_rows, i) < 0) z = 0.0f;  // (zeros times infinite weights are NaN)
     if (p.z_in) {
         const float d = load_elem(p.z_in, p.z_bf16, i * p.n + c);
         z *= p.act == ACT_GELU_ERF ? act_slope<ACT_GELU_ERF>(d) : p.act == ACT_GELU_TANH ? act_slope<ACT_GELU_TANH>(d) : 1.0f;

@@ -93,8 +93,12 @@ __global__ __launch_bounds__(G::THREADS, 2) void grouped_grad_kernel(GroupedGrad
             const int64_t i = c * CH + e;
             row_dy[u] = row_x[u] = -1;
             if (e < CH && i < count) {
-                row_dy[u] = int32_t(entry_row(p.dy_index, 1, p.dy_rows, lo + i));
-                row_x[u] = int32_t(entry_row(p.x_index, p.x_div, p.x_rows, lo + i));
+                const int32_t dy = int32_t(entry_row(p.dy_index, 1, p.dy_rows, lo + i));
+                const int32_t x = int32_t(entry_row(p.x_index, p.x_div, p.x_rows, lo + i));
+                if (dy >= 0 && x >= 0) {  // else neither is read: the other's infinities times zero are NaN
+                    row_dy[u] = dy;
+                    row_x[u] = x;
+                }
             }
         }
     };

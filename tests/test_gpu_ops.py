@@ -420,6 +420,34 @@ def test_grouped_weight_grad(fff_lib, E, G, K, N, t):
         ref.check(got, want + base.cpu().double(), err + ref.U * (want.abs() + base.cpu().double().abs()), "accumulated")
 
 
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+@pytest.mark.parametrize("E,G,K,N", [(20, 4, 64, 40), (20, 4, 61, 33), (900, 3, 128, 256), (900, 3, 61, 33)])
+def test_grouped_entries_without_a_row_beside_infinities(fff_lib, E, G, K, N, t):
+    """Entries without a row give 0 and add nothing, whatever the operand beside them holds."""
+    gen = _gen(E + K)
+    flush_print(f"[gpu] grouped products, entries without a row {E} x {G}: {K} -> {N} {t}")
+    x, dy = _randn(gen, E, K, dtype=t).to(DEV), _randn(gen, E, N, dtype=t).to(DEV)
+    w = torch.full((G, N, K), math.inf, dtype=x.dtype, device=DEV)
+    cuts = torch.linspace(0, E, G + 1).to(torch.int32).to(DEV)
+    none = torch.arange(E, dtype=torch.int32) % 3 == 1
+    index = torch.where(none, -1, torch.arange(E, dtype=torch.int32)).to(DEV)
+    for transpose in (False, True):
+        y = fff_lib.grouped_matmul(x, w.transpose(1, 2).contiguous() if transpose else w, cuts, x_index=index,
+                                   transpose_w=transpose)
+        assert (y[none.to(DEV)] == 0).all() and not torch.isfinite(y[~none.to(DEV)]).any()
+    full = x.clone()
+    full[none.to(DEV)] = math.nan
+    zero_dy, zero_x = dy.clone(), x.clone()
+    zero_dy[none.to(DEV)] = 0
+    zero_x[none.to(DEV)] = 0
+    want = fff_lib.grouped_weight_grad(zero_dy, zero_x, cuts)
+    assert torch.isfinite(want).all()
+    assert torch.equal(fff_lib.grouped_weight_grad(dy, full, cuts, dy_index=index), want)
+    full = dy.clone()
+    full[none.to(DEV)] = math.inf
+    assert torch.equal(fff_lib.grouped_weight_grad(full, x, cuts, x_index=index), want)
+
+
 def test_grouped_offsets_that_name_entries_again(fff_lib):
     """Offsets that rise and fall over many groups: more tiles than the launch holds, every access in bounds."""
     E, G, K, N = 300, 5000, 32, 40
