@@ -586,15 +586,15 @@ bool matrix_bytes(int64_t a, int64_t rows, int64_t cols, int64_t elem, int64_t* 
     return mul_ok(a, rows, out) && mul_ok(*out, cols, out) && mul_ok(*out, elem, out);
 }
 
-// No output overlaps another output or an input, but that output 0 may be the very buffer
-// in_place (an input of its size and type).
-bool disjoint(const Span* outs, int n_outs, const Span* ins, int n_ins, const void* in_place, const void* in_place2) {
+// No output overlaps another output or an input, but that output 0 may be the very buffer of the
+// inputs in_place (a bit each; of its size and type).
+bool disjoint(const Span* outs, int n_outs, const Span* ins, int n_ins, unsigned in_place) {
     for (int i = 0; i < n_outs; ++i) {
         if (!outs[i].ptr) continue;
         for (int j = i + 1; j < n_outs; ++j)
             if (overlap(outs[i].ptr, outs[i].bytes, outs[j].ptr, outs[j].bytes)) return false;
         for (int j = 0; j < n_ins; ++j) {
-            const bool same = i == 0 && ins[j].ptr == outs[0].ptr && (ins[j].ptr == in_place || ins[j].ptr == in_place2);
+            const bool same = i == 0 && (in_place >> j & 1) && ins[j].ptr == outs[0].ptr;
             if (!same && overlap(outs[i].ptr, outs[i].bytes, ins[j].ptr, ins[j].bytes)) return false;
         }
     }
@@ -642,7 +642,7 @@ FFF_EXPORT int fff_layer_norm(const fff_layer_norm_args* a) {
         return FFF_ERR_INVALID_ARG;
     const Span outs[] = {{a->s, sb}, {a->y, yb}, {a->mean, 4 * B}, {a->rstd, 4 * B}};
     const Span ins[] = {{a->x, xb}, {a->residual, sb}, {a->gamma, 4 * H}, {a->beta, 4 * H}, {a->drop.rng_offset, 8}};
-    if (!disjoint(outs, 4, ins, 5, a->residual, nullptr)) return FFF_ERR_INVALID_ARG;
+    if (!disjoint(outs, 4, ins, 5, 1u << 1)) return FFF_ERR_INVALID_ARG;
     fff::DeviceInfo dev;
     const int rc = current_device_info(&dev);
     if (rc != FFF_OK) return rc;
@@ -699,7 +699,7 @@ FFF_EXPORT int fff_layer_norm_backward(const fff_layer_norm_backward_args* a) {
                          {need ? a->workspace : nullptr, need}};
     const Span ins[] = {{a->dy, yb},        {a->s, sb},     {a->mean, 4 * B}, {a->rstd, 4 * B},
                         {a->gamma, 4 * H}, {a->ds_in, sb}, {a->drop.rng_offset, 8}};
-    if (!disjoint(outs, 5, ins, 7, a->ds_in, nullptr)) return FFF_ERR_INVALID_ARG;
+    if (!disjoint(outs, 5, ins, 7, 1u << 5)) return FFF_ERR_INVALID_ARG;
     fff::DeviceInfo dev;
     const int rc = current_device_info(&dev);
     if (rc != FFF_OK) return rc;
@@ -741,8 +741,7 @@ FFF_EXPORT int fff_dropout(const fff_dropout_args* a) {
         return FFF_ERR_INVALID_ARG;
     const Span outs[] = {{a->y, yb}};
     const Span ins[] = {{a->x, xb}, {a->residual, rb}, {a->drop.rng_offset, 8}};
-    if (!disjoint(outs, 1, ins, 3, a->x_dtype == a->y_dtype ? a->x : nullptr,
-                  a->r_dtype == a->y_dtype ? a->residual : nullptr))
+    if (!disjoint(outs, 1, ins, 3, (a->x_dtype == a->y_dtype ? 1u : 0u) | (a->r_dtype == a->y_dtype ? 2u : 0u)))
         return FFF_ERR_INVALID_ARG;
     fff::DeviceInfo dev;
     const int rc = current_device_info(&dev);
@@ -790,7 +789,7 @@ FFF_EXPORT int fff_group_rows(const fff_group_rows_args* a) {
     }
     const Span outs[] = {{a->order, 4 * E}, {a->offsets, 4 * (G + 1)}, {a->bad_ids, 4}, {need ? a->workspace : nullptr, need}};
     const Span ins[] = {{a->ids, 4 * E}};
-    if (!disjoint(outs, 4, ins, 1, nullptr, nullptr)) return FFF_ERR_INVALID_ARG;
+    if (!disjoint(outs, 4, ins, 1, 0)) return FFF_ERR_INVALID_ARG;
     fff::DeviceInfo dev;
     rc = current_device_info(&dev);
     if (rc != FFF_OK) return rc;
@@ -846,7 +845,7 @@ FFF_EXPORT int fff_grouped_matmul(const fff_grouped_matmul_args* a) {
     const Span outs[] = {{a->y, yb}, {a->z_out, zb}};
     const Span ins[] = {{a->x, xb}, {a->w, wb}, {a->offsets, 4 * (int64_t(a->n_groups) + 1)},
                         {a->x_index, 4 * E}, {a->y_index, 4 * E}, {a->z_in, zb}};
-    if (!disjoint(outs, 2, ins, 6, nullptr, nullptr)) return FFF_ERR_INVALID_ARG;
+    if (!disjoint(outs, 2, ins, 6, 0)) return FFF_ERR_INVALID_ARG;
     if (a->x_dtype != a->w_dtype) return FFF_ERR_UNSUPPORTED;
     fff::DeviceInfo dev;
     const int rc = current_device_info(&dev);
@@ -914,7 +913,7 @@ FFF_EXPORT int fff_grouped_weight_grad(const fff_grouped_weight_grad_args* a) {
     const Span outs[] = {{a->dw, wb}, {need ? a->workspace : nullptr, need}};
     const Span ins[] = {{a->dy, yb}, {a->x, xb}, {a->offsets, 4 * (int64_t(a->n_groups) + 1)},
                         {a->dy_index, 4 * E}, {a->x_index, 4 * E}};
-    if (!disjoint(outs, 2, ins, 5, nullptr, nullptr)) return FFF_ERR_INVALID_ARG;
+    if (!disjoint(outs, 2, ins, 5, 0)) return FFF_ERR_INVALID_ARG;
     if (a->dy_dtype != a->x_dtype) return FFF_ERR_UNSUPPORTED;
     fff::DeviceInfo dev;
     const int rc = current_device_info(&dev);

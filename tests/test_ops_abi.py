@@ -115,6 +115,16 @@ def test_dropout_refusals(lib, over):
     _refused(lib, "fff_dropout", _fill(ops.FffDropoutArgs, DROP, over), INVALID)
 
 
+def test_in_place_is_for_one_input(lib):
+    """The buffer that may be written in place must not be another input too, whatever that one's type."""
+    for x_dtype in (0, 1):
+        _refused(lib, "fff_layer_norm", _fill(ops.FffLayerNormArgs, NORM, dict(x=2 * P, s=2 * P, x_dtype=x_dtype)), INVALID)
+        _refused(lib, "fff_layer_norm_backward",
+                 _fill(ops.FffLayerNormBackwardArgs, NORM_BWD, dict(dy=6 * P, ds=6 * P, y_dtype=x_dtype)), INVALID)
+    _refused(lib, "fff_dropout", _fill(ops.FffDropoutArgs, DROP, dict(residual=P, y=P, r_dtype=1)), INVALID)
+    _refused(lib, "fff_dropout", _fill(ops.FffDropoutArgs, DROP, dict(residual=P, y=P, x_dtype=1)), INVALID)
+
+
 GROUP = dict(ids=P, order=2 * P, offsets=3 * P, bad_ids=4 * P, n_entries=100000, n_ids=16, n_trees=2, first=15,
              workspace=5 * P, workspace_bytes=1 << 24)
 
