@@ -544,7 +544,8 @@ int fff_grouped_matmul(const fff_grouped_matmul_args* a);
  * dst(i) = dy_index[i], or i; src(i) as above.  Groups
  * without entries get zeros (with accumulate: stay).  Offsets out of range as
  * above; an entry with an index outside dy or x adds nothing.  dy and x are
- * both bf16 or both fp32.  The sums run in a fixed order: the same bits on
+ * both bf16 or both fp32.  More 128 x 128 tiles of dW than a launch holds (2^24)
+ * are FFF_ERR_UNSUPPORTED.  The sums run in a fixed order: the same bits on
  * every run.
  */
 typedef struct {

@@ -408,7 +408,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void grouped_few_kernel(GroupedPara
 
 hipError_t launch_few(const GroupedParams& p, hipStream_t stream, int* status) {
     const int64_t tiles = most_tiles(p.n_entries, p.n_groups, 16) * ((int64_t(p.n) + 15) / 16);
-    *status = tiles > INT32_MAX ? ST_UNSUPPORTED_ : ST_OK_;
+    *status = tiles > UINT32_MAX / (64 * FEW_WAVES) ? ST_UNSUPPORTED_ : ST_OK_;  // a launch's threads
     if (*status != ST_OK_) return hipSuccess;
     auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(unsigned(tiles)), dim3(64 * FEW_WAVES), 0, stream, p); };
     if (p.bf16) p.k % 8 == 0 ? launch(grouped_few_kernel<true, true>) : launch(grouped_few_kernel<true, false>);

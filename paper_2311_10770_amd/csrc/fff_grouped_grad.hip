@@ -231,11 +231,14 @@ __global__ __launch_bounds__(256) void grouped_grad_sum_kernel(GroupedGradParams
     }
 }
 
+// A launch holds less than 2^32 threads.
 template <class G>
-hipError_t launch_grad(const GroupedGradParams& p, const GradPlan& plan, hipStream_t stream) {
+hipError_t launch_grad(const GroupedGradParams& p, const GradPlan& plan, hipStream_t stream, int* status) {
     const int tk = int((int64_t(p.k) + G::BN - 1) / G::BN);
     const int64_t round = XCDS * grad_run(int(plan.tiles / p.n_groups), plan.splits);
     const int64_t grid = (plan.tiles * plan.splits + round - 1) / round * round;
+    *status = grid > UINT32_MAX / G::THREADS ? ST_UNSUPPORTED_ : ST_OK_;
+    if (*status != ST_OK_) return hipSuccess;
     auto launch = [&](auto kernel) {
         hipLaunchKernelGGL(kernel, dim3(unsigned(grid)), dim3(G::THREADS), G::LDS, stream, p, tk, int(plan.tiles),
                            plan.splits);
@@ -265,11 +268,10 @@ size_t grouped_grad_workspace_bytes(int64_t n_entries, int32_t n_groups, int32_t
 
 hipError_t run_grouped_weight_grad(const GroupedGradParams& p, const DeviceInfo&, hipStream_t stream, int* status) {
     const GradPlan plan = grad_plan(p.n_entries, p.n_groups, p.k, p.n, p.bf16);
-    *status = plan.tiles * plan.splits > INT32_MAX / 2 ? ST_UNSUPPORTED_ : ST_OK_;  // the grid rounds up
-    if (*status != ST_OK_) return hipSuccess;
-    if (plan.bm == 256) return launch_grad<GradBig>(p, plan, stream);
-    if (plan.bm == 128) return p.bf16 ? launch_grad<GradSmall>(p, plan, stream) : launch_grad<GradSmallF32>(p, plan, stream);
-    return p.bf16 ? launch_grad<GradTiny>(p, plan, stream) : launch_grad<GradTinyF32>(p, plan, stream);
+    if (plan.bm == 256) return launch_grad<GradBig>(p, plan, stream, status);
+    if (plan.bm == 128)
+        return p.bf16 ? launch_grad<GradSmall>(p, plan, stream, status) : launch_grad<GradSmallF32>(p, plan, stream, status);
+    return p.bf16 ? launch_grad<GradTiny>(p, plan, stream, status) : launch_grad<GradTinyF32>(p, plan, stream, status);
 }
 
 }  // namespace fff

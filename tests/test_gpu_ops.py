@@ -463,6 +463,19 @@ def test_grouped_offsets_that_name_entries_again(fff_lib):
     assert (dw[0::2] == E).all() and (dw[1::2] == 0).all()
 
 
+def test_grouped_weight_grad_of_more_groups_than_a_launch_holds(fff_lib):
+    flush_print("[gpu] grouped_weight_grad of 2^24 groups")
+    x = torch.ones((3, 1), device=DEV)
+    dw = torch.full((1 << 24, 1, 1), 7.0, device=DEV)
+    with pytest.raises(fff_lib.FffError):
+        fff_lib.grouped_weight_grad(x, x, torch.zeros((1 << 24) + 1, dtype=torch.int32, device=DEV), dw=dw)
+    assert (dw == 7).all()
+    offsets = torch.full(((1 << 23) + 1,), 3, dtype=torch.int32, device=DEV)
+    offsets[0] = 0
+    dw = fff_lib.grouped_weight_grad(x, x, offsets)
+    assert dw[0, 0, 0] == 3 and (dw[1:] == 0).all()
+
+
 def test_grouped_no_entries(fff_lib):
     w = torch.ones((3, 4, 8), device=DEV)
     e8, e4, off = torch.empty((0, 8), device=DEV), torch.empty((0, 4), device=DEV), torch.zeros(4, dtype=torch.int32, device=DEV)
