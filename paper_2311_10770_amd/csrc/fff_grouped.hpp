@@ -40,10 +40,12 @@ struct Tile {
 // times tn column tiles of bn.  Every thread keeps the sum over a few consecutive groups and all
 // before them; the thread whose groups hold a tile finds it (find) for the workgroup.  Number h runs
 // on XCD h % 8: each XCD takes a contiguous range of the tiles, MB row tiles deep before the next
-// column tile, so that neighbours share rows and columns in their L2.
+// column tile, so that neighbours share rows and columns in their L2: about a square of its 32 CUs'
+// tiles (65536 entries, 1024 -> 4096, 4, 6, 8 and 16 deep: 648, 647, 651, 668 us; 16384 x 1, 4096 -> 4096: 500, 485,
+// 490, 496; 16384 x 8, 1024 -> 4096 -> 1024: 6 deep 349, 8 deep 375).
 template <int THREADS>
 struct TileMap {
-    static constexpr int MB = 8;
+    static constexpr int MB = 6;
     const int32_t* offsets;
     int64_t n_entries;
     int n_groups, bm, bn, tn;
