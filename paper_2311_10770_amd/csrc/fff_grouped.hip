@@ -228,7 +228,7 @@ __global__ __launch_bounds__(G::THREADS, 2) void grouped_kernel(GroupedParams p)
     // code stands once, in a rolled loop: unrolled over the blocks it was 45000 instructions, which
     // every workgroup fetched anew (65536 entries, 1024 -> 4096, then a workgroup per tile: 888 against 762 us).
     constexpr int COLS = 32 * G::TN, PITCH = COLS + 8;
-    static_assert(G::STAGE + size_t(G::WAVES) * 16 * PITCH * 4 <= G::LDS, "half rows of blocks fit behind the first stage");
+    static_assert(size_t(G::WAVES) * 16 * PITCH * 4 <= G::STAGE, "half rows of blocks fit behind the first stage");
     float* blk = reinterpret_cast<float*>(glds + G::STAGE) + wave * 16 * PITCH;
     const int wm = wave / G::WGN, wn = wave % G::WGN;
     const int kind = p.act == ACT_IDENTITY ? EPI_STORE : (p.z_in ? EPI_GELU_GRAD : EPI_GELU) + (p.act == ACT_GELU_TANH);
@@ -289,10 +289,12 @@ hipError_t launch_grouped(const GroupedParams& p, int cus, hipStream_t stream, i
     const int64_t tiles = most_tiles(p.n_entries, p.n_groups, G::BM) * ((int64_t(p.n) + G::BN - 1) / G::BN);
     *status = tiles > INT32_MAX ? ST_UNSUPPORTED_ : ST_OK_;
     if (*status != ST_OK_) return hipSuccess;
-    const int grid = int(std::min<int64_t>(tiles, int64_t(cus) * G::PER_CU));
-    auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(unsigned(grid)), dim3(G::THREADS), G::LDS, stream, p); };
-    // rows of whole 16-byte vectors go straight to LDS
+    // rows of whole 16-byte vectors go straight to LDS; two stages of those loaded through registers
     const bool dma = whole_vectors(p);
+    const int grid = int(std::min<int64_t>(tiles, int64_t(cus) * (dma ? G::PER_CU : 8 / G::WAVES)));
+    auto launch = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, dim3(unsigned(grid)), dim3(G::THREADS), dma ? G::LDS : 2 * G::STAGE, stream, p);
+    };
     if (dma) p.w_transposed ? launch(grouped_kernel<G, true, true>) : launch(grouped_kernel<G, true, false>);
     else if constexpr (G::BM < 256) p.w_transposed ? launch(grouped_kernel<G, false, true>) : launch(grouped_kernel<G, false, false>);
     return hipGetLastError();

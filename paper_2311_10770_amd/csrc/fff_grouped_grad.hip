@@ -239,12 +239,11 @@ hipError_t launch_grad(const GroupedGradParams& p, const GradPlan& plan, hipStre
     const int64_t grid = (plan.tiles * plan.splits + round - 1) / round * round;
     *status = grid > UINT32_MAX / G::THREADS ? ST_UNSUPPORTED_ : ST_OK_;
     if (*status != ST_OK_) return hipSuccess;
-    auto launch = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, dim3(unsigned(grid)), dim3(G::THREADS), G::LDS, stream, p, tk, int(plan.tiles),
-                           plan.splits);
+    auto launch = [&](auto kernel, size_t lds) {
+        hipLaunchKernelGGL(kernel, dim3(unsigned(grid)), dim3(G::THREADS), lds, stream, p, tk, int(plan.tiles), plan.splits);
     };
-    if (p.n % G::EV == 0 && p.k % G::EV == 0) launch(grouped_grad_kernel<G, true>);
-    else if constexpr (G::BM < 256) launch(grouped_grad_kernel<G, false>);
+    if (p.n % G::EV == 0 && p.k % G::EV == 0) launch(grouped_grad_kernel<G, true>, G::LDS);
+    else if constexpr (G::BM < 256) launch(grouped_grad_kernel<G, false>, 2 * G::STAGE);  // two stages of registers' loads
     if (plan.splits > 1) {
         const int64_t all = int64_t(p.n_groups) * p.n * p.k;
         const unsigned blocks = unsigned(std::min<int64_t>((all + 1023) / 1024, 2048));
