@@ -450,7 +450,8 @@ int grouped_variant(const GroupedParams& p, int cus) {
         least = rounds < 1 ? 2.5 + 0.115 * kb * std::max(rounds, 0.35) * slow : rounds * (2.5 + 0.115 * kb) * slow;
     }
     const TileCost* cost = p.bf16 ? COST_BF16 : COST_F32;
-    // (256 x 256 tiles through registers spill: 65536 entries, 1023 -> 4095: 1042 us)
+    // (256 x 256 tiles are not built through registers: they spill, and took as long as 128 x 128: 65536
+    // entries, 1023 -> 4095, 1042 and 1046 us)
     for (int v = 0; v < (p.bf16 && whole_vectors(p) ? 4 : 3); ++v) {
         // (the half tile a group is an estimate: a tenth of a round does not make one)
         const double per_cu =

@@ -306,8 +306,9 @@ struct GCfg {
 // step's first reads, and the loads into the stage just read, run under those MFMAs (with the
 // barrier between the steps the matrix cores waited for a whole LDS read each step).  Those loads start at
 // once behind the barrier, which is soonest, or (SPREAD: two column tiles, whose reads take twice the
-// instructions) between the MFMAs: 65536 entries, 1024 -> 4096, weight gradients 762 us spread, 812 at
-// once; forward 835 and 822.
+// instructions) between the MFMAs.  At once and spread, us, 65536 entries in 32 groups: weight gradients
+// 4096 x 1024: 705, 670; 1024 -> 4096 with GELU 828, 825; its data gradient 695, 713; fp32, 16384 entries
+// x 8, 1024 -> 1024: 334, 345.
 template <class G, bool DMA, bool ACOL, bool BCOL, class Prepare, class Issue, class Commit>
 __device__ __forceinline__ void grouped_loop(unsigned char* lds, int64_t steps, tile_v16f (&acc)[G::TM][G::TN],
                                              Prepare prepare, Issue issue, Commit commit) {
