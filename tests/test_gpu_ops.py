@@ -670,6 +670,90 @@ def test_two_graphs_share_no_scratch(fff_lib):
             assert all(torch.equal(a, b) for a, b in zip(outs[i], want[i]))
 
 
+def test_captured_long_forms_and_sums(fff_lib):
+    """The forms of several launches in a graph, adding to gradients, against eager calls between the replays."""
+    gen = _gen(31)
+    E, G = 50000, 300
+    ids = torch.randint(-1, G, (E,), generator=gen, device=DEV).to(torch.int32)
+    x, dy = _randn(gen, 3000, 256, dtype="bf16"), _randn(gen, 3000, 136, dtype="bf16")
+    offsets = torch.tensor([0, 2900, 2950], dtype=torch.int32, device=DEV)
+    long = [_randn(gen, 3, 20000) for _ in range(3)]
+    gamma, stats = _randn(gen, 20000), (torch.zeros(3, device=DEV), torch.ones(3, device=DEV))
+    assert fff_lib.grouped_weight_grad_workspace_bytes(3000, 2, 256, 136) > 0
+
+    def sums():
+        return {"bad": torch.zeros(1, dtype=torch.int32, device=DEV), "dw": torch.ones((2, 136, 256), device=DEV),
+                "dgamma": torch.ones(20000, device=DEV), "dbeta": torch.ones(20000, device=DEV)}
+
+    def work(t):
+        out = [*fff_lib.group_rows(ids, G, bad_ids=t["bad"])]
+        out[0] = out[0][:E - int((ids < 0).sum())] if not torch.cuda.is_current_stream_capturing() else out[0]
+        fff_lib.grouped_weight_grad(dy, x, offsets, dw=t["dw"], accumulate=True)
+        out += fff_lib.layer_norm_backward(long[0], long[1], *stats, gamma, ds_in=long[2], dgamma=t["dgamma"],
+                                           dbeta=t["dbeta"], accumulate=True, p=0.5, seed=3)[:2]
+        return out
+
+    flush_print("[gpu] long forms and sums in a graph")
+    mine, eager = sums(), sums()
+    work(sums())
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        inside = work(mine)
+    for _ in range(3):
+        graph.replay()
+        torch.cuda.synchronize()
+        want = work(eager)
+        torch.cuda.synchronize()
+        assert torch.equal(inside[0][:want[0].numel()], want[0])
+        assert all(torch.equal(a, b) for a, b in zip(inside[1:], want[1:]))
+        assert all(torch.equal(mine[k], eager[k]) for k in mine)
+    assert int(mine["bad"]) == 3 * int((ids < 0).sum())
+
+
+@pytest.mark.parametrize("H", [768, 20000])
+def test_in_place_equals_out_of_place(fff_lib, H):
+    """The stream and its gradient written over their inputs, rows in registers and long ones, with dropout."""
+    gen = _gen(H)
+    x, r, dy, up = (_randn(gen, 5, H) for _ in range(4))
+    drop = {"p": 0.3, "seed": 11, "offset": 4}
+    flush_print(f"[gpu] layer_norm in place, {H}")
+    want = fff_lib.layer_norm(x, residual=r, **drop)
+    got = fff_lib.layer_norm(x, residual=r, s=r, **drop)
+    assert got[1] is r and all(torch.equal(a, b) for a, b in zip(got, want))
+    want = fff_lib.layer_norm_backward(dy, *want[1:], ds_in=up, **drop)
+    got = fff_lib.layer_norm_backward(dy, *got[1:], ds_in=up, ds=up, **drop)
+    assert got[0] is up and all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("E,G,K,N,t", [(9, 4, 72, 40, "bf16"), (700, 5, 61, 47, "f32"), (700, 5, 64, 128, "bf16"),
+                                       (6000, 6, 256, 512, "bf16"), (6000, 6, 72, 264, "f32")])
+def test_grouped_entries_and_groups_apart(fff_lib, E, G, K, N, t):
+    """NaN in one entry's row or one group's matrix stays with that entry and that group."""
+    gen = _gen(E + N)
+    flush_print(f"[gpu] grouped products with NaN, {E} x {G}: {K} -> {N} {t}")
+    offsets = torch.linspace(0, E, G + 1).to(torch.int32).to(DEV)
+    x, dy, w = _randn(gen, E, K, dtype=t), _randn(gen, E, N, dtype=t), _randn(gen, G, N, K, dtype=t)
+    for transpose in (False, True):
+        wt = w.transpose(1, 2).contiguous() if transpose else w.clone()
+        clean = fff_lib.grouped_matmul(x, wt, offsets, act="gelu", transpose_w=transpose)
+        wt[1] = math.nan
+        xn = x.clone()
+        xn[0], xn[E - 1] = math.nan, math.inf
+        got = fff_lib.grouped_matmul(xn, wt, offsets, act="gelu", transpose_w=transpose)
+        hit = torch.zeros(E, dtype=torch.bool, device=DEV)
+        hit[0] = hit[E - 1] = True
+        hit[int(offsets[1]):int(offsets[2])] = True
+        assert torch.equal(got[~hit], clean[~hit]) and not torch.isfinite(got[0]).any()
+        assert torch.isnan(got[int(offsets[1]):int(offsets[2])]).all()
+    clean = fff_lib.grouped_weight_grad(dy, x, offsets)
+    xn = x.clone()
+    xn[int(offsets[1])] = math.nan
+    got = fff_lib.grouped_weight_grad(dy, xn, offsets)
+    rest = [g for g in range(G) if g != 1]
+    assert torch.equal(got[rest], clean[rest]) and torch.isnan(got[1]).all()
+
+
 def test_training_step_of_the_tree_block(fff_lib):
     """x + drop(FFF(LN(x))) and its gradients: the layer's own forward and backward between the new operators."""
     B, H, depth = 64, 64, 3
