@@ -476,6 +476,35 @@ def test_grouped_weight_grad_of_more_groups_than_a_launch_holds(fff_lib):
     assert dw[0, 0, 0] == 3 and (dw[1:] == 0).all()
 
 
+@pytest.mark.parametrize("K,N", [(4096, 4104), (4100, 4099)])
+@pytest.mark.parametrize("E", [40, 700])
+def test_grouped_past_four_billion_elements(fff_lib, E, K, N):
+    """The last of 300 groups, rows behind 2^20 of x, y and dy: every matrix holds more than 2^32 elements."""
+    G, B, gen, bf = 300, (1 << 20) + E, _gen(E + K), torch.bfloat16
+    offsets = torch.zeros(G + 1, dtype=torch.int32, device=DEV)
+    offsets[G] = E
+    index = (B - 1 - torch.randperm(E, generator=gen, device=DEV)).to(torch.int32)
+    x, dy = torch.empty((B, K), dtype=bf, device=DEV), torch.empty((B, N), dtype=bf, device=DEV)
+    near_x, near_w = _randn(gen, E, K, dtype="bf16"), _randn(gen, 1, N, K, dtype="bf16") * K ** -0.5
+    near_dy = _randn(gen, E, N, dtype="bf16")
+    x[B - E:], dy[B - E:] = near_x, near_dy
+    ends, at = torch.tensor([0, E], dtype=torch.int32, device=DEV), (index - (B - E)).to(torch.int32)
+    (want, _), (err, _) = ref.grouped(near_x, near_w, ends, at)
+    for transpose in (False, True):
+        w = torch.empty((G, K, N) if transpose else (G, N, K), dtype=bf, device=DEV)
+        w[G - 1] = near_w[0].T if transpose else near_w[0]
+        y = torch.empty((B, N), dtype=bf, device=DEV)
+        flush_print(f"[gpu] grouped_matmul past 2^32 elements, {E} entries {K} -> {N}, transposed {transpose}")
+        fff_lib.grouped_matmul(x, w, offsets, x_index=index, y=y, y_index=index, transpose_w=transpose)
+        ref.check(y[index.long()], want, err, "y")
+        del w, y
+    flush_print(f"[gpu] grouped_weight_grad past 2^32 elements, {E} entries {K} -> {N}")
+    dw = fff_lib.grouped_weight_grad(dy, x, offsets, dy_index=index, x_index=index)
+    want, err = ref.weight_grad(near_dy, near_x, ends, at, at)
+    ref.check(dw[G - 1:], want, err, "dw")
+    assert (dw[0] == 0).all() and (dw[G - 2] == 0).all()
+
+
 def test_grouped_no_entries(fff_lib):
     w = torch.ones((3, 4, 8), device=DEV)
     e8, e4, off = torch.empty((0, 8), device=DEV), torch.empty((0, 4), device=DEV), torch.zeros(4, dtype=torch.int32, device=DEV)
