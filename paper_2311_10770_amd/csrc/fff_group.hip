@@ -10,9 +10,9 @@
 // Up to GROUP_ONE entries take one workgroup and one launch; more take three
 // (count, scan, place), every workgroup with a chunk of its own.  The work is a
 // few bytes per entry: launches and the latency of dependent steps are the time.
-// 16384 entries of 64 groups: 15.1 us in one launch, called or in a graph (a
-// single entry a lane: 8.9), 11.4 in three launches in a graph, but 19.1 called.
-// 524288 entries of 4096 groups: 24.5 us.
+// 16384 entries of 64 groups: 12.3 us in one launch, called or in a graph (15.0 with the entries read again
+// for placing; three launches took 11.4 in a graph, but 19.1 called).  524288 entries of 4096 groups: 23.4
+// us; 100000 of 32768: 52.6, a row of counters there being all that LDS holds, one wave places.
 #include "fff_internal.hpp"
 
 #include <hip/hip_runtime.h>
@@ -54,69 +54,77 @@ __device__ __forceinline__ int group_of(const GroupParams& p, uint32_t e) {
     return id >= 0 && id < p.n_ids ? tree * p.n_ids + int(id) : -1;
 }
 
-// One wave's entries [e0, e1) counted into its row of counters, RB rounds loaded at a time.
+// Groups of RB rounds of 64 entries from b + lane on: -1 for an entry without one, -2 behind e1.
 template <int RB>
-__device__ __forceinline__ void count_run(const GroupParams& p, int64_t e0, int64_t e1, int32_t* row, bool tell) {
-    const int lane = threadIdx.x & 63;
-    int lost = 0;
-    for (int64_t b = e0 + lane; b < e1; b += 64 * RB) {
-        int g[RB];
+__device__ __forceinline__ void load_groups(const GroupParams& p, int64_t b, int64_t e1, int* g) {
 #pragma unroll
-        for (int r = 0; r < RB; ++r) g[r] = b + 64 * r < e1 ? group_of(p, uint32_t(b + 64 * r)) : -2;
-#pragma unroll
-        for (int r = 0; r < RB; ++r) {
-            if (g[r] >= 0) atomicAdd(&row[g[r]], 1);
-            lost += g[r] == -1;
-        }
+    for (int r = 0; r < RB; ++r) {
+        const int64_t e = b + 64 * r + (threadIdx.x & 63);
+        g[r] = e < e1 ? group_of(p, uint32_t(e)) : -2;
     }
-    if (tell && p.bad && lost) atomicAdd(p.bad, lost);
 }
 
-// One wave's entries [e0, e1) placed in order, RB rounds loaded at a time; row[g]: the wave's next
-// place in group g.  Entries go to order, or (STAGE) as 16 bits to `staged` in LDS.
+// RB rounds counted into the wave's row of counters; returns how many have no group.
+template <int RB>
+__device__ __forceinline__ int count_groups(const int* g, int32_t* row) {
+    int lost = 0;
+#pragma unroll
+    for (int r = 0; r < RB; ++r) {
+        if (g[r] >= 0) atomicAdd(&row[g[r]], 1);
+        lost += g[r] == -1;
+    }
+    return lost;
+}
+
+// RB rounds from entry b on placed in order; row[g]: the wave's next place in group g.  Entries go to
+// order, or (STAGE) as 16 bits to `staged` in LDS.
 template <int RB, bool STAGE>
-__device__ __forceinline__ void place_run(const GroupParams& p, int64_t e0, int64_t e1, int32_t* row, uint16_t* staged,
-                                          int bits) {
+__device__ __forceinline__ void place_groups(const int* g, int64_t b, int32_t* row, int32_t* order, uint16_t* staged,
+                                             int bits) {
     const int lane = threadIdx.x & 63;
-    for (int64_t b = e0; b < e1; b += 64 * RB) {
-        int g[RB];
+    // the lanes of each round with this lane's group; the rounds' chains of ballots run side by side
+    uint32_t lo[RB], hi[RB];
+#pragma unroll
+    for (int r = 0; r < RB; ++r) {
+        const uint64_t any = __ballot(g[r] >= 0);
+        lo[r] = uint32_t(any);
+        hi[r] = uint32_t(any >> 32);
+    }
+    for (int k = 0; k < bits; ++k) {
 #pragma unroll
         for (int r = 0; r < RB; ++r) {
-            const int64_t e = b + 64 * r + lane;
-            g[r] = e < e1 ? group_of(p, uint32_t(e)) : -1;
-        }
-        // the lanes of each round with this lane's group; the rounds' chains of ballots run side by side
-        uint32_t lo[RB], hi[RB];
-#pragma unroll
-        for (int r = 0; r < RB; ++r) {
-            const uint64_t any = __ballot(g[r] >= 0);
-            lo[r] = uint32_t(any);
-            hi[r] = uint32_t(any >> 32);
-        }
-        for (int k = 0; k < bits; ++k) {
-#pragma unroll
-            for (int r = 0; r < RB; ++r) {
-                const int32_t one = int32_t(uint32_t(g[r]) << (31 - k)) >> 31;  // bit k in every bit
-                const uint64_t set = __ballot(one != 0);
-                lo[r] &= ~(uint32_t(set) ^ uint32_t(one));
-                hi[r] &= ~(uint32_t(set >> 32) ^ uint32_t(one));
-            }
-        }
-#pragma unroll
-        for (int r = 0; r < RB; ++r) {
-            if (g[r] >= 0) {
-                const uint64_t same = uint64_t(hi[r]) << 32 | lo[r];
-                const int before = __popcll(same & ((uint64_t(1) << lane) - 1));
-                const int32_t at = row[g[r]];
-                // every lane has read its group's counter before the group's first lane moves it on
-                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-                if (before == 0) row[g[r]] = at + __popcll(same);
-                if constexpr (STAGE) staged[at + before] = uint16_t(b + 64 * r + lane);
-                else p.order[at + before] = int32_t(b + 64 * r + lane);
-            }
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            const int32_t one = __builtin_amdgcn_sbfe(g[r], k, 1);  // bit k in every bit
+            const uint64_t set = __ballot(one != 0);
+            lo[r] &= ~(uint32_t(set) ^ uint32_t(one));
+            hi[r] &= ~(uint32_t(set >> 32) ^ uint32_t(one));
         }
     }
+#pragma unroll
+    for (int r = 0; r < RB; ++r) {
+        if (g[r] >= 0) {
+            const uint64_t same = uint64_t(hi[r]) << 32 | lo[r];
+            const int before = __popcll(same & ((uint64_t(1) << lane) - 1));
+            const int32_t at = row[g[r]];
+            // every lane has read its group's counter before the group's first lane moves it on
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            if (before == 0) row[g[r]] = at + __popcll(same);
+            if constexpr (STAGE) staged[at + before] = uint16_t(b + 64 * r + lane);
+            else order[at + before] = int32_t(b + 64 * r + lane);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
+}
+
+// One wave's entries [e0, e1) counted, RB rounds loaded at a time.
+template <int RB>
+__device__ __forceinline__ void count_run(const GroupParams& p, int64_t e0, int64_t e1, int32_t* row, bool tell) {
+    int lost = 0;
+    for (int64_t b = e0; b < e1; b += 64 * RB) {
+        int g[RB];
+        load_groups<RB>(p, b, e1, g);
+        lost += count_groups<RB>(g, row);
+    }
+    if (tell && p.bad && lost) atomicAdd(p.bad, lost);
 }
 
 // Counters of group g in W rows of n_groups: exclusive sums from `at` on; returns their end.
@@ -162,11 +170,15 @@ __global__ __launch_bounds__(1024) void group_one_kernel(GroupParams p, int bits
     __shared__ int32_t sums[16], listed;
     const int G = p.n_groups, tid = threadIdx.x, wave = tid >> 6;
     uint16_t* staged = reinterpret_cast<uint16_t*>(g_cnt + 16 * G);
+    constexpr int ROUNDS = GROUP_ONE / 1024;
+    const int64_t run = (p.n_entries + 1023) / 1024 * 64;  // at most ROUNDS rounds: a wave's groups stay in registers
+    const int64_t e0 = std::min<int64_t>(p.n_entries, wave * run), e1 = std::min<int64_t>(p.n_entries, e0 + run);
+    int mine_of[ROUNDS];
+    load_groups<ROUNDS>(p, e0, e1, mine_of);
     for (int i = tid; i < 16 * G; i += 1024) g_cnt[i] = 0;
     __syncthreads();
-    const int64_t run = (p.n_entries + 1023) / 1024 * 64;
-    const int64_t e0 = std::min<int64_t>(p.n_entries, wave * run), e1 = std::min<int64_t>(p.n_entries, e0 + run);
-    count_run<16>(p, e0, e1, g_cnt + wave * G, true);
+    const int lost = count_groups<ROUNDS>(mine_of, g_cnt + wave * G);
+    if (p.bad && lost) atomicAdd(p.bad, lost);
     __syncthreads();
     // a thread takes a few consecutive groups: their totals, then every wave's first place in them
     const int per = (G + 1023) / 1024, g0 = std::min(G, tid * per), g1 = std::min(G, g0 + per);
@@ -182,7 +194,7 @@ __global__ __launch_bounds__(1024) void group_one_kernel(GroupParams p, int bits
         if (g == G - 1) p.offsets[G] = listed = at;
     }
     __syncthreads();
-    place_run<16, true>(p, e0, e1, g_cnt + wave * G, staged, bits);
+    place_groups<ROUNDS, true>(mine_of, e0, g_cnt + wave * G, nullptr, staged, bits);
     __syncthreads();
     for (int i = tid; i < listed; i += 1024) p.order[i] = staged[i];
 }
@@ -239,31 +251,48 @@ __global__ __launch_bounds__(1024) void group_scan_kernel(GroupParams p, int chu
 // the last act of the scan's last workgroup to finish 50, for the device-scope release that it needs of
 // every workgroup writes back its XCD's L2).
 template <int W>
-__global__ __launch_bounds__(1024) void group_place_kernel(GroupParams p, int64_t chunk, const int32_t* hist,
-                                                           const int32_t* totals, int bits) {
+__global__ __launch_bounds__(1024) void group_place_kernel(GroupParams p, int64_t chunk,
+                                                           const int32_t* __restrict__ hist,
+                                                           const int32_t* __restrict__ totals, int bits) {
     extern __shared__ int32_t g_cnt[];  // [W][n_groups]
     __shared__ int32_t sums[16];
     const int G = p.n_groups, tid = threadIdx.x, wave = tid >> 6;
     const int64_t c0 = int64_t(blockIdx.x) * chunk, run = chunk / W;
     const int64_t e0 = std::min<int64_t>(p.n_entries, c0 + wave * run);
     const int64_t e1 = wave < W ? std::min<int64_t>(p.n_entries, e0 + run) : e0;
+    constexpr int64_t BATCH = 64 * GROUP_ROUNDS;
+    int first[GROUP_ROUNDS];  // the first batch's groups stay in registers (up to 2^19 entries, all there are)
+    load_groups<GROUP_ROUNDS>(p, e0, e1, first);
     for (int i = tid; i < W * G; i += 1024) g_cnt[i] = 0;
-    const int per = (G + 1023) / 1024, g0 = std::min(G, tid * per), g1 = std::min(G, g0 + per);
+    // a wave takes consecutive groups, 64 at a time (a thread with consecutive groups met its neighbours' LDS
+    // banks: 32768 groups 145 us)
+    const int lane = tid & 63, part = (G + 1023) / 1024 * 64, g0 = std::min(G, wave * part), g1 = std::min(G, g0 + part);
     int32_t mine = 0;
 #pragma unroll 4
-    for (int g = g0; g < g1; ++g) mine += totals[g];
-    int32_t at = block_scan(mine, sums, 16);  // (a barrier: the counters are clear)
-    count_run<GROUP_ROUNDS>(p, e0, e1, g_cnt + wave * G, false);
+    for (int g = g0 + lane; g < g1; g += 64) mine += totals[g];
+    block_scan(mine, sums, 16);  // (a barrier: the counters are clear)
+    int32_t at = 0;
+    for (int w = 0; w < wave; ++w) at += sums[w];
+    count_groups<GROUP_ROUNDS>(first, g_cnt + wave * G);
+    if (e0 + BATCH < e1) count_run<GROUP_ROUNDS>(p, e0 + BATCH, e1, g_cnt + wave * G, false);
     __syncthreads();
     hist += int64_t(blockIdx.x) * G;
-    for (int g = g0; g < g1; ++g) {
-        if (blockIdx.x == 0) p.offsets[g] = at;
-        rows_scan<W>(g_cnt, G, g, at + hist[g]);
-        at += totals[g];
-        if (blockIdx.x == 0 && g == G - 1) p.offsets[G] = at;
+    for (int g = g0 + lane; g - lane < g1; g += 64) {
+        const int32_t all = g < g1 ? totals[g] : 0, before = g < g1 ? hist[g] : 0, end = at + wave_scan(all);
+        if (g < g1) {
+            if (blockIdx.x == 0) p.offsets[g] = end - all;
+            rows_scan<W>(g_cnt, G, g, end - all + before);
+            if (blockIdx.x == 0 && g == G - 1) p.offsets[G] = end;
+        }
+        at = __builtin_amdgcn_readlane(end, 63);
     }
     __syncthreads();
-    place_run<GROUP_ROUNDS, false>(p, e0, e1, g_cnt + wave * G, nullptr, bits);
+    place_groups<GROUP_ROUNDS, false>(first, e0, g_cnt + wave * G, p.order, nullptr, bits);
+    for (int64_t b = e0 + BATCH; b < e1; b += BATCH) {
+        int g[GROUP_ROUNDS];
+        load_groups<GROUP_ROUNDS>(p, b, e1, g);
+        place_groups<GROUP_ROUNDS, false>(g, b, g_cnt + wave * G, p.order, nullptr, bits);
+    }
 }
 
 template <int W>
@@ -296,8 +325,7 @@ hipError_t run_group_rows(const GroupParams& p, hipStream_t stream) {
     const int chunks = int(group_chunks(p.n_entries, G));
     int32_t* hist = static_cast<int32_t*>(p.workspace);  // [chunks][n_groups], then the totals
     int32_t* totals = hist + size_t(chunks) * G;
-    hipLaunchKernelGGL(group_count_kernel, dim3(chunks), dim3(64 * waves), size_t(G) * sizeof(int32_t), stream, p, chunk,
-                       hist);
+    hipLaunchKernelGGL(group_count_kernel, dim3(chunks), dim3(1024), size_t(G) * sizeof(int32_t), stream, p, chunk, hist);
     hipLaunchKernelGGL(group_scan_kernel, dim3((G + 31) / 32), dim3(1024), 0, stream, p, chunks, hist, totals);
     launch_place<16>(waves, p, chunks, chunk, hist, totals, bits, stream);
     return hipGetLastError();
