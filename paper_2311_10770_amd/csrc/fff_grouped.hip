@@ -420,20 +420,22 @@ hipError_t launch_few(const GroupedParams& p, hipStream_t stream, int* status) {
 
 // Which kernel: the one of the least time by what each took (us, measured with 1 to 64 groups, 64 to 16384
 // entries, k and n 128 to 4096): a tile costs `start` and `alone` a 128-byte step of the reduction axis,
-// or `pair` where two workgroups share its CU.  Small tiles lose rate (32 x 128: 0.35 of 256 x 256's, whose
+// or `pair` where two workgroups share its CU.  Small tiles lose rate (32 x 128: 0.4 of 256 x 256's, whose
 // two workgroups' worth of tile has a CU to itself) and win where large ones leave CUs idle or rows of
-// the tile empty; sixteen-entry tiles read the weights again for every sixteen entries of a group.  Some
+// the tile empty; sixteen-entry tiles read the weights again for every sixteen entries of a group; 64 x 64 are
+// for fp32, whose matrix cores are the bound, where columns of wider tiles are empty.  Some
 // of both sides, bf16 (few, 32, 64, 128, 256 rows): 64 entries x 1 group, 4096 -> 1024: 11, 27, 33, 39, 99;
 // 1000 x 16 groups, 768 -> 768: 26, 10, 12, 15, 28; 4000 x 64, 1024 -> 1024: 139, 44, 30, 39, 40;
-// 16000 x 16, 768 -> 768: -, 81, 42, 38, 34; fp32: 500 x 16, 768 -> 768: 28, 25, 35, 57;
-// 16000 x 64, 1024 -> 1024: -, 448, 338, 352.
+// 9025 x 23, 3224 -> 448 transposed: -, 82, 71, 63, -; fp32 (32, 64, 64 x 64): 8757 x 1, 640 -> 64 transposed: 33, 32,
+// 21; 1334 x 18, 2816 -> 448 transposed: 79, 121, 73; 9001 x 16, 768 -> 1000: 144, 142, 158.
 struct TileCost {
     int bm, bn;
     double start, alone, pair;
 };
-constexpr TileCost COST_BF16[] = {{32, 128, 2, 0.34, 0.70}, {64, 128, 2.5, 0.43, 0.58}, {128, 128, 4, 0.50, 0.95},
+constexpr TileCost COST_BF16[] = {{32, 128, 2, 0.34, 0.52}, {64, 128, 2.5, 0.43, 0.58}, {128, 128, 4, 0.50, 0.95},
                                   {256, 256, 6, 1.85, 3.70}};
-constexpr TileCost COST_F32[] = {{32, 128, 2, 0.74, 1.60}, {64, 128, 2.5, 1.18, 2.20}, {128, 128, 4, 2.00, 3.60}};
+constexpr TileCost COST_F32[] = {{32, 128, 2, 0.80, 1.25}, {64, 128, 2.5, 1.18, 2.20}, {128, 128, 4, 2.00, 3.60},
+                                 {64, 64, 2, 0.77, 1.22}};
 
 // 0: few entries a group; 1 ..: the tiles of the tables.
 int grouped_variant(const GroupedParams& p, int cus) {
@@ -452,12 +454,12 @@ int grouped_variant(const GroupedParams& p, int cus) {
     const TileCost* cost = p.bf16 ? COST_BF16 : COST_F32;
     // (256 x 256 tiles are not built through registers: they spill, and took as long as 128 x 128: 65536
     // entries, 1023 -> 4095, 1042 and 1046 us)
-    for (int v = 0; v < (p.bf16 && whole_vectors(p) ? 4 : 3); ++v) {
+    for (int v = 0; v < (!p.bf16 || whole_vectors(p) ? 4 : 3); ++v) {
         // (the half tile a group is an estimate: a tenth of a round does not make one)
         const double per_cu =
             std::max(1.0, std::ceil(row_tiles(cost[v].bm) * ((p.n + cost[v].bn - 1) / cost[v].bn) / cus - 0.1));
         const double pairs = std::floor(per_cu / 2), odd = per_cu - 2 * pairs;
-        const double t = pairs * (cost[v].start * (v == 3 ? 2 : 1) + steps * cost[v].pair) +
+        const double t = pairs * (cost[v].start * (cost[v].bm == 256 ? 2 : 1) + steps * cost[v].pair) +
                          odd * (cost[v].start + steps * cost[v].alone);
         if (t < least) {
             least = t;
@@ -473,13 +475,14 @@ hipError_t run_grouped_matmul(const GroupedParams& p, const DeviceInfo& dev, hip
     const int cus = dev.cu_count > 0 ? dev.cu_count : 256;
     switch (grouped_variant(p, cus)) {
         case 0: return launch_few(p, stream, status);
-        case 1: return p.bf16 ? launch_grouped<GCfg<true, 1, 1, 1, 4, 4, 128>>(p, cus, stream, status)
-                              : launch_grouped<GCfg<false, 1, 1, 1, 4, 4, 128>>(p, cus, stream, status);
+        case 1: return p.bf16 ? launch_grouped<GCfg<true, 1, 1, 1, 4, 3, 128>>(p, cus, stream, status)
+                              : launch_grouped<GCfg<false, 1, 1, 1, 4, 3, 128>>(p, cus, stream, status);
         case 2: return p.bf16 ? launch_grouped<GCfg<true, 1, 2, 2, 2, 3, 128>>(p, cus, stream, status)
                               : launch_grouped<GCfg<false, 1, 2, 2, 2, 3, 128>>(p, cus, stream, status);
         case 3: return p.bf16 ? launch_grouped<GCfg<true, 2, 2, 2, 2, 2, 128>>(p, cus, stream, status)
                               : launch_grouped<GCfg<false, 2, 2, 2, 2, 2, 128>>(p, cus, stream, status);
-        default: return launch_grouped<GCfg<true, 4, 2, 2, 4, 2, 128>>(p, cus, stream, status);
+        default: return p.bf16 ? launch_grouped<GCfg<true, 4, 2, 2, 4, 2, 128>>(p, cus, stream, status)
+                               : launch_grouped<GCfg<false, 1, 1, 2, 2, 3, 128>>(p, cus, stream, status);
     }
 }
 
