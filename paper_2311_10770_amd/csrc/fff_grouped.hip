@@ -10,6 +10,7 @@
 #include "fff_grouped.hpp"
 
 #include <cmath>
+#include <type_traits>
 
 namespace fff {
 
@@ -45,8 +46,8 @@ __device__ __forceinline__ void put8(char* row, int bf, int col, int left, const
 // Epilogue and store of sixteen rows of a tile from row m0 on, COLS columns from n0 on, out of the
 // wave's LDS: eight columns a lane.  FULL: all these columns are in the matrix.  The instructions of
 // this loop are what the epilogue costs: offsets are one 32 x 32 + 64 bit product, and rows without
-// a row of x are looked for in tiles that have some (bad).
-template <int KIND, bool FULL, int COLS, int PITCH>
+// a row of x are looked for in tiles that have some (bad).  FINE: y is fp32.
+template <int KIND, bool FINE, bool FULL, int COLS, int PITCH>
 __device__ __forceinline__ void grouped_rows(const GroupedParams& p, const float* blk, int m0, int rows, int64_t e0, int n0,
                                              const int32_t* s_dst, const uint8_t* s_src, bool bad) {
     constexpr int LPR = COLS / 8, RPI = 64 / LPR, U = 16 / RPI;
@@ -82,25 +83,27 @@ __device__ __forceinline__ void grouped_rows(const GroupedParams& p, const float
             unpack4(g, d[u][0], p.z_bf16);
             unpack4(g + 4, d[u][1], p.z_bf16);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) z[j] *= act_slope<KIND == EPI_GELU_GRAD ? ACT_GELU_ERF : ACT_GELU_TANH>(g[j]);
+            for (int j = 0; j < 8; ++j) z[j] *= act_slope<KIND == EPI_GELU_GRAD ? ACT_GELU_ERF : ACT_GELU_TANH, FINE>(g[j]);
         } else {
             if (p.z_out) put8<FULL>(static_cast<char*>(p.z_out) + uint64_t(ze + m) * zpitch, p.z_bf16, n, left, z);
             constexpr int ACT = KIND == EPI_GELU ? ACT_GELU_ERF : KIND == EPI_TANH ? ACT_GELU_TANH : ACT_IDENTITY;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) z[j] = act_value<ACT>(z[j]);
+            for (int j = 0; j < 8; ++j) z[j] = act_value<ACT, FINE>(z[j]);
         }
         if (dst >= 0) put8<FULL>(static_cast<char*>(p.y) + uint64_t(uint32_t(dst)) * ypitch, p.y_bf16, n, left, z);
     }
 }
-template <int COLS, int PITCH, bool FULL>
+template <int COLS, int PITCH, bool FULL, bool FINE>
 __device__ __forceinline__ void grouped_epilogue(int kind, const GroupedParams& p, const float* blk, int m0, int rows,
                                                  int64_t e0, int n0, const int32_t* dst, const uint8_t* src, bool bad) {
     switch (kind) {
-        case EPI_GELU: return grouped_rows<EPI_GELU, FULL, COLS, PITCH>(p, blk, m0, rows, e0, n0, dst, src, bad);
-        case EPI_TANH: return grouped_rows<EPI_TANH, FULL, COLS, PITCH>(p, blk, m0, rows, e0, n0, dst, src, bad);
-        case EPI_GELU_GRAD: return grouped_rows<EPI_GELU_GRAD, FULL, COLS, PITCH>(p, blk, m0, rows, e0, n0, dst, src, bad);
-        case EPI_TANH_GRAD: return grouped_rows<EPI_TANH_GRAD, FULL, COLS, PITCH>(p, blk, m0, rows, e0, n0, dst, src, bad);
-        default: return grouped_rows<EPI_STORE, FULL, COLS, PITCH>(p, blk, m0, rows, e0, n0, dst, src, bad);
+        case EPI_GELU: return grouped_rows<EPI_GELU, FINE, FULL, COLS, PITCH>(p, blk, m0, rows, e0, n0, dst, src, bad);
+        case EPI_TANH: return grouped_rows<EPI_TANH, FINE, FULL, COLS, PITCH>(p, blk, m0, rows, e0, n0, dst, src, bad);
+        case EPI_GELU_GRAD:
+            return grouped_rows<EPI_GELU_GRAD, FINE, FULL, COLS, PITCH>(p, blk, m0, rows, e0, n0, dst, src, bad);
+        case EPI_TANH_GRAD:
+            return grouped_rows<EPI_TANH_GRAD, FINE, FULL, COLS, PITCH>(p, blk, m0, rows, e0, n0, dst, src, bad);
+        default: return grouped_rows<EPI_STORE, false, FULL, COLS, PITCH>(p, blk, m0, rows, e0, n0, dst, src, bad);
     }
 }
 
@@ -267,8 +270,12 @@ __global__ __launch_bounds__(G::THREADS, 2) void grouped_kernel(GroupedParams p)
             }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             const int m0 = wm * G::TM * 32 + i * 16;
-            if (full) grouped_epilogue<COLS, PITCH, true>(kind, p, blk, m0, rows, t.m0, c0, s_dst[turn], s_src[turn], bad);
-            else grouped_epilogue<COLS, PITCH, false>(kind, p, blk, m0, rows, t.m0, c0, s_dst[turn], s_src[turn], bad);
+            auto rows_out = [&](auto full_cols, auto fine) {
+                grouped_epilogue<COLS, PITCH, full_cols.value, fine.value>(kind, p, blk, m0, rows, t.m0, c0, s_dst[turn],
+                                                                           s_src[turn], bad);
+            };
+            if (p.y_bf16) full ? rows_out(std::true_type{}, std::false_type{}) : rows_out(std::false_type{}, std::false_type{});
+            else full ? rows_out(std::true_type{}, std::true_type{}) : rows_out(std::false_type{}, std::true_type{});
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         }
         if (next.g < 0) return;
@@ -399,10 +406,14 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void grouped_few_kernel(GroupedPara
     if (entry_row(p.x_index, p.x_div, p.x_rows, i) < 0) z = 0.0f;  // (zeros times infinite weights are NaN)
     if (p.z_in) {
         const float d = load_elem(p.z_in, p.z_bf16, i * p.n + c);
-        z *= p.act == ACT_GELU_ERF ? act_slope<ACT_GELU_ERF>(d) : p.act == ACT_GELU_TANH ? act_slope<ACT_GELU_TANH>(d) : 1.0f;
+        z *= p.act == ACT_GELU_ERF    ? act_slope<ACT_GELU_ERF, true>(d)
+             : p.act == ACT_GELU_TANH ? act_slope<ACT_GELU_TANH, true>(d)
+                                      : 1.0f;
     } else {
         if (p.z_out) store_elem(p.z_out, p.z_bf16, i * p.n + c, z);
-        z = p.act == ACT_GELU_ERF ? act_value<ACT_GELU_ERF>(z) : p.act == ACT_GELU_TANH ? act_value<ACT_GELU_TANH>(z) : z;
+        z = p.act == ACT_GELU_ERF    ? act_value<ACT_GELU_ERF, true>(z)
+            : p.act == ACT_GELU_TANH ? act_value<ACT_GELU_TANH, true>(z)
+                                     : z;
     }
     const int64_t dst = entry_row(p.y_index, 1, p.y_rows, i);
     if (dst >= 0) store_elem(p.y, p.y_bf16, dst * p.n + c, z);

@@ -811,3 +811,35 @@ def test_training_step_of_the_tree_block(fff_lib):
         rel = (a.cpu().double() - b).norm() / b.norm()
         # chains of three sums of at most 64 terms, a factor of a hundred for conditioning
         assert rel < 100 * 64 * ref.U, (name, float(rel))
+
+
+@pytest.mark.parametrize("t,E", [("f32", 1 << 18), ("bf16", 1 << 18), ("f32", 16)])
+@pytest.mark.parametrize("act", ["gelu", "gelu_tanh"])
+def test_activations_stored_in_fp32_are_as_exact_as_fp32_allows(fff_lib, t, E, act):
+    """Root mean square errors over z ~ N(0, 1) against the least that the formulas' own fp32 roundings leave.
+
+    z Phi(z) from a correctly rounded Phi, and the derivative as the sum of correctly rounded Phi and z phi, are
+    the ideals (evaluated here).  A value may have twice that variance: as much again from what Phi is
+    computed of (the polynomial, or the exponential and the reciprocal).  The derivative of the tanh form has one more
+    such operand, u' beside u, and may have 2.5 times it.  The product before the activation is exact (k = 1, W = 1)."""
+    n = 1 << 14 if E == 16 else 1  # few entries take the kernel for them, here over many columns
+    z = _randn(_gen(12), E, 1, dtype=t)
+    ones = torch.ones((1, n, 1), dtype=DT[t], device=DEV)
+    if E == 16:
+        z, ones = torch.ones((E, 1), device=DEV), _randn(_gen(12), 1, n, 1)
+    offsets = torch.tensor([0, E], dtype=torch.int32, device=DEV)
+    flush_print(f"[gpu] {act} in fp32, {E} x {n} {t}")
+    y, zs = fff_lib.grouped_matmul(z, ones, offsets, act=act, keep_z=True, y_dtype=torch.float32)
+    assert torch.equal(zs, (z.float() @ ones[0].float().T))
+    unit = fff_lib.grouped_matmul(torch.ones_like(z), torch.ones_like(ones), offsets, act=act, z_in=zs, y_dtype=torch.float32)
+    v = zs.cpu().double()
+    share = ref.act(v, act) / v  # Phi, or the logistic of 2 u
+    slope = ref.act_grad(v, act)
+
+    def rms(got, want):
+        return float(((got.double() - want) / ref.U).square().mean().sqrt())
+
+    least = rms((v * share.float().double()).float(), v * share)
+    assert rms(y.cpu(), v * share) <= math.sqrt(2) * least
+    least = rms((share.float().double() + (slope - share).float().double()).float(), slope)
+    assert rms(unit.cpu(), slope) <= math.sqrt(2 if act == "gelu" else 2.5) * least
