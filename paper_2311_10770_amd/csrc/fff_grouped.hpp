@@ -196,7 +196,9 @@ __device__ __forceinline__ float act_slope(float z) {
         const float u = 2.88539008177792681472f * gelu_tanh_u(z);
         const float up = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-u));
         const float down = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(u));
-        return __builtin_fmaf(2.0f * z * up * down, 0.79788456080286535588f * __builtin_fmaf(0.134145f * z, z, 1.0f), up);
+        // far out up * down is 0, and so are its products with a finite z and a square kept from overflow
+        const float du = __builtin_fminf(__builtin_fmaf(0.134145f * z, z, 1.0f), 1e38f);
+        return __builtin_fmaf(z * up * down, 1.59576912160573071176f * du, up);
     } else {
         return 1.0f;
     }

@@ -843,3 +843,26 @@ def test_activations_stored_in_fp32_are_as_exact_as_fp32_allows(fff_lib, t, E, a
     assert rms(y.cpu(), v * share) <= math.sqrt(2) * least
     least = rms((share.float().double() + (slope - share).float().double()).float(), slope)
     assert rms(unit.cpu(), slope) <= math.sqrt(2 if act == "gelu" else 2.5) * least
+
+
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+@pytest.mark.parametrize("E", [16, 4096])
+@pytest.mark.parametrize("act", ["gelu", "gelu_tanh"])
+def test_activations_far_out(fff_lib, t, E, act):
+    """Where either GELU is z or 0 to every bit, up to the largest numbers: its derivative is 1 or 0, nothing overflows."""
+    far = torch.tensor([20.0, 1e4, 1e10, 6e18, 8e18, 1e20, 1.5e38, 3e38], device=DEV).repeat(E // 8)[:, None]
+    one, offsets = torch.ones((1, 1, 1), dtype=DT[t], device=DEV), torch.tensor([0, E], dtype=torch.int32, device=DEV)
+    for yt in ("f32", "bf16"):
+        for sign in (1, -1):
+            z = (sign * far).to(DT[t])
+            flush_print(f"[gpu] {act} far out, {E} {t}/{yt} {sign}")
+            y = fff_lib.grouped_matmul(z, one, offsets, act=act, y_dtype=DT[yt])
+            assert torch.equal(y, z.to(DT[yt]) if sign > 0 else torch.zeros_like(y))
+            d = fff_lib.grouped_matmul(torch.ones_like(z), one, offsets, act=act, z_in=z, y_dtype=DT[yt])
+            assert torch.equal(d, torch.full_like(d, float(sign > 0)))
+    # a positive infinity is itself, a NaN stays one
+    z = torch.tensor([math.inf, math.nan], device=DEV).repeat(E // 2)[:, None].to(DT[t])
+    for yt in ("f32", "bf16"):
+        y = fff_lib.grouped_matmul(z, one, offsets, act=act, y_dtype=DT[yt])
+        assert (y[0::2] == math.inf).all() and torch.isnan(y[1::2]).all()
+        assert torch.isnan(fff_lib.grouped_matmul(torch.ones_like(z), one, offsets, act=act, z_in=z)[1::2]).all()
