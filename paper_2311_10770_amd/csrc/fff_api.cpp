@@ -11,6 +11,7 @@
 #include <mutex>
 
 #include "fff_internal.hpp"
+#include "fff_operators.hpp"
 
 #define FFF_EXPORT extern "C" __attribute__((visibility("default")))
 

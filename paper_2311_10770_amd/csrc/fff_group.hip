@@ -13,7 +13,7 @@
 // 16384 entries of 64 groups: 12.3 us in one launch, called or in a graph (15.0 with the entries read again
 // for placing; three launches took 11.4 in a graph, but 19.1 called).  524288 entries of 4096 groups: 23.4
 // us; 100000 of 32768: 52.6, a row of counters there being all that LDS holds, one wave places.
-#include "fff_internal.hpp"
+#include "fff_operators.hpp"
 
 #include <hip/hip_runtime.h>
 

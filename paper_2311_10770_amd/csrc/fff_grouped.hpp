@@ -13,7 +13,7 @@
 
 #include "fff_device.hpp"
 #include "fff_gemm.hpp"
-#include "fff_internal.hpp"
+#include "fff_operators.hpp"
 #include "fff_rows.hpp"
 
 #include <hip/hip_runtime.h>

@@ -9,7 +9,7 @@
 // are held in fp32; the variance is taken of the centred values (a sum of
 // squares less the squared mean would cancel for rows with a large mean).
 #include "fff_device.hpp"
-#include "fff_internal.hpp"
+#include "fff_operators.hpp"
 #include "fff_rows.hpp"
 
 #include <hip/hip_runtime.h>

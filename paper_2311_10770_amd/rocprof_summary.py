@@ -15,20 +15,35 @@ import argparse
 import csv
 import hashlib
 import json
+import re
 from pathlib import Path
 
 PKG = Path(__file__).resolve().parent
 COPY_KERNEL = "copy_kernel"
 
 
+def _local_headers(src: Path) -> set:
+    """Headers beside a source that it includes, through others too."""
+    found, todo = set(), [src]
+    while todo:
+        for name in re.findall(r'^#include "([^"]+)"', todo.pop().read_text(), re.M):
+            h = src.parent / name
+            if h.exists() and h not in found:
+                found.add(h)
+                todo.append(h)
+    return found
+
+
 def kernel_source_hash(backward: bool = False) -> str:
     """Hash of the sources the forward (or backward) kernels are compiled from: counter figures
-    taken on them are void once these change."""
+    taken on them are void once these change.  The operators around the layer (sources that reach
+    fff_operators.hpp) are kernels of their own and count for neither."""
     h = hashlib.sha256()
     csrc = PKG / "csrc"
-    kernels = [csrc / "fff_backward.hip"] if backward else [
-        p for p in csrc.glob("fff_*.hip") if p.name != "fff_backward.hip"]
-    for p in sorted(kernels) + sorted(csrc.glob("fff_*.hpp")):
+    layer = {p: _local_headers(p) for p in csrc.glob("fff_*.hip")}
+    layer = {p: hs for p, hs in layer.items() if csrc / "fff_operators.hpp" not in hs}
+    kernels = [p for p in layer if (p.name == "fff_backward.hip") == backward]
+    for p in sorted(kernels) + sorted(set().union(*layer.values())):
         h.update(p.read_bytes())
     return h.hexdigest()[:16]
 
