@@ -571,6 +571,11 @@ int fff_grouped_weight_grad(const fff_grouped_weight_grad_args* a);
  * there are enough groups, and for invalid shapes). */
 size_t fff_grouped_weight_grad_workspace_bytes(int64_t n_entries, int32_t n_groups, int32_t k, int32_t n);
 
+/* The kernel and launch that the product or weight gradient would use for these arguments (after the
+ * same checks), as fff_describe gives them for the layer.  Enqueues nothing. */
+int fff_describe_grouped_matmul(const fff_grouped_matmul_args* a, char* buf, size_t len);
+int fff_describe_grouped_weight_grad(const fff_grouped_weight_grad_args* a, char* buf, size_t len);
+
 const char* fff_status_str(int status);
 int fff_last_hip_error(void); /* raw hipError_t behind the calling thread's last FFF_ERR_HIP */
 int fff_version(void);

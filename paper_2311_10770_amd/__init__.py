@@ -12,6 +12,7 @@ from .fff import (  # noqa: F401
     workspace_bytes,
 )
 from .ops import (  # noqa: F401
-    dropout, group_rows, group_rows_workspace_bytes, grouped_matmul, grouped_weight_grad,
-    grouped_weight_grad_workspace_bytes, layer_norm, layer_norm_backward, layer_norm_backward_workspace_bytes,
+    describe_grouped_matmul, describe_grouped_weight_grad, dropout, group_rows, group_rows_workspace_bytes,
+    grouped_matmul, grouped_weight_grad, grouped_weight_grad_workspace_bytes, layer_norm, layer_norm_backward,
+    layer_norm_backward_workspace_bytes,
 )

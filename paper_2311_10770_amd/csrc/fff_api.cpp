@@ -821,7 +821,9 @@ bool rows_ok(int64_t rows, int64_t n_entries, const int32_t* index) {
 }
 }  // namespace
 
-FFF_EXPORT int fff_grouped_matmul(const fff_grouped_matmul_args* a) {
+namespace {
+// fff_grouped_matmul, or (buf) its description.
+int grouped_matmul(const fff_grouped_matmul_args* a, char* buf, size_t len) {
     if (!a || !grouped_sizes_ok(a->n_entries, a->n_groups, a->k, a->n, a->x_div)) return FFF_ERR_INVALID_ARG;
     for (int32_t dt : {a->x_dtype, a->w_dtype, a->y_dtype, a->z_dtype})
         if (!dtype_ok(dt)) return FFF_ERR_INVALID_ARG;
@@ -873,9 +875,22 @@ FFF_EXPORT int fff_grouped_matmul(const fff_grouped_matmul_args* a) {
     p.z_bf16 = a->z_dtype == FFF_BF16;
     p.act = a->act;
     int status = FFF_OK;
-    const hipError_t e = fff::run_grouped_matmul(p, dev, stream_of(a->hip_stream), &status);
+    const hipError_t e = fff::run_grouped_matmul(p, dev, stream_of(a->hip_stream), &status, buf, len);
     if (status != FFF_OK) return status;
     return e == hipSuccess ? FFF_OK : hip_fail(e);
+}
+}  // namespace
+
+FFF_EXPORT int fff_grouped_matmul(const fff_grouped_matmul_args* a) { return grouped_matmul(a, nullptr, 0); }
+
+FFF_EXPORT int fff_describe_grouped_matmul(const fff_grouped_matmul_args* a, char* buf, size_t len) {
+    char unread[8];
+    if (!buf || !len) {
+        buf = unread;
+        len = sizeof unread;
+    }
+    std::snprintf(buf, len, "none");  // without work
+    return grouped_matmul(a, buf, len);
 }
 
 FFF_EXPORT size_t fff_grouped_weight_grad_workspace_bytes(int64_t n_entries, int32_t n_groups, int32_t k, int32_t n) {
@@ -884,7 +899,9 @@ FFF_EXPORT size_t fff_grouped_weight_grad_workspace_bytes(int64_t n_entries, int
     return fff::grouped_grad_workspace_bytes(n_entries, n_groups, k, n);
 }
 
-FFF_EXPORT int fff_grouped_weight_grad(const fff_grouped_weight_grad_args* a) {
+namespace {
+// fff_grouped_weight_grad, or (buf) its description.
+int grouped_weight_grad(const fff_grouped_weight_grad_args* a, char* buf, size_t len) {
     if (!a || !grouped_sizes_ok(a->n_entries, a->n_groups, a->k, a->n, a->x_div)) return FFF_ERR_INVALID_ARG;
     if (!dtype_ok(a->dy_dtype) || !dtype_ok(a->x_dtype)) return FFF_ERR_INVALID_ARG;
     if (a->accumulate != 0 && a->accumulate != 1) return FFF_ERR_INVALID_ARG;
@@ -937,9 +954,22 @@ FFF_EXPORT int fff_grouped_weight_grad(const fff_grouped_weight_grad_args* a) {
     p.accumulate = a->accumulate;
     p.part = static_cast<float*>(a->workspace);
     int status = FFF_OK;
-    const hipError_t e = fff::run_grouped_weight_grad(p, dev, stream_of(a->hip_stream), &status);
+    const hipError_t e = fff::run_grouped_weight_grad(p, stream_of(a->hip_stream), &status, buf, len);
     if (status != FFF_OK) return status;
     return e == hipSuccess ? FFF_OK : hip_fail(e);
+}
+}  // namespace
+
+FFF_EXPORT int fff_grouped_weight_grad(const fff_grouped_weight_grad_args* a) { return grouped_weight_grad(a, nullptr, 0); }
+
+FFF_EXPORT int fff_describe_grouped_weight_grad(const fff_grouped_weight_grad_args* a, char* buf, size_t len) {
+    char unread[8];
+    if (!buf || !len) {
+        buf = unread;
+        len = sizeof unread;
+    }
+    std::snprintf(buf, len, "none");  // without work
+    return grouped_weight_grad(a, buf, len);
 }
 
 FFF_EXPORT const char* fff_status_str(int status) {

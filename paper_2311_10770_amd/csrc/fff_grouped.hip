@@ -10,6 +10,7 @@
 #include "fff_grouped.hpp"
 
 #include <cmath>
+#include <cstdio>
 #include <type_traits>
 
 namespace fff {
@@ -292,16 +293,20 @@ bool whole_vectors(const GroupedParams& p) {
 }
 
 template <class G>
-hipError_t launch_grouped(const GroupedParams& p, int cus, hipStream_t stream, int* status) {
+hipError_t launch_grouped(const GroupedParams& p, int cus, hipStream_t stream, int* status, char* buf, size_t len) {
     const int64_t tiles = most_tiles(p.n_entries, p.n_groups, G::BM) * ((int64_t(p.n) + G::BN - 1) / G::BN);
     *status = tiles > INT32_MAX ? ST_UNSUPPORTED_ : ST_OK_;
     if (*status != ST_OK_) return hipSuccess;
     // rows of whole 16-byte vectors go straight to LDS; two stages of those loaded through registers
     const bool dma = whole_vectors(p);
     const int grid = int(std::min<int64_t>(tiles, int64_t(cus) * (dma ? G::PER_CU : 8 / G::WAVES)));
-    auto launch = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, dim3(unsigned(grid)), dim3(G::THREADS), dma ? G::LDS : 2 * G::STAGE, stream, p);
-    };
+    const size_t lds = dma ? G::LDS : 2 * G::STAGE;
+    if (buf) {
+        std::snprintf(buf, len, "tiles<%s,%dx%d,%s,%s> grid=%d block=%d lds_bytes=%zu", p.bf16 ? "bf16" : "f32", G::BM,
+                      G::BN, dma ? "direct" : "registers", p.w_transposed ? "w_kn" : "w_nk", grid, G::THREADS, lds);
+        return hipSuccess;
+    }
+    auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(unsigned(grid)), dim3(G::THREADS), lds, stream, p); };
     if (dma) p.w_transposed ? launch(grouped_kernel<G, true, true>) : launch(grouped_kernel<G, true, false>);
     else if constexpr (G::BM < 256) p.w_transposed ? launch(grouped_kernel<G, false, true>) : launch(grouped_kernel<G, false, false>);
     return hipGetLastError();
@@ -419,13 +424,18 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void grouped_few_kernel(GroupedPara
     if (dst >= 0) store_elem(p.y, p.y_bf16, dst * p.n + c, z);
 }
 
-hipError_t launch_few(const GroupedParams& p, hipStream_t stream, int* status) {
+hipError_t launch_few(const GroupedParams& p, hipStream_t stream, int* status, char* buf, size_t len) {
     const int64_t tiles = most_tiles(p.n_entries, p.n_groups, 16) * ((int64_t(p.n) + 15) / 16);
     *status = tiles > UINT32_MAX / (64 * FEW_WAVES) ? ST_UNSUPPORTED_ : ST_OK_;  // a launch's threads
     if (*status != ST_OK_) return hipSuccess;
+    if (buf) {
+        std::snprintf(buf, len, "few<%s,%s> grid=%lld block=%d", p.bf16 ? "bf16" : "f32",
+                      whole_vectors(p) ? "aligned" : "unaligned", (long long)tiles, 64 * FEW_WAVES);
+        return hipSuccess;
+    }
     auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(unsigned(tiles)), dim3(64 * FEW_WAVES), 0, stream, p); };
-    if (p.bf16) p.k % 8 == 0 ? launch(grouped_few_kernel<true, true>) : launch(grouped_few_kernel<true, false>);
-    else p.k % 4 == 0 ? launch(grouped_few_kernel<false, true>) : launch(grouped_few_kernel<false, false>);
+    if (p.bf16) whole_vectors(p) ? launch(grouped_few_kernel<true, true>) : launch(grouped_few_kernel<true, false>);
+    else whole_vectors(p) ? launch(grouped_few_kernel<false, true>) : launch(grouped_few_kernel<false, false>);
     return hipGetLastError();
 }
 
@@ -482,18 +492,19 @@ int grouped_variant(const GroupedParams& p, int cus) {
 
 }  // namespace
 
-hipError_t run_grouped_matmul(const GroupedParams& p, const DeviceInfo& dev, hipStream_t stream, int* status) {
+hipError_t run_grouped_matmul(const GroupedParams& p, const DeviceInfo& dev, hipStream_t stream, int* status, char* buf,
+                              size_t len) {
     const int cus = dev.cu_count > 0 ? dev.cu_count : 256;
     switch (grouped_variant(p, cus)) {
-        case 0: return launch_few(p, stream, status);
-        case 1: return p.bf16 ? launch_grouped<GCfg<true, 1, 1, 1, 4, 3, 128>>(p, cus, stream, status)
-                              : launch_grouped<GCfg<false, 1, 1, 1, 4, 3, 128>>(p, cus, stream, status);
-        case 2: return p.bf16 ? launch_grouped<GCfg<true, 1, 2, 2, 2, 3, 128>>(p, cus, stream, status)
-                              : launch_grouped<GCfg<false, 1, 2, 2, 2, 3, 128>>(p, cus, stream, status);
-        case 3: return p.bf16 ? launch_grouped<GCfg<true, 2, 2, 2, 2, 2, 128>>(p, cus, stream, status)
-                              : launch_grouped<GCfg<false, 2, 2, 2, 2, 2, 128>>(p, cus, stream, status);
-        default: return p.bf16 ? launch_grouped<GCfg<true, 4, 2, 2, 4, 2, 128>>(p, cus, stream, status)
-                               : launch_grouped<GCfg<false, 1, 1, 2, 2, 3, 128>>(p, cus, stream, status);
+        case 0: return launch_few(p, stream, status, buf, len);
+        case 1: return p.bf16 ? launch_grouped<GCfg<true, 1, 1, 1, 4, 3, 128>>(p, cus, stream, status, buf, len)
+                              : launch_grouped<GCfg<false, 1, 1, 1, 4, 3, 128>>(p, cus, stream, status, buf, len);
+        case 2: return p.bf16 ? launch_grouped<GCfg<true, 1, 2, 2, 2, 3, 128>>(p, cus, stream, status, buf, len)
+                              : launch_grouped<GCfg<false, 1, 2, 2, 2, 3, 128>>(p, cus, stream, status, buf, len);
+        case 3: return p.bf16 ? launch_grouped<GCfg<true, 2, 2, 2, 2, 2, 128>>(p, cus, stream, status, buf, len)
+                              : launch_grouped<GCfg<false, 2, 2, 2, 2, 2, 128>>(p, cus, stream, status, buf, len);
+        default: return p.bf16 ? launch_grouped<GCfg<true, 4, 2, 2, 4, 2, 128>>(p, cus, stream, status, buf, len)
+                               : launch_grouped<GCfg<false, 1, 1, 2, 2, 3, 128>>(p, cus, stream, status, buf, len);
     }
 }
 

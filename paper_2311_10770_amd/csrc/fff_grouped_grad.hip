@@ -8,6 +8,8 @@
 // their own; their partial sums are added in order.
 #include "fff_grouped.hpp"
 
+#include <cstdio>
+
 namespace fff {
 
 namespace {
@@ -233,17 +235,25 @@ __global__ __launch_bounds__(256) void grouped_grad_sum_kernel(GroupedGradParams
 
 // A launch holds less than 2^32 threads.
 template <class G>
-hipError_t launch_grad(const GroupedGradParams& p, const GradPlan& plan, hipStream_t stream, int* status) {
+hipError_t launch_grad(const GroupedGradParams& p, const GradPlan& plan, hipStream_t stream, int* status, char* buf,
+                       size_t len) {
     const int tk = int((int64_t(p.k) + G::BN - 1) / G::BN);
     const int64_t round = XCDS * grad_run(int(plan.tiles / p.n_groups), plan.splits);
     const int64_t grid = (plan.tiles * plan.splits + round - 1) / round * round;
     *status = grid > UINT32_MAX / G::THREADS ? ST_UNSUPPORTED_ : ST_OK_;
     if (*status != ST_OK_) return hipSuccess;
-    auto launch = [&](auto kernel, size_t lds) {
+    const bool dma = p.n % G::EV == 0 && p.k % G::EV == 0;
+    const size_t lds = dma ? G::LDS : 2 * G::STAGE;  // two stages of registers' loads
+    if (buf) {
+        std::snprintf(buf, len, "tiles<%s,%dx%d,%s> splits=%d grid=%lld block=%d lds_bytes=%zu", G::BF ? "bf16" : "f32",
+                      G::BM, G::BN, dma ? "direct" : "registers", plan.splits, (long long)grid, G::THREADS, lds);
+        return hipSuccess;
+    }
+    auto launch = [&](auto kernel) {
         hipLaunchKernelGGL(kernel, dim3(unsigned(grid)), dim3(G::THREADS), lds, stream, p, tk, int(plan.tiles), plan.splits);
     };
-    if (p.n % G::EV == 0 && p.k % G::EV == 0) launch(grouped_grad_kernel<G, true>, G::LDS);
-    else if constexpr (G::BM < 256) launch(grouped_grad_kernel<G, false>, 2 * G::STAGE);  // two stages of registers' loads
+    if (dma) launch(grouped_grad_kernel<G, true>);
+    else if constexpr (G::BM < 256) launch(grouped_grad_kernel<G, false>);
     if (plan.splits > 1) {
         const int64_t all = int64_t(p.n_groups) * p.n * p.k;
         const unsigned blocks = unsigned(std::min<int64_t>((all + 1023) / 1024, 2048));
@@ -265,12 +275,14 @@ size_t grouped_grad_workspace_bytes(int64_t n_entries, int32_t n_groups, int32_t
     return most;
 }
 
-hipError_t run_grouped_weight_grad(const GroupedGradParams& p, const DeviceInfo&, hipStream_t stream, int* status) {
+hipError_t run_grouped_weight_grad(const GroupedGradParams& p, hipStream_t stream, int* status, char* buf, size_t len) {
     const GradPlan plan = grad_plan(p.n_entries, p.n_groups, p.k, p.n, p.bf16);
-    if (plan.bm == 256) return launch_grad<GradBig>(p, plan, stream, status);
+    if (plan.bm == 256) return launch_grad<GradBig>(p, plan, stream, status, buf, len);
     if (plan.bm == 128)
-        return p.bf16 ? launch_grad<GradSmall>(p, plan, stream, status) : launch_grad<GradSmallF32>(p, plan, stream, status);
-    return p.bf16 ? launch_grad<GradTiny>(p, plan, stream, status) : launch_grad<GradTinyF32>(p, plan, stream, status);
+        return p.bf16 ? launch_grad<GradSmall>(p, plan, stream, status, buf, len)
+                      : launch_grad<GradSmallF32>(p, plan, stream, status, buf, len);
+    return p.bf16 ? launch_grad<GradTiny>(p, plan, stream, status, buf, len)
+                  : launch_grad<GradTinyF32>(p, plan, stream, status, buf, len);
 }
 
 }  // namespace fff

@@ -102,7 +102,9 @@ struct GroupedParams {
     int32_t act;
 };
 // *status: ST_OK, or FFF_ERR_UNSUPPORTED's value when the grid would be too large (nothing enqueued).
-hipError_t run_grouped_matmul(const GroupedParams& p, const DeviceInfo& dev, hipStream_t stream, int* status);
+// With buf nothing is enqueued: the kernel and its launch are named there (describe).
+hipError_t run_grouped_matmul(const GroupedParams& p, const DeviceInfo& dev, hipStream_t stream, int* status,
+                              char* buf = nullptr, size_t len = 0);
 
 struct GroupedGradParams {
     const void* dy;          // [dy_rows, n]
@@ -118,6 +120,7 @@ struct GroupedGradParams {
     float* part;             // partial sums, or null
 };
 size_t grouped_grad_workspace_bytes(int64_t n_entries, int32_t n_groups, int32_t k, int32_t n);
-hipError_t run_grouped_weight_grad(const GroupedGradParams& p, const DeviceInfo& dev, hipStream_t stream, int* status);
+hipError_t run_grouped_weight_grad(const GroupedGradParams& p, hipStream_t stream, int* status, char* buf = nullptr,
+                                   size_t len = 0);
 
 }  // namespace fff

@@ -72,7 +72,8 @@ EXPORTS = ("fff_forward", "fff_forward_ex", "fff_forward_static", "fff_workspace
            "fff_describe_stack", "fff_backward", "fff_backward_workspace_bytes", "fff_status_str",
            "fff_last_hip_error", "fff_version", "fff_layer_norm", "fff_layer_norm_backward",
            "fff_layer_norm_backward_workspace_bytes", "fff_dropout", "fff_group_rows", "fff_group_rows_workspace_bytes",
-           "fff_grouped_matmul", "fff_grouped_weight_grad", "fff_grouped_weight_grad_workspace_bytes")
+           "fff_grouped_matmul", "fff_grouped_weight_grad", "fff_grouped_weight_grad_workspace_bytes",
+           "fff_describe_grouped_matmul", "fff_describe_grouped_weight_grad")
 
 
 def load_library(path: Path | str | None = None):
@@ -107,6 +108,9 @@ def load_library(path: Path | str | None = None):
     for name in ("fff_layer_norm", "fff_layer_norm_backward", "fff_dropout", "fff_group_rows", "fff_grouped_matmul",
                  "fff_grouped_weight_grad"):
         getattr(lib, name).argtypes = [c_void_p]  # the struct's address
+        getattr(lib, name).restype = c_int
+    for name in ("fff_describe_grouped_matmul", "fff_describe_grouped_weight_grad"):
+        getattr(lib, name).argtypes = [c_void_p, c_char_p, c_size_t]
         getattr(lib, name).restype = c_int
     lib.fff_layer_norm_backward_workspace_bytes.argtypes = [c_int64, c_int32]
     lib.fff_group_rows_workspace_bytes.argtypes = [c_int64, c_int32, c_int32]

@@ -201,6 +201,12 @@ def _run(fn, args):
         _check(rc)
 
 
+def _describe(fn, args) -> str:
+    buf = ctypes.create_string_buffer(256)
+    _check(fn(ctypes.addressof(args), buf, len(buf)))
+    return buf.value.decode()
+
+
 @_on_call
 def layer_norm(x, gamma=None, beta=None, *, eps=1e-12, residual=None, p=0.0, seed=0, offset=0, rng_offset=None, y=None,
                s=None, mean=None, rstd=None, y_dtype=None, s_dtype=None, stats=True, stream=None):
@@ -334,18 +340,9 @@ def group_rows(ids, n_ids: int, *, first: int = 0, n_trees: int = 1, order=None,
     return order, offsets
 
 
-@_on_call
-def grouped_matmul(x, w, offsets, *, x_index=None, x_div=1, y=None, y_index=None, y_dtype=None, transpose_w=False,
-                   act="identity", z_out=None, keep_z=False, z_in=None, stream=None):
-    """Every entry's row times its group's matrix, through ``fff_grouped_matmul``.
-
-    ``w`` [n_groups, n, k] gives ``act(x W_g^T)``, with ``transpose_w`` [n_groups, k, n] gives
-    ``act(x W_g)``, for the entries offsets[g] .. offsets[g + 1] of each group.  Entry i reads row
-    ``x_index[i] // x_div`` of x (i // x_div without an index) and writes row ``y_index[i]`` of y (i
-    without).  ``keep_z`` (or a ``z_out``) also stores the product before the activation, in grouped
-    order; with ``z_in`` the result is ``z * act'(z_in)``, the data gradient through the activation.
-    Returns y, or (y, z) when z is kept.  y without an argument is allocated with a row per entry;
-    its rows that no entry names are not written."""
+def _product(x, w, offsets, *, x_index=None, x_div=1, y=None, y_index=None, y_dtype=None, transpose_w=False,
+             act="identity", z_out=None, keep_z=False, z_in=None, stream=None):
+    """Checked arguments and results of a product."""
     _gpu(x, "x")
     device, at = x.device, x.get_device()
     _gpu(w, "w", at)
@@ -372,27 +369,46 @@ def grouped_matmul(x, w, offsets, *, x_index=None, x_div=1, y=None, y_index=None
     if keep_z and z_out is None:
         z_out = torch.empty((E, N), dtype=y.dtype, device=device)
     z = z_out if z_out is not None else z_in
-    _run(_lib().fff_grouped_matmul, FffGroupedMatmulArgs(
+    args = FffGroupedMatmulArgs(
         x.data_ptr(), w.data_ptr(), _index(offsets, "offsets", at, G + 1), _index(x_index, "x_index", at, E),
         _index(y_index, "y_index", at, E), y.data_ptr(), _like(z_out, "z_out", at, (E, N)), _like(z_in, "z_in", at, (E, N)),
         E, x.shape[0], y.shape[0], G, K, N, x_div, int(bool(transpose_w)), _dt(x, "x"), _dt(w, "w"), _dt(y, "y"),
         _dt(z, "z") if z is not None else FFF_F32, ACTS[act] if isinstance(act, str) else int(act),
-        _raw_stream(device, stream)))
-    return (y, z_out) if keep_z else y
+        _raw_stream(device, stream))
+    return args, (y, z_out) if keep_z else y
+
+
+@_on_call
+def grouped_matmul(x, w, offsets, *, x_index=None, x_div=1, y=None, y_index=None, y_dtype=None, transpose_w=False,
+                   act="identity", z_out=None, keep_z=False, z_in=None, stream=None):
+    """Every entry's row times its group's matrix, through ``fff_grouped_matmul``.
+
+    ``w`` [n_groups, n, k] gives ``act(x W_g^T)``, with ``transpose_w`` [n_groups, k, n] gives
+    ``act(x W_g)``, for the entries offsets[g] .. offsets[g + 1] of each group.  Entry i reads row
+    ``x_index[i] // x_div`` of x (i // x_div without an index) and writes row ``y_index[i]`` of y (i
+    without).  ``keep_z`` (or a ``z_out``) also stores the product before the activation, in grouped
+    order; with ``z_in`` the result is ``z * act'(z_in)``, the data gradient through the activation.
+    Returns y, or (y, z) when z is kept.  y without an argument is allocated with a row per entry;
+    its rows that no entry names are not written."""
+    args, out = _product(x, w, offsets, x_index=x_index, x_div=x_div, y=y, y_index=y_index, y_dtype=y_dtype,
+                         transpose_w=transpose_w, act=act, z_out=z_out, keep_z=keep_z, z_in=z_in, stream=stream)
+    _run(_lib().fff_grouped_matmul, args)
+    return out
+
+
+@_on_call
+def describe_grouped_matmul(x, w, offsets, **kw) -> str:
+    """The kernel and launch shape that ``grouped_matmul`` would use."""
+    return _describe(_lib().fff_describe_grouped_matmul, _product(x, w, offsets, **kw)[0])
 
 
 def grouped_weight_grad_workspace_bytes(n_entries: int, n_groups: int, k: int, n: int) -> int:
     return int(_lib().fff_grouped_weight_grad_workspace_bytes(n_entries, n_groups, k, n))
 
 
-@_on_call
-def grouped_weight_grad(dy, x, offsets, *, dy_index=None, x_index=None, x_div=1, dw=None, accumulate=False,
-                        workspace=None, stream=None):
-    """``dW_g = sum dy_i^T x_i`` over every group's entries, through ``fff_grouped_weight_grad``.
-
-    Returns dw, float32 [n_groups, n, k] (zeros for groups without entries), added to with
-    ``accumulate``.  Entry i reads row ``dy_index[i]`` of dy (i without) and ``x_index[i] // x_div`` of
-    x (i // x_div without).  For a W used transposed, pass x as ``dy`` and dy as ``x``."""
+def _weight_grad(dy, x, offsets, *, dy_index=None, x_index=None, x_div=1, dw=None, accumulate=False,
+                 workspace=None, stream=None):
+    """Checked arguments, result and scratch of a weight gradient."""
     _gpu(dy, "dy")
     device, at = dy.device, dy.get_device()
     _gpu(x, "x", at)
@@ -411,9 +427,30 @@ def grouped_weight_grad(dy, x, offsets, *, dy_index=None, x_index=None, x_div=1,
     if workspace is None:
         need = grouped_weight_grad_workspace_bytes(E, G, K, N)
         workspace = torch.empty(need, dtype=torch.uint8, device=device) if need else None
-    _run(_lib().fff_grouped_weight_grad, FffGroupedWeightGradArgs(
+    args = FffGroupedWeightGradArgs(
         dy.data_ptr(), x.data_ptr(), _index(offsets, "offsets", at, G + 1), _index(dy_index, "dy_index", at, E),
         _index(x_index, "x_index", at, E), _like(dw, "dw", at, (G, N, K), torch.float32), E, dy.shape[0], x.shape[0],
         G, K, N, x_div, _dt(dy, "dy"), _dt(x, "x"), int(bool(accumulate)), *_scratch(workspace, "workspace", at),
-        _raw_stream(device, stream)))
+        _raw_stream(device, stream))
+    return args, dw, workspace
+
+
+@_on_call
+def grouped_weight_grad(dy, x, offsets, *, dy_index=None, x_index=None, x_div=1, dw=None, accumulate=False,
+                        workspace=None, stream=None):
+    """``dW_g = sum dy_i^T x_i`` over every group's entries, through ``fff_grouped_weight_grad``.
+
+    Returns dw, float32 [n_groups, n, k] (zeros for groups without entries), added to with
+    ``accumulate``.  Entry i reads row ``dy_index[i]`` of dy (i without) and ``x_index[i] // x_div`` of
+    x (i // x_div without).  For a W used transposed, pass x as ``dy`` and dy as ``x``."""
+    args, dw, _scratch_held = _weight_grad(dy, x, offsets, dy_index=dy_index, x_index=x_index, x_div=x_div, dw=dw,
+                                           accumulate=accumulate, workspace=workspace, stream=stream)
+    _run(_lib().fff_grouped_weight_grad, args)
     return dw
+
+
+@_on_call
+def describe_grouped_weight_grad(dy, x, offsets, **kw) -> str:
+    """The kernel and launch shape that ``grouped_weight_grad`` would use."""
+    args, _dw, _scratch_held = _weight_grad(dy, x, offsets, **kw)
+    return _describe(_lib().fff_describe_grouped_weight_grad, args)

@@ -229,3 +229,17 @@ def test_plain_and_reference_masks_agree():
     assert torch.equal(a, b[:, :10])
     assert torch.equal(ref.kept([4], 10, 0.3, 7, 9), a[4:])
     assert abs(float(ref.kept(400, 400, 0.3, 7, 9).double().mean()) - 0.7) < 6 * np.sqrt(0.21 / 160000)
+
+
+def test_descriptions_check_what_the_calls_check(lib):
+    buf = ctypes.create_string_buffer(64)
+    for fn, cls, base, bad in (("fff_describe_grouped_matmul", ops.FffGroupedMatmulArgs, PRODUCT, dict(k=0)),
+                               ("fff_describe_grouped_weight_grad", ops.FffGroupedWeightGradArgs, GRAD, dict(dw=P))):
+        call = getattr(lib, fn)
+        assert call(None, buf, len(buf)) == INVALID
+        a = _fill(cls, base, bad)
+        assert call(ctypes.addressof(a), buf, len(buf)) == INVALID
+        a = _fill(cls, base, dict(n_entries=0, accumulate=1) if "dw" in base else dict(n_entries=0))
+        assert call(ctypes.addressof(a), buf, len(buf)) == OK and buf.value == b"none"
+        assert call(ctypes.addressof(a), None, 0) == OK
+    assert lib.fff_last_hip_error() == 0
