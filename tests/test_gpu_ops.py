@@ -866,3 +866,42 @@ def test_activations_far_out(fff_lib, t, E, act):
         y = fff_lib.grouped_matmul(z, one, offsets, act=act, y_dtype=DT[yt])
         assert (y[0::2] == math.inf).all() and torch.isnan(y[1::2]).all()
         assert torch.isnan(fff_lib.grouped_matmul(torch.ones_like(z), one, offsets, act=act, z_in=z)[1::2]).all()
+
+
+def test_two_graphs_of_long_forms_share_no_scratch(fff_lib):
+    """As above at sizes where all three operators need scratch: two graphs replayed at once, eager calls beside them."""
+    E, G = 50000, 300
+    ids = [torch.randint(0, G, (E,), generator=_gen(40 + i), device=DEV).to(torch.int32) for i in range(2)]
+    rows = [(_randn(_gen(50 + i), 3000, 136, dtype="bf16"), _randn(_gen(60 + i), 3000, 256, dtype="bf16")) for i in range(2)]
+    norm = [[_randn(_gen(70 + i), 900, 512, dtype="bf16") for _ in range(2)] for i in range(2)]
+    offsets = torch.tensor([0, 2900, 3000], dtype=torch.int32, device=DEV)
+    stats = torch.zeros(900, device=DEV), torch.ones(900, device=DEV)
+    assert fff_lib.group_rows_workspace_bytes(E, G) > 0
+    assert fff_lib.grouped_weight_grad_workspace_bytes(3000, 2, 256, 136) > 0
+    assert fff_lib.layer_norm_backward_workspace_bytes(900, 512) > 0
+    plan = fff_lib.describe_grouped_weight_grad(*rows[0], offsets)
+    assert "splits=1 " not in plan, plan
+
+    def work(i):
+        return [*fff_lib.group_rows(ids[i], G), fff_lib.grouped_weight_grad(*rows[i], offsets),
+                *fff_lib.layer_norm_backward(*norm[i], *stats)]
+
+    flush_print("[gpu] two graphs of long forms")
+    want = [work(i) for i in range(2)]
+    torch.cuda.synchronize()
+    graphs, outs, streams = [], [], [torch.cuda.Stream() for _ in range(2)]
+    for i in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append(work(i))
+        graphs.append(g)
+    for _ in range(4):
+        torch.cuda.synchronize()
+        for g, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                g.replay()
+        eager = work(0)
+        torch.cuda.synchronize()
+        for i in range(2):
+            assert all(torch.equal(a, b) for a, b in zip(outs[i], want[i]))
+        assert all(torch.equal(a, b) for a, b in zip(eager, want[0]))
