@@ -515,7 +515,9 @@ size_t fff_group_rows_workspace_bytes(int64_t n_entries, int32_t n_ids, int32_t 
  * taken as empty where they fall, z is 0 where x_index is outside x (whatever
  * W holds), and a y_index outside y stores nothing.  x and W are both bf16
  * (MFMA on bf16, fp32 sums) or both fp32; anything else is
- * FFF_ERR_UNSUPPORTED.  Any k and n from 1 to 2^28 - 1.
+ * FFF_ERR_UNSUPPORTED, and so are entries and groups that can make 2^31 or more
+ * tiles (of 32 entries x 128 columns or more, in fp32 also 64 x 64).  Any k and
+ * n from 1 to 2^28 - 1.
  */
 typedef struct {
     const void* x;          /* [x_rows, k] (x_dtype) */

@@ -424,10 +424,14 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void grouped_few_kernel(GroupedPara
     if (dst >= 0) store_elem(p.y, p.y_bf16, dst * p.n + c, z);
 }
 
-hipError_t launch_few(const GroupedParams& p, hipStream_t stream, int* status, char* buf, size_t len) {
-    const int64_t tiles = most_tiles(p.n_entries, p.n_groups, 16) * ((int64_t(p.n) + 15) / 16);
-    *status = tiles > UINT32_MAX / (64 * FEW_WAVES) ? ST_UNSUPPORTED_ : ST_OK_;  // a launch's threads
-    if (*status != ST_OK_) return hipSuccess;
+// Workgroups of the few-entries kernel, and whether a launch holds their threads.
+int64_t few_tiles(const GroupedParams& p) { return most_tiles(p.n_entries, p.n_groups, 16) * ((int64_t(p.n) + 15) / 16); }
+bool few_fits(const GroupedParams& p) {
+    return p.n_entries < FEW_ENTRIES && few_tiles(p) <= UINT32_MAX / (64 * FEW_WAVES);
+}
+
+hipError_t launch_few(const GroupedParams& p, hipStream_t stream, char* buf, size_t len) {
+    const int64_t tiles = few_tiles(p);
     if (buf) {
         std::snprintf(buf, len, "few<%s,%s> grid=%lld block=%d", p.bf16 ? "bf16" : "f32",
                       whole_vectors(p) ? "aligned" : "unaligned", (long long)tiles, 64 * FEW_WAVES);
@@ -466,7 +470,7 @@ int grouped_variant(const GroupedParams& p, int cus) {
     auto row_tiles = [&](int bm) { return std::max(used, E / bm + 0.5 * used); };
     int best = 0;
     double least = 1e300;
-    if (!p.w_transposed && p.n_entries < FEW_ENTRIES) {
+    if (!p.w_transposed && few_fits(p)) {
         // 768 workgroups at once; rows off 16-byte addresses take 2.4 times as long
         const double rounds = row_tiles(16) * ((p.n + 15) / 16) / (3.0 * cus);
         const double kb = double(p.k) * esz / 64, slow = p.k % (16 / esz) ? 2.4 : 1.0;
@@ -496,7 +500,7 @@ hipError_t run_grouped_matmul(const GroupedParams& p, const DeviceInfo& dev, hip
                               size_t len) {
     const int cus = dev.cu_count > 0 ? dev.cu_count : 256;
     switch (grouped_variant(p, cus)) {
-        case 0: return launch_few(p, stream, status, buf, len);
+        case 0: *status = ST_OK_; return launch_few(p, stream, buf, len);
         case 1: return p.bf16 ? launch_grouped<GCfg<true, 1, 1, 1, 4, 3, 128>>(p, cus, stream, status, buf, len)
                               : launch_grouped<GCfg<false, 1, 1, 1, 4, 3, 128>>(p, cus, stream, status, buf, len);
         case 2: return p.bf16 ? launch_grouped<GCfg<true, 1, 2, 2, 2, 3, 128>>(p, cus, stream, status, buf, len)

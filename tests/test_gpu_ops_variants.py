@@ -178,3 +178,20 @@ def test_weight_gradients(fff_lib, kernel, split):
     base = _randn(gen, G, N, K, dtype="f32")
     got = fff_lib.grouped_weight_grad(dy, x, offsets, dw=base.clone(), accumulate=True, **kw)
     ref.check(got, (want + base.to(F8)).cpu(), (err + ref.U * (want.abs() + base.to(F8).abs())).cpu(), "accumulated")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("t,k", [("bf16", 8), ("f32", 4)])
+def test_more_tiles_than_the_few_entries_form_launches(fff_lib, t, k):
+    """2^23 groups of an entry: more workgroups than the few-entries form may launch, so tiles take them."""
+    import ctypes
+
+    from paper_2311_10770_amd import ops
+
+    P, buf = 1 << 40, ctypes.create_string_buffer(256)  # addresses that nothing reads: a description only
+    for n_groups, form in ((1 << 22, "few"), (1 << 23, "tiles")):
+        a = ops.FffGroupedMatmulArgs(x=P, w=2 * P, offsets=3 * P, y=4 * P, n_entries=n_groups, x_rows=n_groups, y_rows=n_groups,
+                                     n_groups=n_groups, k=k, n=16, x_div=1, x_dtype=int(t == "bf16"), w_dtype=int(t == "bf16"))
+        assert ops._lib().fff_describe_grouped_matmul(ctypes.addressof(a), buf, len(buf)) == 0
+        flush_print(f"[gpu] {n_groups} groups {t}: {buf.value.decode()}")
+        assert buf.value.decode().startswith(form + "<")
