@@ -409,23 +409,31 @@ __global__ __launch_bounds__(256) void norm_bwd_cols_kernel(NormBwdParams p, int
 }
 
 // dgamma and dbeta: the partial sums of 32 columns of a workgroup, 32 pieces apart, then over those.
+// A launch holds less than 2^32 threads: columns past its workgroups' are taken in further turns.
+constexpr int64_t SUM_GROUPS = int64_t(1) << 20;
 __global__ __launch_bounds__(1024) void norm_bwd_sum_kernel(NormBwdParams p, int parts) {
     __shared__ float sum[32][33];
     const int H = p.hidden, col = threadIdx.x % 32, lane = threadIdx.x / 32;
-    const int64_t c = int64_t(blockIdx.x) * 32 + col;  // dgamma's columns, then dbeta's
-    float v = 0.0f;
-    if (c < 2 * int64_t(H))
-        for (int q = lane; q < parts; q += 32) v += p.part[int64_t(q) * 2 * H + c];
-    sum[lane][col] = v;
-    __syncthreads();
-    if (lane != 0 || c >= 2 * int64_t(H)) return;
-    v = 0.0f;
+    const int64_t all = 2 * int64_t(H);  // dgamma's columns, then dbeta's
+    for (int64_t c0 = int64_t(blockIdx.x) * 32; c0 < all; c0 += int64_t(gridDim.x) * 32) {
+        const int64_t c = c0 + col;
+        float v = 0.0f;
+        if (c < all)
+            for (int q = lane; q < parts; q += 32) v += p.part[int64_t(q) * 2 * H + c];
+        sum[lane][col] = v;
+        __syncthreads();
+        if (lane == 0 && c < all) {
+            v = 0.0f;
 #pragma unroll
-    for (int l = 0; l < 32; ++l) v += sum[l][col];
-    float* out = c < H ? p.dgamma : p.dbeta;
-    if (!out) return;
-    out += c < H ? c : c - H;
-    *out = p.accumulate ? *out + v : v;
+            for (int l = 0; l < 32; ++l) v += sum[l][col];
+            float* out = c < H ? p.dgamma : p.dbeta;
+            if (out) {
+                out += c < H ? c : c - H;
+                *out = p.accumulate ? *out + v : v;
+            }
+        }
+        __syncthreads();
+    }
 }
 
 // A thread takes DU generator blocks, 256 apart; a workgroup's blocks are consecutive, rows being
@@ -551,11 +559,12 @@ hipError_t run_layer_norm_backward(const NormBwdParams& p, const DeviceInfo& dev
             hipLaunchKernelGGL(norm_bwd_any_kernel, dim3(grid), dim3(256), 0, stream, p);
         }
         if (sums)
-            hipLaunchKernelGGL(norm_bwd_cols_kernel, dim3(unsigned((int64_t(p.hidden) + 255) / 256), unsigned(parts)), dim3(256), 0, stream,
-                               p, parts, (p.n_tokens + parts - 1) / parts);
+            hipLaunchKernelGGL(norm_bwd_cols_kernel, dim3(unsigned((int64_t(p.hidden) + 255) / 256), unsigned(parts)),
+                               dim3(256), 0, stream, p, parts, (p.n_tokens + parts - 1) / parts);
     }
     if (sums)
-        hipLaunchKernelGGL(norm_bwd_sum_kernel, dim3((2 * int64_t(p.hidden) + 31) / 32), dim3(1024), 0, stream, p, parts);
+        hipLaunchKernelGGL(norm_bwd_sum_kernel, dim3(unsigned(std::min<int64_t>(SUM_GROUPS, (2 * int64_t(p.hidden) + 31) / 32))),
+                           dim3(1024), 0, stream, p, parts);
     return hipGetLastError();
 }
 

@@ -22,7 +22,7 @@ struct DropRng {
 };
 
 struct NormParams {
-    const void* x;           // may be null only in the backward
+    const void* x;
     const void* residual;    // or null
     const float* gamma;      // or null
     const float* beta;       // or null

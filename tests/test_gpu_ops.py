@@ -905,3 +905,19 @@ def test_two_graphs_of_long_forms_share_no_scratch(fff_lib):
         for i in range(2):
             assert all(torch.equal(a, b) for a, b in zip(outs[i], want[i]))
         assert all(torch.equal(a, b) for a, b in zip(eager, want[0]))
+
+
+@pytest.mark.parametrize("H", [(1 << 26) + 5, 1 << 24])
+def test_layer_norm_backward_sums_of_very_long_rows(fff_lib, H):
+    """dgamma and dbeta of more columns than one launch has threads for, and of as many as its workgroups take at once."""
+    gen = _gen(H)
+    dy, s = (torch.empty((1, H), dtype=torch.bfloat16, device=DEV).normal_(generator=gen) for _ in range(2))
+    mean, rstd = torch.full((1,), 0.25, device=DEV), torch.full((1,), 2.0, device=DEV)  # (s - mean) rstd: one rounding
+    dgamma, dbeta = torch.full((H,), 1.0, device=DEV), torch.full((H,), 1.0, device=DEV)
+    flush_print(f"[gpu] layer_norm_backward sums of {H} columns")
+    out = fff_lib.layer_norm_backward(dy, s, mean, rstd, want=("dgamma", "dbeta"))
+    want = dy.double() * (s.double() - 0.25) * 2
+    assert torch.equal(out[3], dy[0].float())
+    assert ((out[2].double() - want[0]).abs() <= 2.02 * ref.U * want[0].abs()).all()  # of the difference, of the product
+    fff_lib.layer_norm_backward(dy, s, mean, rstd, dgamma=dgamma, dbeta=dbeta, accumulate=True, want=())
+    assert torch.equal(dgamma, out[2] + 1) and torch.equal(dbeta, out[3] + 1)
