@@ -256,14 +256,15 @@ def layer_norm_backward(dy, s, mean, rstd, gamma=None, *, ds_in=None, p=0.0, see
     ``s``, ``mean`` and ``rstd`` are the forward's, ``p``, ``seed`` and ``offset`` its dropout's.
     ``ds_in`` is the gradient that reaches s past the norm; ``ds`` (of s's type; may be ``ds_in``) is
     the gradient of s and of the residual, ``dx`` (``dx_dtype`` or dy's type) that of x behind the
-    dropout: ds itself where p = 0, unless a dx is passed.  Gradients named in ``want`` are allocated when
-    not given; ``accumulate`` adds to dgamma and dbeta, which must then be given."""
+    dropout: ds itself where p = 0, unless a dx or another ``dx_dtype`` than ds's is passed.
+    Gradients named in ``want`` are allocated when not given; ``accumulate`` adds to dgamma and dbeta,
+    which must then be given."""
     B, H = shape = _rows(dy, "dy")
     device, at, f32 = dy.device, dy.get_device(), torch.float32
     if s is None or mean is None or rstd is None:
         raise ValueError("s, mean and rstd are needed")
     _like(s, "s", at, shape)
-    alias = dx is None and p == 0  # dx is ds
+    alias = dx is None and p == 0 and dx_dtype in (None, s.dtype)  # dx is ds
     if alias and "dx" in want and "ds" not in want:
         want = tuple(want) + ("ds",)
     if accumulate and (("dgamma" in want and dgamma is None) or ("dbeta" in want and dbeta is None)):

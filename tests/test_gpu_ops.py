@@ -921,3 +921,26 @@ def test_layer_norm_backward_sums_of_very_long_rows(fff_lib, H):
     assert ((out[2].double() - want[0]).abs() <= 2.02 * ref.U * want[0].abs()).all()  # of the difference, of the product
     fff_lib.layer_norm_backward(dy, s, mean, rstd, dgamma=dgamma, dbeta=dbeta, accumulate=True, want=())
     assert torch.equal(dgamma, out[2] + 1) and torch.equal(dbeta, out[3] + 1)
+
+
+@pytest.mark.parametrize("p", [0.0, 0.1])
+@pytest.mark.parametrize("H", [96, 20000])
+def test_layer_norm_backward_dx_has_the_type_that_is_asked_for(fff_lib, H, p):
+    """The branch's gradient in the branch's type, with dropout and without; ds itself only where both are one."""
+    gen = _gen(H)
+    for st in ("f32", "bf16"):
+        s, dy, up = _randn(gen, 9, H, dtype=st), _randn(gen, 9, H, dtype="bf16"), _randn(gen, 9, H, dtype=st)
+        mean, rstd = torch.zeros(9, device=DEV), torch.ones(9, device=DEV)
+        kw = {"ds_in": up, "p": p, "seed": SEED, "offset": OFFSET} if p else {"ds_in": up}
+        want, err = ref.layer_norm_backward(dy, s, mean, rstd, None, up, p, SEED, OFFSET)
+        for xt in ("f32", "bf16"):
+            for names in (("ds", "dx"), ("dx",), ("ds", "dx", "dgamma", "dbeta")):
+                flush_print(f"[gpu] layer_norm_backward 9x{H} stream {st} branch {xt} p={p} {names}")
+                got = fff_lib.layer_norm_backward(dy, s, mean, rstd, dx_dtype=DT[xt], want=names, **kw)
+                assert got[1].dtype == DT[xt]
+                ref.check(got[1], want[1], err[1], "dx")
+                if "ds" in names:
+                    assert got[0].dtype == DT[st] and (got[0] is got[1]) == (p == 0 and st == xt)
+                    ref.check(got[0], want[0], err[0], "ds")
+        free = fff_lib.layer_norm_backward(dy, s, mean, rstd, **kw)  # no type asked for
+        assert free[1].dtype == (DT[st] if p == 0 else torch.bfloat16)
