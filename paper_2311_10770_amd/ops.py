@@ -104,6 +104,16 @@ def _lib():
     return _LIB
 
 
+_INT32 = (1 << 31) - 1  # the library's sizes: a larger one would arrive cut to its low 32 bits
+
+
+def _sizes(*named):
+    """Refuses sizes, as (value, name) pairs, that the library's 32 bits do not hold."""
+    for v, what in named:
+        if not -_INT32 - 1 <= v <= _INT32:
+            raise ValueError(f"{what} must fit 32 bits, got {v}")
+
+
 def _gpu(t, what: str, index=None):
     """``t`` as a contiguous GPU tensor (on GPU ``index``)."""
     if not isinstance(t, torch.Tensor):
@@ -192,6 +202,8 @@ def _rows(x, what: str):
     _gpu(x, what)
     if x.dim() != 2:
         raise ValueError(f"{what} must be a 2-D tensor [n_tokens, hidden]")
+    if x.shape[1] > _INT32:
+        raise ValueError(f"{what} has rows of {x.shape[1]}: hidden must fit 32 bits")
     return x.shape
 
 
@@ -244,6 +256,7 @@ def layer_norm(x, gamma=None, beta=None, *, eps=1e-12, residual=None, p=0.0, see
 
 
 def layer_norm_backward_workspace_bytes(n_tokens: int, hidden: int) -> int:
+    _sizes((hidden, "hidden"))
     return int(_lib().fff_layer_norm_backward_workspace_bytes(n_tokens, hidden))
 
 
@@ -308,6 +321,7 @@ def dropout(x, p, seed, offset=0, *, rng_offset=None, residual=None, y=None, y_d
 
 
 def group_rows_workspace_bytes(n_entries: int, n_ids: int, n_trees: int = 1) -> int:
+    _sizes((n_ids, "n_ids"), (n_trees, "n_trees"))
     return int(_lib().fff_group_rows_workspace_bytes(n_entries, n_ids, n_trees))
 
 
@@ -326,6 +340,8 @@ def group_rows(ids, n_ids: int, *, first: int = 0, n_trees: int = 1, order=None,
         raise ValueError("ids must be int32")
     if n_ids < 1 or n_trees < 1:
         raise ValueError("n_ids and n_trees must be positive")
+    if max(n_ids, n_trees, abs(first)) > _INT32:
+        _sizes((n_ids, "n_ids"), (n_trees, "n_trees"), (first, "first"))
     G = n_ids * n_trees
     if order is None:
         order = torch.empty(E, dtype=torch.int32, device=device)
@@ -358,6 +374,8 @@ def _product(x, w, offsets, *, x_index=None, x_div=1, y=None, y_index=None, y_dt
         N, K = K, N
     if x.shape[1] != K:
         raise ValueError(f"x has rows of {x.shape[1]}, w takes {K}")
+    if max(G, K, N, x_div) > _INT32:
+        _sizes((G, "the number of groups"), (K, "k"), (N, "n"), (x_div, "x_div"))
     E = x_index.numel() if x_index is not None else x.shape[0] * x_div
     keep_z = keep_z or z_out is not None
     if keep_z and z_in is not None:
@@ -404,6 +422,7 @@ def describe_grouped_matmul(x, w, offsets, **kw) -> str:
 
 
 def grouped_weight_grad_workspace_bytes(n_entries: int, n_groups: int, k: int, n: int) -> int:
+    _sizes((n_groups, "n_groups"), (k, "k"), (n, "n"))
     return int(_lib().fff_grouped_weight_grad_workspace_bytes(n_entries, n_groups, k, n))
 
 
@@ -420,6 +439,8 @@ def _weight_grad(dy, x, offsets, *, dy_index=None, x_index=None, x_div=1, dw=Non
     if offsets is None or offsets.numel() < 2:
         raise ValueError("offsets must hold n_groups + 1 values")
     N, K, G = dy.shape[1], x.shape[1], offsets.numel() - 1
+    if max(G, K, N, x_div) > _INT32:
+        _sizes((G, "the number of groups"), (K, "k"), (N, "n"), (x_div, "x_div"))
     E = dy_index.numel() if dy_index is not None else dy.shape[0]
     if accumulate and dw is None:
         raise ValueError("accumulate adds to the dw that is given")

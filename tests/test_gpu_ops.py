@@ -944,3 +944,20 @@ def test_layer_norm_backward_dx_has_the_type_that_is_asked_for(fff_lib, H, p):
                     ref.check(got[0], want[0], err[0], "ds")
         free = fff_lib.layer_norm_backward(dy, s, mean, rstd, **kw)  # no type asked for
         assert free[1].dtype == (DT[st] if p == 0 else torch.bfloat16)
+
+
+def test_sizes_past_32_bits_are_refused(fff_lib):
+    """Not handed on as their low 32 bits: the trees, ids and divisors of calls that would be in order, and long rows."""
+    ids = torch.zeros(8, dtype=torch.int32, device=DEV)
+    x, w = torch.ones((4, 8), device=DEV), torch.ones((1, 8, 8), device=DEV)
+    offsets = torch.tensor([0, 4], dtype=torch.int32, device=DEV)
+    wide = torch.empty((1, (1 << 32) + 8), dtype=torch.bfloat16, device=DEV)
+    flush_print("[gpu] sizes past 32 bits")
+    for call in (lambda: fff_lib.group_rows(ids, 4, first=1 << 32), lambda: fff_lib.group_rows(ids, 4, first=-(1 << 32)),
+                 lambda: fff_lib.group_rows(ids, (1 << 32) + 4), lambda: fff_lib.group_rows(ids, 4, n_trees=(1 << 32) + 1),
+                 lambda: fff_lib.grouped_matmul(x, w, offsets, x_index=ids[:4], x_div=(1 << 32) + 1),
+                 lambda: fff_lib.grouped_weight_grad(x, x, offsets, x_index=ids[:4], x_div=(1 << 32) + 1),
+                 lambda: fff_lib.layer_norm(wide), lambda: fff_lib.dropout(wide, 0.1, 1),
+                 lambda: fff_lib.layer_norm_backward(wide, wide, x[0, :1].clone(), x[0, :1].clone())):
+        with pytest.raises(ValueError):
+            call()

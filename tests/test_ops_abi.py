@@ -243,3 +243,15 @@ def test_descriptions_check_what_the_calls_check(lib):
         assert call(ctypes.addressof(a), buf, len(buf)) == OK and buf.value == b"none"
         assert call(ctypes.addressof(a), None, 0) == OK
     assert lib.fff_last_hip_error() == 0
+
+
+@pytest.mark.parametrize("call", [
+    lambda: fff.layer_norm_backward_workspace_bytes(4, (1 << 32) + 8),
+    lambda: fff.group_rows_workspace_bytes(100000, (1 << 32) + 16), lambda: fff.group_rows_workspace_bytes(100000, 16, 1 << 32 | 1),
+    lambda: fff.grouped_weight_grad_workspace_bytes(100000, (1 << 32) + 1, 64, 64),
+    lambda: fff.grouped_weight_grad_workspace_bytes(100000, 1, (1 << 32) + 64, 64),
+    lambda: fff.grouped_weight_grad_workspace_bytes(100000, 1, 64, -(1 << 32) + 64)])
+def test_sizes_past_32_bits_are_refused(lib, call):
+    """ctypes would hand on their low 32 bits."""
+    with pytest.raises(ValueError):
+        call()
