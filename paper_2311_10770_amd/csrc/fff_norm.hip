@@ -216,10 +216,10 @@ __global__ __launch_bounds__(row_threads(LPR)) void norm_bwd_kernel(NormBwdParam
         for (int c = 0; c < NV; ++c) {
             unpack4(g[c], ry[c], p.y_bf16);
             unpack4(xh[c], rs[c], p.s_bf16);
-            // columns behind the row hold dy = 0, so their xh counts nowhere
+            const int left = H - (c * LPR + sl) * 4;  // columns behind the row hold zeros (-mean rstd may overflow)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                xh[c][j] = (xh[c][j] - mean) * rstd;
+                xh[c][j] = FULL || j < left ? (xh[c][j] - mean) * rstd : 0.0f;
                 dg[c][j] = __builtin_fmaf(g[c][j], xh[c][j], dg[c][j]);
                 db[c][j] += g[c][j];
                 g[c][j] *= gain[c][j];

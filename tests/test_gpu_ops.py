@@ -961,3 +961,18 @@ def test_sizes_past_32_bits_are_refused(fff_lib):
                  lambda: fff_lib.layer_norm_backward(wide, wide, x[0, :1].clone(), x[0, :1].clone())):
         with pytest.raises(ValueError):
             call()
+
+
+@pytest.mark.parametrize("H", [1, 30, 100, 250, 768, 1000, 2001, 4099, 12289, 20000])
+def test_layer_norm_backward_of_constant_rows_of_any_size(fff_lib, H):
+    """xh is 0 in them, however large the value times 1 / sqrt(eps) would be: ds = rstd (g - mean(g))."""
+    s = torch.tensor([0.0, 2.0 ** 100, -(2.0 ** 112), 2.0 ** 20], device=DEV)[:, None].repeat(1, H)
+    dy = torch.zeros_like(s)
+    dy[:, 0] = 1.0
+    flush_print(f"[gpu] layer_norm_backward of constant rows, {H}")
+    y, _, mean, rstd = fff_lib.layer_norm(s, eps=2.0 ** -40)
+    assert (y == 0).all() and torch.equal(mean, s[:, 0]) and (rstd == 2.0 ** 20).all()
+    ds, _, dgamma, dbeta = fff_lib.layer_norm_backward(dy, s, mean, rstd)
+    want = 2.0 ** 20 * (dy.double() - dy.double().mean(1, keepdim=True))
+    assert ((ds.double() - want).abs() <= 3 * ref.U * 2.0 ** 20).all()  # of the mean, of the difference, of the product
+    assert (dgamma == 0).all() and torch.equal(dbeta, dy.sum(0))
