@@ -224,14 +224,13 @@ def layer_norm(x, gamma=None, beta=None, *, eps=1e-12, residual=None, p=0.0, see
                s=None, mean=None, rstd=None, y_dtype=None, s_dtype=None, stats=True, stream=None):
     """``s = residual + drop(x)``, then ``y = (s - mean) * rstd * gamma + beta`` per row, through ``fff_layer_norm``.
 
-    Returns (y, s, mean, rstd).  Without a residual and with p = 0, s is x itself.  With ``stats``
-    false, mean and rstd are None unless passed.  ``s`` may be ``residual`` (the stream updated in
-    place).  Types of what is allocated: y as ``y_dtype`` or x; s as ``s_dtype``, residual or x."""
+    Returns (y, s, mean, rstd).  Without a residual and with p = 0, s is x itself, unless an s or another
+    ``s_dtype`` than x's is passed.  With ``stats`` false, mean and rstd are None unless passed.  ``s``
+    may be ``residual`` (the stream updated in place).  Types of what is allocated: y as ``y_dtype`` or x;
+    s as ``s_dtype``, residual or x."""
     B, H = shape = _rows(x, "x")
     device, at = x.device, x.get_device()
-    summed = residual is not None or p > 0
-    if not summed and s is not None:
-        raise ValueError("s is x itself without a residual and dropout")
+    summed = residual is not None or p > 0 or s is not None or s_dtype not in (None, x.dtype)
     if residual is not None and s_dtype is not None and s_dtype != residual.dtype:
         raise ValueError("residual and s share a dtype")
     s_dt = residual.dtype if residual is not None else s.dtype if s is not None else s_dtype or x.dtype

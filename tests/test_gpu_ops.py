@@ -976,3 +976,25 @@ def test_layer_norm_backward_of_constant_rows_of_any_size(fff_lib, H):
     want = 2.0 ** 20 * (dy.double() - dy.double().mean(1, keepdim=True))
     assert ((ds.double() - want).abs() <= 3 * ref.U * 2.0 ** 20).all()  # of the mean, of the difference, of the product
     assert (dgamma == 0).all() and torch.equal(dbeta, dy.sum(0))
+
+
+@pytest.mark.parametrize("H", [100, 768, 20000])
+def test_layer_norm_stream_has_the_type_that_is_asked_for(fff_lib, H):
+    """A stream that starts from a branch in another type, or in a buffer of the caller's, with dropout and without."""
+    gen = _gen(H)
+    x = _randn(gen, 7, H, dtype="bf16", mean=0.5)
+    flush_print(f"[gpu] layer_norm 7x{H}, a stream of its own type")
+    for p in (0.0, 0.3):
+        kw = {"p": p, "seed": SEED, "offset": OFFSET} if p else {}
+        want, err = ref.layer_norm(x, None, None, 1e-5, None, p, SEED, OFFSET)
+        y, s, mean, rstd = fff_lib.layer_norm(x, eps=1e-5, s_dtype=torch.float32, **kw)
+        assert s.dtype == torch.float32
+        for got, w, e, what in zip((y, s, mean, rstd), want, err, ("y", "s", "mean", "rstd")):
+            ref.check(got, w, e, what)
+        for dt in (torch.float32, torch.bfloat16):
+            buf = torch.full((7, H), 9.0, dtype=dt, device=DEV)
+            got = fff_lib.layer_norm(x, eps=1e-5, s=buf, **kw)
+            assert got[1] is buf and torch.equal(buf, s.to(dt)) and torch.equal(got[0], y)
+    assert fff_lib.layer_norm(x, s_dtype=torch.bfloat16)[1] is x and fff_lib.layer_norm(x)[1] is x
+    with pytest.raises(fff_lib.FffError):
+        fff_lib.layer_norm(x, s=x)
