@@ -109,8 +109,11 @@ __device__ __forceinline__ void grouped_epilogue(int kind, const GroupedParams& 
 }
 
 // Workgroups take tiles gridDim.x apart.  BCOL: W is [k, n].  The next tile is looked up while this one
-// is multiplied, and its first step is on its way to LDS (DMA) while this one's results are stored.
-template <class G, bool DMA, bool BCOL>
+// is multiplied, and its first step is on its way to LDS (DMA) while this one's results are stored.  Y: the
+// type of y, bf16 (1) or fp32 (0), where the tile has a kernel for each, else -1: with either's activations beside
+// the other's in one kernel the 256 x 256 tiles' registers spilled further (65536 x 32, 1024 -> 4096 with
+// GELU 815 -> 823 us).
+template <class G, bool DMA, bool BCOL, int Y = -1>
 __global__ __launch_bounds__(G::THREADS, 2) void grouped_kernel(GroupedParams p) {
     extern __shared__ __align__(16) unsigned char glds[];
     __shared__ int32_t s_dst[2][G::BM];   // row of y, or -1
@@ -271,12 +274,13 @@ __global__ __launch_bounds__(G::THREADS, 2) void grouped_kernel(GroupedParams p)
             }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             const int m0 = wm * G::TM * 32 + i * 16;
-            auto rows_out = [&](auto full_cols, auto fine) {
-                grouped_epilogue<COLS, PITCH, full_cols.value, fine.value>(kind, p, blk, m0, rows, t.m0, c0, s_dst[turn],
-                                                                           s_src[turn], bad);
+            auto rows_out = [&](auto fine) {
+                if (full) grouped_epilogue<COLS, PITCH, true, fine.value>(kind, p, blk, m0, rows, t.m0, c0, s_dst[turn], s_src[turn], bad);
+                else grouped_epilogue<COLS, PITCH, false, fine.value>(kind, p, blk, m0, rows, t.m0, c0, s_dst[turn], s_src[turn], bad);
             };
-            if (p.y_bf16) full ? rows_out(std::true_type{}, std::false_type{}) : rows_out(std::false_type{}, std::false_type{});
-            else full ? rows_out(std::true_type{}, std::true_type{}) : rows_out(std::false_type{}, std::true_type{});
+            if constexpr (Y >= 0) rows_out(std::bool_constant<Y == 0>{});
+            else if (p.y_bf16) rows_out(std::false_type{});
+            else rows_out(std::true_type{});
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         }
         if (next.g < 0) return;
@@ -307,8 +311,14 @@ hipError_t launch_grouped(const GroupedParams& p, int cus, hipStream_t stream, i
         return hipSuccess;
     }
     auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(unsigned(grid)), dim3(G::THREADS), lds, stream, p); };
-    if (dma) p.w_transposed ? launch(grouped_kernel<G, true, true>) : launch(grouped_kernel<G, true, false>);
-    else if constexpr (G::BM < 256) p.w_transposed ? launch(grouped_kernel<G, false, true>) : launch(grouped_kernel<G, false, false>);
+    if constexpr (G::BM == 256) {  // not built through registers
+        if (p.w_transposed) p.y_bf16 ? launch(grouped_kernel<G, true, true, 1>) : launch(grouped_kernel<G, true, true, 0>);
+        else p.y_bf16 ? launch(grouped_kernel<G, true, false, 1>) : launch(grouped_kernel<G, true, false, 0>);
+    } else if (dma) {
+        p.w_transposed ? launch(grouped_kernel<G, true, true>) : launch(grouped_kernel<G, true, false>);
+    } else {
+        p.w_transposed ? launch(grouped_kernel<G, false, true>) : launch(grouped_kernel<G, false, false>);
+    }
     return hipGetLastError();
 }
 
