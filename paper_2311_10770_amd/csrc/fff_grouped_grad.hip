@@ -33,7 +33,11 @@ struct GradPlan {
 // they and their splits leave a fifth of the CUs' 512 places empty in their only or second round, where
 // 64 x 64 does better (us, 128 and 64: 5003 fp32 entries, 64 groups of 203 x 300: 39, 30; 8000 x 16 of
 // 768 x 768: 169, 140; where 128 fills them, 16384 x 8 of 1024 x 1024: 444, 511; bf16, 65536 x 1 of
-// 768 x 768: 172, 276).  Splits: up to two workgroups a CU, eight steps of the mean group each at least,
+// 768 x 768: 172, 276).  64 tiles of 256 x 256 are a coarse bound: what they gain goes by the entries a tile
+// sums, too (us, 256 and the smaller: below it 65536 entries in 9 tiles of 768 x 768: 160, 119, in 16 of
+// 1024 x 1024: 164, 192; 16384 in 60 of 1280 x 1024: 65, 72; above it 65536 in 64 of 1024 x 1024: 168, 197, in 72 of
+// 768 x 768: 109, 213; 16384 in 64: 58, 60, in 128: 62, 54; 8192 in 128: 50, 34; 65536 in 64 of one group each,
+// 256 x 256: 37, 31).  Splits: up to two workgroups a CU, eight steps of the mean group each at least,
 // within GRAD_PART_BYTES.  By the sizes alone, so the workspace's size and the result's bits are too.
 GradPlan grad_plan(int64_t n_entries, int32_t n_groups, int32_t k, int32_t n, bool bf16) {
     auto cdiv = [](int64_t a, int64_t b) { return (a + b - 1) / b; };

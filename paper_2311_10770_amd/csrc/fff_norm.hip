@@ -98,7 +98,7 @@ __global__ __launch_bounds__(row_threads(LPR)) void norm_kernel(NormParams p) {
     constexpr int NT = row_threads(LPR), RPB = NT / LPR;
     __shared__ float red[2][2 * (LPR / 64 + 1)];
     const int sl = threadIdx.x % LPR, H = p.hidden;
-    const float width = float(H);  // divided by, not multiplied by its inverse: the mean of a constant row is exact
+    const float width = float(H);  // divided by: its inverse would be another rounding of every mean
     const uint64_t off = DROP ? rng_offset(p.drop) : 0;
     for (int64_t r0 = int64_t(blockIdx.x) * RPB; r0 < p.n_tokens; r0 += int64_t(gridDim.x) * RPB) {
         const int64_t row = r0 + threadIdx.x / LPR;
@@ -179,7 +179,7 @@ __global__ __launch_bounds__(row_threads(LPR)) void norm_bwd_kernel(NormBwdParam
     __shared__ float red[2][2 * (LPR / 64 + 1)];
     __shared__ float cols[RPB > 1 ? 2 * W : 1];
     const int sl = threadIdx.x % LPR, H = p.hidden;
-    const float width = float(H);  // divided by, not multiplied by its inverse: the mean of a constant row is exact
+    const float width = float(H);  // divided by: its inverse would be another rounding of every mean
     const uint64_t off = DROP ? rng_offset(p.drop) : 0;
     const bool sums = p.dgamma || p.dbeta, rows_out = p.ds || p.dx;
     float gain[NV][4], dg[NV][4] = {}, db[NV][4] = {};
@@ -301,7 +301,8 @@ __device__ __forceinline__ float block_sum(float v, float* red) {
     return (red[0] + red[1]) + (red[2] + red[3]);
 }
 
-// Rows of any length: a workgroup per row, the row read again in every pass.
+// Rows of any length: a workgroup per row, the row read again in every pass, an element a load (4096 rows of 20000
+// bf16 with residual: 821 us, 0.8 TB/s of what has to move; 16384 columns in registers: 126 us, 4.3 TB/s).
 __global__ __launch_bounds__(256) void norm_any_kernel(NormParams p) {
     __shared__ float red[4];
     const uint64_t off = p.drop.on ? rng_offset(p.drop) : 0;
