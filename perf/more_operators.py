@@ -1,0 +1,524 @@
+"""Timed cases of a routed expert block's operators: the routing of tokens to experts, the sum of their
+experts' rows, RMS norm with the residual's addition, and activations kept in 8 bits for the backward pass.
+
+A case is a dict of plain values; "op" names the operator and the other keys its sizes and types:
+
+  route      "direction" forward or backward; tokens, experts, k (experts of a token); score: softmax or
+             sigmoid; "bias": a balancing bias is added to the scores for the choice; groups, top_groups:
+             experts come from a token's best groups only; group_score: top2 (sum of a group's two best) or
+             max; renormalise; x: type of the logits; "padded": tokens of every 16 that are padding (all logits
+             -inf) and get no expert
+  combine    "direction"; tokens, k, hidden; rows, y: types of the experts' rows and of the stream;
+             "residual"; "weighted": the rows are weighted, else added as they are; "dropped": entries of
+             every 16 without an expert, whose rows hold nothing
+  rms_norm   "direction"; tokens, hidden; x, s, y: types of the branch, of the residual stream and of the
+             normalised rows; "residual": the branch is added to a stream first; "packed": the normalised rows are
+             kept in 8 bits too, and read back
+  checkpoint "direction" forward: rows are packed to 8 bits and read back; backward: the gradient through an
+             activation whose input was kept in 8 bits, and the activation itself ("keep": wanted too);
+             tokens, hidden; x: type of the rows; act
+
+Eight bits are e4m3 values with a power of two for every 32 columns of a row.  `own` chooses between the plain
+forms below and the framework's calls.
+"""
+from __future__ import annotations
+
+import math
+
+import torch
+
+own = False
+
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+BYTES = {"f32": 4, "bf16": 2}
+EPS = 1e-6
+SCALE = 2.5  # the routing weights' factor
+BLOCK = 32   # columns that share a scale
+
+
+def _route(direction, tokens, experts, k, score, bias, groups, top_groups, group_score, renormalise, x, padded):
+    return {"op": "route", "direction": direction, "tokens": tokens, "experts": experts, "k": k, "score": score,
+            "bias": bias, "groups": groups, "top_groups": top_groups, "group_score": group_score,
+            "renormalise": renormalise, "x": x, "padded": padded}
+
+
+def _combine(direction, tokens, k, hidden, rows, y, residual, weighted, dropped):
+    return {"op": "combine", "direction": direction, "tokens": tokens, "k": k, "hidden": hidden, "rows": rows, "y": y,
+            "residual": residual, "weighted": weighted, "dropped": dropped}
+
+
+def _rms(direction, tokens, hidden, x, s, y, residual, packed):
+    return {"op": "rms_norm", "direction": direction, "tokens": tokens, "hidden": hidden, "x": x, "s": s, "y": y,
+            "residual": residual, "packed": packed}
+
+
+def _checkpoint(direction, tokens, hidden, x, act, keep):
+    return {"op": "checkpoint", "direction": direction, "tokens": tokens, "hidden": hidden, "x": x, "act": act,
+            "keep": keep}
+
+
+def listed():
+    cases = {
+        # one token over 64 experts: a serving step, latency alone
+        "route_token_64": _route("forward", 1, 64, 2, "softmax", False, 1, 1, "max", True, "f32", 0),
+        # the throughput batch over 256 experts in 8 groups, balanced by a bias, some tokens padding
+        "route_65536x256_groups": _route("forward", 65536, 256, 8, "sigmoid", True, 8, 4, "top2", True, "f32", 1),
+        # gradient of plain softmax routing over 64 experts, logits as a bf16 product leaves them
+        "route_backward_65536x64_bf16": _route("backward", 65536, 64, 4, "softmax", False, 1, 1, "max", False, "bf16",
+                                               0),
+        # decoding eight tokens of LLM width with eight experts each, onto the stream
+        "combine_decode_8x8x4096": _combine("forward", 8, 8, 4096, "bf16", "bf16", True, True, 0),
+        # the end of a training block: eight rows a token, some entries without an expert, an fp32 stream
+        "combine_16384x8x1024": _combine("forward", 16384, 8, 1024, "bf16", "f32", True, True, 1),
+        # gradients of rows and weights at an odd width
+        "combine_backward_16384x4x1001": _combine("backward", 16384, 4, 1001, "bf16", "bf16", False, True, 1),
+        # one token before a block of LLM width: latency alone
+        "rms_token_4096": _rms("forward", 1, 4096, "bf16", "bf16", "bf16", True, False),
+        # between two blocks of a training step: the stream's sum, the normalised rows, and their 8-bit copy that
+        # the backward pass reads back for the weight gradients
+        "rms_packed_65536x1024_mixed": _rms("forward", 65536, 1024, "bf16", "f32", "bf16", True, True),
+        # the same step's gradients at the base width
+        "rms_backward_65536x768": _rms("backward", 65536, 768, "bf16", "bf16", "bf16", True, False),
+        # a small ragged batch of an odd width, single precision
+        "checkpoint_333x101_f32": _checkpoint("forward", 333, 101, "f32", "identity", False),
+        # pre-activations of the experts' first product, kept in 8 bits, and the activation formed from them again
+        "checkpoint_65536x4096_gelu": _checkpoint("forward", 65536, 4096, "bf16", "gelu", False),
+        # the backward pass through that activation: its gradient and, for the second product's weights, itself
+        "checkpoint_backward_65536x4096_gelu": _checkpoint("backward", 65536, 4096, "bf16", "gelu", True),
+    }
+    return [dict(name=n, **c) for n, c in cases.items()]
+
+
+def _log_int(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def _width(rng, lo, hi):
+    """A width of lo..hi: as often a multiple of 64 or of 8 as any number."""
+    w = _log_int(rng, lo, hi)
+    step = rng.choice((1, 8, 64, 64))
+    return max(step, w // step * step)
+
+
+def draw(rng):
+    op = rng.choice(("route", "route", "combine", "rms_norm", "checkpoint"))
+    direction = rng.choice(("forward", "forward", "backward"))
+    types = ("f32", "bf16")
+    if op == "route":
+        score, groups, top_groups = rng.choice(("softmax", "sigmoid")), 1, 1
+        if rng.random() < 0.4:
+            groups, size = rng.choice((2, 4, 5, 8, 16)), _log_int(rng, 2, 32)
+            top_groups, experts = rng.randint(1, groups), groups * size
+            k = rng.randint(1, min(16, top_groups * size))
+        else:
+            experts = rng.choice((8, 64, 128, 256, _log_int(rng, 2, 512)))
+            k = min(experts, _log_int(rng, 1, 16))
+        tokens = _log_int(rng, 1, 65536 * 256 // max(256, experts))
+        return _route(direction, tokens, experts, k, score, rng.random() < 0.5, groups, top_groups,
+                      rng.choice(("max", "top2")), rng.random() < 0.6, rng.choice(types), rng.choice((0, 0, 1, 4)))
+    if op == "combine":
+        hidden, k = _width(rng, 16, 8192), _log_int(rng, 1, 16)
+        tokens = _log_int(rng, 1, min(65536, 16384 * 8 * 512 // (hidden * k)))
+        return _combine(direction, tokens, k, hidden, rng.choice(types), rng.choice(types), rng.random() < 0.6,
+                        rng.random() < 0.8, rng.choice((0, 0, 1, 4)))
+    hidden = _width(rng, 16, 8192)
+    if op == "rms_norm":
+        tokens = _log_int(rng, 1, min(65536, 65536 * 512 // hidden))
+        residual, s = rng.random() < 0.7, rng.choice(types)
+        return _rms(direction, tokens, hidden, rng.choice(types) if residual else s, s, rng.choice(types), residual,
+                    direction == "forward" and rng.random() < 0.5)
+    tokens = _log_int(rng, 1, min(65536, 65536 * 2048 // hidden))
+    act = rng.choice(("identity", "gelu", "gelu_tanh")) if direction == "forward" else rng.choice(("gelu", "gelu_tanh"))
+    return _checkpoint(direction, tokens, hidden, rng.choice(types), act, direction == "backward" and rng.random() < 0.6)
+
+
+# ------------------------------------------------------------------------------------------ inputs
+
+
+def _stream(randn, gen, tokens, hidden, dtype):
+    """Rows of a residual stream: a few channels are large and a mean is left, as in trained models."""
+    scale = torch.exp(0.5 * torch.randn(hidden, generator=gen, device="cuda"))
+    return (randn(tokens, hidden) * scale + 0.3).to(dtype)
+
+
+def _some(gen, n, sixteenths):
+    """Which of n entries, `sixteenths` of 16 on average."""
+    return torch.rand(n, generator=gen, device="cuda") < sixteenths / 16
+
+
+def prepare(case, seed):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+
+    def randn(*shape, dtype=torch.float32, scale=1.0):
+        return (torch.randn(shape, generator=gen, device="cuda") * scale).to(dtype)
+
+    st, op = {"case": case}, case["op"]
+    back = case["direction"] == "backward"
+    if op == "route":
+        T, E, k = case["tokens"], case["experts"], case["k"]
+        # some experts are likelier than others, as in training
+        st["logits"] = (randn(T, E) + 0.5 * randn(E)).to(DT[case["x"]])
+        st["logits"][_some(gen, T, case["padded"])] = -math.inf
+        st["bias"] = randn(E, scale=0.05) if case["bias"] else None
+        if back:
+            # some k experts of every token, in any order; none for padding
+            ids = torch.rand((T, E), generator=gen, device="cuda").argsort(1)[:, :k].to(torch.int32)
+            st["ids"] = ids.masked_fill(torch.isinf(st["logits"][:, :1]), -1).contiguous()
+            st["dweights"] = randn(T, k)
+    elif op == "combine":
+        T, k, H = case["tokens"], case["k"], case["hidden"]
+        none = _some(gen, T * k, case["dropped"]).view(T, k)
+        st["rows"] = randn(T * k, H, dtype=DT[case["rows"]])
+        st["rows"][none.flatten()] = math.nan  # whatever the memory held
+        st["ids"] = torch.randint(64, (T, k), generator=gen, device="cuda", dtype=torch.int32).masked_fill(none, -1)
+        st["ids"] = st["ids"] if case["dropped"] else None
+        w = torch.exp(randn(T, k)).masked_fill(none, 0.0)
+        st["weights"] = SCALE * w / (w.sum(1, keepdim=True) + 1e-9) if case["weighted"] else None
+        if back:
+            st["dy"] = randn(T, H, dtype=DT[case["y"]])
+        else:
+            st["residual"] = _stream(randn, gen, T, H, DT[case["y"]]) if case["residual"] else None
+    elif op == "rms_norm":
+        B, H, s = case["tokens"], case["hidden"], DT[case["s"]]
+        st["gamma"] = 1 + 0.2 * randn(H)
+        if back:
+            st["s"] = _stream(randn, gen, B, H, s)
+            st["rstd"] = 1 / torch.sqrt(st["s"].float().square().mean(1) + EPS)
+            st["dy"] = randn(B, H, dtype=DT[case["y"]])
+            st["ds_in"] = randn(B, H, dtype=s) if case["residual"] else None
+        else:
+            st["x"] = randn(B, H, dtype=DT[case["x"]]) if case["residual"] else _stream(randn, gen, B, H, s)
+            st["residual"] = _stream(randn, gen, B, H, s) if case["residual"] else None
+    else:
+        B, H, t = case["tokens"], case["hidden"], DT[case["x"]]
+        # pre-activations: rows of different sizes
+        z = randn(B, H) * torch.exp(0.3 * randn(B, 1))
+        if back:
+            values, scales = _packed(z)
+            st["values"] = values.to(torch.float8_e4m3fn)
+            st["scales"] = (scales + 127).to(torch.uint8).view(torch.float8_e8m0fnu)
+            st["dy"] = randn(B, H, dtype=t)
+        else:
+            st["x"] = z.to(t)
+    return st
+
+
+# -------------------------------------------------------------------------------------- plain forms
+
+
+def _blocks(x):
+    """[rows, blocks, BLOCK] of x, zeros behind a row."""
+    B, H = x.shape
+    n = -(-H // BLOCK)
+    out = x.new_zeros((B, n * BLOCK))
+    out[:, :H] = x
+    return out.view(B, n, BLOCK)
+
+
+def _packed(x):
+    """The e4m3 values (as fp32) of x's rows and the exponents of their blocks' scales."""
+    blocks = _blocks(x)
+    most = blocks.abs().amax(2)
+    part, power = torch.frexp(most)  # most = part 2^power, part in [0.5, 1): at most 448 = 0.875 2^9 behind the scale
+    power = torch.where(part > 0.875, power - 8, power - 9).clamp(min=-127)
+    v = torch.ldexp(blocks, -power[:, :, None])
+    step = torch.ldexp(torch.ones_like(v), torch.frexp(v)[1].clamp(min=-5) - 4)  # three bits behind the first
+    return (torch.round(v / step) * step).flatten(1)[:, :x.shape[1]], power
+
+
+def _unpacked(values, power):
+    return torch.ldexp(_blocks(values), power[:, :, None]).flatten(1)[:, :values.shape[1]]
+
+
+_ROOT_HALF = math.sqrt(0.5)
+_ROOT_2_PI = math.sqrt(2 / math.pi)
+
+
+def _act(z, act):
+    if act == "gelu":
+        return 0.5 * z * torch.erfc(-z * _ROOT_HALF)
+    if act == "gelu_tanh":
+        return z / (1 + torch.exp(-2 * _ROOT_2_PI * (z + 0.044715 * z * z * z)))
+    return z
+
+
+def _act_grad(z, act):
+    if act == "gelu":
+        return 0.5 * torch.erfc(-z * _ROOT_HALF) + z * torch.exp(-0.5 * z * z) * (0.5 * _ROOT_2_PI)
+    u = _ROOT_2_PI * (z + 0.044715 * z * z * z)
+    up, down = 1 / (1 + torch.exp(-2 * u)), 1 / (1 + torch.exp(2 * u))
+    return up + 2 * z * up * down * _ROOT_2_PI * (1 + 0.134145 * z * z)
+
+
+def _scores(logits, score):
+    """Scores in 64 bits (the choice needs them), 0 for masked experts, and which are not masked."""
+    l = logits.double()
+    there = l > -math.inf
+    if score == "sigmoid":
+        return torch.where(there, 1 / (1 + torch.exp(-l)), 0.0), there
+    most = torch.where(there, l, -math.inf).amax(1, keepdim=True).clamp(min=-1e300)
+    e = torch.where(there, torch.exp(l - most), 0.0)
+    return e / e.sum(1, keepdim=True).clamp(min=1e-300), there
+
+
+def _plain_route(st):
+    c, k = st["case"], st["case"]["k"]
+    s, there = _scores(st["logits"], c["score"])
+    T, E = s.shape
+    if c["direction"] == "backward":
+        there = st["ids"] >= 0
+        at = st["ids"].clamp(min=0).long()
+        dw = torch.where(there, SCALE * st["dweights"].double(), 0.0)
+        picked = torch.where(there, s.gather(1, at), 0.0)
+        if c["renormalise"]:
+            total = picked.sum(1, keepdim=True).clamp(min=1e-300)
+            dw = (dw - (dw * picked).sum(1, keepdim=True) / total) / total
+        ds = torch.zeros_like(s).scatter_add_(1, at, torch.where(there, dw, 0.0))
+        if c["score"] == "sigmoid":
+            return [(ds * s * (1 - s)).to(DT[c["x"]])]
+        return [(s * (ds - (ds * s).sum(1, keepdim=True))).to(DT[c["x"]])]
+    choice = s + st["bias"].double() if c["bias"] else st["logits"].double()
+    choice = torch.where(there, choice, -math.inf)
+    if c["groups"] > 1:
+        G, size = c["groups"], E // c["groups"]
+        by = choice if c["group_score"] == "max" or c["bias"] else torch.where(there, s, -math.inf)
+        best = by.view(T, G, size).sort(dim=2, descending=True).values[:, :, :1 if c["group_score"] == "max" else 2]
+        value = torch.where(best[:, :, 0] > -math.inf, torch.where(best > -math.inf, best, 0.0).sum(2), -math.inf)
+        order = value.sort(dim=1, descending=True, stable=True).indices[:, :c["top_groups"]]
+        kept = torch.zeros((T, G), dtype=torch.bool, device=s.device).scatter_(1, order, True)
+        choice = torch.where(kept[:, :, None], choice.view(T, G, size), -math.inf).view(T, E)
+    value, at = choice.sort(dim=1, descending=True, stable=True)
+    value, at = value[:, :k], at[:, :k]
+    got = value > -math.inf
+    w = torch.where(got, s.gather(1, at), 0.0)
+    if c["renormalise"]:
+        w = w / w.sum(1, keepdim=True).clamp(min=1e-300)
+    return [torch.where(got, at, -1).to(torch.int32), (SCALE * w).float()]
+
+
+def _plain(st):
+    c = st["case"]
+    op, back = c["op"], c["direction"] == "backward"
+    if op == "route":
+        return _plain_route(st)
+    if op == "combine":
+        T, k, H = c["tokens"], c["k"], c["hidden"]
+        rows = st["rows"].float().view(T, k, H)
+        w = st["weights"] if c["weighted"] else torch.ones((T, k), device=rows.device)
+        if c["dropped"]:
+            rows = torch.where((st["ids"] >= 0)[:, :, None], rows, 0.0)
+            w = torch.where(st["ids"] >= 0, w, 0.0)
+        if back:
+            dy = st["dy"].float()[:, None, :]
+            drows = (w[:, :, None] * dy).view(T * k, H).to(DT[c["rows"]])
+            return [drows, (dy * rows).sum(2)] if c["weighted"] else [drows]
+        y = (w[:, :, None] * rows).sum(1)
+        return [(y + st["residual"].float() if c["residual"] else y).to(DT[c["y"]])]
+    if op == "rms_norm" and not back:
+        s = st["x"].float()
+        if c["residual"]:
+            s = s + st["residual"].float()
+        rstd = 1 / torch.sqrt(s.square().mean(1) + EPS)
+        y = s * rstd[:, None] * st["gamma"]
+        out = [y.to(DT[c["y"]]), rstd] + ([s.to(DT[c["s"]])] if c["residual"] else [])
+        return out + [_unpacked(*_packed(y)).to(torch.bfloat16)] if c["packed"] else out
+    if op == "rms_norm":
+        rstd = st["rstd"][:, None]
+        xh = st["s"].float() * rstd
+        dy = st["dy"].float()
+        g = dy * st["gamma"]
+        ds = rstd * (g - xh * (g * xh).mean(1, keepdim=True))
+        if c["residual"]:
+            ds = ds + st["ds_in"].float()
+        out = [ds.to(DT[c["s"]]), (dy * xh).sum(0)]
+        return out + [ds.to(DT[c["x"]])] if c["x"] != c["s"] else out
+    if back:
+        z = _unpacked(st["values"].float(), st["scales"].view(torch.uint8).int() - 127)
+        dz = (st["dy"].float() * _act_grad(z, c["act"])).to(DT[c["x"]])
+        return [dz, _act(z, c["act"]).to(DT[c["x"]])] if c["keep"] else [dz]
+    return [_act(_unpacked(*_packed(st["x"].float())), c["act"]).to(DT[c["x"]])]
+
+
+# ------------------------------------------------------------------------------ the framework's calls
+
+
+def _framework(st):
+    import paper_2311_10770_amd as fff
+
+    c = st["case"]
+    op, back = c["op"], c["direction"] == "backward"
+    if op == "route" and back:
+        return [fff.route_backward(st["dweights"], st["logits"], st["ids"], score=c["score"],
+                                   renormalise=c["renormalise"], scale=SCALE)]
+    if op == "route":
+        return list(fff.route(st["logits"], c["k"], bias=st["bias"], score=c["score"], n_groups=c["groups"],
+                              top_groups=c["top_groups"], group_score=c["group_score"],
+                              renormalise=c["renormalise"], scale=SCALE))
+    if op == "combine" and back:
+        drows, dweights = fff.combine_backward(st["dy"], c["k"], st["rows"] if c["weighted"] else None, st["weights"],
+                                               ids=st["ids"], drows_dtype=DT[c["rows"]])
+        return [drows, dweights] if c["weighted"] else [drows]
+    if op == "combine":
+        return [fff.combine(st["rows"], c["k"], st["weights"], ids=st["ids"], residual=st["residual"],
+                            y_dtype=DT[c["y"]])]
+    if op == "rms_norm" and back:
+        ds, dx, dgamma = fff.rms_norm_backward(st["dy"], st["s"], st["rstd"], st["gamma"], ds_in=st["ds_in"],
+                                               dx_dtype=DT[c["x"]])
+        return [ds, dgamma, dx] if c["x"] != c["s"] else [ds, dgamma]
+    if op == "rms_norm":
+        y, s, rstd, packed = fff.rms_norm(st["x"], st["gamma"], eps=EPS, residual=st["residual"], y_dtype=DT[c["y"]],
+                                          pack=c["packed"])
+        out = [y, rstd, s] if c["residual"] else [y, rstd]
+        return out + [fff.unpack_rows(packed)] if c["packed"] else out
+    if back:
+        packed = fff.Packed(st["values"], st["scales"])
+        got = fff.activation_backward(st["dy"], packed, c["act"], keep_y=c["keep"], y_dtype=DT[c["x"]])
+        return list(got) if c["keep"] else [got]
+    return [fff.unpack_rows(fff.pack_rows(st["x"]), act=c["act"], dtype=DT[c["x"]])]
+
+
+def run(state):
+    return _framework(state) if own else _plain(state)
+
+
+# ------------------------------------------------------------------------------------------ the bill
+
+
+def work(case):
+    op, back = case["op"], case["direction"] == "backward"
+    if op == "route":
+        T, E, k, b = case["tokens"], case["experts"], case["k"], BYTES[case["x"]]
+        if back:
+            return {"bytes": 2 * T * E * b + 8 * T * k, "flops": 8 * T * E}
+        return {"bytes": T * E * b + 8 * T * k + (4 * E if case["bias"] else 0), "flops": 8 * T * E}
+    if op == "combine":
+        T, k, H, r, y = case["tokens"], case["k"], case["hidden"], BYTES[case["rows"]], BYTES[case["y"]]
+        live = T * k * (16 - case["dropped"]) // 16
+        lists = T * k * ((4 if case["weighted"] else 0) + (4 if case["dropped"] else 0))
+        if back:
+            more = live * H * r + 4 * T * k if case["weighted"] else 0
+            return {"bytes": T * k * H * r + T * H * y + lists + more, "flops": 3 * T * k * H}
+        return {"bytes": live * H * r + T * H * y * (2 if case["residual"] else 1) + lists, "flops": 2 * T * k * H}
+    B, H = case["tokens"], case["hidden"]
+    if op == "rms_norm":
+        x, s, y = BYTES[case["x"]], BYTES[case["s"]], BYTES[case["y"]]
+        if back:
+            a = y + 2 * s + (s if case["residual"] else 0) + (x if case["x"] != case["s"] else 0)
+            return {"bytes": B * H * a + 4 * B + 8 * H, "flops": 12 * B * H}
+        a = x + y + (2 * s if case["residual"] else 0) + (2 if case["packed"] else 0)
+        return {"bytes": B * H * a + 4 * B + 4 * H, "flops": 6 * B * H}
+    t = BYTES[case["x"]]
+    if back:
+        return {"bytes": B * (H * (2 * t + 1 + (t if case["keep"] else 0)) + -(-H // BLOCK)), "flops": 40 * B * H}
+    return {"bytes": 2 * B * H * t, "flops": (4 if case["act"] == "identity" else 30) * B * H}
+
+
+# --------------------------------------------------------------------------- the definitions in 64 bits
+
+# the finite values of e4m3 that are not negative, in order: their codes are their places
+_E4M3 = [m / 8 * 2.0 ** -6 for m in range(8)]
+_E4M3 += [(1 + m / 8) * 2.0 ** (e - 7) for e in range(1, 16) for m in range(8)][:119]
+
+
+def _eight_bits(x):
+    """x (64 bits) as it comes back from e4m3 blocks: the nearest of the format's values, even codes at ties."""
+    B, H = x.shape
+    table = torch.tensor(_E4M3, dtype=x.dtype, device=x.device)
+    between = (table[1:] + table[:-1]) / 2
+    out = torch.empty_like(x)
+    for c in range(0, H, BLOCK):
+        part = x[:, c:c + BLOCK]
+        most = part.abs().amax(1, keepdim=True)
+        scale = torch.exp2(torch.ceil(torch.log2(most / 448)).clamp(min=-127))
+        # the logarithm may be a step off at the borders
+        less = (2 * most <= 448 * scale) & (scale > 2.0 ** -127)
+        scale = torch.where(most > 448 * scale, 2 * scale, torch.where(less, scale / 2, scale))
+        v = part.abs() / scale
+        low, high = torch.searchsorted(between, v), torch.searchsorted(between, v, right=True)  # differ at ties
+        out[:, c:c + BLOCK] = torch.copysign(table[torch.where(low % 2 == 0, low, high)] * scale, part)
+    return out
+
+
+def _exact_act(z, act, back):
+    v = z.clone().requires_grad_(back)
+    if act == "gelu":
+        a = v * 0.5 * torch.special.erfc(-v * 0.5 ** 0.5)
+    elif act == "gelu_tanh":
+        a = v * torch.sigmoid(2 * math.sqrt(2 / math.pi) * (v + 0.044715 * v ** 3))
+    else:
+        a = v * 1
+    return (a.detach(), torch.autograd.grad(a.sum(), v)[0]) if back else a
+
+
+def _exact_route(st):
+    c = st["case"]
+    l = st["logits"].to(torch.float64)
+    T, E = l.shape
+    if c["direction"] == "forward":
+        # the chosen experts are whole numbers: the plain form's, each weight anew from its logit
+        ids = _plain_route(st)[0]
+    else:
+        ids = st["ids"]
+    l.requires_grad_(True)
+    live = ids >= 0
+    some = live.any(1)
+    chosen = torch.gather(l, 1, ids.clamp(min=0).long())
+    if c["score"] == "softmax" and c["renormalise"]:
+        w = torch.softmax(chosen.masked_fill(~live, -math.inf)[some], 1)
+    elif c["score"] == "softmax":
+        w = torch.exp(chosen - torch.logsumexp(l, 1, keepdim=True))[some].masked_fill(~live[some], 0.0)
+    else:
+        w = torch.sigmoid(chosen).masked_fill(~live, 0.0)[some]
+        w = w / w.sum(1, keepdim=True) if c["renormalise"] else w
+    w = SCALE * w
+    if c["direction"] == "forward":
+        weights = torch.zeros(ids.shape, dtype=torch.float64, device=l.device)
+        weights[some] = w.detach()
+        return [None, weights]
+    grad, = torch.autograd.grad((w * st["dweights"].to(torch.float64)[some]).sum(), l)
+    return [torch.where(some[:, None], grad, 0.0)]
+
+
+def exact(case, seed):
+    st = prepare(case, seed)
+    f8 = torch.float64
+    op, back = case["op"], case["direction"] == "backward"
+    if op == "route":
+        return _exact_route(st)
+    if op == "combine":
+        T, k, H = case["tokens"], case["k"], case["hidden"]
+        live = (st["ids"] >= 0 if case["dropped"] else torch.ones((T, k), dtype=torch.bool, device="cuda")).to(f8)
+        w = st["weights"].to(f8) * live if case["weighted"] else live
+        total = torch.zeros((T, H), dtype=f8, device="cuda")
+        drows = torch.empty((T, k, H), dtype=f8, device="cuda") if back else None
+        dweights = torch.empty((T, k), dtype=f8, device="cuda")
+        for j in range(k):
+            row = torch.nan_to_num(st["rows"].view(T, k, H)[:, j].to(f8), nan=0.0)
+            if back:
+                drows[:, j] = w[:, j:j + 1] * st["dy"].to(f8)
+                dweights[:, j] = torch.linalg.vecdot(row, st["dy"].to(f8)) * live[:, j]
+            else:
+                total += w[:, j:j + 1] * row
+        if back:
+            return [drows.view(T * k, H), dweights] if case["weighted"] else [drows.view(T * k, H)]
+        return [total + st["residual"].to(f8) if case["residual"] else total]
+    if op == "rms_norm" and not back:
+        s = st["x"].to(f8)
+        s = s + st["residual"].to(f8) if case["residual"] else s
+        rstd = (torch.linalg.vecdot(s, s) / case["hidden"] + EPS) ** -0.5
+        y = s * (rstd[:, None] * st["gamma"].to(f8))
+        out = [y, rstd, s] if case["residual"] else [y, rstd]
+        return out + [_eight_bits(y)] if case["packed"] else out
+    if op == "rms_norm":
+        # the gradient as the projection that the norm's derivative is
+        s, rstd, dy = st["s"].to(f8), st["rstd"].to(f8)[:, None], st["dy"].to(f8)
+        g = dy * st["gamma"].to(f8) * rstd
+        ds = g - s * (torch.linalg.vecdot(g, s)[:, None] * rstd ** 2 / case["hidden"])
+        ds = ds + st["ds_in"].to(f8) if case["residual"] else ds
+        out = [ds, torch.linalg.vecdot(dy, s * rstd, dim=0)]
+        return out + [ds] if case["x"] != case["s"] else out
+    if not back:
+        return [_exact_act(_eight_bits(st["x"].to(f8)), case["act"], False)]
+    spread = st["scales"].to(torch.float32).to(f8).repeat_interleave(BLOCK, 1)[:, :case["hidden"]]
+    a, slope = _exact_act(st["values"].to(torch.float32).to(f8) * spread, case["act"], True)
+    return [slope * st["dy"].to(f8), a] if case["keep"] else [slope * st["dy"].to(f8)]
