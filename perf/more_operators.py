@@ -114,8 +114,10 @@ def draw(rng):
             experts = rng.choice((8, 64, 128, 256, _log_int(rng, 2, 512)))
             k = min(experts, _log_int(rng, 1, 16))
         tokens = _log_int(rng, 1, 65536 * 256 // max(256, experts))
+        # one renormalised weight is a constant: no gradient to take
+        renormalise = rng.random() < 0.6 and (direction == "forward" or k > 1)
         return _route(direction, tokens, experts, k, score, rng.random() < 0.5, groups, top_groups,
-                      rng.choice(("max", "top2")), rng.random() < 0.6, rng.choice(types), rng.choice((0, 0, 1, 4)))
+                      rng.choice(("max", "top2")), renormalise, rng.choice(types), rng.choice((0, 0, 1, 4)))
     if op == "combine":
         hidden, k = _width(rng, 16, 8192), _log_int(rng, 1, 16)
         tokens = _log_int(rng, 1, min(65536, 16384 * 8 * 512 // (hidden * k)))
@@ -272,7 +274,7 @@ def _plain_route(st):
         picked = torch.where(there, s.gather(1, at), 0.0)
         if c["renormalise"]:
             total = picked.sum(1, keepdim=True).clamp(min=1e-300)
-            dw = (dw - (dw * picked).sum(1, keepdim=True) / total) / total
+            dw = (dw - (dw * (picked / total)).sum(1, keepdim=True)) / total
         ds = torch.zeros_like(s).scatter_add_(1, at, torch.where(there, dw, 0.0))
         if c["score"] == "sigmoid":
             return [(ds * s * (1 - s)).to(DT[c["x"]])]
