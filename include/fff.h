@@ -578,6 +578,230 @@ size_t fff_grouped_weight_grad_workspace_bytes(int64_t n_entries, int32_t n_grou
 int fff_describe_grouped_matmul(const fff_grouped_matmul_args* a, char* buf, size_t len);
 int fff_describe_grouped_weight_grad(const fff_grouped_weight_grad_args* a, char* buf, size_t len);
 
+/* ---------------------------------------------------------------------------
+ * Operators of a routed expert block: a learned router beside the tree, the
+ * sum of a token's experts' rows, RMS norm, and activations kept in 8 bits
+ * between the forward and the backward pass.  The conventions of the operators
+ * above hold (8-bit rows and their scales need no alignment beyond their base's
+ * 16 bytes).
+ * ------------------------------------------------------------------------- */
+
+typedef enum { FFF_SCORE_SOFTMAX = 0, FFF_SCORE_SIGMOID = 1 } fff_score;
+typedef enum { FFF_GROUP_MAX = 0, FFF_GROUP_TOP2 = 1 } fff_group_score;
+
+/*
+ * fff_route -- every token's top_k of n_experts experts.  With logit l_e of a token,
+ *   s_e = exp(l_e) / sum over the token's experts of exp(l), or 1 / (1 + exp(-l_e))
+ *   c_e = s_e + bias_e    (what experts are chosen by; without a bias the logit itself)
+ * the experts of the largest c are written to ids in falling order of c (the lower
+ * index where two are equal), and with `scale`
+ *   weights = scale s, or with renormalise  scale s / sum of s over the chosen.
+ * A bias (to balance the experts' loads) moves the choice and no weight.  c is
+ * compared in fp64, so that a choice does not hang on fp32 roundings.
+ * With n_groups > 1 the experts form n_groups runs of equal length, and a token
+ * chooses only among the top_groups groups of the largest
+ *   max c (FFF_GROUP_MAX), or the sum of the group's two largest c (FFF_GROUP_TOP2;
+ *   without a bias of its two largest s; of one where it has no second).
+ * An expert whose logit is -inf or NaN (or whose c is) is never chosen, and such
+ * logits count nothing in the softmax; +inf counts as the largest fp32 value.  A
+ * group without any other expert is not chosen either.  Where fewer than top_k
+ * experts can be, the rest of the token's ids are -1 with weight 0: a padding
+ * token, all of whose logits are -inf, goes to no expert.  fff_group_rows takes
+ * ids as they are (first 0): entries of id -1 are in no group.
+ */
+#define FFF_MAX_TOP_K 64
+#define FFF_MAX_ROUTE_GROUPS 1024
+typedef struct {
+    const void* logits;    /* [n_tokens, n_experts] (x_dtype) */
+    const float* bias;     /* [n_experts], or NULL */
+    int32_t* ids;          /* [n_tokens, top_k] */
+    float* weights;        /* [n_tokens, top_k] */
+    int64_t n_tokens;      /* n_tokens x top_k below 2^31 */
+    int32_t n_experts;     /* 1 .. FFF_MAX_GROUPS */
+    int32_t top_k;         /* 1 .. min(FFF_MAX_TOP_K, n_experts) */
+    int32_t n_groups;      /* divides n_experts; 1 .. FFF_MAX_ROUTE_GROUPS */
+    int32_t top_groups;    /* 1 .. n_groups */
+    int32_t x_dtype;       /* fff_dtype */
+    int32_t score;         /* fff_score */
+    int32_t group_score;   /* fff_group_score */
+    int32_t renormalise;
+    float scale;           /* finite */
+    void* hip_stream;
+} fff_route_args;
+
+int fff_route(const fff_route_args* a);
+
+/*
+ * fff_route_backward -- dlogits of fff_route for the experts it chose: with
+ * d_e the sum of scale dweights over the token's entries of expert e and
+ * p_j = s_j / sum of s over the entries (renormalise),
+ *   softmax:                 dl_e = s_e (d_e - sum over all experts of d s)
+ *   softmax, renormalised:   dl_e = sum over e's entries j of p_j (scale dw_j - D)
+ *   sigmoid:                 dl_e = d_e s_e (1 - s_e)
+ *   sigmoid, renormalised:   dl_e = (1 - s_e) sum over e's entries of p_j (scale dw_j - D)
+ * with D = sum over the entries of scale dw p.  The choice itself has no gradient,
+ * and neither has the bias.  Entries whose id is outside [0, n_experts) or whose
+ * logit is -inf or NaN take no part, and the gradient of such logits is 0.
+ */
+typedef struct {
+    const float* dweights; /* [n_tokens, top_k] */
+    const void* logits;    /* [n_tokens, n_experts] (x_dtype), the forward's */
+    const int32_t* ids;    /* [n_tokens, top_k], the forward's */
+    void* dlogits;         /* [n_tokens, n_experts] (d_dtype) */
+    int64_t n_tokens;
+    int32_t n_experts, top_k; /* as above; top_k may pass n_experts here */
+    int32_t x_dtype, d_dtype;
+    int32_t score;
+    int32_t renormalise;
+    float scale;
+    void* hip_stream;
+} fff_route_backward_args;
+
+int fff_route_backward(const fff_route_backward_args* a);
+
+/*
+ * fff_combine -- a token's experts' (or trees') rows added up:
+ *   y_t = residual_t + sum over j < top_k of weights_tj rows_(t top_k + j)
+ * in fp32, in the order of j, the residual last.  Entries whose id is negative take no
+ * part, whatever their row holds.  y may be the buffer residual.
+ */
+typedef struct {
+    const void* rows;      /* [n_tokens top_k, hidden] (rows_dtype): fff_grouped_matmul's, in entry order */
+    const float* weights;  /* [n_tokens, top_k], or NULL for ones */
+    const int32_t* ids;    /* [n_tokens, top_k], or NULL: every entry takes part */
+    const void* residual;  /* [n_tokens, hidden] (y_dtype), or NULL */
+    void* y;               /* [n_tokens, hidden] (y_dtype) */
+    int64_t n_tokens;      /* n_tokens x top_k below 2^31 */
+    int32_t hidden, top_k; /* any, 1 at least */
+    int32_t rows_dtype, y_dtype;
+    void* hip_stream;
+} fff_combine_args;
+
+int fff_combine(const fff_combine_args* a);
+
+/*
+ * fff_combine_backward -- drows_(t top_k + j) = weights_tj dy_t and
+ * dweights_tj = <dy_t, rows_(t top_k + j)>; both are 0 for entries that take no part.
+ * (dy is the residual's gradient.)  drows may be the buffer rows, of its type.
+ */
+typedef struct {
+    const void* dy;        /* [n_tokens, hidden] (y_dtype) */
+    const void* rows;      /* [n_tokens top_k, hidden] (rows_dtype); may be NULL when dweights is */
+    const float* weights;  /* [n_tokens, top_k], or NULL for ones */
+    const int32_t* ids;    /* or NULL */
+    void* drows;           /* [n_tokens top_k, hidden] (drows_dtype), or NULL to skip */
+    float* dweights;       /* [n_tokens, top_k], or NULL to skip */
+    int64_t n_tokens;
+    int32_t hidden, top_k;
+    int32_t y_dtype, rows_dtype, drows_dtype;
+    void* hip_stream;
+} fff_combine_backward_args;
+
+int fff_combine_backward(const fff_combine_backward_args* a);
+
+/* Rows in 8 bits: OCP e4m3 values [rows, hidden] and one scale for every
+ * FFF_PACK_BLOCK columns of a row (the last block of a row may be shorter),
+ * [rows, ceil(hidden / FFF_PACK_BLOCK)] bytes holding the exponent of a power of
+ * two + 127 (255: NaN), the layout of the OCP microscaling format MXFP8.  The
+ * scale written is the smallest power of two (2^-127 at least) that brings the
+ * block's largest finite value to at most 448; values are then rounded to the
+ * nearest, even at ties, and none is cut off, but that what would round to 2^128
+ * becomes 240 x 2^120, the largest finite number of the format that fp32 holds.
+ * Infinite and NaN values become NaN and leave the others' scale alone.  Such
+ * values are exact in bf16. */
+#define FFF_PACK_BLOCK 32
+
+/*
+ * fff_rms_norm -- s = residual + x (residual optional), then
+ *   y = s / sqrt(mean(s^2) + eps) * gamma
+ * per row, y in y_dtype and, with q, in 8 bits too (from the fp32 y).  y, q and rstd
+ * come from the fp32 s, before it is rounded to s_dtype for the stream.  Any
+ * hidden >= 1; n_tokens < 2^32.
+ */
+typedef struct {
+    const void* x;         /* [n_tokens, hidden] (x_dtype) */
+    const void* residual;  /* [n_tokens, hidden] (s_dtype), or NULL */
+    const float* gamma;    /* [hidden], or NULL for ones */
+    void* y;               /* [n_tokens, hidden] (y_dtype), or NULL with q */
+    void* s;               /* [n_tokens, hidden] (s_dtype), or NULL; may be the buffer residual */
+    float* rstd;           /* [n_tokens] 1 / sqrt(mean(s^2) + eps), or NULL */
+    uint8_t* q;            /* [n_tokens, hidden] 8-bit y, or NULL */
+    uint8_t* q_scale;      /* [n_tokens, ceil(hidden / 32)], with q */
+    int64_t n_tokens;
+    int32_t hidden;
+    int32_t x_dtype, s_dtype, y_dtype;
+    float eps;             /* >= 0 and finite */
+    void* hip_stream;
+} fff_rms_norm_args;
+
+int fff_rms_norm(const fff_rms_norm_args* a);
+
+/*
+ * fff_rms_norm_backward -- with xh = s rstd and g = dy gamma,
+ *   ds = rstd (g - xh mean(g xh)) + ds_in,   dgamma = sum over rows of dy xh,
+ * where ds_in is the gradient that reaches s past the norm.  ds is the gradient of
+ * residual and of x; dx is the same in x_dtype, from the fp32 ds.  The sums over
+ * rows run in a fixed order: the same bits on every run.
+ */
+typedef struct {
+    const void* dy;        /* [n_tokens, hidden] (y_dtype) */
+    const void* s;         /* [n_tokens, hidden] (s_dtype): the forward's s, or its x without a residual */
+    const float* rstd;     /* [n_tokens], from the forward */
+    const float* gamma;    /* [hidden], or NULL for ones */
+    const void* ds_in;     /* [n_tokens, hidden] (s_dtype), or NULL */
+    void* ds;              /* [n_tokens, hidden] (s_dtype), or NULL to skip; may be the buffer ds_in */
+    void* dx;              /* [n_tokens, hidden] (x_dtype), or NULL to skip */
+    float* dgamma;         /* [hidden], or NULL to skip */
+    int64_t n_tokens;
+    int32_t hidden;
+    int32_t x_dtype, s_dtype, y_dtype;
+    int32_t accumulate;    /* 0: dgamma overwritten; 1: added to */
+    void* workspace;       /* with dgamma: device scratch of the size below, 256-byte aligned */
+    size_t workspace_bytes;
+    void* hip_stream;
+} fff_rms_norm_backward_args;
+
+int fff_rms_norm_backward(const fff_rms_norm_backward_args* a);
+
+/* Scratch of fff_rms_norm_backward: partial sums of dgamma.  0 for invalid shapes. */
+size_t fff_rms_norm_backward_workspace_bytes(int64_t n_tokens, int32_t hidden);
+
+/* fff_pack_rows -- x's rows in 8 bits, as above: an activation kept for the backward pass.
+ * Infinite and NaN values: as above.  n_rows < 2^32. */
+typedef struct {
+    const void* x;         /* [n_rows, hidden] (x_dtype) */
+    uint8_t* q;            /* [n_rows, hidden] */
+    uint8_t* q_scale;      /* [n_rows, ceil(hidden / 32)] */
+    int64_t n_rows;
+    int32_t hidden;
+    int32_t x_dtype;
+    void* hip_stream;
+} fff_pack_rows_args;
+
+int fff_pack_rows(const fff_pack_rows_args* a);
+
+/*
+ * fff_unpack_rows -- what the backward pass takes from packed rows z: with dy the
+ * gradient of the activation's output, in one pass
+ *   y = act(z)         (the next product's input, for its weight gradient)
+ *   dx = dy act'(z)    (the gradient through the activation)
+ * either part optional.  dx may be the buffer dy, of its type.  n_rows < 2^32.
+ */
+typedef struct {
+    const uint8_t* q;      /* [n_rows, hidden] */
+    const uint8_t* q_scale; /* [n_rows, ceil(hidden / 32)] */
+    const void* dy;        /* [n_rows, hidden] (dy_dtype), with dx */
+    void* y;               /* [n_rows, hidden] (y_dtype), or NULL to skip */
+    void* dx;              /* [n_rows, hidden] (dx_dtype), or NULL to skip */
+    int64_t n_rows;
+    int32_t hidden;
+    int32_t dy_dtype, y_dtype, dx_dtype;
+    int32_t act;           /* fff_act */
+    void* hip_stream;
+} fff_unpack_rows_args;
+
+int fff_unpack_rows(const fff_unpack_rows_args* a);
+
 const char* fff_status_str(int status);
 int fff_last_hip_error(void); /* raw hipError_t behind the calling thread's last FFF_ERR_HIP */
 int fff_version(void);

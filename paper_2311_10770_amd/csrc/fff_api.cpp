@@ -8,6 +8,7 @@
 #include <algorithm>
 #include <cstdio>
 #include <cstring>
+#include <initializer_list>
 #include <mutex>
 
 #include "fff_internal.hpp"
@@ -970,6 +971,325 @@ FFF_EXPORT int fff_describe_grouped_weight_grad(const fff_grouped_weight_grad_ar
     }
     std::snprintf(buf, len, "none");  // without work
     return grouped_weight_grad(a, buf, len);
+}
+
+// ---- operators of a routed expert block -----------------------------------
+
+namespace {
+
+constexpr int64_t pack_bytes(int64_t hidden) { return (hidden + FFF_PACK_BLOCK - 1) / FFF_PACK_BLOCK; }
+
+// Bytes of a [rows, cols] matrix of a type.
+bool typed_bytes(int64_t rows, int64_t cols, int32_t dtype, int64_t* out) {
+    return matrix_bytes(1, rows, cols, dtype_bytes(dtype), out);
+}
+
+bool all_aligned16(std::initializer_list<const void*> ptrs) {
+    for (const void* q : ptrs)
+        if (!aligned16(q)) return false;
+    return true;
+}
+
+bool finite(float v) { return v - v == 0.0f; }
+
+// Entries of n_tokens tokens, top_k each: below 2^31.
+bool entries_ok(int64_t n_tokens, int32_t top_k) {
+    return n_tokens >= 0 && n_tokens < kMaxEntries && top_k >= 1 && n_tokens * top_k < kMaxEntries;
+}
+
+}  // namespace
+
+FFF_EXPORT int fff_route(const fff_route_args* a) {
+    static_assert(FFF_MAX_TOP_K == fff::MAX_TOP_K && FFF_MAX_ROUTE_GROUPS == fff::MAX_ROUTE_GROUPS, "one limit");
+    if (!a || a->n_experts < 1 || a->top_k < 1 || a->top_k > a->n_experts || !entries_ok(a->n_tokens, a->top_k))
+        return FFF_ERR_INVALID_ARG;
+    if (a->n_groups < 1 || a->n_experts % a->n_groups != 0 || a->top_groups < 1 || a->top_groups > a->n_groups)
+        return FFF_ERR_INVALID_ARG;
+    if (!dtype_ok(a->x_dtype) || (a->score != FFF_SCORE_SOFTMAX && a->score != FFF_SCORE_SIGMOID) ||
+        (a->group_score != FFF_GROUP_MAX && a->group_score != FFF_GROUP_TOP2) ||
+        (a->renormalise != 0 && a->renormalise != 1) || !finite(a->scale))
+        return FFF_ERR_INVALID_ARG;
+    if (a->n_experts > FFF_MAX_GROUPS || a->top_k > FFF_MAX_TOP_K || a->n_groups > FFF_MAX_ROUTE_GROUPS)
+        return FFF_ERR_UNSUPPORTED;
+    if (a->n_tokens == 0) return FFF_OK;
+    if (!a->logits || !a->ids || !a->weights) return FFF_ERR_INVALID_ARG;
+    if (!all_aligned16({a->logits, a->bias}) || !aligned4(a->ids) || !aligned4(a->weights)) return FFF_ERR_INVALID_ARG;
+    int64_t xb;
+    if (!typed_bytes(a->n_tokens, a->n_experts, a->x_dtype, &xb)) return FFF_ERR_INVALID_ARG;
+    const int64_t eb = 4 * a->n_tokens * a->top_k;
+    const Span outs[] = {{a->ids, eb}, {a->weights, eb}};
+    const Span ins[] = {{a->logits, xb}, {a->bias, 4 * int64_t(a->n_experts)}};
+    if (!disjoint(outs, 2, ins, 2, 0)) return FFF_ERR_INVALID_ARG;
+    fff::DeviceInfo dev;
+    const int rc = current_device_info(&dev);
+    if (rc != FFF_OK) return rc;
+    fff::RouteParams p;
+    p.logits = a->logits;
+    p.bias = a->bias;
+    p.ids = a->ids;
+    p.weights = a->weights;
+    p.n_tokens = a->n_tokens;
+    p.n_experts = a->n_experts;
+    p.top_k = a->top_k;
+    p.n_groups = a->n_groups;
+    p.top_groups = a->top_groups;
+    p.bf16 = a->x_dtype == FFF_BF16;
+    p.score = a->score;
+    p.group_score = a->group_score;
+    p.renormalise = a->renormalise;
+    p.scale = a->scale;
+    const hipError_t e = fff::run_route(p, dev, stream_of(a->hip_stream));
+    return e == hipSuccess ? FFF_OK : hip_fail(e);
+}
+
+FFF_EXPORT int fff_route_backward(const fff_route_backward_args* a) {
+    if (!a || a->n_experts < 1 || !entries_ok(a->n_tokens, a->top_k)) return FFF_ERR_INVALID_ARG;
+    if (!dtype_ok(a->x_dtype) || !dtype_ok(a->d_dtype) ||
+        (a->score != FFF_SCORE_SOFTMAX && a->score != FFF_SCORE_SIGMOID) ||
+        (a->renormalise != 0 && a->renormalise != 1) || !finite(a->scale))
+        return FFF_ERR_INVALID_ARG;
+    if (a->n_experts > FFF_MAX_GROUPS || a->top_k > FFF_MAX_TOP_K) return FFF_ERR_UNSUPPORTED;
+    if (a->n_tokens == 0) return FFF_OK;
+    if (!a->dweights || !a->logits || !a->ids || !a->dlogits) return FFF_ERR_INVALID_ARG;
+    if (!all_aligned16({a->logits, a->dlogits}) || !aligned4(a->ids) || !aligned4(a->dweights)) return FFF_ERR_INVALID_ARG;
+    int64_t xb, db;
+    if (!typed_bytes(a->n_tokens, a->n_experts, a->x_dtype, &xb) ||
+        !typed_bytes(a->n_tokens, a->n_experts, a->d_dtype, &db))
+        return FFF_ERR_INVALID_ARG;
+    const int64_t eb = 4 * a->n_tokens * a->top_k;
+    const Span outs[] = {{a->dlogits, db}};
+    const Span ins[] = {{a->logits, xb}, {a->ids, eb}, {a->dweights, eb}};
+    if (!disjoint(outs, 1, ins, 3, 0)) return FFF_ERR_INVALID_ARG;
+    fff::DeviceInfo dev;
+    const int rc = current_device_info(&dev);
+    if (rc != FFF_OK) return rc;
+    fff::RouteBwdParams p;
+    p.dweights = a->dweights;
+    p.logits = a->logits;
+    p.ids = a->ids;
+    p.dlogits = a->dlogits;
+    p.n_tokens = a->n_tokens;
+    p.n_experts = a->n_experts;
+    p.top_k = a->top_k;
+    p.bf16 = a->x_dtype == FFF_BF16;
+    p.d_bf16 = a->d_dtype == FFF_BF16;
+    p.score = a->score;
+    p.renormalise = a->renormalise;
+    p.scale = a->scale;
+    const hipError_t e = fff::run_route_backward(p, dev, stream_of(a->hip_stream));
+    return e == hipSuccess ? FFF_OK : hip_fail(e);
+}
+
+FFF_EXPORT int fff_combine(const fff_combine_args* a) {
+    if (!a || a->hidden < 1 || !entries_ok(a->n_tokens, a->top_k)) return FFF_ERR_INVALID_ARG;
+    if (!dtype_ok(a->rows_dtype) || !dtype_ok(a->y_dtype)) return FFF_ERR_INVALID_ARG;
+    if (a->n_tokens == 0) return FFF_OK;
+    if (!a->rows || !a->y) return FFF_ERR_INVALID_ARG;
+    if (!all_aligned16({a->rows, a->residual, a->y}) || !aligned4(a->weights) || !aligned4(a->ids))
+        return FFF_ERR_INVALID_ARG;
+    const int64_t E = a->n_tokens * a->top_k;
+    int64_t rb, yb;
+    if (!typed_bytes(E, a->hidden, a->rows_dtype, &rb) || !typed_bytes(a->n_tokens, a->hidden, a->y_dtype, &yb))
+        return FFF_ERR_INVALID_ARG;
+    const Span outs[] = {{a->y, yb}};
+    const Span ins[] = {{a->rows, rb}, {a->weights, 4 * E}, {a->ids, 4 * E}, {a->residual, yb}};
+    if (!disjoint(outs, 1, ins, 4, 1u << 3)) return FFF_ERR_INVALID_ARG;
+    fff::DeviceInfo dev;
+    const int rc = current_device_info(&dev);
+    if (rc != FFF_OK) return rc;
+    fff::CombineParams p;
+    p.rows = a->rows;
+    p.weights = a->weights;
+    p.ids = a->ids;
+    p.residual = a->residual;
+    p.y = a->y;
+    p.n_tokens = a->n_tokens;
+    p.hidden = a->hidden;
+    p.top_k = a->top_k;
+    p.rows_bf16 = a->rows_dtype == FFF_BF16;
+    p.y_bf16 = a->y_dtype == FFF_BF16;
+    const hipError_t e = fff::run_combine(p, dev, stream_of(a->hip_stream));
+    return e == hipSuccess ? FFF_OK : hip_fail(e);
+}
+
+FFF_EXPORT int fff_combine_backward(const fff_combine_backward_args* a) {
+    if (!a || a->hidden < 1 || !entries_ok(a->n_tokens, a->top_k)) return FFF_ERR_INVALID_ARG;
+    if (!dtype_ok(a->y_dtype) || !dtype_ok(a->rows_dtype) || !dtype_ok(a->drows_dtype)) return FFF_ERR_INVALID_ARG;
+    if (a->n_tokens == 0 || (!a->drows && !a->dweights)) return FFF_OK;
+    if (!a->dy || (a->dweights && !a->rows)) return FFF_ERR_INVALID_ARG;
+    if (!all_aligned16({a->dy, a->rows, a->drows}) || !aligned4(a->weights) || !aligned4(a->ids) ||
+        !aligned4(a->dweights))
+        return FFF_ERR_INVALID_ARG;
+    const int64_t E = a->n_tokens * a->top_k;
+    int64_t yb, rb, db;
+    if (!typed_bytes(a->n_tokens, a->hidden, a->y_dtype, &yb) || !typed_bytes(E, a->hidden, a->rows_dtype, &rb) ||
+        !typed_bytes(E, a->hidden, a->drows_dtype, &db))
+        return FFF_ERR_INVALID_ARG;
+    const Span outs[] = {{a->drows, db}, {a->dweights, 4 * E}};
+    const Span ins[] = {{a->dy, yb}, {a->rows, rb}, {a->weights, 4 * E}, {a->ids, 4 * E}};
+    if (!disjoint(outs, 2, ins, 4, a->rows_dtype == a->drows_dtype ? 1u << 1 : 0)) return FFF_ERR_INVALID_ARG;
+    fff::DeviceInfo dev;
+    const int rc = current_device_info(&dev);
+    if (rc != FFF_OK) return rc;
+    fff::CombineBwdParams p;
+    p.dy = a->dy;
+    p.rows = a->rows;
+    p.weights = a->weights;
+    p.ids = a->ids;
+    p.drows = a->drows;
+    p.dweights = a->dweights;
+    p.n_tokens = a->n_tokens;
+    p.hidden = a->hidden;
+    p.top_k = a->top_k;
+    p.y_bf16 = a->y_dtype == FFF_BF16;
+    p.rows_bf16 = a->rows_dtype == FFF_BF16;
+    p.drows_bf16 = a->drows_dtype == FFF_BF16;
+    const hipError_t e = fff::run_combine_backward(p, dev, stream_of(a->hip_stream));
+    return e == hipSuccess ? FFF_OK : hip_fail(e);
+}
+
+FFF_EXPORT int fff_rms_norm(const fff_rms_norm_args* a) {
+    if (!a || a->n_tokens < 0 || a->n_tokens >= kMaxRows || a->hidden < 1) return FFF_ERR_INVALID_ARG;
+    if (!dtype_ok(a->x_dtype) || !dtype_ok(a->s_dtype) || !dtype_ok(a->y_dtype)) return FFF_ERR_INVALID_ARG;
+    if (!(a->eps >= 0.0f && finite(a->eps))) return FFF_ERR_INVALID_ARG;
+    if (a->n_tokens == 0) return FFF_OK;
+    if (!a->x || (!a->y && !a->q) || (a->q == nullptr) != (a->q_scale == nullptr)) return FFF_ERR_INVALID_ARG;
+    if (!all_aligned16({a->x, a->residual, a->gamma, a->y, a->s, a->q, a->q_scale}) || !aligned4(a->rstd))
+        return FFF_ERR_INVALID_ARG;
+    const int64_t B = a->n_tokens, H = a->hidden;
+    int64_t xb, sb, yb;
+    if (!typed_bytes(B, H, a->x_dtype, &xb) || !typed_bytes(B, H, a->s_dtype, &sb) || !typed_bytes(B, H, a->y_dtype, &yb))
+        return FFF_ERR_INVALID_ARG;
+    const Span outs[] = {{a->s, sb}, {a->y, yb}, {a->rstd, 4 * B}, {a->q, B * H}, {a->q_scale, B * pack_bytes(H)}};
+    const Span ins[] = {{a->x, xb}, {a->residual, sb}, {a->gamma, 4 * H}};
+    if (!disjoint(outs, 5, ins, 3, 1u << 1)) return FFF_ERR_INVALID_ARG;
+    fff::DeviceInfo dev;
+    const int rc = current_device_info(&dev);
+    if (rc != FFF_OK) return rc;
+    fff::RmsParams p;
+    p.x = a->x;
+    p.residual = a->residual;
+    p.gamma = a->gamma;
+    p.y = a->y;
+    p.s = a->s;
+    p.rstd = a->rstd;
+    p.q = a->q;
+    p.q_scale = a->q_scale;
+    p.n_tokens = B;
+    p.hidden = a->hidden;
+    p.x_bf16 = a->x_dtype == FFF_BF16;
+    p.s_bf16 = a->s_dtype == FFF_BF16;
+    p.y_bf16 = a->y_dtype == FFF_BF16;
+    p.eps = a->eps;
+    const hipError_t e = fff::run_rms_norm(p, dev, stream_of(a->hip_stream));
+    return e == hipSuccess ? FFF_OK : hip_fail(e);
+}
+
+FFF_EXPORT size_t fff_rms_norm_backward_workspace_bytes(int64_t n_tokens, int32_t hidden) {
+    if (n_tokens < 0 || n_tokens >= kMaxRows || hidden < 1) return 0;
+    return fff::rms_bwd_workspace_bytes(n_tokens, hidden);
+}
+
+FFF_EXPORT int fff_rms_norm_backward(const fff_rms_norm_backward_args* a) {
+    if (!a || a->n_tokens < 0 || a->n_tokens >= kMaxRows || a->hidden < 1) return FFF_ERR_INVALID_ARG;
+    if (!dtype_ok(a->x_dtype) || !dtype_ok(a->s_dtype) || !dtype_ok(a->y_dtype)) return FFF_ERR_INVALID_ARG;
+    if (a->accumulate != 0 && a->accumulate != 1) return FFF_ERR_INVALID_ARG;
+    const int64_t B = a->n_tokens, H = a->hidden;
+    if (!a->ds && !a->dx && !a->dgamma) return FFF_OK;
+    if (B == 0 && (!a->dgamma || a->accumulate)) return FFF_OK;
+    if (B > 0 && (!a->dy || !a->s || !a->rstd)) return FFF_ERR_INVALID_ARG;
+    if (!all_aligned16({a->dy, a->s, a->gamma, a->ds_in, a->ds, a->dx, a->dgamma}) || !aligned4(a->rstd))
+        return FFF_ERR_INVALID_ARG;
+    int64_t xb, sb, yb;
+    if (!typed_bytes(B, H, a->x_dtype, &xb) || !typed_bytes(B, H, a->s_dtype, &sb) || !typed_bytes(B, H, a->y_dtype, &yb))
+        return FFF_ERR_INVALID_ARG;
+    int64_t need = 0;
+    if (a->dgamma) {
+        need = int64_t(fff::rms_bwd_workspace_bytes(B, a->hidden));
+        if (need > 0 && (!a->workspace || a->workspace_bytes < size_t(need))) return FFF_ERR_WORKSPACE;
+        if (reinterpret_cast<uintptr_t>(a->workspace) & 255u) return FFF_ERR_INVALID_ARG;
+    }
+    const Span outs[] = {{a->ds, sb}, {a->dx, xb}, {a->dgamma, 4 * H}, {need ? a->workspace : nullptr, need}};
+    const Span ins[] = {{a->dy, yb}, {a->s, sb}, {a->rstd, 4 * B}, {a->gamma, 4 * H}, {a->ds_in, sb}};
+    if (!disjoint(outs, 4, ins, 5, 1u << 4)) return FFF_ERR_INVALID_ARG;
+    fff::DeviceInfo dev;
+    const int rc = current_device_info(&dev);
+    if (rc != FFF_OK) return rc;
+    fff::RmsBwdParams p;
+    p.dy = a->dy;
+    p.s = a->s;
+    p.rstd = a->rstd;
+    p.gamma = a->gamma;
+    p.ds_in = a->ds_in;
+    p.ds = a->ds;
+    p.dx = a->dx;
+    p.dgamma = a->dgamma;
+    p.part = static_cast<float*>(a->workspace);
+    p.n_tokens = B;
+    p.hidden = a->hidden;
+    p.x_bf16 = a->x_dtype == FFF_BF16;
+    p.s_bf16 = a->s_dtype == FFF_BF16;
+    p.y_bf16 = a->y_dtype == FFF_BF16;
+    p.accumulate = a->accumulate;
+    const hipError_t e = fff::run_rms_norm_backward(p, dev, stream_of(a->hip_stream));
+    return e == hipSuccess ? FFF_OK : hip_fail(e);
+}
+
+FFF_EXPORT int fff_pack_rows(const fff_pack_rows_args* a) {
+    if (!a || a->n_rows < 0 || a->n_rows >= kMaxRows || a->hidden < 1 || !dtype_ok(a->x_dtype)) return FFF_ERR_INVALID_ARG;
+    if (a->n_rows == 0) return FFF_OK;
+    if (!a->x || !a->q || !a->q_scale || !all_aligned16({a->x, a->q, a->q_scale})) return FFF_ERR_INVALID_ARG;
+    const int64_t B = a->n_rows, H = a->hidden;
+    int64_t xb;
+    if (!typed_bytes(B, H, a->x_dtype, &xb)) return FFF_ERR_INVALID_ARG;
+    const Span outs[] = {{a->q, B * H}, {a->q_scale, B * pack_bytes(H)}};
+    const Span ins[] = {{a->x, xb}};
+    if (!disjoint(outs, 2, ins, 1, 0)) return FFF_ERR_INVALID_ARG;
+    fff::DeviceInfo dev;
+    const int rc = current_device_info(&dev);
+    if (rc != FFF_OK) return rc;
+    fff::PackParams p;
+    p.x = a->x;
+    p.q = a->q;
+    p.q_scale = a->q_scale;
+    p.n_rows = B;
+    p.hidden = a->hidden;
+    p.x_bf16 = a->x_dtype == FFF_BF16;
+    const hipError_t e = fff::run_pack_rows(p, dev, stream_of(a->hip_stream));
+    return e == hipSuccess ? FFF_OK : hip_fail(e);
+}
+
+FFF_EXPORT int fff_unpack_rows(const fff_unpack_rows_args* a) {
+    if (!a || a->n_rows < 0 || a->n_rows >= kMaxRows || a->hidden < 1) return FFF_ERR_INVALID_ARG;
+    if (!dtype_ok(a->dy_dtype) || !dtype_ok(a->y_dtype) || !dtype_ok(a->dx_dtype)) return FFF_ERR_INVALID_ARG;
+    if (a->act < FFF_ACT_GELU_ERF || a->act > FFF_ACT_IDENTITY) return FFF_ERR_INVALID_ARG;
+    if (a->n_rows == 0 || (!a->y && !a->dx)) return FFF_OK;
+    if (!a->q || !a->q_scale || (a->dx && !a->dy)) return FFF_ERR_INVALID_ARG;
+    if (!all_aligned16({a->q, a->q_scale, a->dy, a->y, a->dx})) return FFF_ERR_INVALID_ARG;
+    const int64_t B = a->n_rows, H = a->hidden;
+    int64_t ib, yb, db;
+    if (!typed_bytes(B, H, a->dy_dtype, &ib) || !typed_bytes(B, H, a->y_dtype, &yb) || !typed_bytes(B, H, a->dx_dtype, &db))
+        return FFF_ERR_INVALID_ARG;
+    const Span outs[] = {{a->dx, db}, {a->y, yb}};
+    const Span ins[] = {{a->q, B * H}, {a->q_scale, B * pack_bytes(H)}, {a->dx ? a->dy : nullptr, ib}};
+    if (!disjoint(outs, 2, ins, 3, a->dy_dtype == a->dx_dtype ? 1u << 2 : 0)) return FFF_ERR_INVALID_ARG;
+    fff::DeviceInfo dev;
+    const int rc = current_device_info(&dev);
+    if (rc != FFF_OK) return rc;
+    fff::UnpackParams p;
+    p.q = a->q;
+    p.q_scale = a->q_scale;
+    p.dy = a->dy;
+    p.y = a->y;
+    p.dx = a->dx;
+    p.n_rows = B;
+    p.hidden = a->hidden;
+    p.dy_bf16 = a->dy_dtype == FFF_BF16;
+    p.y_bf16 = a->y_dtype == FFF_BF16;
+    p.dx_bf16 = a->dx_dtype == FFF_BF16;
+    p.act = a->act;
+    const hipError_t e = fff::run_unpack_rows(p, dev, stream_of(a->hip_stream));
+    return e == hipSuccess ? FFF_OK : hip_fail(e);
 }
 
 FFF_EXPORT const char* fff_status_str(int status) {

@@ -1,0 +1,122 @@
+// fff_combine.hip -- the rows of a token's experts added up, and the gradients
+// (fff_combine, fff_combine_backward).
+//
+//   y_t = residual_t + sum_j w_tj row_tj;  drow_tj = w_tj dy_t;  dw_tj = <dy_t, row_tj>
+//
+// Bound by the rows' bytes: every row is read or written once, eight columns a lane.
+#include "fff_device.hpp"
+#include "fff_operators.hpp"
+#include "fff_rows.hpp"
+
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cstdint>
+
+namespace fff {
+
+namespace {
+
+// A thread takes eight columns of a token; U rows are in flight at a time.
+constexpr int U = 4;
+__global__ __launch_bounds__(256) void combine_kernel(CombineParams p, int vecs, int64_t all) {
+    const int64_t entries = p.n_tokens * p.top_k, total = entries * p.hidden, ytotal = p.n_tokens * p.hidden;
+    for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < all; i += int64_t(gridDim.x) * 256) {
+        const int64_t t = i / vecs;
+        const int col = int(i - t * vecs) * 8;
+        const int64_t e0 = t * p.top_k;
+        float acc[8] = {};
+        for (int j0 = 0; j0 < p.top_k; j0 += U) {
+            Raw8 r[U];
+            float w[U];
+            bool live[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int j = j0 + u;
+                live[u] = j < p.top_k && (!p.ids || p.ids[e0 + j] >= 0);
+                w[u] = live[u] && p.weights ? p.weights[e0 + j] : 1.0f;
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (live[u]) r[u] = load8(p.rows, p.rows_bf16, (e0 + j0 + u) * p.hidden + col, total);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (!live[u]) continue;
+                float f[8];
+                unpack8(f, r[u], p.rows_bf16);
+#pragma unroll
+                for (int c = 0; c < 8; ++c) acc[c] = __builtin_fmaf(w[u], f[c], acc[c]);
+            }
+        }
+        if (p.residual) {
+            float f[8];
+            unpack8(f, load8(p.residual, p.y_bf16, t * p.hidden + col, ytotal), p.y_bf16);
+#pragma unroll
+            for (int c = 0; c < 8; ++c) acc[c] += f[c];
+        }
+        store8(p.y, p.y_bf16, t * p.hidden + col, p.hidden - col, acc);
+    }
+}
+
+// LPE lanes an entry.  A row is read before the same lane writes its gradient there, so drows may be
+// the buffer rows; a token's entries are neighbours, so its dy comes from the caches but once.
+template <int LPE>
+__global__ __launch_bounds__(256) void combine_bwd_kernel(CombineBwdParams p) {
+    constexpr int EPB = 256 / LPE;
+    const int sl = threadIdx.x % LPE, H = p.hidden;
+    const int64_t entries = p.n_tokens * p.top_k, total = entries * H, ytotal = p.n_tokens * H;
+    for (int64_t e0 = int64_t(blockIdx.x) * EPB; e0 < entries; e0 += int64_t(gridDim.x) * EPB) {
+        const int64_t e = e0 + threadIdx.x / LPE;
+        if (e >= entries) break;
+        const int64_t t = uint32_t(e) / uint32_t(p.top_k);
+        const bool live = !p.ids || p.ids[e] >= 0;
+        const float w = live && p.weights ? p.weights[e] : 1.0f;
+        const bool dot = live && p.dweights;
+        float acc = 0.0f;
+        for (uint32_t col = sl * 8; col < uint32_t(H); col += LPE * 8) {
+            float f[8] = {}, g[8];
+            if (live) unpack8(f, load8(p.dy, p.y_bf16, t * H + col, ytotal), p.y_bf16);
+            if (dot) {
+                unpack8(g, load8(p.rows, p.rows_bf16, e * H + col, total), p.rows_bf16);
+#pragma unroll
+                for (int c = 0; c < 8; ++c)
+                    if (col + c < uint32_t(H)) acc = __builtin_fmaf(f[c], g[c], acc);
+            }
+            if (!p.drows) continue;
+            if (live) {
+#pragma unroll
+                for (int c = 0; c < 8; ++c) f[c] *= w;
+            }
+            store8(p.drows, p.drows_bf16, e * H + col, H - int(col), f);
+        }
+        if (p.dweights) {
+            acc = group_sum<LPE>(acc);
+            if (sl == 0) p.dweights[e] = acc;
+        }
+    }
+}
+
+}  // namespace
+
+hipError_t run_combine(const CombineParams& p, const DeviceInfo& dev, hipStream_t stream) {
+    const int vecs = int((int64_t(p.hidden) + 7) / 8);
+    const int64_t all = p.n_tokens * vecs;
+    const unsigned grid = unsigned(std::min<int64_t>((all + 255) / 256, 64 * std::max(dev.cu_count, 1)));
+    hipLaunchKernelGGL(combine_kernel, dim3(grid), dim3(256), 0, stream, p, vecs, all);
+    return hipGetLastError();
+}
+
+hipError_t run_combine_backward(const CombineBwdParams& p, const DeviceInfo& dev, hipStream_t stream) {
+    const int64_t entries = p.n_tokens * p.top_k;
+    auto launch = [&](auto kernel, int lanes) {
+        const int per = 256 / lanes;
+        const unsigned grid = unsigned(std::min<int64_t>((entries + per - 1) / per, 64 * std::max(dev.cu_count, 1)));
+        hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, stream, p);
+    };
+    if (p.hidden <= 128) launch(combine_bwd_kernel<16>, 16);
+    else if (p.hidden <= 256) launch(combine_bwd_kernel<32>, 32);
+    else launch(combine_bwd_kernel<64>, 64);
+    return hipGetLastError();
+}
+
+}  // namespace fff

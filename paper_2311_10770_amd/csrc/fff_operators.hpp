@@ -123,4 +123,118 @@ size_t grouped_grad_workspace_bytes(int64_t n_entries, int32_t n_groups, int32_t
 hipError_t run_grouped_weight_grad(const GroupedGradParams& p, hipStream_t stream, int* status, char* buf = nullptr,
                                    size_t len = 0);
 
+// ---- a routed expert block --------------------------------------------------
+
+enum { SCORE_SOFTMAX = 0, SCORE_SIGMOID = 1 };
+enum { GROUP_MAX = 0, GROUP_TOP2 = 1 };
+constexpr int32_t MAX_TOP_K = 64, MAX_ROUTE_GROUPS = 1024;
+
+struct RouteParams {
+    const void* logits;
+    const float* bias;       // or null
+    int32_t* ids;
+    float* weights;
+    int64_t n_tokens;
+    int32_t n_experts, top_k, n_groups, top_groups;
+    int32_t bf16;
+    int32_t score, group_score, renormalise;
+    float scale;
+};
+hipError_t run_route(const RouteParams& p, const DeviceInfo& dev, hipStream_t stream);
+
+struct RouteBwdParams {
+    const float* dweights;
+    const void* logits;
+    const int32_t* ids;
+    void* dlogits;
+    int64_t n_tokens;
+    int32_t n_experts, top_k;
+    int32_t bf16, d_bf16;
+    int32_t score, renormalise;
+    float scale;
+};
+hipError_t run_route_backward(const RouteBwdParams& p, const DeviceInfo& dev, hipStream_t stream);
+
+struct CombineParams {
+    const void* rows;
+    const float* weights;    // or null
+    const int32_t* ids;      // or null
+    const void* residual;    // or null
+    void* y;
+    int64_t n_tokens;
+    int32_t hidden, top_k;
+    int32_t rows_bf16, y_bf16;
+};
+hipError_t run_combine(const CombineParams& p, const DeviceInfo& dev, hipStream_t stream);
+
+struct CombineBwdParams {
+    const void* dy;
+    const void* rows;        // or null
+    const float* weights;    // or null
+    const int32_t* ids;      // or null
+    void* drows;             // or null
+    float* dweights;         // or null
+    int64_t n_tokens;
+    int32_t hidden, top_k;
+    int32_t y_bf16, rows_bf16, drows_bf16;
+};
+hipError_t run_combine_backward(const CombineBwdParams& p, const DeviceInfo& dev, hipStream_t stream);
+
+struct RmsParams {
+    const void* x;
+    const void* residual;    // or null
+    const float* gamma;      // or null
+    void* y;                 // or null
+    void* s;                 // or null
+    float* rstd;             // or null
+    uint8_t* q;              // or null
+    uint8_t* q_scale;
+    int64_t n_tokens;
+    int32_t hidden;
+    int32_t x_bf16, s_bf16, y_bf16;
+    float eps;
+};
+hipError_t run_rms_norm(const RmsParams& p, const DeviceInfo& dev, hipStream_t stream);
+
+struct RmsBwdParams {
+    const void* dy;
+    const void* s;
+    const float* rstd;
+    const float* gamma;      // or null
+    const void* ds_in;       // or null
+    void* ds;                // or null
+    void* dx;                // or null
+    float* dgamma;           // or null
+    float* part;             // [parts, hidden] partial sums of dgamma
+    int64_t n_tokens;
+    int32_t hidden;
+    int32_t x_bf16, s_bf16, y_bf16;
+    int32_t accumulate;
+};
+size_t rms_bwd_workspace_bytes(int64_t n_tokens, int32_t hidden);
+hipError_t run_rms_norm_backward(const RmsBwdParams& p, const DeviceInfo& dev, hipStream_t stream);
+
+struct PackParams {
+    const void* x;
+    uint8_t* q;
+    uint8_t* q_scale;
+    int64_t n_rows;
+    int32_t hidden;
+    int32_t x_bf16;
+};
+hipError_t run_pack_rows(const PackParams& p, const DeviceInfo& dev, hipStream_t stream);
+
+struct UnpackParams {
+    const uint8_t* q;
+    const uint8_t* q_scale;
+    const void* dy;          // with dx
+    void* y;                 // or null
+    void* dx;                // or null
+    int64_t n_rows;
+    int32_t hidden;
+    int32_t dy_bf16, y_bf16, dx_bf16;
+    int32_t act;
+};
+hipError_t run_unpack_rows(const UnpackParams& p, const DeviceInfo& dev, hipStream_t stream);
+
 }  // namespace fff

@@ -1,0 +1,448 @@
+// fff_rms.hip -- RMS norm with the residual's addition, an 8-bit copy of its rows, and
+// its gradients (fff_rms_norm, fff_rms_norm_backward).
+//
+//   s = residual + x;  y = s rstd gamma,  rstd = 1 / sqrt(mean(s^2) + eps)
+//   ds = rstd (g - xh mean(g xh)) + ds_in,  xh = s rstd,  g = dy gamma;  dgamma = sum dy xh
+//
+// All of it is bound by the bytes of the rows; statistics, sums and gradients are held in fp32.
+#include "fff_device.hpp"
+#include "fff_operators.hpp"
+#include "fff_pack.hpp"
+#include "fff_rows.hpp"
+
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cstdint>
+
+namespace fff {
+
+namespace {
+
+// Threads of a row kernel's workgroup for LPR lanes a row.
+constexpr int row_threads(int lpr) { return lpr > 256 ? lpr : 256; }
+
+// Sum over the LPR lanes of a row; every lane gets the same bits.  Rows of several waves add over LDS;
+// calls alternate between two buffers, so one barrier a call is enough.
+template <int LPR>
+__device__ __forceinline__ float row_sum(float v, float* red) {
+    if constexpr (LPR <= 64) {
+        return group_sum<LPR>(v);
+    } else {
+        v = group_sum<64>(v);
+        if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+        __syncthreads();
+        v = 0.0f;
+#pragma unroll
+        for (int w = 0; w < LPR / 64; ++w) v += red[w];
+        return v;
+    }
+}
+
+// Four columns (col .. col + 3, `left` of them in the row) of a row in 8 bits; eight neighbouring lanes hold a
+// block of 32 and all take part.  q and scale: the row's.
+typedef uint32_t u32_a1 __attribute__((aligned(1)));
+__device__ __forceinline__ void put_packed(uint8_t* q, uint8_t* scale, int col, int left, const float* f) {
+    uint32_t most = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) most = max(most, j < left ? finite_bits(f[j]) : 0);
+    const uint32_t code = scale_code(max_eight(most));
+    const float inverse = scale_inverse(code);
+    const uint32_t w = pack_e4m3(scaled(f[0], code, inverse), scaled(f[1], code, inverse), scaled(f[2], code, inverse),
+                                 scaled(f[3], code, inverse));
+    if (left >= 4) {
+        *reinterpret_cast<u32_a1*>(q + col) = w;
+    } else {
+        for (int j = 0; j < left; ++j) q[col + j] = uint8_t(w >> (8 * j));
+    }
+    if (left > 0 && col % PACK_BLOCK == 0) scale[col / PACK_BLOCK] = uint8_t(code);
+}
+
+template <bool FULL>
+__device__ __forceinline__ void gain4(float* f, const float* g, int col, int left) {
+    if (g) {
+        unpack4(f, load4<FULL>(g, 0, col, left), 0);
+    } else {
+        f[0] = f[1] = f[2] = f[3] = 1.0f;
+    }
+}
+
+// Rows held in registers: LPR lanes a row, lane sl holding the NV vectors of four columns
+// c LPR + sl.  One read and one write of every byte.  FULL: the row is exactly LPR NV vectors long.
+template <int LPR, int NV, bool FULL>
+__global__ __launch_bounds__(row_threads(LPR)) void rms_kernel(RmsParams p) {
+    constexpr int NT = row_threads(LPR), RPB = NT / LPR;
+    __shared__ float red[2][LPR / 64 + 1];
+    const int sl = threadIdx.x % LPR, H = p.hidden;
+    const int64_t blocks = pack_blocks(H);
+    const float width = float(H);
+    int turn = 0;
+    for (int64_t r0 = int64_t(blockIdx.x) * RPB; r0 < p.n_tokens; r0 += int64_t(gridDim.x) * RPB) {
+        const int64_t row = r0 + threadIdx.x / LPR;
+        if (RPB > 1 && row >= p.n_tokens) break;
+        Raw4 rx[NV], rr[NV];
+#pragma unroll
+        for (int c = 0; c < NV; ++c) {
+            const int col = (c * LPR + sl) * 4;
+            rx[c] = load4<FULL>(p.x, p.x_bf16, row * H + col, H - col);
+        }
+        if (p.residual) {
+#pragma unroll
+            for (int c = 0; c < NV; ++c) {
+                const int col = (c * LPR + sl) * 4;
+                rr[c] = load4<FULL>(p.residual, p.s_bf16, row * H + col, H - col);
+            }
+        }
+        float f[NV][4], sq = 0.0f;
+#pragma unroll
+        for (int c = 0; c < NV; ++c) unpack4(f[c], rx[c], p.x_bf16);
+        if (p.residual) {
+#pragma unroll
+            for (int c = 0; c < NV; ++c) {
+                float g[4];
+                unpack4(g, rr[c], p.s_bf16);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) f[c][j] += g[j];
+            }
+        }
+        if (p.s) {
+#pragma unroll
+            for (int c = 0; c < NV; ++c) {
+                const int col = (c * LPR + sl) * 4;
+                store4<FULL>(p.s, p.s_bf16, row * H + col, H - col, f[c]);
+            }
+        }
+#pragma unroll
+        for (int c = 0; c < NV; ++c)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sq = __builtin_fmaf(f[c][j], f[c][j], sq);
+        sq = row_sum<LPR>(sq, red[turn]);
+        turn ^= 1;
+        const float rstd = 1.0f / sqrtf(sq / width + p.eps);
+#pragma unroll
+        for (int c = 0; c < NV; ++c) {
+            const int col = (c * LPR + sl) * 4;
+            float g[4];
+            gain4<FULL>(g, p.gamma, col, H - col);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) f[c][j] = f[c][j] * rstd * g[j];
+            if (p.y) store4<FULL>(p.y, p.y_bf16, row * H + col, H - col, f[c]);
+            if (p.q) put_packed(p.q + row * H, p.q_scale + row * blocks, col, H - col, f[c]);
+        }
+        if (sl == 0 && p.rstd) p.rstd[row] = rstd;
+    }
+}
+
+// The gradients of rows held in registers, as rms_kernel holds them.  Every workgroup sums dgamma over its
+// rows in registers and leaves one partial row.
+template <int LPR, int NV, bool FULL>
+__global__ __launch_bounds__(row_threads(LPR)) void rms_bwd_kernel(RmsBwdParams p) {
+    constexpr int NT = row_threads(LPR), RPB = NT / LPR, W = LPR * NV * 4;
+    __shared__ float red[2][LPR / 64 + 1];
+    __shared__ float cols[RPB > 1 ? W : 1];
+    const int sl = threadIdx.x % LPR, H = p.hidden;
+    const float width = float(H);
+    const bool rows_out = p.ds || p.dx;
+    float gain[NV][4], dg[NV][4] = {};
+#pragma unroll
+    for (int c = 0; c < NV; ++c) {
+        const int col = (c * LPR + sl) * 4;
+        gain4<FULL>(gain[c], p.gamma, col, H - col);
+    }
+    int turn = 0;
+    for (int64_t r0 = int64_t(blockIdx.x) * RPB; r0 < p.n_tokens; r0 += int64_t(gridDim.x) * RPB) {
+        const int64_t row = r0 + threadIdx.x / LPR;
+        if (RPB > 1 && row >= p.n_tokens) break;
+        Raw4 ry[NV], rs[NV], ru[NV];
+#pragma unroll
+        for (int c = 0; c < NV; ++c) {
+            const int col = (c * LPR + sl) * 4;
+            ry[c] = load4<FULL>(p.dy, p.y_bf16, row * H + col, H - col);
+        }
+#pragma unroll
+        for (int c = 0; c < NV; ++c) {
+            const int col = (c * LPR + sl) * 4;
+            rs[c] = load4<FULL>(p.s, p.s_bf16, row * H + col, H - col);
+        }
+        if (p.ds_in && rows_out) {
+#pragma unroll
+            for (int c = 0; c < NV; ++c) {
+                const int col = (c * LPR + sl) * 4;
+                ru[c] = load4<FULL>(p.ds_in, p.s_bf16, row * H + col, H - col);
+            }
+        }
+        const float rstd = p.rstd[row];
+        float g[NV][4], xh[NV][4], b = 0.0f;
+#pragma unroll
+        for (int c = 0; c < NV; ++c) {
+            unpack4(g[c], ry[c], p.y_bf16);
+            unpack4(xh[c], rs[c], p.s_bf16);
+            const int left = H - (c * LPR + sl) * 4;  // columns behind the row hold zeros (0 rstd may be NaN)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                xh[c][j] = FULL || j < left ? xh[c][j] * rstd : 0.0f;
+                dg[c][j] = __builtin_fmaf(g[c][j], xh[c][j], dg[c][j]);
+                g[c][j] *= gain[c][j];
+                b = __builtin_fmaf(g[c][j], xh[c][j], b);
+            }
+        }
+        if (!rows_out) continue;
+        const float c2 = row_sum<LPR>(b, red[turn]) / width;
+        turn ^= 1;
+#pragma unroll
+        for (int c = 0; c < NV; ++c)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) g[c][j] = rstd * (g[c][j] - xh[c][j] * c2);
+        if (p.ds_in) {
+#pragma unroll
+            for (int c = 0; c < NV; ++c) {
+                float u[4];
+                unpack4(u, ru[c], p.s_bf16);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) g[c][j] += u[j];
+            }
+        }
+#pragma unroll
+        for (int c = 0; c < NV; ++c) {
+            const int col = (c * LPR + sl) * 4;
+            if (p.ds) store4<FULL>(p.ds, p.s_bf16, row * H + col, H - col, g[c]);
+            if (p.dx) store4<FULL>(p.dx, p.x_bf16, row * H + col, H - col, g[c]);
+        }
+    }
+    if (!p.dgamma) return;
+    // the workgroup's row groups add up in order, then one row of dgamma is stored
+    float* part = p.part + int64_t(blockIdx.x) * H;
+    if constexpr (RPB > 1) {
+        const int group = threadIdx.x / LPR;
+        for (int q = 0; q < RPB; ++q) {
+            if (group == q) {
+#pragma unroll
+                for (int c = 0; c < NV; ++c)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        float* d = cols + (c * LPR + sl) * 4 + j;
+                        d[0] = q ? d[0] + dg[c][j] : dg[c][j];
+                    }
+            }
+            __syncthreads();
+        }
+        for (int i = threadIdx.x; i < H; i += NT) part[i] = cols[i];
+    } else {
+#pragma unroll
+        for (int c = 0; c < NV; ++c) {
+            const int col = (c * LPR + sl) * 4;
+            store4<FULL>(part, 0, col, H - col, dg[c]);
+        }
+    }
+}
+
+// Rows of any length: a workgroup of 1024 a row, which is read again for the second pass.
+constexpr int LONG = 1024;
+__global__ __launch_bounds__(LONG) void rms_any_kernel(RmsParams p) {
+    __shared__ float red[2][LONG / 64 + 1];
+    const int H = p.hidden;
+    const int64_t blocks = pack_blocks(H), turns = (int64_t(H) + 4 * LONG - 1) / (4 * LONG);
+    int turn = 0;
+    for (int64_t row = blockIdx.x; row < p.n_tokens; row += gridDim.x) {
+        auto sum4 = [&](int64_t col, float* f) {
+            const int left = int(std::min<int64_t>(4, H - col));
+            unpack4(f, load4<false>(p.x, p.x_bf16, row * H + col, left), p.x_bf16);
+            if (p.residual) {
+                float g[4];
+                unpack4(g, load4<false>(p.residual, p.s_bf16, row * H + col, left), p.s_bf16);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) f[j] += g[j];
+            }
+            return left;
+        };
+        float f[4], sq = 0.0f;
+        for (int64_t i = 0; i < turns; ++i) {
+            sum4((i * LONG + threadIdx.x) * 4, f);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sq = __builtin_fmaf(f[j], f[j], sq);
+        }
+        sq = row_sum<LONG>(sq, red[turn]);
+        turn ^= 1;
+        const float rstd = 1.0f / sqrtf(sq / float(H) + p.eps);
+        for (int64_t i = 0; i < turns; ++i) {
+            const int64_t col = (i * LONG + threadIdx.x) * 4;
+            const int left = sum4(col, f);  // may be none, but a block's lanes all take part below
+            float g[4] = {1.0f, 1.0f, 1.0f, 1.0f};
+            if (p.gamma) unpack4(g, load4<false>(p.gamma, 0, col, left), 0);
+            if (p.s) store4<false>(p.s, p.s_bf16, row * H + col, left, f);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) f[j] = f[j] * rstd * g[j];
+            if (p.y) store4<false>(p.y, p.y_bf16, row * H + col, left, f);
+            if (p.q) put_packed(p.q + row * H, p.q_scale + row * blocks, int(col), left, f);
+        }
+        if (threadIdx.x == 0 && p.rstd) p.rstd[row] = rstd;
+    }
+}
+
+// ds and dx of rows of any length.
+__global__ __launch_bounds__(LONG) void rms_bwd_any_kernel(RmsBwdParams p) {
+    __shared__ float red[2][LONG / 64 + 1];
+    const int64_t H = p.hidden;
+    int turn = 0;
+    for (int64_t row = blockIdx.x; row < p.n_tokens; row += gridDim.x) {
+        const float rstd = p.rstd[row];
+        auto gh = [&](int64_t col, float* g, float* xh) {
+            const int left = int(std::min<int64_t>(4, H - col));
+            unpack4(xh, load4<false>(p.s, p.s_bf16, row * H + col, left), p.s_bf16);
+            unpack4(g, load4<false>(p.dy, p.y_bf16, row * H + col, left), p.y_bf16);
+            float gain[4] = {1.0f, 1.0f, 1.0f, 1.0f};
+            if (p.gamma) unpack4(gain, load4<false>(p.gamma, 0, col, left), 0);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                xh[j] = j < left ? xh[j] * rstd : 0.0f;
+                g[j] *= gain[j];
+            }
+            return left;
+        };
+        float g[4], xh[4], b = 0.0f;
+        for (int64_t col = threadIdx.x * 4; col < H; col += LONG * 4) {
+            gh(col, g, xh);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) b = __builtin_fmaf(g[j], xh[j], b);
+        }
+        const float c2 = row_sum<LONG>(b, red[turn]) / float(H);
+        turn ^= 1;
+        for (int64_t col = threadIdx.x * 4; col < H; col += LONG * 4) {
+            const int left = gh(col, g, xh);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) g[j] = rstd * (g[j] - xh[j] * c2);
+            if (p.ds_in) {
+                float u[4];
+                unpack4(u, load4<false>(p.ds_in, p.s_bf16, row * H + col, left), p.s_bf16);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) g[j] += u[j];
+            }
+            if (p.ds) store4<false>(p.ds, p.s_bf16, row * H + col, left, g);
+            if (p.dx) store4<false>(p.dx, p.x_bf16, row * H + col, left, g);
+        }
+    }
+}
+
+// Partial sums of dgamma for rows of any length: a thread takes four columns of one piece of rows.
+__global__ __launch_bounds__(256) void rms_bwd_cols_kernel(RmsBwdParams p, int parts, int64_t rows_per) {
+    const int64_t H = p.hidden, col = (int64_t(blockIdx.x) * 256 + threadIdx.x) * 4;
+    if (col >= H) return;
+    const int left = int(std::min<int64_t>(4, H - col));
+    for (int q = blockIdx.y; q < parts; q += gridDim.y) {
+        const int64_t r1 = std::min<int64_t>(p.n_tokens, (q + 1) * rows_per);
+        float dg[4] = {};
+        for (int64_t r = q * rows_per; r < r1; ++r) {
+            float d[4], s[4];
+            unpack4(d, load4<false>(p.dy, p.y_bf16, r * H + col, left), p.y_bf16);
+            unpack4(s, load4<false>(p.s, p.s_bf16, r * H + col, left), p.s_bf16);
+            const float rstd = p.rstd[r];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) dg[j] = __builtin_fmaf(d[j], s[j] * rstd, dg[j]);
+        }
+        store4<false>(p.part, 0, q * H + col, left, dg);
+    }
+}
+
+// dgamma: the partial sums of 32 columns a workgroup, 32 pieces apart, then over those.
+constexpr int64_t SUM_GROUPS = int64_t(1) << 20;  // a launch holds less than 2^32 threads
+__global__ __launch_bounds__(1024) void rms_bwd_sum_kernel(RmsBwdParams p, int parts) {
+    __shared__ float sum[32][33];
+    const int64_t H = p.hidden;
+    const int col = threadIdx.x % 32, lane = threadIdx.x / 32;
+    for (int64_t c0 = int64_t(blockIdx.x) * 32; c0 < H; c0 += int64_t(gridDim.x) * 32) {
+        const int64_t c = c0 + col;
+        float v = 0.0f;
+        if (c < H)
+            for (int q = lane; q < parts; q += 32) v += p.part[q * H + c];
+        sum[lane][col] = v;
+        __syncthreads();
+        if (lane == 0 && c < H) {
+            v = 0.0f;
+#pragma unroll
+            for (int l = 0; l < 32; ++l) v += sum[l][col];
+            p.dgamma[c] = p.accumulate ? p.dgamma[c] + v : v;
+        }
+        __syncthreads();
+    }
+}
+
+// Lanes a row and vectors of four a lane of the register kernels: the first that holds the row.
+struct RowShape {
+    int lanes, nv;
+};
+constexpr RowShape ROW_SHAPES[] = {{16, 1},  {32, 1},  {64, 1},  {64, 2},   {64, 3},  {64, 4},
+                                    {256, 2}, {256, 3}, {256, 4}, {1024, 2}, {1024, 4}};
+constexpr int N_ROW_SHAPES = sizeof ROW_SHAPES / sizeof ROW_SHAPES[0];
+int row_shape(int32_t hidden) {
+    for (int i = 0; i < N_ROW_SHAPES; ++i)
+        if (int64_t(ROW_SHAPES[i].lanes) * ROW_SHAPES[i].nv * 4 >= hidden) return i;
+    return -1;
+}
+int rows_per_group(int32_t hidden) {
+    const int i = row_shape(hidden);
+    return i < 0 ? 8 : row_threads(ROW_SHAPES[i].lanes) / ROW_SHAPES[i].lanes;
+}
+
+template <int I, bool FULL>
+void launch_rms(const RmsParams& p, unsigned grid, hipStream_t stream) {
+    hipLaunchKernelGGL((rms_kernel<ROW_SHAPES[I].lanes, ROW_SHAPES[I].nv, FULL>), dim3(grid),
+                       dim3(row_threads(ROW_SHAPES[I].lanes)), 0, stream, p);
+}
+template <int I, bool FULL>
+void launch_rms(const RmsBwdParams& p, unsigned grid, hipStream_t stream) {
+    hipLaunchKernelGGL((rms_bwd_kernel<ROW_SHAPES[I].lanes, ROW_SHAPES[I].nv, FULL>), dim3(grid),
+                       dim3(row_threads(ROW_SHAPES[I].lanes)), 0, stream, p);
+}
+template <int I, class P>
+void launch_rows(int shape, const P& p, unsigned grid, hipStream_t stream) {
+    if constexpr (I < N_ROW_SHAPES) {
+        if (shape != I) return launch_rows<I + 1>(shape, p, grid, stream);
+        const bool full = p.hidden == ROW_SHAPES[I].lanes * ROW_SHAPES[I].nv * 4;
+        full ? launch_rms<I, true>(p, grid, stream) : launch_rms<I, false>(p, grid, stream);
+    }
+}
+
+// Workgroups of the backward, each leaving one partial row: two a CU at most.
+int rms_parts(int64_t n_tokens, int32_t hidden) {
+    const int per = rows_per_group(hidden);
+    return int(std::min<int64_t>(512, (n_tokens + per - 1) / per));
+}
+
+}  // namespace
+
+hipError_t run_rms_norm(const RmsParams& p, const DeviceInfo& dev, hipStream_t stream) {
+    const int shape = row_shape(p.hidden), cus = std::max(dev.cu_count, 1);
+    if (shape < 0) {
+        const unsigned grid = unsigned(std::min<int64_t>(p.n_tokens, 8 * cus));
+        hipLaunchKernelGGL(rms_any_kernel, dim3(grid), dim3(LONG), 0, stream, p);
+        return hipGetLastError();
+    }
+    const int per = rows_per_group(p.hidden);
+    launch_rows<0>(shape, p, unsigned(std::min<int64_t>((p.n_tokens + per - 1) / per, 16 * cus)), stream);
+    return hipGetLastError();
+}
+
+size_t rms_bwd_workspace_bytes(int64_t n_tokens, int32_t hidden) {
+    return size_t(rms_parts(n_tokens, hidden)) * size_t(hidden) * sizeof(float);
+}
+
+hipError_t run_rms_norm_backward(const RmsBwdParams& p, const DeviceInfo& dev, hipStream_t stream) {
+    const int shape = row_shape(p.hidden), parts = rms_parts(p.n_tokens, p.hidden);
+    if (p.n_tokens > 0 && shape >= 0) {
+        launch_rows<0>(shape, p, unsigned(parts), stream);
+    } else if (p.n_tokens > 0) {
+        if (p.ds || p.dx) {
+            const unsigned grid = unsigned(std::min<int64_t>(p.n_tokens, 8 * std::max(dev.cu_count, 1)));
+            hipLaunchKernelGGL(rms_bwd_any_kernel, dim3(grid), dim3(LONG), 0, stream, p);
+        }
+        if (p.dgamma)
+            hipLaunchKernelGGL(rms_bwd_cols_kernel, dim3(unsigned((int64_t(p.hidden) + 1023) / 1024), unsigned(parts)),
+                               dim3(256), 0, stream, p, parts, (p.n_tokens + parts - 1) / parts);
+    }
+    if (p.dgamma)
+        hipLaunchKernelGGL(rms_bwd_sum_kernel, dim3(unsigned(std::min<int64_t>(SUM_GROUPS, (int64_t(p.hidden) + 31) / 32))),
+                           dim3(1024), 0, stream, p, parts);
+    return hipGetLastError();
+}
+
+}  // namespace fff

@@ -87,4 +87,55 @@ __device__ __forceinline__ void store4(void* base, int bf, int64_t e, int left, 
     }
 }
 
+// Eight values from element e on of a matrix of `all` elements: bf16 in one 16-byte load, fp32 in two.
+// A vector may run on into the next row (its values are the caller's to leave out): only those that
+// end behind the matrix are read one by one, so that no row's tail costs eight loads.
+struct Raw8 {
+    Raw4 a, b;  // bf16: a alone
+};
+typedef uint32_t u32x4_a2 __attribute__((ext_vector_type(4), aligned(2)));
+
+__device__ __forceinline__ Raw8 load8(const void* base, int bf, int64_t e, int64_t all) {
+    Raw8 r = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+    if (bf) {
+        const uint16_t* p = static_cast<const uint16_t*>(base) + e;
+        if (e + 8 <= all) {
+            r.a = *reinterpret_cast<const u32x4_a2*>(p);
+        } else {
+            for (int j = 0; j < 8 && e + j < all; ++j) r.a[j / 2] |= uint32_t(p[j]) << (j % 2 * 16);
+        }
+    } else {
+        const uint32_t* p = static_cast<const uint32_t*>(base) + e;
+        if (e + 8 <= all) {
+            r.a = *reinterpret_cast<const u32x4_a4*>(p);
+            r.b = *reinterpret_cast<const u32x4_a4*>(p + 4);
+        } else {
+            for (int j = 0; j < 8 && e + j < all; ++j) (j < 4 ? r.a : r.b)[j % 4] = p[j];
+        }
+    }
+    return r;
+}
+__device__ __forceinline__ void unpack8(float* f, const Raw8& r, int bf) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        f[2 * j] = __uint_as_float(bf ? r.a[j] << 16 : j < 2 ? r.a[2 * j] : r.b[2 * j - 4]);
+        f[2 * j + 1] = __uint_as_float(bf ? r.a[j] & 0xffff0000u : j < 2 ? r.a[2 * j + 1] : r.b[2 * j - 3]);
+    }
+}
+// `left` of the eight are in the row.
+__device__ __forceinline__ void store8(void* base, int bf, int64_t e, int left, const float* f) {
+    if (left >= 8) {
+        if (bf) {
+            *reinterpret_cast<u32x4_a2*>(static_cast<uint16_t*>(base) + e) =
+                u32x4_a2{pack2(f[0], f[1]), pack2(f[2], f[3]), pack2(f[4], f[5]), pack2(f[6], f[7])};
+        } else {
+            store4<true>(base, 0, e, 4, f);
+            store4<true>(base, 0, e + 4, 4, f + 4);
+        }
+    } else {
+        store4<false>(base, bf, e, left, f);
+        if (left > 4) store4<false>(base, bf, e + 4, left - 4, f + 4);
+    }
+}
+
 }  // namespace fff

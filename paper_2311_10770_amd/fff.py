@@ -73,7 +73,9 @@ EXPORTS = ("fff_forward", "fff_forward_ex", "fff_forward_static", "fff_workspace
            "fff_last_hip_error", "fff_version", "fff_layer_norm", "fff_layer_norm_backward",
            "fff_layer_norm_backward_workspace_bytes", "fff_dropout", "fff_group_rows", "fff_group_rows_workspace_bytes",
            "fff_grouped_matmul", "fff_grouped_weight_grad", "fff_grouped_weight_grad_workspace_bytes",
-           "fff_describe_grouped_matmul", "fff_describe_grouped_weight_grad")
+           "fff_describe_grouped_matmul", "fff_describe_grouped_weight_grad", "fff_route", "fff_route_backward",
+           "fff_combine", "fff_combine_backward", "fff_rms_norm", "fff_rms_norm_backward",
+           "fff_rms_norm_backward_workspace_bytes", "fff_pack_rows", "fff_unpack_rows")
 
 
 def load_library(path: Path | str | None = None):
@@ -106,7 +108,8 @@ def load_library(path: Path | str | None = None):
     lib.fff_backward_workspace_bytes.argtypes = [c_int64, c_int32, c_int32, c_int32]
     lib.fff_backward_workspace_bytes.restype = c_size_t
     for name in ("fff_layer_norm", "fff_layer_norm_backward", "fff_dropout", "fff_group_rows", "fff_grouped_matmul",
-                 "fff_grouped_weight_grad"):
+                 "fff_grouped_weight_grad", "fff_route", "fff_route_backward", "fff_combine", "fff_combine_backward",
+                 "fff_rms_norm", "fff_rms_norm_backward", "fff_pack_rows", "fff_unpack_rows"):
         getattr(lib, name).argtypes = [c_void_p]  # the struct's address
         getattr(lib, name).restype = c_int
     for name in ("fff_describe_grouped_matmul", "fff_describe_grouped_weight_grad"):
@@ -115,8 +118,9 @@ def load_library(path: Path | str | None = None):
     lib.fff_layer_norm_backward_workspace_bytes.argtypes = [c_int64, c_int32]
     lib.fff_group_rows_workspace_bytes.argtypes = [c_int64, c_int32, c_int32]
     lib.fff_grouped_weight_grad_workspace_bytes.argtypes = [c_int64, c_int32, c_int32, c_int32]
+    lib.fff_rms_norm_backward_workspace_bytes.argtypes = [c_int64, c_int32]
     for name in ("fff_layer_norm_backward_workspace_bytes", "fff_group_rows_workspace_bytes",
-                 "fff_grouped_weight_grad_workspace_bytes"):
+                 "fff_grouped_weight_grad_workspace_bytes", "fff_rms_norm_backward_workspace_bytes"):
         getattr(lib, name).restype = c_size_t
     lib.fff_status_str.argtypes = [c_int]
     lib.fff_status_str.restype = c_char_p
