@@ -13,6 +13,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <type_traits>
 
 namespace fff {
 
@@ -169,6 +170,375 @@ __global__ __launch_bounds__(ANY) void route_any_kernel(RouteParams p) {
     }
 }
 
+// ---- up to 1024 experts: LPT lanes a token ---------------------------------
+
+// Largest v of the LPT lanes of a token, for each of them.
+template <int LPT>
+__device__ __forceinline__ float group_max(float v) {
+    auto dpp = [&](auto ctrl) {
+        v = __builtin_fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), ctrl.value, 0xf, 0xf, false)));
+    };
+    dpp(std::integral_constant<int, 0x128>{});  // row_ror:8, 4, 2, 1
+    dpp(std::integral_constant<int, 0x124>{});
+    dpp(std::integral_constant<int, 0x122>{});
+    dpp(std::integral_constant<int, 0x121>{});
+    if constexpr (LPT >= 32) v = __builtin_fmaxf(v, __shfl_xor(v, 16));
+    if constexpr (LPT == 64) v = __builtin_fmaxf(v, __shfl_xor(v, 32));
+    return v;
+}
+// How many of the 16 values of o that lane's row holds are at least v.
+template <int R = 0>
+__device__ __forceinline__ int row_at_least(float v, float o) {
+    if constexpr (R == 16) {
+        return 0;
+    } else {
+        const float w = R == 0 ? o : __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(o), 0x120 + R, 0xf, 0xf, false));
+        return (w >= v) + row_at_least<R + 1>(v, o);
+    }
+}
+// How many of the LPT lanes' values are at least v.
+template <int LPT>
+__device__ __forceinline__ int group_at_least(float v) {
+    int n = row_at_least(v, v);
+    if constexpr (LPT >= 32) n += row_at_least(v, __shfl_xor(v, 16));
+    if constexpr (LPT == 64) n += row_at_least(v, __shfl_xor(v, 32)) + row_at_least(v, __shfl_xor(v, 48));
+    return n;
+}
+// Sum of v over the token's lanes before this one.
+template <int LPT>
+__device__ __forceinline__ int group_before(int v, int sl) {
+    int sum = v;
+#pragma unroll
+    for (int d = 1; d < LPT; d *= 2) {
+        const int w = __shfl_up(sum, d);
+        if (sl >= d) sum += w;
+    }
+    return sum - v;
+}
+template <int LPT>
+__device__ __forceinline__ double group_add(double v) {
+#pragma unroll
+    for (int d = 1; d < LPT; d *= 2) v += __shfl_xor(v, d);
+    return v;
+}
+__device__ __forceinline__ void wave_sync() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// What one wave holds in LDS: scores by expert while groups are chosen, then the candidates of its tokens.
+template <int LPT, int V>
+struct RouteLds {
+    static constexpr int CAP = 4 * LPT;  // candidates of a token
+    union {
+        float score[64 * V];
+        struct {
+            double c[256];
+            float l[256];
+            int e[256];
+        } can;
+    };
+    float chosen[64];  // logits of the chosen
+};
+
+// LPT lanes a token, four neighbouring experts a vector, V experts a lane.
+//
+// Choices are first formed in fp32 (c32, whose error is below `slack` / 2).  Of the LPT lanes' largest, the
+// top_k-th is no more than the top_k-th largest of all, so only experts within the slack of it
+// can be chosen: a dozen of 256.  These candidates alone are evaluated and ordered in fp64, each
+// by counting those before it.  Where something would need more than the candidates' own scores (the softmax's sum
+// behind a close order, groups whose sums lie within the slack, more candidates than there is room for, as
+// where all logits are equal) the wave forms that in fp64, too.
+template <int LPT, int V>
+__global__ __launch_bounds__(256, 4) void route_kernel(RouteParams p) {
+    using Lds = RouteLds<LPT, V>;
+    constexpr int TPW = 64 / LPT, CAP = Lds::CAP;
+    __shared__ Lds lds4[4];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, sl = lane % LPT, tok = lane / LPT, first = tok * LPT;
+    Lds& lds = lds4[wave];
+    const int E = p.n_experts, K = p.top_k, G = p.n_groups, size = E / G;
+    const uint32_t inverse = ((1u << 20) + size - 1) / size;  // e / size = e inverse >> 20 for e < 1024
+    const bool sigmoid = p.score != SCORE_SOFTMAX, top2 = p.group_score == GROUP_TOP2;
+    const bool by_score = p.bias || (G > 1 && top2);  // whether fp32 scores take part in the choice
+    const bool sums = !sigmoid && (by_score || !p.renormalise);
+    for (int64_t r0 = (int64_t(blockIdx.x) * 4 + wave) * TPW; r0 < p.n_tokens; r0 += int64_t(gridDim.x) * (4 * TPW)) {
+        const int64_t row = r0 + tok;
+        const bool in = row < p.n_tokens;
+        float l[V], c[V];
+#pragma unroll
+        for (int q = 0; q < V / 4; ++q) {
+            const int col = (q * LPT + sl) * 4, left = in ? E - col : 0;
+            unpack4(l + 4 * q, load4<false>(p.logits, p.bf16, row * E + col, left), p.bf16);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) l[4 * q + j] = j < left ? clean_logit(l[4 * q + j]) : NONE;
+        }
+        Softmax soft{0.0f, 1.0};
+        float z = 1.0f;
+        if (!sigmoid) {
+            float most = l[0];
+#pragma unroll
+            for (int v = 1; v < V; ++v) most = __builtin_fmaxf(most, l[v]);
+            most = group_max<LPT>(most);
+            soft.most = most > NONE ? most : 0.0f;
+        }
+        if (sums) {
+            z = 0.0f;
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                c[v] = expf(l[v] - soft.most);  // 0 where there is none
+                z += c[v];
+            }
+            z = group_sum<LPT>(z);
+            z = z > 0.0f ? z : 1.0f;
+            soft.sum = double(z);
+        }
+        bool exact_sum = false;  // soft.sum is formed in fp64
+        auto sum64 = [&] {
+            if (exact_sum || sigmoid) return;
+            double t = 0.0;
+#pragma unroll 1
+            for (int v = 0; v < V; ++v) {
+                float u = l[0];
+#pragma unroll
+                for (int i = 1; i < V; ++i) u = v == i ? l[i] : u;
+                t += u > NONE ? exp(double(u) - double(soft.most)) : 0.0;
+            }
+            t = group_add<LPT>(t);
+            soft.sum = t > 0.0 ? t : 1.0;
+            exact_sum = true;
+        };
+        const float share = sigmoid ? 1.0f : 1.0f / z;  // no score is larger
+        if (by_score) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                if (sigmoid) c[v] = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504088896341f * l[v]));
+                else c[v] *= share;
+            }
+        }
+        const float* bias = p.bias;
+        auto add_bias = [&] {
+#pragma unroll
+            for (int q = 0; q < V / 4; ++q) {
+                const int col = (q * LPT + sl) * 4;
+                float b[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                if (bias) unpack4(b, load4<false>(bias, 0, col, E - col), 0);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int v = 4 * q + j;
+                    const float s = bias ? c[v] + b[j] : l[v];
+                    c[v] = l[v] > NONE && s > NONE ? s : NONE;
+                }
+            }
+        };
+        // an expert's choice in 64 bits
+        auto choice = [&](float lg, int e) {
+            if (lg == NONE) return -HUGE_VAL;
+            const double d = bias ? score(lg, sigmoid, soft) + double(bias[e]) : double(lg);
+            return d > -HUGE_VAL ? d : -HUGE_VAL;
+        };
+        const float slack = by_score ? (sigmoid ? 7.62939453125e-06f : 1.52587890625e-05f * share) : 0.0f;  // 2^-17, 2^-16
+
+        uint64_t kept = ~0ull;
+        if (G > 1) {
+            // every lane below G has a group, and reads its scores from a place of its own on
+            const bool plain = top2 && !bias;  // by s, not by c
+            if (!plain) add_bias();
+#pragma unroll
+            for (int q = 0; q < V / 4; ++q)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int v = 4 * q + j;
+                    lds.score[tok * (LPT * V) + (q * LPT + sl) * 4 + j] = plain && l[v] == NONE ? NONE : c[v];
+                }
+            wave_sync();
+            float a = NONE, b = NONE;
+            if (sl < G) {
+                const float* group = lds.score + tok * (LPT * V) + sl * size;
+                int at = sl % size;
+                for (int i = 0; i < size; ++i) {
+                    const float v = group[at];
+                    at = at + 1 == size ? 0 : at + 1;
+                    b = __builtin_fmaxf(b, __builtin_fminf(a, v));
+                    a = __builtin_fmaxf(a, v);
+                }
+            }
+            const float value = top2 && b > NONE ? a + b : a;
+            int before = 0;
+            for (int h = 0; h < G; ++h) {
+                const float v = __shfl(value, first + h);
+                before += v > value || (v == value && h < sl);
+            }
+            bool keep = value > NONE && before < p.top_groups;
+            if (by_score) {
+                const float worst = -group_max<LPT>(keep ? -value : NONE);
+                const float next = group_max<LPT>(!keep ? value : NONE);
+                const float near = 2.0f * slack + 4.76837158203125e-07f * (__builtin_fabsf(worst) + __builtin_fabsf(next));
+                if (__any(next > NONE && !(worst - next > near))) {
+                    sum64();
+                    double x = -HUGE_VAL, y = -HUGE_VAL;
+                    if (sl < G && in) {
+                        for (int e = sl * size; e < (sl + 1) * size; ++e) {
+                            const float lg = logit(p, row, e);
+                            double d = choice(lg, e);
+                            if (plain && d > -HUGE_VAL) d = score(lg, sigmoid, soft);
+                            y = fmax(y, fmin(x, d));
+                            x = fmax(x, d);
+                        }
+                    }
+                    const double exact = top2 && y > -HUGE_VAL ? x + y : x;
+                    before = 0;
+                    for (int h = 0; h < G; ++h) {
+                        const double v = __shfl(exact, first + h);
+                        before += v > exact || (v == exact && h < sl);
+                    }
+                    keep = exact > -HUGE_VAL && before < p.top_groups;
+                }
+            }
+            kept = __ballot(keep) >> first;
+            if (plain) add_bias();
+#pragma unroll
+            for (int q = 0; q < V / 4; ++q)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t g = uint32_t((q * LPT + sl) * 4 + j) * inverse >> 20;
+                    c[4 * q + j] = kept >> (g & 63) & 1 ? c[4 * q + j] : NONE;
+                }
+            wave_sync();
+        } else {
+            add_bias();
+        }
+
+        // candidates: not below the top_k-th largest of the lanes' largest, less the slack
+        float most = c[0];
+#pragma unroll
+        for (int v = 1; v < V; ++v) most = __builtin_fmaxf(most, c[v]);
+        float bar = group_max<LPT>(group_at_least<LPT>(most) >= K ? most : NONE);
+        if (bias && bar > NONE && bar < __builtin_inff()) bar -= slack + 4.76837158203125e-07f * __builtin_fabsf(bar);
+        int n = 0;
+#pragma unroll
+        for (int v = 0; v < V; ++v) n += c[v] > NONE && c[v] >= bar;
+        int at = group_before<LPT>(n, sl);
+        n = __shfl(at + n, first + LPT - 1);  // of the token
+        const bool over = n > CAP;
+        if (!over) {
+#pragma unroll
+            for (int q = 0; q < V / 4; ++q)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int v = 4 * q + j;
+                    if (c[v] > NONE && c[v] >= bar) {
+                        lds.can.l[tok * CAP + at] = l[v];
+                        lds.can.e[tok * CAP + at] = (q * LPT + sl) * 4 + j;
+                        ++at;
+                    }
+                }
+        }
+        const uint64_t overs = __ballot(over);
+        int got = over ? 0 : n;  // candidates of the token, and below the chosen
+        int longest = got;
+#pragma unroll
+        for (int d = LPT; d < 64; d *= 2) longest = max(longest, __shfl_xor(longest, d));
+        longest = __builtin_amdgcn_readfirstlane(longest);
+        wave_sync();
+        for (bool again = true; again;) {
+            for (int i = sl; i < got; i += LPT) lds.can.c[tok * CAP + i] = choice(lds.can.l[tok * CAP + i], lds.can.e[tok * CAP + i]);
+            wave_sync();
+            bool close = false;
+            for (int i0 = 0; i0 < longest; i0 += LPT) {
+                const int i = i0 + sl;
+                const bool mine = i < got;
+                const double d = mine ? lds.can.c[tok * CAP + i] : 0.0;
+                const int e = mine ? lds.can.e[tok * CAP + i] : 0;
+                int before = 0;
+                for (int o = 0; o < longest; ++o) {
+                    const double w = lds.can.c[tok * CAP + o];
+                    const int f = lds.can.e[tok * CAP + o];
+                    if (o < got) {
+                        before += w > d || (w == d && f < e);
+                        // the softmax's sum is fp32's: an order within its error of the scores needs it in fp64
+                        close |= fabs(w - d) < double(slack) && f != e;
+                    }
+                }
+                if (mine && before < K) {
+                    p.ids[row * K + before] = e;
+                    lds.chosen[first + before] = lds.can.l[tok * CAP + i];
+                }
+            }
+            again = bias && !sigmoid && !exact_sum && __any(close);
+            if (again) sum64();
+            wave_sync();
+        }
+        got = min(got, K);
+        // tokens with more candidates: the next pick is the best behind the one before it, by the whole wave
+        for (uint64_t left = overs; left;) {
+            const int src = __builtin_ctzll(left), t2 = src / LPT;
+            left &= ~(((LPT == 64 ? 0 : 1ull << LPT % 64) - 1) << (t2 * LPT));
+            const int64_t r2 = r0 + t2;
+            if (bias) sum64();
+            const double total = __shfl(soft.sum, src);
+            const Softmax s2{__shfl(soft.most, src), total};
+            const uint64_t k2 = uint64_t(uint32_t(__shfl(int(uint32_t(kept)), src))) |
+                                uint64_t(uint32_t(__shfl(int(uint32_t(kept >> 32)), src))) << 32;
+            double last = HUGE_VAL;
+            int last_at = -1, picks = 0;
+            for (; picks < K; ++picks) {
+                double best = -HUGE_VAL;
+                int where = E;
+                float picked = NONE;
+                for (int e = lane; e < E; e += 64) {
+                    if (G > 1 && !(k2 >> (uint32_t(e) * inverse >> 20 & 63) & 1)) continue;
+                    const float lg = logit(p, r2, e);
+                    if (lg == NONE) continue;
+                    const double d = bias ? score(lg, sigmoid, s2) + double(bias[e]) : double(lg);
+                    if (d > best && (d < last || (d == last && e > last_at))) {
+                        best = d;
+                        where = e;
+                        picked = lg;
+                    }
+                }
+#pragma unroll
+                for (int x = 1; x < 64; x *= 2) {
+                    const double w = __shfl_xor(best, x);
+                    const int f = __shfl_xor(where, x);
+                    const float u = __shfl_xor(picked, x);
+                    if (w > best || (w == best && f < where)) {
+                        best = w;
+                        where = f;
+                        picked = u;
+                    }
+                }
+                if (best == -HUGE_VAL) break;
+                last = best;
+                last_at = where;
+                if (lane == 0) {
+                    p.ids[r2 * K + picks] = where;
+                    lds.chosen[t2 * LPT + picks] = picked;
+                }
+            }
+            if (tok == t2) got = picks;
+        }
+        wave_sync();
+        // weights of the chosen, a lane each
+        const float lg = sl < got ? lds.chosen[lane] : NONE;
+        float w = 0.0f;
+        if (p.renormalise) {
+            // from the largest chosen logit where scores underflow: they keep their shares
+            const float top = group_max<LPT>(lg);
+            const bool shifted = !sigmoid || top < -60.0f;
+            if (sl < got) w = shifted ? expf(lg - top) : 1.0f / (1.0f + expf(-lg));
+            const float total = group_sum<LPT>(w);
+            w = sl < got ? w / total : 0.0f;
+        } else if (sl < got) {
+            w = sigmoid ? 1.0f / (1.0f + expf(-lg)) : expf(lg - soft.most) / z;
+        }
+        if (in && sl < K) {
+            p.weights[row * K + sl] = p.scale * w;
+            if (sl >= got) p.ids[row * K + sl] = -1;
+        }
+        wave_sync();
+    }
+}
+
 // The gradient: a wave a token.
 __global__ __launch_bounds__(256) void route_bwd_any_kernel(RouteBwdParams p) {
     const int lane = threadIdx.x & 63, E = p.n_experts, K = p.top_k;
@@ -237,7 +607,25 @@ __global__ __launch_bounds__(256) void route_bwd_any_kernel(RouteBwdParams p) {
 }  // namespace
 
 hipError_t run_route(const RouteParams& p, const DeviceInfo& dev, hipStream_t stream) {
-    const unsigned grid = unsigned(std::min<int64_t>(p.n_tokens, 8 * std::max(dev.cu_count, 1)));
+    const int cus = std::max(dev.cu_count, 1);
+    auto launch = [&](auto lpt, auto v) {
+        constexpr int per = 4 * 64 / lpt.value;
+        const unsigned grid = unsigned(std::min<int64_t>((p.n_tokens + per - 1) / per, 16 * cus));
+        hipLaunchKernelGGL((route_kernel<lpt.value, v.value>), dim3(grid), dim3(256), 0, stream, p);
+    };
+    auto of = [&](auto lpt) {
+        using N = decltype(lpt);
+        if (p.n_experts <= 4 * N::value) launch(lpt, std::integral_constant<int, 4>{});
+        else if (p.n_experts <= 8 * N::value) launch(lpt, std::integral_constant<int, 8>{});
+        else launch(lpt, std::integral_constant<int, 16>{});
+        return hipGetLastError();
+    };
+    // lanes a token: twice as many as it chooses experts (fewer candidates), one at least a group
+    const int lanes = std::max({2 * p.top_k, p.n_groups, (p.n_experts + 15) / 16});
+    if (lanes <= 16) return of(std::integral_constant<int, 16>{});
+    if (lanes <= 32) return of(std::integral_constant<int, 32>{});
+    if (p.n_groups <= 64 && p.n_experts <= 1024) return of(std::integral_constant<int, 64>{});
+    const unsigned grid = unsigned(std::min<int64_t>(p.n_tokens, 8 * cus));
     hipLaunchKernelGGL(route_any_kernel, dim3(grid), dim3(ANY), 0, stream, p);
     return hipGetLastError();
 }
