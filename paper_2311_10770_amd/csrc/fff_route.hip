@@ -39,6 +39,27 @@ __device__ __forceinline__ double score(float l, int sigmoid, const Softmax& m) 
     return sigmoid ? 1.0 / (1.0 + exp(-double(l))) : exp(double(l) - double(m.most)) / m.sum;
 }
 
+// What an expert is chosen by.
+__device__ __forceinline__ double choice(const RouteParams& p, float l, int e, const Softmax& m) {
+    if (l == NONE) return -HUGE_VAL;
+    const double c = p.bias ? score(l, p.score, m) + double(p.bias[e]) : double(l);
+    return c > -HUGE_VAL ? c : -HUGE_VAL;
+}
+
+// The value of a token's group g in fp64.
+__device__ __forceinline__ double group_value(const RouteParams& p, int64_t row, int g, Softmax m) {
+    const int size = p.n_experts / p.n_groups;
+    double a = -HUGE_VAL, b = -HUGE_VAL;
+    for (int e = g * size; e < (g + 1) * size; ++e) {
+        const float l = logit(p, row, e);
+        double c = choice(p, l, e, m);
+        if (!p.bias && p.group_score == GROUP_TOP2 && c > -HUGE_VAL) c = score(l, p.score, m);
+        b = fmax(b, fmin(a, c));
+        a = fmax(a, c);
+    }
+    return p.group_score == GROUP_TOP2 && b > -HUGE_VAL ? a + b : a;
+}
+
 constexpr int ANY = 256;  // threads of the kernel for any size
 
 // Largest v (lowest i among equals) of the workgroup, for every thread.
@@ -99,23 +120,10 @@ __global__ __launch_bounds__(ANY) void route_any_kernel(RouteParams p) {
             }
             m.sum = block_add(sum, sv);
         }
-        auto choice = [&](int e) {
-            const float l = logit(p, row, e);
-            if (l == NONE) return -HUGE_VAL;
-            const double c = p.bias ? score(l, p.score, m) + double(p.bias[e]) : double(l);
-            return c > -HUGE_VAL ? c : -HUGE_VAL;
-        };
         if (G > 1) {
             __syncthreads();
             for (int g = tid; g < G; g += ANY) {
-                double a = -HUGE_VAL, b = -HUGE_VAL;
-                for (int e = g * size; e < (g + 1) * size; ++e) {
-                    double c = choice(e);
-                    if (!p.bias && p.group_score == GROUP_TOP2 && c > -HUGE_VAL) c = score(logit(p, row, e), p.score, m);
-                    b = fmax(b, fmin(a, c));
-                    a = fmax(a, c);
-                }
-                s_group[g] = p.group_score == GROUP_TOP2 && b > -HUGE_VAL ? a + b : a;
+                s_group[g] = group_value(p, row, g, m);
             }
             __syncthreads();
             for (int g = tid; g < G; g += ANY) {
@@ -133,7 +141,7 @@ __global__ __launch_bounds__(ANY) void route_any_kernel(RouteParams p) {
             int at = E;
             for (int e = tid; e < E; e += ANY) {
                 if (G > 1 && !s_kept[e / size]) continue;
-                const double c = choice(e);
+                const double c = choice(p, logit(p, row, e), e, m);
                 if (c > best && (c < last || (c == last && e > last_at))) {
                     best = c;
                     at = e;
@@ -215,15 +223,96 @@ __device__ __forceinline__ int group_before(int v, int sl) {
     }
     return sum - v;
 }
-template <int LPT>
-__device__ __forceinline__ double group_add(double v) {
-#pragma unroll
-    for (int d = 1; d < LPT; d *= 2) v += __shfl_xor(v, d);
-    return v;
-}
 __device__ __forceinline__ void wave_sync() {
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
+}
+
+// A whole token in fp64 by a whole wave: each pick is the best expert behind the one before it in the order.  For
+// the few tokens that route_kernel leaves.  At most 64 groups.
+__device__ __forceinline__ void route_token(const RouteParams& p, int64_t row) {
+    const int lane = threadIdx.x & 63, E = p.n_experts, G = p.n_groups, size = E / G;
+    auto best_of = [](double& v, int& i, float& l) {
+#pragma unroll 1
+        for (int x = 1; x < 64; x *= 2) {
+            const double w = __shfl_xor(v, x);
+            const int f = __shfl_xor(i, x);
+            const float u = __shfl_xor(l, x);
+            if (w > v || (w == v && f < i)) {
+                v = w;
+                i = f;
+                l = u;
+            }
+        }
+    };
+    Softmax m{0.0f, 1.0};
+    if (p.score == SCORE_SOFTMAX) {
+        float most = NONE;
+        for (int e = lane; e < E; e += 64) most = __builtin_fmaxf(most, logit(p, row, e));
+#pragma unroll 1
+        for (int x = 1; x < 64; x *= 2) most = __builtin_fmaxf(most, __shfl_xor(most, x));
+        m.most = most > NONE ? most : 0.0f;
+        double sum = 0.0;
+        for (int e = lane; e < E; e += 64) {
+            const float l = logit(p, row, e);
+            sum += l > NONE ? exp(double(l) - double(m.most)) : 0.0;
+        }
+#pragma unroll 1
+        for (int x = 1; x < 64; x *= 2) sum += __shfl_xor(sum, x);
+        m.sum = sum > 0.0 ? sum : 1.0;
+    }
+    uint64_t kept = ~0ull;
+    if (G > 1) {
+        const double value = lane < G ? group_value(p, row, lane, m) : -HUGE_VAL;
+        int before = 0;
+        for (int h = 0; h < G; ++h) {
+            const double v = __shfl(value, h);
+            before += v > value || (v == value && h < lane);
+        }
+        kept = __ballot(value > -HUGE_VAL && before < p.top_groups);
+    }
+    double last = HUGE_VAL;
+    int last_at = -1, picks = 0, mine = -1;
+    float own = NONE;  // logit of the pick that this lane keeps
+    for (; picks < p.top_k; ++picks) {
+        double best = -HUGE_VAL;
+        int where = E;
+        float picked = NONE;
+        for (int e = lane; e < E; e += 64) {
+            if (!(kept >> (e / size & 63) & 1) && G > 1) continue;
+            const float l = logit(p, row, e);
+            const double c = choice(p, l, e, m);
+            if (c > best && (c < last || (c == last && e > last_at))) {
+                best = c;
+                where = e;
+                picked = l;
+            }
+        }
+        best_of(best, where, picked);
+        if (best == -HUGE_VAL) break;
+        last = best;
+        last_at = where;
+        if (lane == picks) {
+            mine = where;
+            own = picked;
+        }
+    }
+    // renormalised sums start from the largest chosen logit: scores that underflow keep their shares
+    float top = own;
+#pragma unroll 1
+    for (int x = 1; x < 64; x *= 2) top = __builtin_fmaxf(top, __shfl_xor(top, x));
+    double w = 0.0;
+    if (mine >= 0) w = p.renormalise && (p.score == SCORE_SOFTMAX || top < -300.0f) ? exp(double(own) - double(top)) : score(own, p.score, m);
+    if (p.renormalise) {
+        double sum = w;
+#pragma unroll 1
+        for (int x = 1; x < 64; x *= 2) sum += __shfl_xor(sum, x);
+        w = mine >= 0 ? w / sum : 0.0;
+    }
+    if (lane < p.top_k) {
+        p.ids[row * p.top_k + lane] = mine;
+        p.weights[row * p.top_k + lane] = float(double(p.scale) * w);
+    }
 }
 
 // What one wave holds in LDS: scores by expert while groups are chosen, then the candidates of its tokens.
@@ -238,7 +327,8 @@ struct RouteLds {
             int e[256];
         } can;
     };
-    float chosen[64];  // logits of the chosen
+    float chosen[64];  // logits of the chosen, and the experts
+    int ids[64];
 };
 
 // LPT lanes a token, four neighbouring experts a vector, V experts a lane.
@@ -246,11 +336,11 @@ struct RouteLds {
 // Choices are first formed in fp32 (c32, whose error is below `slack` / 2).  Of the LPT lanes' largest, the
 // top_k-th is no more than the top_k-th largest of all, so only experts within the slack of it
 // can be chosen: a dozen of 256.  These candidates alone are evaluated and ordered in fp64, each
-// by counting those before it.  Where something would need more than the candidates' own scores (the softmax's sum
-// behind a close order, groups whose sums lie within the slack, more candidates than there is room for, as
-// where all logits are equal) the wave forms that in fp64, too.
+// by counting those before it.  Tokens that need more than the candidates' own scores in fp64 (the softmax's sum
+// behind a close order, groups whose values lie within the slack) or have more candidates than there is room for (as
+// where all logits are equal) are left to route_token.
 template <int LPT, int V>
-__global__ __launch_bounds__(256, 4) void route_kernel(RouteParams p) {
+__global__ __launch_bounds__(256, 5) void route_kernel(RouteParams p, int64_t row0) {
     using Lds = RouteLds<LPT, V>;
     constexpr int TPW = 64 / LPT, CAP = Lds::CAP;
     __shared__ Lds lds4[4];
@@ -261,282 +351,191 @@ __global__ __launch_bounds__(256, 4) void route_kernel(RouteParams p) {
     const bool sigmoid = p.score != SCORE_SOFTMAX, top2 = p.group_score == GROUP_TOP2;
     const bool by_score = p.bias || (G > 1 && top2);  // whether fp32 scores take part in the choice
     const bool sums = !sigmoid && (by_score || !p.renormalise);
-    for (int64_t r0 = (int64_t(blockIdx.x) * 4 + wave) * TPW; r0 < p.n_tokens; r0 += int64_t(gridDim.x) * (4 * TPW)) {
-        const int64_t row = r0 + tok;
-        const bool in = row < p.n_tokens;
-        float l[V], c[V];
+    const int64_t r0 = (row0 / TPW + int64_t(blockIdx.x) * 4 + wave) * TPW;
+    const int64_t row = r0 + tok;
+    const bool in = row < p.n_tokens;
+    float l[V], c[V];
+#pragma unroll
+    for (int q = 0; q < V / 4; ++q) {
+        const int col = (q * LPT + sl) * 4, left = in ? E - col : 0;
+        unpack4(l + 4 * q, load4<false>(p.logits, p.bf16, row * E + col, left), p.bf16);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) l[4 * q + j] = j < left ? clean_logit(l[4 * q + j]) : NONE;
+    }
+    Softmax soft{0.0f, 1.0};
+    float z = 1.0f;
+    if (!sigmoid) {
+        float most = l[0];
+#pragma unroll
+        for (int v = 1; v < V; ++v) most = __builtin_fmaxf(most, l[v]);
+        most = group_max<LPT>(most);
+        soft.most = most > NONE ? most : 0.0f;
+    }
+    if (sums) {
+        z = 0.0f;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            c[v] = expf(l[v] - soft.most);  // 0 where there is none
+            z += c[v];
+        }
+        z = group_sum<LPT>(z);
+        z = z > 0.0f ? z : 1.0f;
+        soft.sum = double(z);
+    }
+    bool redo = false;  // left to route_token
+    const float share = sigmoid ? 1.0f : 1.0f / z;  // no score is larger
+    if (by_score) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            if (sigmoid) c[v] = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504088896341f * l[v]));
+            else c[v] *= share;
+        }
+    }
+    const float* bias = p.bias;
+    auto add_bias = [&] {
 #pragma unroll
         for (int q = 0; q < V / 4; ++q) {
-            const int col = (q * LPT + sl) * 4, left = in ? E - col : 0;
-            unpack4(l + 4 * q, load4<false>(p.logits, p.bf16, row * E + col, left), p.bf16);
+            const int col = (q * LPT + sl) * 4;
+            float b[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            if (bias) unpack4(b, load4<false>(bias, 0, col, E - col), 0);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) l[4 * q + j] = j < left ? clean_logit(l[4 * q + j]) : NONE;
-        }
-        Softmax soft{0.0f, 1.0};
-        float z = 1.0f;
-        if (!sigmoid) {
-            float most = l[0];
-#pragma unroll
-            for (int v = 1; v < V; ++v) most = __builtin_fmaxf(most, l[v]);
-            most = group_max<LPT>(most);
-            soft.most = most > NONE ? most : 0.0f;
-        }
-        if (sums) {
-            z = 0.0f;
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                c[v] = expf(l[v] - soft.most);  // 0 where there is none
-                z += c[v];
+            for (int j = 0; j < 4; ++j) {
+                const int v = 4 * q + j;
+                const float s = bias ? c[v] + b[j] : l[v];
+                c[v] = l[v] > NONE && s > NONE ? s : NONE;
             }
-            z = group_sum<LPT>(z);
-            z = z > 0.0f ? z : 1.0f;
-            soft.sum = double(z);
         }
-        bool exact_sum = false;  // soft.sum is formed in fp64
-        auto sum64 = [&] {
-            if (exact_sum || sigmoid) return;
-            double t = 0.0;
-#pragma unroll 1
-            for (int v = 0; v < V; ++v) {
-                float u = l[0];
+    };
+    const float slack = by_score ? (sigmoid ? 7.62939453125e-06f : 1.52587890625e-05f * share) : 0.0f;  // 2^-17, 2^-16
+
+    uint64_t kept = ~0ull;
+    if (G > 1) {
+        // every lane below G has a group, and reads its scores from a place of its own on
+        const bool plain = top2 && !bias;  // by s, not by c
+        if (!plain) add_bias();
 #pragma unroll
-                for (int i = 1; i < V; ++i) u = v == i ? l[i] : u;
-                t += u > NONE ? exp(double(u) - double(soft.most)) : 0.0;
+        for (int q = 0; q < V / 4; ++q)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int v = 4 * q + j;
+                lds.score[tok * (LPT * V) + (q * LPT + sl) * 4 + j] = plain && l[v] == NONE ? NONE : c[v];
             }
-            t = group_add<LPT>(t);
-            soft.sum = t > 0.0 ? t : 1.0;
-            exact_sum = true;
-        };
-        const float share = sigmoid ? 1.0f : 1.0f / z;  // no score is larger
+        wave_sync();
+        float a = NONE, b = NONE;
+        if (sl < G) {
+            const float* group = lds.score + tok * (LPT * V) + sl * size;
+            int at = sl % size;
+            for (int i = 0; i < size; ++i) {
+                const float v = group[at];
+                at = at + 1 == size ? 0 : at + 1;
+                b = __builtin_fmaxf(b, __builtin_fminf(a, v));
+                a = __builtin_fmaxf(a, v);
+            }
+        }
+        const float value = top2 && b > NONE ? a + b : a;
+        int before = 0;
+        for (int h = 0; h < G; ++h) {
+            const float v = __shfl(value, first + h);
+            before += v > value || (v == value && h < sl);
+        }
+        bool keep = value > NONE && before < p.top_groups;
         if (by_score) {
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                if (sigmoid) c[v] = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504088896341f * l[v]));
-                else c[v] *= share;
-            }
+            const float worst = -group_max<LPT>(keep ? -value : NONE);
+            const float next = group_max<LPT>(!keep ? value : NONE);
+            const float near = 2.0f * slack + 4.76837158203125e-07f * (__builtin_fabsf(worst) + __builtin_fabsf(next));
+            redo = next > NONE && !(worst - next > near);
         }
-        const float* bias = p.bias;
-        auto add_bias = [&] {
+        kept = __ballot(keep) >> first;
+        if (plain) add_bias();
 #pragma unroll
-            for (int q = 0; q < V / 4; ++q) {
-                const int col = (q * LPT + sl) * 4;
-                float b[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-                if (bias) unpack4(b, load4<false>(bias, 0, col, E - col), 0);
+        for (int q = 0; q < V / 4; ++q)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int v = 4 * q + j;
-                    const float s = bias ? c[v] + b[j] : l[v];
-                    c[v] = l[v] > NONE && s > NONE ? s : NONE;
-                }
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t g = uint32_t((q * LPT + sl) * 4 + j) * inverse >> 20;
+                c[4 * q + j] = kept >> (g & 63) & 1 ? c[4 * q + j] : NONE;
             }
-        };
-        // an expert's choice in 64 bits
-        auto choice = [&](float lg, int e) {
-            if (lg == NONE) return -HUGE_VAL;
-            const double d = bias ? score(lg, sigmoid, soft) + double(bias[e]) : double(lg);
-            return d > -HUGE_VAL ? d : -HUGE_VAL;
-        };
-        const float slack = by_score ? (sigmoid ? 7.62939453125e-06f : 1.52587890625e-05f * share) : 0.0f;  // 2^-17, 2^-16
-
-        uint64_t kept = ~0ull;
-        if (G > 1) {
-            // every lane below G has a group, and reads its scores from a place of its own on
-            const bool plain = top2 && !bias;  // by s, not by c
-            if (!plain) add_bias();
-#pragma unroll
-            for (int q = 0; q < V / 4; ++q)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int v = 4 * q + j;
-                    lds.score[tok * (LPT * V) + (q * LPT + sl) * 4 + j] = plain && l[v] == NONE ? NONE : c[v];
-                }
-            wave_sync();
-            float a = NONE, b = NONE;
-            if (sl < G) {
-                const float* group = lds.score + tok * (LPT * V) + sl * size;
-                int at = sl % size;
-                for (int i = 0; i < size; ++i) {
-                    const float v = group[at];
-                    at = at + 1 == size ? 0 : at + 1;
-                    b = __builtin_fmaxf(b, __builtin_fminf(a, v));
-                    a = __builtin_fmaxf(a, v);
-                }
-            }
-            const float value = top2 && b > NONE ? a + b : a;
-            int before = 0;
-            for (int h = 0; h < G; ++h) {
-                const float v = __shfl(value, first + h);
-                before += v > value || (v == value && h < sl);
-            }
-            bool keep = value > NONE && before < p.top_groups;
-            if (by_score) {
-                const float worst = -group_max<LPT>(keep ? -value : NONE);
-                const float next = group_max<LPT>(!keep ? value : NONE);
-                const float near = 2.0f * slack + 4.76837158203125e-07f * (__builtin_fabsf(worst) + __builtin_fabsf(next));
-                if (__any(next > NONE && !(worst - next > near))) {
-                    sum64();
-                    double x = -HUGE_VAL, y = -HUGE_VAL;
-                    if (sl < G && in) {
-                        for (int e = sl * size; e < (sl + 1) * size; ++e) {
-                            const float lg = logit(p, row, e);
-                            double d = choice(lg, e);
-                            if (plain && d > -HUGE_VAL) d = score(lg, sigmoid, soft);
-                            y = fmax(y, fmin(x, d));
-                            x = fmax(x, d);
-                        }
-                    }
-                    const double exact = top2 && y > -HUGE_VAL ? x + y : x;
-                    before = 0;
-                    for (int h = 0; h < G; ++h) {
-                        const double v = __shfl(exact, first + h);
-                        before += v > exact || (v == exact && h < sl);
-                    }
-                    keep = exact > -HUGE_VAL && before < p.top_groups;
-                }
-            }
-            kept = __ballot(keep) >> first;
-            if (plain) add_bias();
-#pragma unroll
-            for (int q = 0; q < V / 4; ++q)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const uint32_t g = uint32_t((q * LPT + sl) * 4 + j) * inverse >> 20;
-                    c[4 * q + j] = kept >> (g & 63) & 1 ? c[4 * q + j] : NONE;
-                }
-            wave_sync();
-        } else {
-            add_bias();
-        }
-
-        // candidates: not below the top_k-th largest of the lanes' largest, less the slack
-        float most = c[0];
-#pragma unroll
-        for (int v = 1; v < V; ++v) most = __builtin_fmaxf(most, c[v]);
-        float bar = group_max<LPT>(group_at_least<LPT>(most) >= K ? most : NONE);
-        if (bias && bar > NONE && bar < __builtin_inff()) bar -= slack + 4.76837158203125e-07f * __builtin_fabsf(bar);
-        int n = 0;
-#pragma unroll
-        for (int v = 0; v < V; ++v) n += c[v] > NONE && c[v] >= bar;
-        int at = group_before<LPT>(n, sl);
-        n = __shfl(at + n, first + LPT - 1);  // of the token
-        const bool over = n > CAP;
-        if (!over) {
-#pragma unroll
-            for (int q = 0; q < V / 4; ++q)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int v = 4 * q + j;
-                    if (c[v] > NONE && c[v] >= bar) {
-                        lds.can.l[tok * CAP + at] = l[v];
-                        lds.can.e[tok * CAP + at] = (q * LPT + sl) * 4 + j;
-                        ++at;
-                    }
-                }
-        }
-        const uint64_t overs = __ballot(over);
-        int got = over ? 0 : n;  // candidates of the token, and below the chosen
-        int longest = got;
-#pragma unroll
-        for (int d = LPT; d < 64; d *= 2) longest = max(longest, __shfl_xor(longest, d));
-        longest = __builtin_amdgcn_readfirstlane(longest);
         wave_sync();
-        for (bool again = true; again;) {
-            for (int i = sl; i < got; i += LPT) lds.can.c[tok * CAP + i] = choice(lds.can.l[tok * CAP + i], lds.can.e[tok * CAP + i]);
-            wave_sync();
-            bool close = false;
-            for (int i0 = 0; i0 < longest; i0 += LPT) {
-                const int i = i0 + sl;
-                const bool mine = i < got;
-                const double d = mine ? lds.can.c[tok * CAP + i] : 0.0;
-                const int e = mine ? lds.can.e[tok * CAP + i] : 0;
-                int before = 0;
-                for (int o = 0; o < longest; ++o) {
-                    const double w = lds.can.c[tok * CAP + o];
-                    const int f = lds.can.e[tok * CAP + o];
-                    if (o < got) {
-                        before += w > d || (w == d && f < e);
-                        // the softmax's sum is fp32's: an order within its error of the scores needs it in fp64
-                        close |= fabs(w - d) < double(slack) && f != e;
-                    }
-                }
-                if (mine && before < K) {
-                    p.ids[row * K + before] = e;
-                    lds.chosen[first + before] = lds.can.l[tok * CAP + i];
-                }
-            }
-            again = bias && !sigmoid && !exact_sum && __any(close);
-            if (again) sum64();
-            wave_sync();
-        }
-        got = min(got, K);
-        // tokens with more candidates: the next pick is the best behind the one before it, by the whole wave
-        for (uint64_t left = overs; left;) {
-            const int src = __builtin_ctzll(left), t2 = src / LPT;
-            left &= ~(((LPT == 64 ? 0 : 1ull << LPT % 64) - 1) << (t2 * LPT));
-            const int64_t r2 = r0 + t2;
-            if (bias) sum64();
-            const double total = __shfl(soft.sum, src);
-            const Softmax s2{__shfl(soft.most, src), total};
-            const uint64_t k2 = uint64_t(uint32_t(__shfl(int(uint32_t(kept)), src))) |
-                                uint64_t(uint32_t(__shfl(int(uint32_t(kept >> 32)), src))) << 32;
-            double last = HUGE_VAL;
-            int last_at = -1, picks = 0;
-            for (; picks < K; ++picks) {
-                double best = -HUGE_VAL;
-                int where = E;
-                float picked = NONE;
-                for (int e = lane; e < E; e += 64) {
-                    if (G > 1 && !(k2 >> (uint32_t(e) * inverse >> 20 & 63) & 1)) continue;
-                    const float lg = logit(p, r2, e);
-                    if (lg == NONE) continue;
-                    const double d = bias ? score(lg, sigmoid, s2) + double(bias[e]) : double(lg);
-                    if (d > best && (d < last || (d == last && e > last_at))) {
-                        best = d;
-                        where = e;
-                        picked = lg;
-                    }
-                }
-#pragma unroll
-                for (int x = 1; x < 64; x *= 2) {
-                    const double w = __shfl_xor(best, x);
-                    const int f = __shfl_xor(where, x);
-                    const float u = __shfl_xor(picked, x);
-                    if (w > best || (w == best && f < where)) {
-                        best = w;
-                        where = f;
-                        picked = u;
-                    }
-                }
-                if (best == -HUGE_VAL) break;
-                last = best;
-                last_at = where;
-                if (lane == 0) {
-                    p.ids[r2 * K + picks] = where;
-                    lds.chosen[t2 * LPT + picks] = picked;
-                }
-            }
-            if (tok == t2) got = picks;
-        }
-        wave_sync();
-        // weights of the chosen, a lane each
-        const float lg = sl < got ? lds.chosen[lane] : NONE;
-        float w = 0.0f;
-        if (p.renormalise) {
-            // from the largest chosen logit where scores underflow: they keep their shares
-            const float top = group_max<LPT>(lg);
-            const bool shifted = !sigmoid || top < -60.0f;
-            if (sl < got) w = shifted ? expf(lg - top) : 1.0f / (1.0f + expf(-lg));
-            const float total = group_sum<LPT>(w);
-            w = sl < got ? w / total : 0.0f;
-        } else if (sl < got) {
-            w = sigmoid ? 1.0f / (1.0f + expf(-lg)) : expf(lg - soft.most) / z;
-        }
-        if (in && sl < K) {
-            p.weights[row * K + sl] = p.scale * w;
-            if (sl >= got) p.ids[row * K + sl] = -1;
-        }
-        wave_sync();
+    } else {
+        add_bias();
     }
+
+    // candidates: not below the top_k-th largest of the lanes' largest, less the slack
+    float most = c[0];
+#pragma unroll
+    for (int v = 1; v < V; ++v) most = __builtin_fmaxf(most, c[v]);
+    float bar = group_max<LPT>(group_at_least<LPT>(most) >= K ? most : NONE);
+    if (bias && bar > NONE && bar < __builtin_inff()) bar -= slack + 4.76837158203125e-07f * __builtin_fabsf(bar);
+    int n = 0;
+#pragma unroll
+    for (int v = 0; v < V; ++v) n += c[v] > NONE && c[v] >= bar;
+    int at = group_before<LPT>(n, sl);
+    n = __shfl(at + n, first + LPT - 1);  // of the token
+    redo |= n > CAP;
+    if (!redo) {
+#pragma unroll
+        for (int q = 0; q < V / 4; ++q)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int v = 4 * q + j;
+                if (c[v] > NONE && c[v] >= bar) {
+                    lds.can.l[tok * CAP + at] = l[v];
+                    lds.can.e[tok * CAP + at] = (q * LPT + sl) * 4 + j;
+                    ++at;
+                }
+            }
+    }
+    int got = redo ? 0 : n;  // candidates of the token, and below the chosen
+    int longest = got;
+#pragma unroll
+    for (int d = LPT; d < 64; d *= 2) longest = max(longest, __shfl_xor(longest, d));
+    longest = __builtin_amdgcn_readfirstlane(longest);
+    wave_sync();
+    for (int i = sl; i < got; i += LPT) lds.can.c[tok * CAP + i] = choice(p, lds.can.l[tok * CAP + i], lds.can.e[tok * CAP + i], soft);
+    wave_sync();
+    // the softmax's sum is fp32's: an order within its error of the scores needs it in fp64
+    const double close = bias && !sigmoid ? double(slack) : 0.0;
+    for (int i0 = 0; i0 < longest; i0 += LPT) {
+        const int i = i0 + sl;
+        const bool mine = i < got;
+        const double d = mine ? lds.can.c[tok * CAP + i] : 0.0;
+        const int e = mine ? lds.can.e[tok * CAP + i] : 0;
+        int before = 0;
+        for (int o = 0; o < longest; ++o) {
+            const double w = lds.can.c[tok * CAP + o];
+            const int f = lds.can.e[tok * CAP + o];
+            if (mine && o < got) {
+                before += w > d || (w == d && f < e);
+                redo |= fabs(w - d) < close && f != e;
+            }
+        }
+        if (mine && before < K) {
+            lds.ids[first + before] = e;
+            lds.chosen[first + before] = lds.can.l[tok * CAP + i];
+        }
+    }
+    got = min(got, K);
+    wave_sync();
+    // weights of the chosen, a lane each
+    const float lg = sl < got ? lds.chosen[lane] : NONE;
+    float w = 0.0f;
+    if (p.renormalise) {
+        // from the largest chosen logit where scores underflow: they keep their shares
+        const float top = group_max<LPT>(lg);
+        const bool shifted = !sigmoid || top < -60.0f;
+        if (sl < got) w = shifted ? expf(lg - top) : 1.0f / (1.0f + expf(-lg));
+        const float total = group_sum<LPT>(w);
+        w = sl < got ? w / total : 0.0f;
+    } else if (sl < got) {
+        w = sigmoid ? 1.0f / (1.0f + expf(-lg)) : expf(lg - soft.most) / z;
+    }
+    constexpr uint64_t TOKEN = LPT == 64 ? ~0ull : (1ull << LPT % 64) - 1;
+    uint64_t left = __ballot(redo);
+    if (in && sl < K && !(left >> first & TOKEN)) {
+        p.weights[row * K + sl] = p.scale * w;
+        p.ids[row * K + sl] = sl < got ? lds.ids[lane] : -1;
+    }
+    for (int t = 0; left; ++t, left = LPT == 64 ? 0 : left >> LPT % 64)
+        if (left & TOKEN) route_token(p, r0 + t);
 }
 
 // The gradient: a wave a token.
@@ -610,8 +609,11 @@ hipError_t run_route(const RouteParams& p, const DeviceInfo& dev, hipStream_t st
     const int cus = std::max(dev.cu_count, 1);
     auto launch = [&](auto lpt, auto v) {
         constexpr int per = 4 * 64 / lpt.value;
-        const unsigned grid = unsigned(std::min<int64_t>((p.n_tokens + per - 1) / per, 16 * cus));
-        hipLaunchKernelGGL((route_kernel<lpt.value, v.value>), dim3(grid), dim3(256), 0, stream, p);
+        constexpr int64_t most = int64_t(1) << 23;  // workgroups: a launch holds less than 2^32 threads
+        for (int64_t row0 = 0; row0 < p.n_tokens; row0 += most * per) {
+            const unsigned grid = unsigned(std::min<int64_t>((p.n_tokens - row0 + per - 1) / per, most));
+            hipLaunchKernelGGL((route_kernel<lpt.value, v.value>), dim3(grid), dim3(256), 0, stream, p, row0);
+        }
     };
     auto of = [&](auto lpt) {
         using N = decltype(lpt);
