@@ -1033,6 +1033,7 @@ FFF_EXPORT int fff_route(const fff_route_args* a) {
     p.top_k = a->top_k;
     p.n_groups = a->n_groups;
     p.top_groups = a->top_groups;
+    p.group_size = a->n_experts / a->n_groups;
     p.bf16 = a->x_dtype == FFF_BF16;
     p.score = a->score;
     p.group_score = a->group_score;

@@ -136,6 +136,7 @@ struct RouteParams {
     float* weights;
     int64_t n_tokens;
     int32_t n_experts, top_k, n_groups, top_groups;
+    int32_t group_size;      // n_experts / n_groups
     int32_t bf16;
     int32_t score, group_score, renormalise;
     float scale;

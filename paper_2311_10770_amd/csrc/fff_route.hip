@@ -23,7 +23,7 @@ constexpr float NONE = -__builtin_inff();
 
 // A logit: -inf where it is NaN (no expert), the largest fp32 value where it is infinite.
 __device__ __forceinline__ float clean_logit(float l) {
-    return l > NONE ? __builtin_fminf(l, 3.4028234663852886e38f) : NONE;
+    return __builtin_fminf(__builtin_fmaxf(l, NONE), 3.4028234663852886e38f);  // the larger of NaN and a number is that
 }
 __device__ __forceinline__ float logit(const RouteParams& p, int64_t row, int e) {
     return clean_logit(load_elem(p.logits, p.bf16, row * p.n_experts + e));
@@ -48,7 +48,7 @@ __device__ __forceinline__ double choice(const RouteParams& p, float l, int e, c
 
 // The value of a token's group g in fp64.
 __device__ __forceinline__ double group_value(const RouteParams& p, int64_t row, int g, Softmax m) {
-    const int size = p.n_experts / p.n_groups;
+    const int size = p.group_size;
     double a = -HUGE_VAL, b = -HUGE_VAL;
     for (int e = g * size; e < (g + 1) * size; ++e) {
         const float l = logit(p, row, e);
@@ -104,7 +104,7 @@ __global__ __launch_bounds__(ANY) void route_any_kernel(RouteParams p) {
     __shared__ int si[ANY / 64];
     __shared__ uint8_t s_kept[MAX_ROUTE_GROUPS];
     __shared__ float s_logit[MAX_TOP_K];
-    const int E = p.n_experts, G = p.n_groups, size = E / G, tid = threadIdx.x;
+    const int E = p.n_experts, G = p.n_groups, size = p.group_size, tid = threadIdx.x;
     for (int64_t row = blockIdx.x; row < p.n_tokens; row += gridDim.x) {
         Softmax m{0.0f, 1.0};
         if (p.score == SCORE_SOFTMAX) {
@@ -180,16 +180,20 @@ __global__ __launch_bounds__(ANY) void route_any_kernel(RouteParams p) {
 
 // ---- up to 1024 experts: LPT lanes a token ---------------------------------
 
+// v of the lane that a DPP control names (one that has a lane for each, as the rotations of a row of 16 do).
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v) {
+    return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+constexpr int ROR = 0x120;  // row_ror: + 1 .. 15
+
 // Largest v of the LPT lanes of a token, for each of them.
 template <int LPT>
 __device__ __forceinline__ float group_max(float v) {
-    auto dpp = [&](auto ctrl) {
-        v = __builtin_fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), ctrl.value, 0xf, 0xf, false)));
-    };
-    dpp(std::integral_constant<int, 0x128>{});  // row_ror:8, 4, 2, 1
-    dpp(std::integral_constant<int, 0x124>{});
-    dpp(std::integral_constant<int, 0x122>{});
-    dpp(std::integral_constant<int, 0x121>{});
+    v = __builtin_fmaxf(v, dpp<ROR + 8>(v));
+    v = __builtin_fmaxf(v, dpp<ROR + 4>(v));
+    v = __builtin_fmaxf(v, dpp<ROR + 2>(v));
+    v = __builtin_fmaxf(v, dpp<ROR + 1>(v));
     if constexpr (LPT >= 32) v = __builtin_fmaxf(v, __shfl_xor(v, 16));
     if constexpr (LPT == 64) v = __builtin_fmaxf(v, __shfl_xor(v, 32));
     return v;
@@ -200,7 +204,7 @@ __device__ __forceinline__ int row_at_least(float v, float o) {
     if constexpr (R == 16) {
         return 0;
     } else {
-        const float w = R == 0 ? o : __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(o), 0x120 + R, 0xf, 0xf, false));
+        const float w = R == 0 ? o : dpp<ROR + (R == 0 ? 1 : R)>(o);
         return (w >= v) + row_at_least<R + 1>(v, o);
     }
 }
@@ -228,84 +232,147 @@ __device__ __forceinline__ void wave_sync() {
     __builtin_amdgcn_wave_barrier();
 }
 
-// A whole token in fp64 by a whole wave: each pick is the best expert behind the one before it in the order.  For
-// the few tokens that route_kernel leaves.  At most 64 groups.
-__device__ __forceinline__ void route_token(const RouteParams& p, int64_t row) {
-    const int lane = threadIdx.x & 63, E = p.n_experts, G = p.n_groups, size = E / G;
-    auto best_of = [](double& v, int& i, float& l) {
-#pragma unroll 1
-        for (int x = 1; x < 64; x *= 2) {
-            const double w = __shfl_xor(v, x);
-            const int f = __shfl_xor(i, x);
-            const float u = __shfl_xor(l, x);
-            if (w > v || (w == v && f < i)) {
-                v = w;
-                i = f;
-                l = u;
+// The larger two of (a, b) and the same pair of the lane that CTRL (a DPP control) names.
+template <int CTRL>
+__device__ __forceinline__ void top2_step(float& a, float& b) {
+    const float x = dpp<CTRL>(a), y = dpp<CTRL>(b);
+    b = __builtin_fmaxf(__builtin_fmaxf(b, y), __builtin_fminf(a, x));
+    a = __builtin_fmaxf(a, x);
+}
+
+// before[q]: how many groups come before this lane's q-th by their values, lane sl's q-th group being number
+// q (16 / m) + sub of a token (m lanes, a power of two, hold a group; sub = sl / m).  Of another vector of experts the group comes
+// earlier or later as the vector does; within one, by sub.
+template <int N, int R = 0>
+__device__ __forceinline__ void rank_groups(const float (&value)[N], int (&before)[N], int m, int sub) {
+    if constexpr (R < 16) {
+        if ((R & (m - 1)) == 0) {
+            constexpr int CTRL = ROR + (R == 0 ? 1 : R);
+            const int s = R == 0 ? sub : __builtin_amdgcn_mov_dpp(sub, CTRL, 0xf, 0xf, true);
+#pragma unroll
+            for (int o = 0; o < N; ++o) {
+                const float v = R == 0 ? value[o] : dpp<CTRL>(value[o]);
+#pragma unroll
+                for (int q = 0; q < N; ++q) {
+                    if (o < q) before[q] += v >= value[q];
+                    else if (o > q) before[q] += v > value[q];
+                    else if (R > 0) before[q] += v > value[q] || (v == value[q] && s < sub);
+                }
             }
         }
+        rank_groups<N, R + 1>(value, before, m, sub);
+    }
+}
+
+// Whether route_kernel<16> finds groups of `size` experts in its lanes' registers: a power of two of whole vectors.
+__host__ __device__ __forceinline__ bool groups_in_lanes(int size) { return size >= 4 && size <= 64 && (size & (size - 1)) == 0; }
+
+// The best (v, then the lowest i) of the wave's lanes, for each of them.
+__device__ __forceinline__ void wave_best(double& v, int& i) {
+    auto meet = [&](double w, int j) {
+        const bool take = w > v || (w == v && j < i);
+        v = take ? w : v;
+        i = take ? j : i;
+    };
+    auto step = [&](auto ctrl) {
+        const uint64_t u = __builtin_bit_cast(uint64_t, v);
+        const uint32_t lo = __builtin_amdgcn_mov_dpp(int(uint32_t(u)), ctrl.value, 0xf, 0xf, true);
+        const uint32_t hi = __builtin_amdgcn_mov_dpp(int(uint32_t(u >> 32)), ctrl.value, 0xf, 0xf, true);
+        meet(__builtin_bit_cast(double, uint64_t(hi) << 32 | lo), __builtin_amdgcn_mov_dpp(i, ctrl.value, 0xf, 0xf, true));
+    };
+    step(std::integral_constant<int, ROR + 8>{});
+    step(std::integral_constant<int, ROR + 4>{});
+    step(std::integral_constant<int, ROR + 2>{});
+    step(std::integral_constant<int, ROR + 1>{});
+    meet(__shfl_xor(v, 16), __shfl_xor(i, 16));
+    meet(__shfl_xor(v, 32), __shfl_xor(i, 32));
+}
+
+// A whole token in fp64 by a whole wave, for the few that route_kernel leaves: the choices of all experts go to LDS
+// (by_e, n_experts of them), and each pick is the best that is left.  At most 64 groups.
+__device__ __forceinline__ void route_token(const RouteParams& p, int64_t row, double* by_e) {
+    const int lane = threadIdx.x & 63, E = p.n_experts, G = p.n_groups, size = p.group_size;
+    const bool plain = G > 1 && p.group_score == GROUP_TOP2 && !p.bias;  // groups by s, then experts by the logits
+    auto logits_of = [&] {
+        for (int e = lane; e < E; e += 64) by_e[e] = double(logit(p, row, e));
     };
     Softmax m{0.0f, 1.0};
+    wave_sync();
+    logits_of();
     if (p.score == SCORE_SOFTMAX) {
         float most = NONE;
-        for (int e = lane; e < E; e += 64) most = __builtin_fmaxf(most, logit(p, row, e));
-#pragma unroll 1
-        for (int x = 1; x < 64; x *= 2) most = __builtin_fmaxf(most, __shfl_xor(most, x));
+        for (int e = lane; e < E; e += 64) most = __builtin_fmaxf(most, float(by_e[e]));
+        most = group_max<64>(most);
         m.most = most > NONE ? most : 0.0f;
         double sum = 0.0;
-        for (int e = lane; e < E; e += 64) {
-            const float l = logit(p, row, e);
-            sum += l > NONE ? exp(double(l) - double(m.most)) : 0.0;
-        }
-#pragma unroll 1
+        for (int e = lane; e < E; e += 64) sum += by_e[e] > -HUGE_VAL ? exp(by_e[e] - double(m.most)) : 0.0;
+#pragma unroll
         for (int x = 1; x < 64; x *= 2) sum += __shfl_xor(sum, x);
         m.sum = sum > 0.0 ? sum : 1.0;
     }
-    uint64_t kept = ~0ull;
+    if (p.bias || plain) {
+        for (int e = lane; e < E; e += 64) {
+            const float l = float(by_e[e]);
+            by_e[e] = plain ? (l > NONE ? score(l, p.score, m) : -HUGE_VAL) : choice(p, l, e, m);
+        }
+    }
+    wave_sync();
     if (G > 1) {
-        const double value = lane < G ? group_value(p, row, lane, m) : -HUGE_VAL;
+        double a = -HUGE_VAL, b = -HUGE_VAL;
+        if (lane < G) {
+            int at = lane % size;  // lanes start at different banks
+            for (int i = 0; i < size; ++i) {
+                const double c = by_e[lane * size + at];
+                at = at + 1 == size ? 0 : at + 1;
+                b = fmax(b, fmin(a, c));
+                a = fmax(a, c);
+            }
+        }
+        const double value = p.group_score == GROUP_TOP2 && b > -HUGE_VAL ? a + b : a;
         int before = 0;
         for (int h = 0; h < G; ++h) {
             const double v = __shfl(value, h);
             before += v > value || (v == value && h < lane);
         }
-        kept = __ballot(value > -HUGE_VAL && before < p.top_groups);
+        const uint64_t kept = __ballot(lane < G && value > -HUGE_VAL && before < p.top_groups);
+        if (plain) logits_of();
+        wave_sync();
+        for (int e = lane; e < E; e += 64)
+            if (!(kept >> (e / size & 63) & 1)) by_e[e] = -HUGE_VAL;
     }
-    double last = HUGE_VAL;
-    int last_at = -1, picks = 0, mine = -1;
-    float own = NONE;  // logit of the pick that this lane keeps
-    for (; picks < p.top_k; ++picks) {
-        double best = -HUGE_VAL;
-        int where = E;
-        float picked = NONE;
+    auto mine_best = [&](double& v, int& i) {
+        v = -HUGE_VAL;
+        i = E;
         for (int e = lane; e < E; e += 64) {
-            if (!(kept >> (e / size & 63) & 1) && G > 1) continue;
-            const float l = logit(p, row, e);
-            const double c = choice(p, l, e, m);
-            if (c > best && (c < last || (c == last && e > last_at))) {
-                best = c;
-                where = e;
-                picked = l;
+            const double c = by_e[e];
+            if (c > v) {
+                v = c;
+                i = e;
             }
         }
-        best_of(best, where, picked);
+    };
+    double v;
+    int at, picks = 0, mine = -1;
+    mine_best(v, at);
+    for (; picks < p.top_k; ++picks) {
+        double best = v;
+        int where = at;
+        wave_best(best, where);
         if (best == -HUGE_VAL) break;
-        last = best;
-        last_at = where;
-        if (lane == picks) {
-            mine = where;
-            own = picked;
+        if (lane == picks) mine = where;
+        if (where == at) {  // this lane's: the next of its own
+            by_e[at] = -HUGE_VAL;
+            mine_best(v, at);
         }
     }
     // renormalised sums start from the largest chosen logit: scores that underflow keep their shares
-    float top = own;
-#pragma unroll 1
-    for (int x = 1; x < 64; x *= 2) top = __builtin_fmaxf(top, __shfl_xor(top, x));
+    const float own = mine >= 0 ? logit(p, row, mine) : NONE, top = group_max<64>(own);
     double w = 0.0;
-    if (mine >= 0) w = p.renormalise && (p.score == SCORE_SOFTMAX || top < -300.0f) ? exp(double(own) - double(top)) : score(own, p.score, m);
+    if (mine >= 0)
+        w = p.renormalise && (p.score == SCORE_SOFTMAX || top < -300.0f) ? exp(double(own) - double(top)) : score(own, p.score, m);
     if (p.renormalise) {
         double sum = w;
-#pragma unroll 1
+#pragma unroll
         for (int x = 1; x < 64; x *= 2) sum += __shfl_xor(sum, x);
         w = mine >= 0 ? w / sum : 0.0;
     }
@@ -313,19 +380,23 @@ __device__ __forceinline__ void route_token(const RouteParams& p, int64_t row) {
         p.ids[row * p.top_k + lane] = mine;
         p.weights[row * p.top_k + lane] = float(double(p.scale) * w);
     }
+    wave_sync();
 }
 
-// What one wave holds in LDS: scores by expert while groups are chosen, then the candidates of its tokens.
+// What one wave holds in LDS: scores by expert while groups are chosen, then its tokens' candidates, then the
+// choices of a token that is done again.
 template <int LPT, int V>
 struct RouteLds {
-    static constexpr int CAP = 4 * LPT;  // candidates of a token
+    static constexpr int CAP = 4 * LPT;  // candidates of a token; one place more, so that tokens lie on other banks
+    struct Candidate {
+        double c;
+        int e;
+        float l;
+    };
     union {
         float score[64 * V];
-        struct {
-            double c[256];
-            float l[256];
-            int e[256];
-        } can;
+        Candidate can[256 + 64 / LPT];
+        double by_e[LPT * V];  // route_token's
     };
     float chosen[64];  // logits of the chosen, and the experts
     int ids[64];
@@ -333,7 +404,7 @@ struct RouteLds {
 
 // LPT lanes a token, four neighbouring experts a vector, V experts a lane.
 //
-// Choices are first formed in fp32 (c32, whose error is below `slack` / 2).  Of the LPT lanes' largest, the
+// Choices are first formed in fp32 (c, whose error is below `slack` / 2).  Of the LPT lanes' largest, the
 // top_k-th is no more than the top_k-th largest of all, so only experts within the slack of it
 // can be chosen: a dozen of 256.  These candidates alone are evaluated and ordered in fp64, each
 // by counting those before it.  Tokens that need more than the candidates' own scores in fp64 (the softmax's sum
@@ -342,33 +413,45 @@ struct RouteLds {
 template <int LPT, int V>
 __global__ __launch_bounds__(256, 5) void route_kernel(RouteParams p, int64_t row0) {
     using Lds = RouteLds<LPT, V>;
-    constexpr int TPW = 64 / LPT, CAP = Lds::CAP;
+    constexpr int TPW = 64 / LPT, CAP = Lds::CAP, N = V / 4;
     __shared__ Lds lds4[4];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, sl = lane % LPT, tok = lane / LPT, first = tok * LPT;
     Lds& lds = lds4[wave];
-    const int E = p.n_experts, K = p.top_k, G = p.n_groups, size = E / G;
-    const uint32_t inverse = ((1u << 20) + size - 1) / size;  // e / size = e inverse >> 20 for e < 1024
+    typename Lds::Candidate* can = lds.can + tok * (CAP + 1);
+    const int E = p.n_experts, K = p.top_k, G = p.n_groups, size = p.group_size;
     const bool sigmoid = p.score != SCORE_SOFTMAX, top2 = p.group_score == GROUP_TOP2;
     const bool by_score = p.bias || (G > 1 && top2);  // whether fp32 scores take part in the choice
     const bool sums = !sigmoid && (by_score || !p.renormalise);
     const int64_t r0 = (row0 / TPW + int64_t(blockIdx.x) * 4 + wave) * TPW;
-    const int64_t row = r0 + tok;
-    const bool in = row < p.n_tokens;
+    if (r0 >= p.n_tokens) return;
+    const bool in = r0 + tok < p.n_tokens;
+    const int64_t row = in ? r0 + tok : p.n_tokens - 1;  // lanes behind the last token do it again
     float l[V], c[V];
+    if (E == LPT * V) {
 #pragma unroll
-    for (int q = 0; q < V / 4; ++q) {
-        const int col = (q * LPT + sl) * 4, left = in ? E - col : 0;
-        unpack4(l + 4 * q, load4<false>(p.logits, p.bf16, row * E + col, left), p.bf16);
+        for (int q = 0; q < N; ++q)
+            unpack4(l + 4 * q, load4<true>(p.logits, p.bf16, row * E + (q * LPT + sl) * 4, 4), p.bf16);
+    } else {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) l[4 * q + j] = j < left ? clean_logit(l[4 * q + j]) : NONE;
+        for (int q = 0; q < N; ++q) {
+            const int col = (q * LPT + sl) * 4;
+            unpack4(l + 4 * q, load4<false>(p.logits, p.bf16, row * E + col, E - col), p.bf16);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) l[4 * q + j] = j < E - col ? l[4 * q + j] : NONE;
+        }
     }
+#pragma unroll
+    for (int v = 0; v < V; ++v) l[v] = clean_logit(l[v]);
+    auto lane_max = [](const float (&x)[V]) {
+        float m = x[0];
+#pragma unroll
+        for (int v = 1; v < V; ++v) m = __builtin_fmaxf(m, x[v]);
+        return m;
+    };
     Softmax soft{0.0f, 1.0};
     float z = 1.0f;
     if (!sigmoid) {
-        float most = l[0];
-#pragma unroll
-        for (int v = 1; v < V; ++v) most = __builtin_fmaxf(most, l[v]);
-        most = group_max<LPT>(most);
+        const float most = group_max<LPT>(lane_max(l));
         soft.most = most > NONE ? most : 0.0f;
     }
     if (sums) {
@@ -392,125 +475,155 @@ __global__ __launch_bounds__(256, 5) void route_kernel(RouteParams p, int64_t ro
         }
     }
     const float* bias = p.bias;
-    auto add_bias = [&] {
+    auto choices = [&] {
+        if (!bias) {
 #pragma unroll
-        for (int q = 0; q < V / 4; ++q) {
+            for (int v = 0; v < V; ++v) c[v] = l[v];
+            return;
+        }
+#pragma unroll
+        for (int q = 0; q < N; ++q) {
             const int col = (q * LPT + sl) * 4;
-            float b[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-            if (bias) unpack4(b, load4<false>(bias, 0, col, E - col), 0);
+            float b[4];
+            unpack4(b, E == LPT * V ? load4<true>(bias, 0, col, 4) : load4<false>(bias, 0, col, E - col), 0);
+            // 0 l is 0, or NaN where there is no expert; the maximum makes that and a bias's NaN -inf
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int v = 4 * q + j;
-                const float s = bias ? c[v] + b[j] : l[v];
-                c[v] = l[v] > NONE && s > NONE ? s : NONE;
-            }
+            for (int j = 0; j < 4; ++j)
+                c[4 * q + j] = __builtin_fmaxf(__builtin_fmaf(l[4 * q + j], 0.0f, c[4 * q + j] + b[j]), NONE);
         }
     };
     const float slack = by_score ? (sigmoid ? 7.62939453125e-06f : 1.52587890625e-05f * share) : 0.0f;  // 2^-17, 2^-16
 
-    uint64_t kept = ~0ull;
     if (G > 1) {
-        // every lane below G has a group, and reads its scores from a place of its own on
-        const bool plain = top2 && !bias;  // by s, not by c
-        if (!plain) add_bias();
+        const bool plain = top2 && !bias;  // groups by s, not by c
+        if (!plain) choices();
+        float worst = NONE, next = NONE;  // -value of the worst group kept, value of the best other
+        auto note = [&](float value, bool keep) {
+            worst = keep ? __builtin_fmaxf(worst, -value) : worst;
+            next = keep ? next : __builtin_fmaxf(next, value);
+        };
+        if (LPT == 16 && groups_in_lanes(size)) {
+            // m lanes hold a group of every vector: pairs of the larger two meet over DPP
+            const int m = size / 4;
+            float value[N];
+            int before[N] = {};
 #pragma unroll
-        for (int q = 0; q < V / 4; ++q)
+            for (int q = 0; q < N; ++q) {
+                float s[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int v = 4 * q + j;
-                lds.score[tok * (LPT * V) + (q * LPT + sl) * 4 + j] = plain && l[v] == NONE ? NONE : c[v];
+                for (int j = 0; j < 4; ++j) s[j] = plain && l[4 * q + j] == NONE ? NONE : c[4 * q + j];
+                const float low = __builtin_fminf(s[0], s[1]), high = __builtin_fmaxf(s[0], s[1]);
+                const float low2 = __builtin_fminf(s[2], s[3]), high2 = __builtin_fmaxf(s[2], s[3]);
+                float a = __builtin_fmaxf(high, high2);
+                float b = __builtin_fmaxf(__builtin_fmaxf(low, low2), __builtin_fminf(high, high2));
+                if (m >= 2) top2_step<0xb1>(a, b);    // quad_perm 1 0 3 2
+                if (m >= 4) top2_step<0x4e>(a, b);    // quad_perm 2 3 0 1
+                if (m >= 8) top2_step<0x141>(a, b);   // row_half_mirror
+                if (m >= 16) top2_step<0x140>(a, b);  // row_mirror
+                value[q] = top2 && b > NONE ? a + b : a;
             }
-        wave_sync();
-        float a = NONE, b = NONE;
-        if (sl < G) {
-            const float* group = lds.score + tok * (LPT * V) + sl * size;
-            int at = sl % size;
-            for (int i = 0; i < size; ++i) {
-                const float v = group[at];
-                at = at + 1 == size ? 0 : at + 1;
-                b = __builtin_fmaxf(b, __builtin_fminf(a, v));
-                a = __builtin_fmaxf(a, v);
+            rank_groups(value, before, m, sl >> __builtin_ctz(m));
+            if (plain) choices();
+#pragma unroll
+            for (int q = 0; q < N; ++q) {
+                const bool keep = value[q] > NONE && before[q] < p.top_groups;
+                note(value[q], keep);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) c[4 * q + j] = keep ? c[4 * q + j] : NONE;
             }
+        } else {
+            // every lane below G has a group, and reads its scores from a place of its own on
+            const uint32_t inverse = ((1u << 20) + size - 1) / size;  // e / size = e inverse >> 20 for e < 1024
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+                lds.score[tok * (LPT * V) + (v / 4 * LPT + sl) * 4 + v % 4] = plain && l[v] == NONE ? NONE : c[v];
+            wave_sync();
+            float a = NONE, b = NONE;
+            if (sl < G) {
+                const float* group = lds.score + tok * (LPT * V) + sl * size;
+                int at = sl % size;
+                for (int i = 0; i < size; ++i) {
+                    const float v = group[at];
+                    at = at + 1 == size ? 0 : at + 1;
+                    b = __builtin_fmaxf(b, __builtin_fminf(a, v));
+                    a = __builtin_fmaxf(a, v);
+                }
+            }
+            const float value = top2 && b > NONE ? a + b : a;
+            int before = 0;
+            for (int h = 0; h < G; ++h) {
+                const float v = __shfl(value, first + h);
+                before += v > value || (v == value && h < sl);
+            }
+            const bool keep = value > NONE && before < p.top_groups;
+            note(value, keep);
+            const uint64_t kept = __ballot(keep) >> first;
+            if (plain) choices();
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const uint32_t g = uint32_t((v / 4 * LPT + sl) * 4 + v % 4) * inverse >> 20;
+                c[v] = kept >> (g & 63) & 1 ? c[v] : NONE;
+            }
+            wave_sync();
         }
-        const float value = top2 && b > NONE ? a + b : a;
-        int before = 0;
-        for (int h = 0; h < G; ++h) {
-            const float v = __shfl(value, first + h);
-            before += v > value || (v == value && h < sl);
-        }
-        bool keep = value > NONE && before < p.top_groups;
         if (by_score) {
-            const float worst = -group_max<LPT>(keep ? -value : NONE);
-            const float next = group_max<LPT>(!keep ? value : NONE);
+            worst = -group_max<LPT>(worst);
+            next = group_max<LPT>(next);
             const float near = 2.0f * slack + 4.76837158203125e-07f * (__builtin_fabsf(worst) + __builtin_fabsf(next));
             redo = next > NONE && !(worst - next > near);
         }
-        kept = __ballot(keep) >> first;
-        if (plain) add_bias();
-#pragma unroll
-        for (int q = 0; q < V / 4; ++q)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const uint32_t g = uint32_t((q * LPT + sl) * 4 + j) * inverse >> 20;
-                c[4 * q + j] = kept >> (g & 63) & 1 ? c[4 * q + j] : NONE;
-            }
-        wave_sync();
     } else {
-        add_bias();
+        choices();
     }
 
     // candidates: not below the top_k-th largest of the lanes' largest, less the slack
-    float most = c[0];
-#pragma unroll
-    for (int v = 1; v < V; ++v) most = __builtin_fmaxf(most, c[v]);
+    const float most = lane_max(c);
     float bar = group_max<LPT>(group_at_least<LPT>(most) >= K ? most : NONE);
-    if (bias && bar > NONE && bar < __builtin_inff()) bar -= slack + 4.76837158203125e-07f * __builtin_fabsf(bar);
-    int n = 0;
+    if (bias && bar < __builtin_inff()) bar -= slack + 4.76837158203125e-07f * __builtin_fabsf(bar);
+    bar = __builtin_fmaxf(bar, -3.4028234663852886e38f);  // of -inf (less inf: NaN): every expert there is
+    uint32_t live = 0;
 #pragma unroll
-    for (int v = 0; v < V; ++v) n += c[v] > NONE && c[v] >= bar;
+    for (int v = 0; v < V; ++v) live |= c[v] >= bar ? 1u << v : 0u;
+    int n = __builtin_popcount(live);
     int at = group_before<LPT>(n, sl);
     n = __shfl(at + n, first + LPT - 1);  // of the token
     redo |= n > CAP;
-    if (!redo) {
-#pragma unroll
-        for (int q = 0; q < V / 4; ++q)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int v = 4 * q + j;
-                if (c[v] > NONE && c[v] >= bar) {
-                    lds.can.l[tok * CAP + at] = l[v];
-                    lds.can.e[tok * CAP + at] = (q * LPT + sl) * 4 + j;
-                    ++at;
-                }
-            }
-    }
+    if (!redo)
+        for (; live; live &= live - 1) {
+            const int v = __builtin_ctz(live);
+            can[at++].e = (v / 4 * LPT + sl) * 4 + v % 4;
+        }
     int got = redo ? 0 : n;  // candidates of the token, and below the chosen
     int longest = got;
 #pragma unroll
     for (int d = LPT; d < 64; d *= 2) longest = max(longest, __shfl_xor(longest, d));
     longest = __builtin_amdgcn_readfirstlane(longest);
     wave_sync();
-    for (int i = sl; i < got; i += LPT) lds.can.c[tok * CAP + i] = choice(p, lds.can.l[tok * CAP + i], lds.can.e[tok * CAP + i], soft);
+    for (int i = sl; i < longest; i += LPT) {
+        int e = E;
+        float lg = NONE;
+        if (i < got) {
+            e = can[i].e;
+            lg = logit(p, row, e);
+        }
+        can[i] = {choice(p, lg, e, soft), e, lg};
+    }
     wave_sync();
     // the softmax's sum is fp32's: an order within its error of the scores needs it in fp64
-    const double close = bias && !sigmoid ? double(slack) : 0.0;
+    const double close = bias && !sigmoid ? double(slack) : -1.0;
     for (int i0 = 0; i0 < longest; i0 += LPT) {
-        const int i = i0 + sl;
-        const bool mine = i < got;
-        const double d = mine ? lds.can.c[tok * CAP + i] : 0.0;
-        const int e = mine ? lds.can.e[tok * CAP + i] : 0;
+        const int i = min(i0 + sl, longest - 1);
+        const typename Lds::Candidate mine = can[i];
         int before = 0;
         for (int o = 0; o < longest; ++o) {
-            const double w = lds.can.c[tok * CAP + o];
-            const int f = lds.can.e[tok * CAP + o];
-            if (mine && o < got) {
-                before += w > d || (w == d && f < e);
-                redo |= fabs(w - d) < close && f != e;
-            }
+            const double w = can[o].c;
+            const int f = can[o].e;
+            before += w > mine.c || (w == mine.c && f < mine.e);
+            if (close >= 0.0) redo |= fabs(w - mine.c) < close && f != mine.e;
         }
-        if (mine && before < K) {
-            lds.ids[first + before] = e;
-            lds.chosen[first + before] = lds.can.l[tok * CAP + i];
+        if (i0 + sl < got && before < K) {
+            lds.ids[first + before] = mine.e;
+            lds.chosen[first + before] = mine.l;
         }
     }
     got = min(got, K);
@@ -529,13 +642,13 @@ __global__ __launch_bounds__(256, 5) void route_kernel(RouteParams p, int64_t ro
         w = sigmoid ? 1.0f / (1.0f + expf(-lg)) : expf(lg - soft.most) / z;
     }
     constexpr uint64_t TOKEN = LPT == 64 ? ~0ull : (1ull << LPT % 64) - 1;
-    uint64_t left = __ballot(redo);
+    uint64_t left = __ballot(redo && in);
     if (in && sl < K && !(left >> first & TOKEN)) {
         p.weights[row * K + sl] = p.scale * w;
         p.ids[row * K + sl] = sl < got ? lds.ids[lane] : -1;
     }
     for (int t = 0; left; ++t, left = LPT == 64 ? 0 : left >> LPT % 64)
-        if (left & TOKEN) route_token(p, r0 + t);
+        if (left & TOKEN) route_token(p, r0 + t, lds.by_e);
 }
 
 // The gradient: a wave a token.
@@ -624,7 +737,7 @@ hipError_t run_route(const RouteParams& p, const DeviceInfo& dev, hipStream_t st
     };
     // lanes a token: twice as many as it chooses experts (fewer candidates), one at least a group
     const int lanes = std::max({2 * p.top_k, p.n_groups, (p.n_experts + 15) / 16});
-    if (lanes <= 16) return of(std::integral_constant<int, 16>{});
+    if (lanes <= 16 || (p.n_experts <= 256 && 2 * p.top_k <= 16 && groups_in_lanes(p.group_size))) return of(std::integral_constant<int, 16>{});
     if (lanes <= 32) return of(std::integral_constant<int, 32>{});
     if (p.n_groups <= 64 && p.n_experts <= 1024) return of(std::integral_constant<int, 64>{});
     const unsigned grid = unsigned(std::min<int64_t>(p.n_tokens, 8 * cus));
