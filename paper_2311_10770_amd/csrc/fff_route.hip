@@ -198,22 +198,31 @@ __device__ __forceinline__ float group_max(float v) {
     if constexpr (LPT == 64) v = __builtin_fmaxf(v, __shfl_xor(v, 32));
     return v;
 }
-// How many of the 16 values of o that lane's row holds are at least v.
+// bits, one place up, with the sign bit of d below them: of differences, a bit for each that is negative in two
+// instructions (a comparison and its count are three).  Of finite values: infinities less themselves are NaN.
+__device__ __forceinline__ uint32_t push_sign(uint32_t bits, float d) {
+    return __builtin_amdgcn_alignbit(bits, __float_as_uint(d), 31);
+}
+__device__ __forceinline__ float finite_value(float v) {
+    return __builtin_amdgcn_fmed3f(v, -3.4028234663852886e38f, 3.4028234663852886e38f);
+}
+// A bit for each of the 16 values of w that the lane's row holds that is larger than v.
 template <int R = 0>
-__device__ __forceinline__ int row_at_least(float v, float o) {
+__device__ __forceinline__ uint32_t row_larger(float v, float w, uint32_t bits = 0) {
     if constexpr (R == 16) {
-        return 0;
+        return bits;
     } else {
-        const float w = R == 0 ? o : dpp<ROR + (R == 0 ? 1 : R)>(o);
-        return (w >= v) + row_at_least<R + 1>(v, o);
+        const float x = R == 0 ? w : dpp<ROR + (R == 0 ? 1 : R)>(w);
+        return row_larger<R + 1>(v, w, push_sign(bits, v - x));
     }
 }
-// How many of the LPT lanes' values are at least v.
+// How many of the LPT lanes' (finite) values are larger than v.
 template <int LPT>
-__device__ __forceinline__ int group_at_least(float v) {
-    int n = row_at_least(v, v);
-    if constexpr (LPT >= 32) n += row_at_least(v, __shfl_xor(v, 16));
-    if constexpr (LPT == 64) n += row_at_least(v, __shfl_xor(v, 32)) + row_at_least(v, __shfl_xor(v, 48));
+__device__ __forceinline__ int group_larger(float v) {
+    int n = __builtin_popcount(row_larger(v, v));
+    if constexpr (LPT >= 32) n += __builtin_popcount(row_larger(v, __shfl_xor(v, 16)));
+    if constexpr (LPT == 64)
+        n += __builtin_popcount(row_larger(v, __shfl_xor(v, 32))) + __builtin_popcount(row_larger(v, __shfl_xor(v, 48)));
     return n;
 }
 // Sum of v over the token's lanes before this one.
@@ -240,27 +249,21 @@ __device__ __forceinline__ void top2_step(float& a, float& b) {
     a = __builtin_fmaxf(a, x);
 }
 
-// before[q]: how many groups come before this lane's q-th by their values, lane sl's q-th group being number
-// q (16 / m) + sub of a token (m lanes, a power of two, hold a group; sub = sl / m).  Of another vector of experts the group comes
-// earlier or later as the vector does; within one, by sub.
+// larger[q]: a bit for each group of a token whose value is larger than this lane's q-th group's.  m lanes, a power
+// of two, hold a group of every vector of experts; values are finite.
 template <int N, int R = 0>
-__device__ __forceinline__ void rank_groups(const float (&value)[N], int (&before)[N], int m, int sub) {
+__device__ __forceinline__ void larger_groups(const float (&value)[N], uint32_t (&larger)[N], int m) {
     if constexpr (R < 16) {
         if ((R & (m - 1)) == 0) {
-            constexpr int CTRL = ROR + (R == 0 ? 1 : R);
-            const int s = R == 0 ? sub : __builtin_amdgcn_mov_dpp(sub, CTRL, 0xf, 0xf, true);
 #pragma unroll
             for (int o = 0; o < N; ++o) {
-                const float v = R == 0 ? value[o] : dpp<CTRL>(value[o]);
+                const float v = R == 0 ? value[o] : dpp<ROR + (R == 0 ? 1 : R)>(value[o]);
 #pragma unroll
-                for (int q = 0; q < N; ++q) {
-                    if (o < q) before[q] += v >= value[q];
-                    else if (o > q) before[q] += v > value[q];
-                    else if (R > 0) before[q] += v > value[q] || (v == value[q] && s < sub);
-                }
+                for (int q = 0; q < N; ++q)
+                    if (R > 0 || o != q) larger[q] = push_sign(larger[q], value[q] - v);
             }
         }
-        rank_groups<N, R + 1>(value, before, m, sub);
+        larger_groups<N, R + 1>(value, larger, m);
     }
 }
 
@@ -383,24 +386,36 @@ __device__ __forceinline__ void route_token(const RouteParams& p, int64_t row, d
     wave_sync();
 }
 
-// What one wave holds in LDS: scores by expert while groups are chosen, then its tokens' candidates, then the
-// choices of a token that is done again.
+// What one wave holds in LDS: the choices by expert (or groups' scores before), a list of its tokens' candidates, and
+// in place of both the fp64 choices of a token that is done again.
 template <int LPT, int V>
 struct RouteLds {
-    static constexpr int CAP = 4 * LPT;  // candidates of a token; one place more, so that tokens lie on other banks
-    struct Candidate {
-        double c;
-        int e;
-        float l;
-    };
+    static constexpr int CAP = 2 * LPT;  // candidates of a token
     union {
-        float score[64 * V];
-        Candidate can[256 + 64 / LPT];
-        double by_e[LPT * V];  // route_token's
+        struct {
+            float c[64 * V];
+            uint16_t e[64 / LPT][CAP];       // candidates
+            uint16_t chosen[64 / LPT][CAP];  // in order
+        };
+        double by_e[LPT * V];
     };
-    float chosen[64];  // logits of the chosen, and the experts
-    int ids[64];
 };
+
+// How many of the values w that the 16 lanes of the row hold come before v: larger ones, and equal ones of a lower
+// expert.  w and f: this row's lanes' or another row's, OWN: whether this lane's is among them.
+template <bool OWN, int R = 0>
+__device__ __forceinline__ int row_before(float v, int e, float w, int f) {
+    if constexpr (R == 16) {
+        return 0;
+    } else if constexpr (OWN && R == 0) {
+        return row_before<OWN, 1>(v, e, w, f);
+    } else {
+        constexpr int CTRL = ROR + (R == 0 ? 1 : R);
+        const float x = R == 0 ? w : dpp<CTRL>(w);
+        const int g = R == 0 ? f : __builtin_amdgcn_mov_dpp(f, CTRL, 0xf, 0xf, true);
+        return (x > v || (x == v && g < e)) + row_before<OWN, R + 1>(v, e, w, f);
+    }
+}
 
 // LPT lanes a token, four neighbouring experts a vector, V experts a lane.
 //
@@ -417,7 +432,8 @@ __global__ __launch_bounds__(256, 5) void route_kernel(RouteParams p, int64_t ro
     __shared__ Lds lds4[4];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, sl = lane % LPT, tok = lane / LPT, first = tok * LPT;
     Lds& lds = lds4[wave];
-    typename Lds::Candidate* can = lds.can + tok * (CAP + 1);
+    uint16_t* const list = lds.e[tok];
+    uint16_t* const order = lds.chosen[tok];
     const int E = p.n_experts, K = p.top_k, G = p.n_groups, size = p.group_size;
     const bool sigmoid = p.score != SCORE_SOFTMAX, top2 = p.group_score == GROUP_TOP2;
     const bool by_score = p.bias || (G > 1 && top2);  // whether fp32 scores take part in the choice
@@ -458,7 +474,7 @@ __global__ __launch_bounds__(256, 5) void route_kernel(RouteParams p, int64_t ro
         z = 0.0f;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            c[v] = expf(l[v] - soft.most);  // 0 where there is none
+            c[v] = __builtin_amdgcn_exp2f(1.44269504088896341f * (l[v] - soft.most));  // 0 where there is none
             z += c[v];
         }
         z = group_sum<LPT>(z);
@@ -477,8 +493,12 @@ __global__ __launch_bounds__(256, 5) void route_kernel(RouteParams p, int64_t ro
     const float* bias = p.bias;
     auto choices = [&] {
         if (!bias) {
+            // bf16 logits are often equal: the lower half of their bits takes the expert's place in the order
 #pragma unroll
-            for (int v = 0; v < V; ++v) c[v] = l[v];
+            for (int v = 0; v < V; ++v) {
+                const uint32_t u = __float_as_uint(l[v]), e = (v / 4 * LPT + sl) * 4 + v % 4;
+                c[v] = p.bf16 && l[v] > NONE ? __uint_as_float(u | (int32_t(u) < 0 ? e : 1023 - e)) : l[v];
+            }
             return;
         }
 #pragma unroll
@@ -492,11 +512,20 @@ __global__ __launch_bounds__(256, 5) void route_kernel(RouteParams p, int64_t ro
                 c[4 * q + j] = __builtin_fmaxf(__builtin_fmaf(l[4 * q + j], 0.0f, c[4 * q + j] + b[j]), NONE);
         }
     };
-    const float slack = by_score ? (sigmoid ? 7.62939453125e-06f : 1.52587890625e-05f * share) : 0.0f;  // 2^-17, 2^-16
+    // Twice the error of a choice c in fp32, but for the 2^-24 |c| of its last addition.  Sigmoid: the exponent's product
+    // (|l| s (1 - s) 1.5 2^-24, at most 0.4 2^-24), exp2, the sum and the reciprocal: 3.5 2^-24 at most, 2^-20 is twice
+    // that.  Softmax: the exponential's own (2 + |l - most|) 2^-24 and its sum's of up to 22 additions and 9 2^-24 of its
+    // terms, each of a score: 36 2^-24 of the largest at most.
+    const float slack = by_score ? (sigmoid ? 9.5367431640625e-07f : 7.62939453125e-06f * share) : 0.0f;  // 2^-20, 2^-17
 
     if (G > 1) {
         const bool plain = top2 && !bias;  // groups by s, not by c
-        if (!plain) choices();
+        if (!plain) {
+            choices();
+        } else {
+#pragma unroll
+            for (int v = 0; v < V; ++v) c[v] = l[v] > NONE ? c[v] : NONE;
+        }
         float worst = NONE, next = NONE;  // -value of the worst group kept, value of the best other
         auto note = [&](float value, bool keep) {
             worst = keep ? __builtin_fmaxf(worst, -value) : worst;
@@ -506,12 +535,10 @@ __global__ __launch_bounds__(256, 5) void route_kernel(RouteParams p, int64_t ro
             // m lanes hold a group of every vector: pairs of the larger two meet over DPP
             const int m = size / 4;
             float value[N];
-            int before[N] = {};
+            uint32_t larger[N] = {};
 #pragma unroll
             for (int q = 0; q < N; ++q) {
-                float s[4];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) s[j] = plain && l[4 * q + j] == NONE ? NONE : c[4 * q + j];
+                const float* s = c + 4 * q;
                 const float low = __builtin_fminf(s[0], s[1]), high = __builtin_fmaxf(s[0], s[1]);
                 const float low2 = __builtin_fminf(s[2], s[3]), high2 = __builtin_fmaxf(s[2], s[3]);
                 float a = __builtin_fmaxf(high, high2);
@@ -520,27 +547,32 @@ __global__ __launch_bounds__(256, 5) void route_kernel(RouteParams p, int64_t ro
                 if (m >= 4) top2_step<0x4e>(a, b);    // quad_perm 2 3 0 1
                 if (m >= 8) top2_step<0x141>(a, b);   // row_half_mirror
                 if (m >= 16) top2_step<0x140>(a, b);  // row_mirror
-                value[q] = top2 && b > NONE ? a + b : a;
+                value[q] = finite_value(top2 && b > NONE ? a + b : a);
             }
-            rank_groups(value, before, m, sl >> __builtin_ctz(m));
+            larger_groups(value, larger, m);
             if (plain) choices();
+            int kept = 0;
 #pragma unroll
             for (int q = 0; q < N; ++q) {
-                const bool keep = value[q] > NONE && before[q] < p.top_groups;
+                const bool keep = __builtin_popcount(larger[q]) < p.top_groups;
                 note(value[q], keep);
+                kept += keep;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) c[4 * q + j] = keep ? c[4 * q + j] : NONE;
             }
+            // more than top_groups where some are equal: not to be left open but among groups without an expert
+            kept = int(group_sum<LPT>(float(kept)));
+            redo = kept > p.top_groups * m && -group_max<LPT>(worst) > -3.4028234663852886e38f;
         } else {
             // every lane below G has a group, and reads its scores from a place of its own on
             const uint32_t inverse = ((1u << 20) + size - 1) / size;  // e / size = e inverse >> 20 for e < 1024
 #pragma unroll
             for (int v = 0; v < V; ++v)
-                lds.score[tok * (LPT * V) + (v / 4 * LPT + sl) * 4 + v % 4] = plain && l[v] == NONE ? NONE : c[v];
+                lds.c[tok * (LPT * V) + (v / 4 * LPT + sl) * 4 + v % 4] = c[v];
             wave_sync();
             float a = NONE, b = NONE;
             if (sl < G) {
-                const float* group = lds.score + tok * (LPT * V) + sl * size;
+                const float* group = lds.c + tok * (LPT * V) + sl * size;
                 int at = sl % size;
                 for (int i = 0; i < size; ++i) {
                     const float v = group[at];
@@ -570,28 +602,33 @@ __global__ __launch_bounds__(256, 5) void route_kernel(RouteParams p, int64_t ro
             worst = -group_max<LPT>(worst);
             next = group_max<LPT>(next);
             const float near = 2.0f * slack + 4.76837158203125e-07f * (__builtin_fabsf(worst) + __builtin_fabsf(next));
-            redo = next > NONE && !(worst - next > near);
+            redo |= next > -3.4028234663852886e38f && !(worst - next > near);
         }
     } else {
         choices();
     }
 
     // candidates: not below the top_k-th largest of the lanes' largest, less the slack
-    const float most = lane_max(c);
-    float bar = group_max<LPT>(group_at_least<LPT>(most) >= K ? most : NONE);
-    if (bias && bar < __builtin_inff()) bar -= slack + 4.76837158203125e-07f * __builtin_fabsf(bar);
-    bar = __builtin_fmaxf(bar, -3.4028234663852886e38f);  // of -inf (less inf: NaN): every expert there is
+    const float most = finite_value(lane_max(c));
+    float bar = -group_max<LPT>(group_larger<LPT>(most) < K ? -most : NONE);
+    if (bias) bar -= slack + 4.76837158203125e-07f * __builtin_fabsf(bar);
+    bar = __builtin_fmaxf(bar, -3.4028234663852886e38f);  // every expert there is
     uint32_t live = 0;
 #pragma unroll
-    for (int v = 0; v < V; ++v) live |= c[v] >= bar ? 1u << v : 0u;
+    for (int v = 0; v < V; ++v) live = push_sign(live, c[v] - bar);
+    live = ~live & ((1u << V) - 1);  // bit V - 1 - v: of c[v]
+    float* const all = lds.c + tok * (LPT * V);
+#pragma unroll
+    for (int q = 0; q < N; ++q)
+        *reinterpret_cast<float4*>(all + (q * LPT + sl) * 4) = make_float4(c[4 * q], c[4 * q + 1], c[4 * q + 2], c[4 * q + 3]);
     int n = __builtin_popcount(live);
     int at = group_before<LPT>(n, sl);
     n = __shfl(at + n, first + LPT - 1);  // of the token
     redo |= n > CAP;
     if (!redo)
         for (; live; live &= live - 1) {
-            const int v = __builtin_ctz(live);
-            can[at++].e = (v / 4 * LPT + sl) * 4 + v % 4;
+            const int v = V - 1 - __builtin_ctz(live);
+            list[at++] = uint16_t((v / 4 * LPT + sl) * 4 + v % 4);
         }
     int got = redo ? 0 : n;  // candidates of the token, and below the chosen
     int longest = got;
@@ -599,53 +636,85 @@ __global__ __launch_bounds__(256, 5) void route_kernel(RouteParams p, int64_t ro
     for (int d = LPT; d < 64; d *= 2) longest = max(longest, __shfl_xor(longest, d));
     longest = __builtin_amdgcn_readfirstlane(longest);
     wave_sync();
-    for (int i = sl; i < longest; i += LPT) {
-        int e = E;
-        float lg = NONE;
-        if (i < got) {
-            e = can[i].e;
-            lg = logit(p, row, e);
+    // their order, in fp32 first: a candidate a lane where there are no more
+    if (LPT < 64 && longest <= LPT) {
+        const int e = sl < got ? list[sl] : E + sl;
+        const float x = sl < got ? finite_value(all[e]) : NONE;
+        int before = __builtin_popcount(row_larger(x, x));
+        if constexpr (LPT == 32) before += __builtin_popcount(row_larger(x, __shfl_xor(x, 16)));
+        // a place each, but for equal ones
+        uint32_t places = sl < got ? 1u << before : 0;
+        places |= uint32_t(__float_as_int(dpp<ROR + 8>(__uint_as_float(places))));
+        places |= uint32_t(__float_as_int(dpp<ROR + 4>(__uint_as_float(places))));
+        places |= uint32_t(__float_as_int(dpp<ROR + 2>(__uint_as_float(places))));
+        places |= uint32_t(__float_as_int(dpp<ROR + 1>(__uint_as_float(places))));
+        if constexpr (LPT == 32) places |= __shfl_xor(places, 16);
+        if (__any(__builtin_popcount(places) != got)) {
+            const float y = sl < got ? all[e] : NONE;
+            before = row_before<true>(y, e, y, e);
+            if constexpr (LPT == 32) before += row_before<false>(y, e, __shfl_xor(y, 16), __shfl_xor(e, 16));
         }
-        can[i] = {choice(p, lg, e, soft), e, lg};
+        if (sl < got) order[before] = uint16_t(e);
+    } else {
+        for (int i = sl; i < got; i += LPT) {
+            const int e = list[i];
+            const float x = all[e];
+            int before = 0;
+            for (int o = 0; o < got; ++o) {
+                const int f = list[o];
+                before += all[f] > x || (all[f] == x && f < e);
+            }
+            order[before] = uint16_t(e);
+        }
     }
     wave_sync();
-    // the softmax's sum is fp32's: an order within its error of the scores needs it in fp64
-    const double close = bias && !sigmoid ? double(slack) : -1.0;
-    for (int i0 = 0; i0 < longest; i0 += LPT) {
-        const int i = min(i0 + sl, longest - 1);
-        const typename Lds::Candidate mine = can[i];
-        int before = 0;
-        for (int o = 0; o < longest; ++o) {
-            const double w = can[o].c;
-            const int f = can[o].e;
-            before += w > mine.c || (w == mine.c && f < mine.e);
-            if (close >= 0.0) redo |= fabs(w - mine.c) < close && f != mine.e;
+    if (bias) {
+        // two neighbours in the order that lie within the slack, and are not of equal logits and biases
+        bool near = false;
+        for (int i = sl; i + 1 < got; i += LPT) {
+            const int e = order[i], f = order[i + 1];
+            const float x = all[e], y = all[f];
+            if (x - y < slack + 2.384185791015625e-07f * __builtin_fabsf(x))
+                near |= logit(p, row, e) != logit(p, row, f) || bias[e] != bias[f];
         }
-        if (i0 + sl < got && before < K) {
-            lds.ids[first + before] = mine.e;
-            lds.chosen[first + before] = mine.l;
+        if (sigmoid && __any(near)) {
+            // in fp64, in the place of the fp32 choices
+            double* const exact = reinterpret_cast<double*>(all);
+            wave_sync();
+            for (int i = sl; i < got; i += LPT) exact[i] = choice(p, logit(p, row, list[i]), list[i], soft);
+            wave_sync();
+            for (int i = sl; i < got; i += LPT) {
+                const double x = exact[i];
+                const int e = list[i];
+                int before = 0;
+                for (int o = 0; o < got; ++o) before += exact[o] > x || (exact[o] == x && list[o] < e);
+                order[before] = uint16_t(e);
+            }
+            wave_sync();
+        } else {
+            redo |= near;  // the softmax's sum is needed in fp64, too
         }
     }
     got = min(got, K);
-    wave_sync();
     // weights of the chosen, a lane each
-    const float lg = sl < got ? lds.chosen[lane] : NONE;
-    float w = 0.0f;
-    if (p.renormalise) {
-        // from the largest chosen logit where scores underflow: they keep their shares
-        const float top = group_max<LPT>(lg);
-        const bool shifted = !sigmoid || top < -60.0f;
-        if (sl < got) w = shifted ? expf(lg - top) : 1.0f / (1.0f + expf(-lg));
-        const float total = group_sum<LPT>(w);
+    const int pick = sl < got ? order[sl] : -1;
+    float lg = NONE;
+    if (sl < got) lg = bias ? logit(p, row, pick) : __uint_as_float(__float_as_uint(all[pick]) & (p.bf16 ? 0xffff0000u : ~0u));
+    // renormalised from the largest chosen logit where scores underflow: they keep their shares
+    const float top = p.renormalise ? group_max<LPT>(lg) : soft.most;
+    const bool shifted = !sigmoid || (p.renormalise && top < -60.0f);
+    float w = expf(shifted ? lg - top : -lg);
+    if (!shifted) w = 1.0f / (1.0f + w);
+    w = sl < got ? w : 0.0f;
+    if (p.renormalise || !sigmoid) {
+        const float total = p.renormalise ? group_sum<LPT>(w) : z;
         w = sl < got ? w / total : 0.0f;
-    } else if (sl < got) {
-        w = sigmoid ? 1.0f / (1.0f + expf(-lg)) : expf(lg - soft.most) / z;
     }
     constexpr uint64_t TOKEN = LPT == 64 ? ~0ull : (1ull << LPT % 64) - 1;
     uint64_t left = __ballot(redo && in);
     if (in && sl < K && !(left >> first & TOKEN)) {
         p.weights[row * K + sl] = p.scale * w;
-        p.ids[row * K + sl] = sl < got ? lds.ids[lane] : -1;
+        p.ids[row * K + sl] = pick;
     }
     for (int t = 0; left; ++t, left = LPT == 64 ? 0 : left >> LPT % 64)
         if (left & TOKEN) route_token(p, r0 + t, lds.by_e);
