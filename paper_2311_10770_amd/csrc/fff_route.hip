@@ -390,7 +390,7 @@ __device__ __forceinline__ void route_token(const RouteParams& p, int64_t row, d
 // in place of both the fp64 choices of a token that is done again.
 template <int LPT, int V>
 struct RouteLds {
-    static constexpr int CAP = 2 * LPT;  // candidates of a token
+    static constexpr int CAP = V >= 8 ? 4 * LPT : 2 * LPT;  // candidates of a token: their fp64 choices fit in the place of c
     union {
         struct {
             float c[64 * V];
