@@ -720,7 +720,123 @@ __global__ __launch_bounds__(256, 5) void route_kernel(RouteParams p, int64_t ro
         if (left & TOKEN) route_token(p, r0 + t, lds.by_e);
 }
 
-// The gradient: a wave a token.
+// v of lane J of every row of 16 (of the LPT lanes of a token).
+template <int LPT, int J>
+__device__ __forceinline__ int of_lane(int v, int first) {
+    if constexpr (LPT == 16) return __builtin_amdgcn_mov_dpp(v, 0x150 + J, 0xf, 0xf, true);  // row_newbcast
+    else return __shfl(v, first + J);
+}
+// The sum of d over the token's entries of this lane's expert, in their order.
+template <int LPT, int J = 0>
+__device__ __forceinline__ float of_expert(int id, float d, int top_k, int first, float sum = 0.0f) {
+    if constexpr (J < LPT) {
+        if (J < top_k) {
+            const int i = of_lane<LPT, J>(id, first);
+            const float x = __int_as_float(of_lane<LPT, J>(__float_as_int(d), first));
+            return of_expert<LPT, J + 1>(id, d, top_k, first, i == id ? sum + x : sum);
+        }
+    }
+    return sum;
+}
+
+// The gradient for up to 1024 experts: LPT lanes a token, as route_kernel has them.  Lane j of a token has its entry
+// j; what the entries give their experts passes through LDS.  Only the plain softmax reads the other experts'
+// logits: else theirs is 0.
+template <int LPT, int V>
+__global__ __launch_bounds__(256) void route_bwd_kernel(RouteBwdParams p, int64_t row0) {
+    constexpr int TPW = 64 / LPT, N = V / 4;
+    __shared__ float s_own[4][64 * V];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, sl = lane % LPT, tok = lane / LPT, first = tok * LPT;
+    const int E = p.n_experts, K = p.top_k;
+    const bool sigmoid = p.score != SCORE_SOFTMAX, every = !sigmoid && !p.renormalise;
+    const int64_t r0 = (row0 / TPW + int64_t(blockIdx.x) * 4 + wave) * TPW;
+    if (r0 >= p.n_tokens) return;
+    const bool in = r0 + tok < p.n_tokens;
+    const int64_t row = in ? r0 + tok : p.n_tokens - 1;  // lanes behind the last token do it again
+    int id = -1;
+    float d = 0.0f, lg = NONE;
+    if (sl < K) {
+        id = p.ids[row * K + sl];
+        d = p.scale * p.dweights[row * K + sl];
+    }
+    float l[V], most = NONE, z = 1.0f;
+    if (every) {
+        if (E == LPT * V) {
+#pragma unroll
+            for (int q = 0; q < N; ++q)
+                unpack4(l + 4 * q, load4<true>(p.logits, p.bf16, row * E + (q * LPT + sl) * 4, 4), p.bf16);
+        } else {
+#pragma unroll
+            for (int q = 0; q < N; ++q) {
+                const int col = (q * LPT + sl) * 4;
+                unpack4(l + 4 * q, load4<false>(p.logits, p.bf16, row * E + col, E - col), p.bf16);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) l[4 * q + j] = j < E - col ? l[4 * q + j] : NONE;
+            }
+        }
+    }
+    float* const own = s_own[wave] + tok * (LPT * V);
+#pragma unroll
+    for (int q = 0; q < N; ++q) *reinterpret_cast<float4*>(own + (q * LPT + sl) * 4) = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    id = id >= 0 && id < E ? id : -1;
+    if (id >= 0) lg = clean_logit(load_elem(p.logits, p.bf16, row * E + id));
+    id = lg > NONE ? id : -1;  // an expert that is masked takes no part
+    d = id >= 0 ? d : 0.0f;
+    if (every) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            l[v] = clean_logit(l[v]);
+            most = __builtin_fmaxf(most, l[v]);
+        }
+        most = group_max<LPT>(most);
+        most = most > NONE ? most : 0.0f;
+        z = 0.0f;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            l[v] = __builtin_amdgcn_exp2f(1.44269504088896341f * (l[v] - most));  // 0 where there is none
+            z += l[v];
+        }
+        z = group_sum<LPT>(z);
+        z = z > 0.0f ? z : 1.0f;
+    } else if (p.renormalise) {
+        most = group_max<LPT>(lg);
+    }
+    // this entry's share of d; all: what the softmax takes from every expert's
+    const bool shifted = !sigmoid || (p.renormalise && most < -60.0f);
+    const float x = expf(shifted ? lg - most : -lg);
+    float s = id < 0 ? 0.0f : shifted ? x : 1.0f / (1.0f + x), all = 0.0f;
+    const float rest = sigmoid ? 1.0f / (1.0f + expf(lg)) : 1.0f;  // 1 - s
+    if (p.renormalise) {
+        const float total = group_sum<LPT>(s);
+        s = id < 0 ? 0.0f : s / total;
+        const float mean = group_sum<LPT>(d * s);  // of all lanes: no condition around it
+        d = id < 0 ? 0.0f : s * (d - mean) * rest;
+    } else if (sigmoid) {
+        d = id < 0 ? 0.0f : d * s * rest;
+    } else {
+        all = group_sum<LPT>(d * (s / z));
+    }
+    const float sum = of_expert<LPT>(id, d, K, first);
+    wave_sync();
+    if (id >= 0) own[id] = sum;  // entries of one expert write the same
+    wave_sync();
+    const float share = 1.0f / z;
+#pragma unroll
+    for (int q = 0; q < N; ++q) {
+        const int col = (q * LPT + sl) * 4;
+        const float4 o = *reinterpret_cast<const float4*>(own + col);
+        float g[4] = {o.x, o.y, o.z, o.w};
+        if (every) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) g[j] = l[4 * q + j] * share * (g[j] - all);
+        }
+        if (!in) continue;
+        if (E == LPT * V) store4<true>(p.dlogits, p.d_bf16, row * E + col, 4, g);
+        else store4<false>(p.dlogits, p.d_bf16, row * E + col, E - col, g);
+    }
+}
+
+// The gradient for any number of experts: a wave a token.
 __global__ __launch_bounds__(256) void route_bwd_any_kernel(RouteBwdParams p) {
     const int lane = threadIdx.x & 63, E = p.n_experts, K = p.top_k;
     const bool sigmoid = p.score != SCORE_SOFTMAX;
@@ -787,34 +903,56 @@ __global__ __launch_bounds__(256) void route_bwd_any_kernel(RouteBwdParams p) {
 
 }  // namespace
 
-hipError_t run_route(const RouteParams& p, const DeviceInfo& dev, hipStream_t stream) {
-    const int cus = std::max(dev.cu_count, 1);
-    auto launch = [&](auto lpt, auto v) {
-        constexpr int per = 4 * 64 / lpt.value;
-        constexpr int64_t most = int64_t(1) << 23;  // workgroups: a launch holds less than 2^32 threads
-        for (int64_t row0 = 0; row0 < p.n_tokens; row0 += most * per) {
-            const unsigned grid = unsigned(std::min<int64_t>((p.n_tokens - row0 + per - 1) / per, most));
-            hipLaunchKernelGGL((route_kernel<lpt.value, v.value>), dim3(grid), dim3(256), 0, stream, p, row0);
-        }
-    };
+namespace {
+
+// Calls launch(lanes, experts a lane) for `need` lanes a token at least; false where no kernel holds the token.
+template <class F>
+bool token_shape(int32_t n_experts, int need, F launch) {
     auto of = [&](auto lpt) {
-        using N = decltype(lpt);
-        if (p.n_experts <= 4 * N::value) launch(lpt, std::integral_constant<int, 4>{});
-        else if (p.n_experts <= 8 * N::value) launch(lpt, std::integral_constant<int, 8>{});
+        using L = decltype(lpt);
+        if (n_experts <= 4 * L::value) launch(lpt, std::integral_constant<int, 4>{});
+        else if (n_experts <= 8 * L::value) launch(lpt, std::integral_constant<int, 8>{});
         else launch(lpt, std::integral_constant<int, 16>{});
-        return hipGetLastError();
+        return true;
     };
-    // lanes a token: twice as many as it chooses experts (fewer candidates), one at least a group
-    const int lanes = std::max({2 * p.top_k, p.n_groups, (p.n_experts + 15) / 16});
-    if (lanes <= 16 || (p.n_experts <= 256 && 2 * p.top_k <= 16 && groups_in_lanes(p.group_size))) return of(std::integral_constant<int, 16>{});
+    const int lanes = std::max(need, (n_experts + 15) / 16);
+    if (lanes <= 16) return of(std::integral_constant<int, 16>{});
     if (lanes <= 32) return of(std::integral_constant<int, 32>{});
-    if (p.n_groups <= 64 && p.n_experts <= 1024) return of(std::integral_constant<int, 64>{});
-    const unsigned grid = unsigned(std::min<int64_t>(p.n_tokens, 8 * cus));
+    return lanes <= 64 && of(std::integral_constant<int, 64>{});
+}
+
+// Launches kernel<<<, 256>>>(p, first token) for `per` tokens a workgroup: a launch holds less than 2^32 threads.
+template <class K, class P>
+void launch_tokens(K kernel, const P& p, int per, hipStream_t stream) {
+    constexpr int64_t most = int64_t(1) << 23;
+    for (int64_t row0 = 0; row0 < p.n_tokens; row0 += most * per) {
+        const unsigned grid = unsigned(std::min<int64_t>((p.n_tokens - row0 + per - 1) / per, most));
+        hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, stream, p, row0);
+    }
+}
+
+}  // namespace
+
+hipError_t run_route(const RouteParams& p, const DeviceInfo& dev, hipStream_t stream) {
+    // lanes a token: twice as many as it chooses experts (fewer candidates), one at least a group that is not found in
+    // registers
+    const bool in_lanes = p.n_experts <= 256 && groups_in_lanes(p.group_size);
+    const int need = std::max(2 * p.top_k, in_lanes ? 1 : p.n_groups);
+    const int lanes = p.top_k > 32 && need <= 128 && p.n_groups <= 64 ? 64 : need;
+    if (token_shape(p.n_experts, lanes, [&](auto lpt, auto v) {
+            launch_tokens(route_kernel<lpt.value, v.value>, p, 256 / lpt.value, stream);
+        }))
+        return hipGetLastError();
+    const unsigned grid = unsigned(std::min<int64_t>(p.n_tokens, 8 * std::max(dev.cu_count, 1)));
     hipLaunchKernelGGL(route_any_kernel, dim3(grid), dim3(ANY), 0, stream, p);
     return hipGetLastError();
 }
 
 hipError_t run_route_backward(const RouteBwdParams& p, const DeviceInfo& dev, hipStream_t stream) {
+    if (token_shape(p.n_experts, p.top_k, [&](auto lpt, auto v) {
+            launch_tokens(route_bwd_kernel<lpt.value, v.value>, p, 256 / lpt.value, stream);
+        }))
+        return hipGetLastError();
     const unsigned grid = unsigned(std::min<int64_t>((p.n_tokens + 3) / 4, 8 * std::max(dev.cu_count, 1)));
     hipLaunchKernelGGL(route_bwd_any_kernel, dim3(grid), dim3(256), 0, stream, p);
     return hipGetLastError();
