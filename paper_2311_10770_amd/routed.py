@@ -13,7 +13,7 @@ from typing import NamedTuple
 import torch
 
 from .fff import _TORCH_DT, ACTS, FFF_F32, _dt, _raw_stream
-from .ops import _gpu, _index, _lib, _like, _on_call, _rows, _run, _scratch, _sizes
+from .ops import _INT32, _gpu, _lib, _like, _on_call, _rows, _run, _scratch, _sizes
 
 SCORES = {"softmax": 0, "sigmoid": 1}
 GROUP_SCORES = {"max": 0, "top2": 1}
@@ -125,9 +125,25 @@ def _top_k(top_k, n_tokens):
     return top_k
 
 
-def _new_packed(shape, device):
-    return Packed(torch.empty(shape, dtype=torch.float8_e4m3fn, device=device),
-                  torch.empty((shape[0], -(-shape[1] // PACK_BLOCK)), dtype=torch.float8_e8m0fnu, device=device))
+def _out(t, what, index, like, shape, dtype=None, new=None):
+    """A result and its pointer: ``t`` (checked; of ``dtype`` where that is given), or a tensor of the type ``new`` or
+    ``dtype`` that is allocated as ``like`` is, of ``shape`` (``like``'s own where it is None)."""
+    if t is None:
+        dtype = new or dtype
+        if shape is None:
+            t = torch.empty_like(like) if dtype is like.dtype else torch.empty_like(like, dtype=dtype)
+        else:
+            t = like.new_empty(shape, dtype=dtype)
+        return t, t.data_ptr()
+    return t, _like(t, what, index, like.shape if shape is None else shape, dtype)
+
+
+def _new_packed(x):
+    """Packed rows for x's, and their pointers."""
+    B, H = x.shape
+    values = torch.empty_like(x, dtype=torch.float8_e4m3fn)
+    scales = x.new_empty((B, -(-H // PACK_BLOCK)), dtype=torch.float8_e8m0fnu)
+    return Packed(values, scales), values.data_ptr(), scales.data_ptr()
 
 
 def _packed(packed, index, shape=None):
@@ -136,12 +152,11 @@ def _packed(packed, index, shape=None):
         values, scales = packed
     except (TypeError, ValueError):
         raise ValueError("packed must be a Packed: values and scales") from None
-    _gpu(values, "packed values", index)
     if shape is None:
         shape = _rows(values, "packed values")
-    at = values.get_device()
-    return (_like(values, "packed values", at, shape, torch.float8_e4m3fn),
-            _like(scales, "packed scales", at, (shape[0], -(-shape[1] // PACK_BLOCK)), torch.float8_e8m0fnu)), shape
+        index = values.get_device() if index is None else index
+    return (_like(values, "packed values", index, shape, torch.float8_e4m3fn),
+            _like(scales, "packed scales", index, (shape[0], -(-shape[1] // PACK_BLOCK)), torch.float8_e8m0fnu), shape)
 
 
 @_on_call
@@ -160,14 +175,12 @@ def route(logits, top_k: int, *, bias=None, score="softmax", n_groups=1, top_gro
     device, at, top_k = logits.device, logits.get_device(), _top_k(top_k, B)
     n_groups = int(n_groups)
     top_groups = n_groups if top_groups is None else int(top_groups)
-    _sizes((top_k, "top_k"), (n_groups, "n_groups"), (top_groups, "top_groups"))
-    if ids is None:
-        ids = torch.empty((B, top_k), dtype=torch.int32, device=device)
-    if weights is None:
-        weights = torch.empty((B, top_k), dtype=torch.float32, device=device)
+    if max(abs(n_groups), abs(top_groups)) > _INT32:
+        _sizes((n_groups, "n_groups"), (top_groups, "top_groups"))
+    ids, ids_at = _out(ids, "ids", at, logits, (B, top_k), torch.int32)
+    weights, weights_at = _out(weights, "weights", at, logits, (B, top_k), torch.float32)
     _run(_lib().fff_route, FffRouteArgs(
-        logits.data_ptr(), _like(bias, "bias", at, (E,), torch.float32), _like(ids, "ids", at, (B, top_k), torch.int32),
-        _like(weights, "weights", at, (B, top_k), torch.float32), B, E, top_k, n_groups, top_groups,
+        logits.data_ptr(), _like(bias, "bias", at, (E,), torch.float32), ids_at, weights_at, B, E, top_k, n_groups, top_groups,
         _dt(logits, "logits"), _choice(SCORES, score, "score"), _choice(GROUP_SCORES, group_score, "group_score"),
         int(bool(renormalise)), scale, _raw_stream(device, stream)))
     return ids, weights
@@ -192,11 +205,9 @@ def route_backward(dweights, logits, ids, *, score="softmax", renormalise=False,
     shape = logits.shape
     if ids is None:
         raise ValueError("ids are needed")
-    if dlogits is None:
-        dlogits = torch.empty(shape, dtype=dlogits_dtype or logits.dtype, device=device)
+    dlogits, dlogits_at = _out(dlogits, "dlogits", at, logits, None, new=dlogits_dtype or logits.dtype)
     _run(_lib().fff_route_backward, FffRouteBackwardArgs(
-        dweights.data_ptr(), logits.data_ptr(), _like(ids, "ids", at, (B, K), torch.int32),
-        _like(dlogits, "dlogits", at, shape), B, shape[1], K, _dt(logits, "logits"), _dt(dlogits, "dlogits"),
+        dweights.data_ptr(), logits.data_ptr(), _like(ids, "ids", at, (B, K), torch.int32), dlogits_at, B, shape[1], K, _dt(logits, "logits"), _dt(dlogits, "dlogits"),
         _choice(SCORES, score, "score"), int(bool(renormalise)), scale, _raw_stream(device, stream)))
     return dlogits
 
@@ -216,12 +227,13 @@ def combine(rows, top_k: int, weights=None, *, ids=None, residual=None, y=None, 
         raise ValueError(f"rows must be n_tokens x top_k: got {R} rows for top_k = {top_k}")
     B = R // top_k
     _top_k(top_k, B)
-    if y is None:
-        y = torch.empty((B, H), dtype=y_dtype or (residual.dtype if residual is not None else rows.dtype), device=device)
-    _like(y, "y", at, (B, H))
+    if y is None and residual is not None and y_dtype in (None, residual.dtype):
+        y, y_at = _out(None, "y", at, _gpu(residual, "residual", at), None, residual.dtype)
+    else:
+        y, y_at = _out(y, "y", at, rows, (B, H), new=y_dtype or rows.dtype)
     _run(_lib().fff_combine, FffCombineArgs(
         rows.data_ptr(), _like(weights, "weights", at, (B, top_k), torch.float32),
-        _like(ids, "ids", at, (B, top_k), torch.int32), _like(residual, "residual", at, (B, H), y.dtype), y.data_ptr(),
+        _like(ids, "ids", at, (B, top_k), torch.int32), _like(residual, "residual", at, (B, H), y.dtype), y_at,
         B, H, top_k, _dt(rows, "rows"), _dt(y, "y"), _raw_stream(device, stream)))
     return y
 
@@ -237,16 +249,15 @@ def combine_backward(dy, top_k: int, rows=None, weights=None, *, ids=None, drows
     not given (dweights only with ``rows``)."""
     B, H = _rows(dy, "dy")
     device, at, top_k = dy.device, dy.get_device(), _top_k(top_k, B)
-    shape = (B * top_k, H)
-    if drows is None and "drows" in want:
+    shape, drows_at, dweights_at = (B * top_k, H), None, None
+    if drows is not None or "drows" in want:
         dtype = drows_dtype or (rows.dtype if rows is not None else dy.dtype)
-        drows = torch.empty(shape, dtype=dtype, device=device)
-    if dweights is None and "dweights" in want and rows is not None:
-        dweights = torch.empty((B, top_k), dtype=torch.float32, device=device)
+        drows, drows_at = _out(drows, "drows", at, dy, shape, new=dtype)
+    if dweights is not None or ("dweights" in want and rows is not None):
+        dweights, dweights_at = _out(dweights, "dweights", at, dy, (B, top_k), torch.float32)
     _run(_lib().fff_combine_backward, FffCombineBackwardArgs(
         dy.data_ptr(), _like(rows, "rows", at, shape), _like(weights, "weights", at, (B, top_k), torch.float32),
-        _like(ids, "ids", at, (B, top_k), torch.int32), _like(drows, "drows", at, shape),
-        _like(dweights, "dweights", at, (B, top_k), torch.float32), B, H, top_k, _dt(dy, "dy"),
+        _like(ids, "ids", at, (B, top_k), torch.int32), drows_at, dweights_at, B, H, top_k, _dt(dy, "dy"),
         _dt(rows, "rows") if rows is not None else FFF_F32, _dt(drows, "drows") if drows is not None else FFF_F32,
         _raw_stream(device, stream)))
     return drows, dweights
@@ -270,20 +281,22 @@ def rms_norm(x, gamma=None, *, eps=1e-6, residual=None, y=None, s=None, rstd=Non
     s_dt = residual.dtype if residual is not None else s.dtype if s is not None else s_dtype or x.dtype
     if s_dt not in _TORCH_DT:
         raise ValueError(f"s must be float32 or bfloat16, got {s_dt}")
-    if packed is None and pack:
-        packed = _new_packed(shape, device)
-    if y is None and want_y:
-        y = torch.empty(shape, dtype=y_dtype or x.dtype, device=device)
-    if y is None and packed is None:
+    q = q_scale = y_at = s_at = rstd_at = None
+    residual_at = _like(residual, "residual", at, shape)
+    if packed is not None:
+        q, q_scale, _ = _packed(packed, at, shape)
+    elif pack:
+        packed, q, q_scale = _new_packed(x)
+    if y is not None or want_y:
+        y, y_at = _out(y, "y", at, x, None, new=y_dtype or x.dtype)
+    elif packed is None:
         raise ValueError("neither y nor packed rows are wanted")
-    if summed and s is None:
-        s = torch.empty(shape, dtype=s_dt, device=device)
-    if stats and rstd is None:
-        rstd = torch.empty(B, dtype=f32, device=device)
-    q, q_scale = _packed(packed, at, shape)[0] if packed is not None else (None, None)
+    if summed:
+        s, s_at = _out(s, "s", at, x, None, s_dt)
+    if stats or rstd is not None:
+        rstd, rstd_at = _out(rstd, "rstd", at, x, (B,), f32)
     _run(_lib().fff_rms_norm, FffRmsNormArgs(
-        x.data_ptr(), _like(residual, "residual", at, shape), _like(gamma, "gamma", at, (H,), f32),
-        _like(y, "y", at, shape), _like(s, "s", at, shape, s_dt), _like(rstd, "rstd", at, (B,), f32), q, q_scale, B, H,
+        x.data_ptr(), residual_at, _like(gamma, "gamma", at, (H,), f32), y_at, s_at, rstd_at, q, q_scale, B, H,
         _dt(x, "x"), _TORCH_DT[s_dt], _dt(y, "y") if y is not None else FFF_F32, eps, _raw_stream(device, stream)))
     return y, s if summed else x, rstd, packed
 
@@ -312,19 +325,20 @@ def rms_norm_backward(dy, s, rstd, gamma=None, *, ds_in=None, ds=None, dx=None, 
         want = tuple(want) + ("ds",)
     if accumulate and "dgamma" in want and dgamma is None:
         raise ValueError("accumulate adds to the dgamma that is given")
-    if ds is None and "ds" in want:
-        ds = torch.empty(shape, dtype=s.dtype, device=device)
-    if dx is None and not alias and "dx" in want:
-        dx = torch.empty(shape, dtype=dx_dtype, device=device)
-    if dgamma is None and "dgamma" in want:
-        dgamma = torch.empty(H, dtype=f32, device=device)
-    if workspace is None and dgamma is not None:
-        workspace = torch.empty(max(256, rms_norm_backward_workspace_bytes(B, H)), dtype=torch.uint8, device=device)
+    ds_at = dx_at = dgamma_at = None
+    if ds is not None or "ds" in want:
+        ds, ds_at = _out(ds, "ds", at, s, None, s.dtype)
+    if dx is not None or (not alias and "dx" in want):
+        dx, dx_at = _out(dx, "dx", at, dy, None, new=dx_dtype or dy.dtype)
+    if dgamma is not None or "dgamma" in want:
+        dgamma, dgamma_at = _out(dgamma, "dgamma", at, dy, (H,), f32)
+        if workspace is None:
+            workspace = dy.new_empty(max(256, rms_norm_backward_workspace_bytes(B, H)), dtype=torch.uint8)
     _run(_lib().fff_rms_norm_backward, FffRmsNormBackwardArgs(
         dy.data_ptr(), s.data_ptr(), _like(rstd, "rstd", at, (B,), f32), _like(gamma, "gamma", at, (H,), f32),
-        _like(ds_in, "ds_in", at, shape, s.dtype), _like(ds, "ds", at, shape, s.dtype), _like(dx, "dx", at, shape),
-        _like(dgamma, "dgamma", at, (H,), f32), B, H, _dt(dx, "dx") if dx is not None else FFF_F32, _dt(s, "s"),
-        _dt(dy, "dy"), int(bool(accumulate)), *_scratch(workspace, "workspace", at), _raw_stream(device, stream)))
+        _like(ds_in, "ds_in", at, shape, s.dtype), ds_at, dx_at, dgamma_at, B, H,
+        _dt(dx, "dx") if dx is not None else FFF_F32, _dt(s, "s"), _dt(dy, "dy"), int(bool(accumulate)),
+        *_scratch(workspace, "workspace", at), _raw_stream(device, stream)))
     return ds, (ds if "dx" in want else None) if alias else dx, dgamma
 
 
@@ -337,29 +351,25 @@ def pack_rows(x, *, packed=None, stream=None):
     shape = _rows(x, "x")
     device, at = x.device, x.get_device()
     if packed is None:
-        packed = _new_packed(shape, device)
-    (q, q_scale), _ = _packed(packed, at, shape)
+        packed, q, q_scale = _new_packed(x)
+    else:
+        q, q_scale, _ = _packed(packed, at, shape)
     _run(_lib().fff_pack_rows, FffPackRowsArgs(x.data_ptr(), q, q_scale, shape[0], shape[1], _dt(x, "x"),
                                                _raw_stream(device, stream)))
     return packed
 
 
-def _unpack(first, packed, act, dy=None, dx=None, y=None, stream=None):
-    at = first.get_device()
-    (q, q_scale), shape = _packed(packed, at)
-    _run(_lib().fff_unpack_rows, FffUnpackRowsArgs(
-        q, q_scale, _like(dy, "dy", at, shape), _like(y, "y", at, shape), _like(dx, "dx", at, shape), shape[0], shape[1],
-        _dt(dy, "dy") if dy is not None else FFF_F32, _dt(y, "y") if y is not None else FFF_F32,
-        _dt(dx, "dx") if dx is not None else FFF_F32, ACTS[act] if isinstance(act, str) else int(act),
-        _raw_stream(first.device, stream)))
+def _act(act):
+    return ACTS[act] if isinstance(act, str) else int(act)
 
 
 @_on_call
 def _unpack_rows(values, packed, act, y, dtype, *, stream=None):
-    shape = _packed(packed, None)[1]
-    if y is None:
-        y = torch.empty(shape, dtype=dtype, device=values.device)
-    _unpack(values, packed, act, y=y, stream=stream)
+    q, q_scale, shape = _packed(packed, None)
+    y, y_at = _out(y, "y", values.get_device(), values, None, new=dtype)
+    _run(_lib().fff_unpack_rows, FffUnpackRowsArgs(
+        q, q_scale, None, y_at, None, shape[0], shape[1], FFF_F32, _dt(y, "y"), FFF_F32, _act(act),
+        _raw_stream(values.device, stream)))
     return y
 
 
@@ -383,10 +393,13 @@ def activation_backward(dy, packed, act="gelu", *, dx=None, dx_dtype=None, y=Non
     Returns dx (of ``dx_dtype`` or dy's type; may be the buffer ``dy``), or (dx, y) with ``keep_y`` (or a
     ``y``): y = act(z), of ``y_dtype`` or dy's type, the next product's input for its weight gradient."""
     shape = _rows(dy, "dy")
-    if dx is None:
-        dx = torch.empty(shape, dtype=dx_dtype or dy.dtype, device=dy.device)
-    keep_y = keep_y or y is not None
-    if keep_y and y is None:
-        y = torch.empty(shape, dtype=y_dtype or dy.dtype, device=dy.device)
-    _unpack(dy, packed, act, dy=dy, dx=dx, y=y, stream=stream)
+    device, at = dy.device, dy.get_device()
+    q, q_scale, _ = _packed(packed, at, shape)
+    dx, dx_at = _out(dx, "dx", at, dy, None, new=dx_dtype or dy.dtype)
+    keep_y, y_at = keep_y or y is not None, None
+    if keep_y:
+        y, y_at = _out(y, "y", at, dy, None, new=y_dtype or dy.dtype)
+    _run(_lib().fff_unpack_rows, FffUnpackRowsArgs(
+        q, q_scale, dy.data_ptr(), y_at, dx_at, shape[0], shape[1], _dt(dy, "dy"),
+        _dt(y, "y") if y is not None else FFF_F32, _dt(dx, "dx"), _act(act), _raw_stream(device, stream)))
     return (dx, y) if keep_y else dx
