@@ -13,6 +13,7 @@
 
 #include <algorithm>
 #include <cstdint>
+#include <type_traits>
 
 namespace fff {
 
@@ -20,105 +21,159 @@ namespace {
 
 typedef uint32_t u32x2_a1 __attribute__((ext_vector_type(2), aligned(1)));
 
-// Place of unit i: eight columns; a row is `upr` units long, four a block.
-struct Unit {
-    int64_t row;
-    int col;
-};
-__device__ __forceinline__ Unit unit_of(int64_t i, int upr) {
-    const int64_t row = i / upr;
-    return {row, int(i - row * upr) * 8};
-}
-
-__global__ __launch_bounds__(256) void pack_kernel(PackParams p, int upr, int64_t all) {
-    const int H = p.hidden, blocks = upr / 4;
-    const int64_t total = p.n_rows * H;
-    // whole waves take part, so that a block's four lanes do
-    for (int64_t i0 = int64_t(blockIdx.x) * 256; i0 < all; i0 += int64_t(gridDim.x) * 256) {
-        const int64_t i = i0 + threadIdx.x;
-        const Unit at = unit_of(std::min<int64_t>(i, all - 1), upr);
-        const int left = i < all ? H - at.col : 0;
-        float f[8];
-        uint32_t most = 0;
-        if (left > 0) unpack8(f, load8(p.x, p.x_bf16, at.row * H + at.col, total), p.x_bf16);
+// Where a thread's units of eight columns lie: a workgroup takes U x 256 that follow each other, a thread those 256
+// apart, four a block.  FLAT: rows are whole blocks, so places need no division.  Units behind the last one, and those
+// behind a row's end, have none of their columns (left <= 0).
+template <bool FLAT, int U>
+struct Units {
+    int64_t e[U], scale[U];
+    int left[U];
+    __device__ __forceinline__ Units(int64_t i0, int64_t all, int hidden, int upr) {
+        if constexpr (FLAT) {
 #pragma unroll
-        for (int c = 0; c < 8; ++c) {
-            if (c >= left) f[c] = 0.0f;
-            most = max(most, finite_bits(f[c]));
-        }
-        const uint32_t code = scale_code(max_quad(most));
-        const float inverse = scale_inverse(code);
-#pragma unroll
-        for (int c = 0; c < 8; ++c) f[c] = scaled(f[c], code, inverse);
-        if (left <= 0) continue;
-        uint8_t* q = p.q + at.row * H + at.col;
-        const uint32_t lo = pack_e4m3(f[0], f[1], f[2], f[3]), hi = pack_e4m3(f[4], f[5], f[6], f[7]);
-        if (left >= 8) {
-            *reinterpret_cast<u32x2_a1*>(q) = u32x2_a1{lo, hi};
+            for (int u = 0; u < U; ++u) {
+                const int64_t i = i0 + u * 256 + threadIdx.x;
+                left[u] = i < all ? 8 : 0;
+                e[u] = i < all ? i * 8 : 0;
+                scale[u] = i / 4;
+            }
         } else {
-            for (int c = 0; c < left; ++c) q[c] = uint8_t((c < 4 ? lo : hi) >> (c % 4 * 8));
+            const int64_t row0 = i0 / upr;
+            const uint32_t rest = uint32_t(i0 - row0 * upr);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const uint32_t at = rest + u * 256 + threadIdx.x, q = at / uint32_t(upr), v = at - q * uint32_t(upr);
+                const bool in = i0 + u * 256 + threadIdx.x < all;
+                left[u] = in ? hidden - int(v * 8) : 0;
+                e[u] = left[u] > 0 ? (row0 + q) * hidden + int64_t(v) * 8 : 0;
+                scale[u] = (row0 + q) * (upr / 4) + v / 4;
+            }
         }
-        if (at.col % PACK_BLOCK == 0) p.q_scale[at.row * blocks + at.col / PACK_BLOCK] = uint8_t(code);
+    }
+};
+
+constexpr int PACK_U = 2, UNPACK_U = 4;
+
+template <bool FLAT>
+__global__ __launch_bounds__(256) void pack_kernel(PackParams p, int upr, int64_t all) {
+    constexpr int U = PACK_U;
+    const int64_t total = p.n_rows * p.hidden;
+    // whole waves take part, so that a block's four lanes do
+    for (int64_t i0 = int64_t(blockIdx.x) * (256 * U); i0 < all; i0 += int64_t(gridDim.x) * (256 * U)) {
+        const Units<FLAT, U> at(i0, all, p.hidden, upr);
+        Raw8 raw[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) raw[u] = load8<FLAT>(p.x, p.x_bf16, at.e[u], total);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int left = at.left[u];
+            float f[8];
+            uint32_t most = 0;
+            unpack8(f, raw[u], p.x_bf16);
+#pragma unroll
+            for (int c = 0; c < 8; ++c) {
+                if (!FLAT && c >= left) f[c] = 0.0f;
+                most = max(most, finite_bits(f[c]));
+            }
+            const uint32_t code = scale_code(max_quad(most));
+            const float inverse = scale_inverse(code);
+#pragma unroll
+            for (int c = 0; c < 8; ++c) f[c] = scaled(f[c], code, inverse);
+            if (left <= 0) continue;
+            uint8_t* q = p.q + at.e[u];
+            const uint32_t lo = pack_e4m3(f[0], f[1], f[2], f[3]), hi = pack_e4m3(f[4], f[5], f[6], f[7]);
+            if (FLAT || left >= 8) {
+                *reinterpret_cast<u32x2_a1*>(q) = u32x2_a1{lo, hi};
+            } else {
+                for (int c = 0; c < left; ++c) q[c] = uint8_t((c < 4 ? lo : hi) >> (c % 4 * 8));
+            }
+            if (threadIdx.x % 4 == 0) p.q_scale[at.scale[u]] = uint8_t(code);
+        }
     }
 }
 
-template <int ACT>
+// FINE: an output is stored in fp32, and the activation as exact as that shows.
+template <int ACT, bool FLAT, bool FINE>
 __global__ __launch_bounds__(256) void unpack_kernel(UnpackParams p, int upr, int64_t all) {
-    const int H = p.hidden, blocks = upr / 4;
-    const int64_t total = p.n_rows * H;
-    for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < all; i += int64_t(gridDim.x) * 256) {
-        const Unit at = unit_of(i, upr);
-        const int left = H - at.col;
-        if (left <= 0) continue;
-        const int64_t e = at.row * H + at.col;
-        uint32_t w[2] = {0, 0};
-        if (e + 8 <= total) {
-            const u32x2_a1 v = *reinterpret_cast<const u32x2_a1*>(p.q + e);
-            w[0] = v.x;
-            w[1] = v.y;
-        } else {
-            for (int c = 0; c < 8 && e + c < total; ++c) w[c / 4] |= uint32_t(p.q[e + c]) << (c % 4 * 8);
-        }
-        const float scale = scale_value(p.q_scale[at.row * blocks + at.col / PACK_BLOCK]);
-        float z[8], f[8];
-        unpack_e4m3(z, w[0]);
-        unpack_e4m3(z + 4, w[1]);
+    constexpr int U = UNPACK_U;
+    const int64_t total = p.n_rows * p.hidden;
+    for (int64_t i0 = int64_t(blockIdx.x) * (256 * U); i0 < all; i0 += int64_t(gridDim.x) * (256 * U)) {
+        const Units<FLAT, U> at(i0, all, p.hidden, upr);
+        uint32_t w[U][2], code[U];
+        Raw8 raw[U];
 #pragma unroll
-        for (int c = 0; c < 8; ++c) z[c] *= scale;
+        for (int u = 0; u < U; ++u) {
+            const int64_t e = at.e[u];
+            w[u][0] = w[u][1] = 0;
+            if (FLAT || e + 8 <= total) {
+                const u32x2_a1 v = *reinterpret_cast<const u32x2_a1*>(p.q + e);
+                w[u][0] = v.x;
+                w[u][1] = v.y;
+            } else {
+                for (int c = 0; c < 8 && e + c < total; ++c) w[u][c / 4] |= uint32_t(p.q[e + c]) << (c % 4 * 8);
+            }
+            code[u] = p.q_scale[at.left[u] > 0 ? at.scale[u] : 0];
+        }
         if (p.dx) {
-            unpack8(f, load8(p.dy, p.dy_bf16, e, total), p.dy_bf16);
 #pragma unroll
-            for (int c = 0; c < 8; ++c) f[c] *= act_slope<ACT, true>(z[c]);
-            store8(p.dx, p.dx_bf16, e, left, f);
+            for (int u = 0; u < U; ++u) raw[u] = load8<FLAT>(p.dy, p.dy_bf16, at.e[u], total);
         }
-        if (p.y) {
 #pragma unroll
-            for (int c = 0; c < 8; ++c) f[c] = act_value<ACT, true>(z[c]);
-            store8(p.y, p.y_bf16, e, left, f);
+        for (int u = 0; u < U; ++u) {
+            const int left = at.left[u];
+            if (left <= 0) continue;
+            const float scale = scale_value(code[u]);
+            float z[8], f[8];
+            unpack_e4m3(z, w[u][0]);
+            unpack_e4m3(z + 4, w[u][1]);
+#pragma unroll
+            for (int c = 0; c < 8; ++c) z[c] *= scale;
+            if (p.dx) {
+                unpack8(f, raw[u], p.dy_bf16);
+#pragma unroll
+                for (int c = 0; c < 8; ++c) f[c] *= act_slope<ACT, FINE>(z[c]);
+                store8(p.dx, p.dx_bf16, at.e[u], FLAT ? 8 : left, f);
+            }
+            if (p.y) {
+#pragma unroll
+                for (int c = 0; c < 8; ++c) f[c] = act_value<ACT, FINE>(z[c]);
+                store8(p.y, p.y_bf16, at.e[u], FLAT ? 8 : left, f);
+            }
         }
     }
 }
 
 int units_of(int32_t hidden) { return int(pack_blocks(hidden)) * 4; }
 
+unsigned grid_of(int64_t all, int per, const DeviceInfo& dev) {
+    return unsigned(std::min<int64_t>((all + per - 1) / per, 64 * std::max(dev.cu_count, 1)));
+}
+
 }  // namespace
 
 hipError_t run_pack_rows(const PackParams& p, const DeviceInfo& dev, hipStream_t stream) {
     const int upr = units_of(p.hidden);
     const int64_t all = p.n_rows * upr;
-    const unsigned grid = unsigned(std::min<int64_t>((all + 255) / 256, 64 * std::max(dev.cu_count, 1)));
-    hipLaunchKernelGGL(pack_kernel, dim3(grid), dim3(256), 0, stream, p, upr, all);
+    const unsigned grid = grid_of(all, 256 * PACK_U, dev);
+    if (p.hidden % PACK_BLOCK == 0) hipLaunchKernelGGL(pack_kernel<true>, dim3(grid), dim3(256), 0, stream, p, upr, all);
+    else hipLaunchKernelGGL(pack_kernel<false>, dim3(grid), dim3(256), 0, stream, p, upr, all);
     return hipGetLastError();
 }
 
 hipError_t run_unpack_rows(const UnpackParams& p, const DeviceInfo& dev, hipStream_t stream) {
     const int upr = units_of(p.hidden);
     const int64_t all = p.n_rows * upr;
-    const unsigned grid = unsigned(std::min<int64_t>((all + 255) / 256, 64 * std::max(dev.cu_count, 1)));
-    auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, stream, p, upr, all); };
-    if (p.act == ACT_GELU_ERF) launch(unpack_kernel<ACT_GELU_ERF>);
-    else if (p.act == ACT_GELU_TANH) launch(unpack_kernel<ACT_GELU_TANH>);
-    else launch(unpack_kernel<ACT_IDENTITY>);
+    const unsigned grid = grid_of(all, 256 * UNPACK_U, dev);
+    const bool flat = p.hidden % PACK_BLOCK == 0, fine = (p.dx && !p.dx_bf16) || (p.y && !p.y_bf16);
+    auto launch = [&](auto act) {
+        constexpr int ACT = act.value;
+        auto of = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, stream, p, upr, all); };
+        if (flat) fine ? of(unpack_kernel<ACT, true, true>) : of(unpack_kernel<ACT, true, false>);
+        else fine ? of(unpack_kernel<ACT, false, true>) : of(unpack_kernel<ACT, false, false>);
+    };
+    if (p.act == ACT_GELU_ERF) launch(std::integral_constant<int, ACT_GELU_ERF>{});
+    else if (p.act == ACT_GELU_TANH) launch(std::integral_constant<int, ACT_GELU_TANH>{});
+    else launch(std::integral_constant<int, ACT_IDENTITY>{});
     return hipGetLastError();
 }
 

@@ -352,8 +352,10 @@ __global__ __launch_bounds__(1024) void rms_bwd_sum_kernel(RmsBwdParams p, int p
     for (int64_t c0 = int64_t(blockIdx.x) * 32; c0 < H; c0 += int64_t(gridDim.x) * 32) {
         const int64_t c = c0 + col;
         float v = 0.0f;
-        if (c < H)
+        if (c < H) {
+#pragma unroll 8
             for (int q = lane; q < parts; q += 32) v += p.part[q * H + c];
+        }
         sum[lane][col] = v;
         __syncthreads();
         if (lane == 0 && c < H) {

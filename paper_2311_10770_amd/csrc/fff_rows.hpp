@@ -89,24 +89,25 @@ __device__ __forceinline__ void store4(void* base, int bf, int64_t e, int left, 
 
 // Eight values from element e on of a matrix of `all` elements: bf16 in one 16-byte load, fp32 in two.
 // A vector may run on into the next row (its values are the caller's to leave out): only those that
-// end behind the matrix are read one by one, so that no row's tail costs eight loads.
+// end behind the matrix are read one by one, so that no row's tail costs eight loads.  WHOLE: none does.
 struct Raw8 {
     Raw4 a, b;  // bf16: a alone
 };
 typedef uint32_t u32x4_a2 __attribute__((ext_vector_type(4), aligned(2)));
 
+template <bool WHOLE = false>
 __device__ __forceinline__ Raw8 load8(const void* base, int bf, int64_t e, int64_t all) {
     Raw8 r = {{0, 0, 0, 0}, {0, 0, 0, 0}};
     if (bf) {
         const uint16_t* p = static_cast<const uint16_t*>(base) + e;
-        if (e + 8 <= all) {
+        if (WHOLE || e + 8 <= all) {
             r.a = *reinterpret_cast<const u32x4_a2*>(p);
         } else {
             for (int j = 0; j < 8 && e + j < all; ++j) r.a[j / 2] |= uint32_t(p[j]) << (j % 2 * 16);
         }
     } else {
         const uint32_t* p = static_cast<const uint32_t*>(base) + e;
-        if (e + 8 <= all) {
+        if (WHOLE || e + 8 <= all) {
             r.a = *reinterpret_cast<const u32x4_a4*>(p);
             r.b = *reinterpret_cast<const u32x4_a4*>(p + 4);
         } else {
