@@ -404,10 +404,12 @@ void launch_rows(int shape, const P& p, unsigned grid, hipStream_t stream) {
     }
 }
 
-// Workgroups of the backward, each leaving one partial row: two a CU at most.
+// Workgroups of the backward, each leaving one partial row: two a CU at most, four where one works on a row at a time
+// with four waves.
 int rms_parts(int64_t n_tokens, int32_t hidden) {
-    const int per = rows_per_group(hidden);
-    return int(std::min<int64_t>(512, (n_tokens + per - 1) / per));
+    const int per = rows_per_group(hidden), shape = row_shape(hidden);
+    const int64_t most = shape >= 0 && ROW_SHAPES[shape].lanes == 256 ? 1024 : 512;
+    return int(std::min<int64_t>(most, (n_tokens + per - 1) / per));
 }
 
 }  // namespace

@@ -287,8 +287,20 @@ __device__ __forceinline__ void wave_best(double& v, int& i) {
     step(std::integral_constant<int, ROR + 4>{});
     step(std::integral_constant<int, ROR + 2>{});
     step(std::integral_constant<int, ROR + 1>{});
-    meet(__shfl_xor(v, 16), __shfl_xor(i, 16));
-    meet(__shfl_xor(v, 32), __shfl_xor(i, 32));
+    // rows, then halves: each swap hands a lane both partners' values, of which it holds one
+    auto swap = [&](auto step32) {
+        auto both = [&](uint32_t u) {
+            if constexpr (step32.value) return __builtin_amdgcn_permlane32_swap(u, u, false, false);
+            else return __builtin_amdgcn_permlane16_swap(u, u, false, false);
+        };
+        const uint64_t u = __builtin_bit_cast(uint64_t, v);
+        const auto lo = both(uint32_t(u)), hi = both(uint32_t(u >> 32)), at = both(uint32_t(i));
+        v = __builtin_bit_cast(double, uint64_t(hi[0]) << 32 | lo[0]);
+        i = int(at[0]);
+        meet(__builtin_bit_cast(double, uint64_t(hi[1]) << 32 | lo[1]), int(at[1]));
+    };
+    swap(std::false_type{});
+    swap(std::true_type{});
 }
 
 // A whole token in fp64 by a whole wave, for the few that route_kernel leaves: the choices of all experts go to LDS
@@ -526,15 +538,20 @@ __global__ __launch_bounds__(256, 5) void route_kernel(RouteParams p, int64_t ro
 #pragma unroll
             for (int v = 0; v < V; ++v) c[v] = l[v] > NONE ? c[v] : NONE;
         }
-        float worst = NONE, next = NONE;  // -value of the worst group kept, value of the best other
-        auto note = [&](float value, bool keep) {
-            worst = keep ? __builtin_fmaxf(worst, -value) : worst;
-            next = keep ? next : __builtin_fmaxf(next, value);
+        // -value of the worst group kept, value of the best other; how many are kept: those without an expert (none)
+        // count for nothing, and are kept or not.  More than top_groups where some are equal: left open
+        float worst = NONE, next = NONE;
+        int count = 0;
+        auto note = [&](float value, bool keep, bool none) {
+            worst = keep && !none ? __builtin_fmaxf(worst, -value) : worst;
+            next = keep || none ? next : __builtin_fmaxf(next, value);
+            count += keep && !none;
         };
         if (LPT == 16 && groups_in_lanes(size)) {
             // m lanes hold a group of every vector: pairs of the larger two meet over DPP
             const int m = size / 4;
             float value[N];
+            bool none[N];
             uint32_t larger[N] = {};
 #pragma unroll
             for (int q = 0; q < N; ++q) {
@@ -548,21 +565,18 @@ __global__ __launch_bounds__(256, 5) void route_kernel(RouteParams p, int64_t ro
                 if (m >= 8) top2_step<0x141>(a, b);   // row_half_mirror
                 if (m >= 16) top2_step<0x140>(a, b);  // row_mirror
                 value[q] = finite_value(top2 && b > NONE ? a + b : a);
+                none[q] = a == NONE;
             }
             larger_groups(value, larger, m);
             if (plain) choices();
-            int kept = 0;
 #pragma unroll
             for (int q = 0; q < N; ++q) {
                 const bool keep = __builtin_popcount(larger[q]) < p.top_groups;
-                note(value[q], keep);
-                kept += keep;
+                note(value[q], keep, none[q]);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) c[4 * q + j] = keep ? c[4 * q + j] : NONE;
             }
-            // more than top_groups where some are equal: not to be left open but among groups without an expert
-            kept = int(group_sum<LPT>(float(kept)));
-            redo = kept > p.top_groups * m && -group_max<LPT>(worst) > -3.4028234663852886e38f;
+            redo = int(group_sum<LPT>(float(count))) > p.top_groups * m;
         } else {
             // every lane below G has a group, and reads its scores from a place of its own on
             const uint32_t inverse = ((1u << 20) + size - 1) / size;  // e / size = e inverse >> 20 for e < 1024
@@ -574,6 +588,7 @@ __global__ __launch_bounds__(256, 5) void route_kernel(RouteParams p, int64_t ro
             if (sl < G) {
                 const float* group = lds.c + tok * (LPT * V) + sl * size;
                 int at = sl % size;
+#pragma unroll 4
                 for (int i = 0; i < size; ++i) {
                     const float v = group[at];
                     at = at + 1 == size ? 0 : at + 1;
@@ -581,15 +596,11 @@ __global__ __launch_bounds__(256, 5) void route_kernel(RouteParams p, int64_t ro
                     a = __builtin_fmaxf(a, v);
                 }
             }
-            const float value = top2 && b > NONE ? a + b : a;
-            int before = 0;
-            for (int h = 0; h < G; ++h) {
-                const float v = __shfl(value, first + h);
-                before += v > value || (v == value && h < sl);
-            }
-            const bool keep = value > NONE && before < p.top_groups;
-            note(value, keep);
-            const uint64_t kept = __ballot(keep) >> first;
+            const float value = finite_value(top2 && b > NONE ? a + b : a);
+            const bool keep = group_larger<LPT>(value) < p.top_groups && sl < G;
+            note(value, keep, a == NONE);  // lanes behind the groups' have none
+            const uint64_t kept = __ballot(keep) >> first;  // a bit a group; other tokens' behind
+            redo = int(group_sum<LPT>(float(count))) > p.top_groups;
             if (plain) choices();
 #pragma unroll
             for (int v = 0; v < V; ++v) {
@@ -602,7 +613,7 @@ __global__ __launch_bounds__(256, 5) void route_kernel(RouteParams p, int64_t ro
             worst = -group_max<LPT>(worst);
             next = group_max<LPT>(next);
             const float near = 2.0f * slack + 4.76837158203125e-07f * (__builtin_fabsf(worst) + __builtin_fabsf(next));
-            redo |= next > -3.4028234663852886e38f && !(worst - next > near);
+            redo |= next > NONE && !(worst - next > near);
         }
     } else {
         choices();
