@@ -688,8 +688,19 @@ __global__ __launch_bounds__(256, 5) void route_kernel(RouteParams p, int64_t ro
             if (x - y < slack + 2.384185791015625e-07f * __builtin_fabsf(x))
                 near |= logit(p, row, e) != logit(p, row, f) || bias[e] != bias[f];
         }
-        if (sigmoid && __any(near)) {
-            // in fp64, in the place of the fp32 choices
+        if (__any(near)) {
+            // in fp64, in the place of the fp32 choices, with the softmax's sum formed in fp64 too
+            if (!sigmoid) {
+                double t = 0.0;
+#pragma unroll 4
+                for (int e = sl; e < E; e += LPT) {
+                    const float x = logit(p, row, e);
+                    t += x > NONE ? exp(double(x) - double(soft.most)) : 0.0;
+                }
+#pragma unroll
+                for (int d = 1; d < LPT; d *= 2) t += __shfl_xor(t, d);
+                soft.sum = t > 0.0 ? t : 1.0;
+            }
             double* const exact = reinterpret_cast<double*>(all);
             wave_sync();
             for (int i = sl; i < got; i += LPT) exact[i] = choice(p, logit(p, row, list[i]), list[i], soft);
@@ -702,8 +713,6 @@ __global__ __launch_bounds__(256, 5) void route_kernel(RouteParams p, int64_t ro
                 order[before] = uint16_t(e);
             }
             wave_sync();
-        } else {
-            redo |= near;  // the softmax's sum is needed in fp64, too
         }
     }
     got = min(got, K);
