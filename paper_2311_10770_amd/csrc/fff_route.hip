@@ -578,34 +578,40 @@ __global__ __launch_bounds__(256, 5) void route_kernel(RouteParams p, int64_t ro
             }
             redo = int(group_sum<LPT>(float(count))) > p.top_groups * m;
         } else {
-            // every lane below G has a group, and reads its scores from a place of its own on
+            // h lanes, a power of two, share a group of any size: every h-th score each, from a place of its own on; pairs
+            // of the larger two meet over DPP (rows of 16 at most: 16 lanes)
             const uint32_t inverse = ((1u << 20) + size - 1) / size;  // e / size = e inverse >> 20 for e < 1024
+            int shift = 0;
+            while (shift < 4 && (G << (shift + 1)) <= LPT) ++shift;
+            const int h = 1 << shift, group = sl >> shift, part = sl & (h - 1);
 #pragma unroll
             for (int v = 0; v < V; ++v)
                 lds.c[tok * (LPT * V) + (v / 4 * LPT + sl) * 4 + v % 4] = c[v];
             wave_sync();
             float a = NONE, b = NONE;
-            if (sl < G) {
-                const float* group = lds.c + tok * (LPT * V) + sl * size;
-                int at = sl % size;
+            if (group < G) {
+                const float* scores = lds.c + tok * (LPT * V) + group * size;
 #pragma unroll 4
-                for (int i = 0; i < size; ++i) {
-                    const float v = group[at];
-                    at = at + 1 == size ? 0 : at + 1;
+                for (int i = part; i < size; i += h) {
+                    const float v = scores[i];
                     b = __builtin_fmaxf(b, __builtin_fminf(a, v));
                     a = __builtin_fmaxf(a, v);
                 }
             }
+            if (h >= 2) top2_step<0xb1>(a, b);
+            if (h >= 4) top2_step<0x4e>(a, b);
+            if (h >= 8) top2_step<0x141>(a, b);
+            if (h >= 16) top2_step<0x140>(a, b);
             const float value = finite_value(top2 && b > NONE ? a + b : a);
-            const bool keep = group_larger<LPT>(value) < p.top_groups && sl < G;
+            const bool keep = group_larger<LPT>(value) < p.top_groups * h && group < G;
             note(value, keep, a == NONE);  // lanes behind the groups' have none
-            const uint64_t kept = __ballot(keep) >> first;  // a bit a group; other tokens' behind
-            redo = int(group_sum<LPT>(float(count))) > p.top_groups;
+            const uint64_t kept = __ballot(keep) >> first;  // h bits a group; other tokens' behind
+            redo = int(group_sum<LPT>(float(count))) > p.top_groups * h;
             if (plain) choices();
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 const uint32_t g = uint32_t((v / 4 * LPT + sl) * 4 + v % 4) * inverse >> 20;
-                c[v] = kept >> (g & 63) & 1 ? c[v] : NONE;
+                c[v] = kept >> (g << shift & 63) & 1 ? c[v] : NONE;
             }
             wave_sync();
         }
