@@ -505,11 +505,13 @@ __global__ __launch_bounds__(256, 5) void route_kernel(RouteParams p, int64_t ro
     const float* bias = p.bias;
     auto choices = [&] {
         if (!bias) {
-            // bf16 logits are often equal: the lower half of their bits takes the expert's place in the order
+            // bf16 logits are often equal: the lower half of their bits takes the expert's place in the order.  -0 becomes
+            // 0, whose equal it is.
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const uint32_t u = __float_as_uint(l[v]), e = (v / 4 * LPT + sl) * 4 + v % 4;
-                c[v] = p.bf16 && l[v] > NONE ? __uint_as_float(u | (int32_t(u) < 0 ? e : 1023 - e)) : l[v];
+                c[v] = l[v] + 0.0f;
+                const uint32_t u = __float_as_uint(c[v]), e = (v / 4 * LPT + sl) * 4 + v % 4;
+                if (p.bf16 && l[v] > NONE) c[v] = __uint_as_float(u | (int32_t(u) < 0 ? e : 1023 - e));
             }
             return;
         }
@@ -725,7 +727,10 @@ __global__ __launch_bounds__(256, 5) void route_kernel(RouteParams p, int64_t ro
     // weights of the chosen, a lane each
     const int pick = sl < got ? order[sl] : -1;
     float lg = NONE;
-    if (sl < got) lg = bias ? logit(p, row, pick) : __uint_as_float(__float_as_uint(all[pick]) & (p.bf16 ? 0xffff0000u : ~0u));
+    if (sl < got) {
+        const uint32_t u = __float_as_uint(all[pick]);  // without a bias: the logit, with its place if it has one
+        lg = bias ? logit(p, row, pick) : __uint_as_float(p.bf16 && (u & 0xffffu) != 0xffffu ? u & 0xffff0000u : u);
+    }
     // renormalised from the largest chosen logit where scores underflow: they keep their shares
     const float top = p.renormalise ? group_max<LPT>(lg) : soft.most;
     const bool shifted = !sigmoid || (p.renormalise && top < -60.0f);

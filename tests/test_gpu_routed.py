@@ -88,6 +88,26 @@ def test_route_ties_go_to_the_lowest_index(fff_lib, E):
                 _check_route(fff_lib, l, k, f"{name} {E}", **kw)
 
 
+@pytest.mark.parametrize("E", [16, 64, 256, 500, 2000])
+def test_route_zeros_and_infinities_of_either_type(fff_lib, E):
+    """0 and -0 are equal, in any order; several infinite logits share a softmax, above the largest finite one."""
+    gen = _gen(E + 4)
+    logits = torch.where(torch.rand((6, E), generator=gen, device=DEV) < 0.5, 0.0, -0.0)
+    logits[1] = -logits[1].abs() - 1.0
+    logits[1, ::3], logits[1, 1::3] = 0.0, -0.0
+    logits[2, 3] = logits[2, 9] = logits[2, 10] = INF
+    logits[3, 3], logits[3, 5] = torch.finfo(torch.bfloat16).max, INF
+    logits[4], logits[4, 7] = -INF, INF
+    logits[5, 2:] = torch.finfo(torch.bfloat16).min
+    for t in ("f32", "bf16"):
+        for score in ("softmax", "sigmoid"):
+            for kw in ({}, {"renormalise": True}, {"n_groups": 2, "top_groups": 1, "group_score": "max"}, {"n_groups": 4, "top_groups": 2},
+                       {"bias": torch.zeros(E, device=DEV)}):
+                flush_print(f"[gpu] route zeros and infinities {E} {t} {score} {sorted(kw)}")
+                ids, w = _check_route(fff_lib, logits.to(DT[t]), 5, f"{E} {t}", score=score, **kw)
+                assert torch.isfinite(w).all()
+
+
 @pytest.mark.parametrize("E,G", [(64, 1), (256, 8), (100, 5), (3000, 1)])
 def test_route_order_of_close_choices(fff_lib, E, G):
     """Choices closer to each other than fp32 resolves: a bias that takes back what the score differs by, to 1e-9."""
