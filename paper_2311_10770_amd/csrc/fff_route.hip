@@ -249,24 +249,6 @@ __device__ __forceinline__ void top2_step(float& a, float& b) {
     a = __builtin_fmaxf(a, x);
 }
 
-// larger[q]: a bit for each group of a token whose value is larger than this lane's q-th group's.  m lanes, a power
-// of two, hold a group of every vector of experts; values are finite.
-template <int N, int R = 0>
-__device__ __forceinline__ void larger_groups(const float (&value)[N], uint32_t (&larger)[N], int m) {
-    if constexpr (R < 16) {
-        if ((R & (m - 1)) == 0) {
-#pragma unroll
-            for (int o = 0; o < N; ++o) {
-                const float v = R == 0 ? value[o] : dpp<ROR + (R == 0 ? 1 : R)>(value[o]);
-#pragma unroll
-                for (int q = 0; q < N; ++q)
-                    if (R > 0 || o != q) larger[q] = push_sign(larger[q], value[q] - v);
-            }
-        }
-        larger_groups<N, R + 1>(value, larger, m);
-    }
-}
-
 // Whether route_kernel<16> finds groups of `size` experts in its lanes' registers: a power of two of whole vectors.
 __host__ __device__ __forceinline__ bool groups_in_lanes(int size) { return size >= 4 && size <= 64 && (size & (size - 1)) == 0; }
 
@@ -303,17 +285,15 @@ __device__ __forceinline__ void wave_best(double& v, int& i) {
     swap(std::true_type{});
 }
 
-// A whole token in fp64 by a whole wave, for the few that route_kernel leaves: the choices of all experts go to LDS
-// (by_e, n_experts of them), and each pick is the best that is left.  At most 64 groups.
-__device__ __forceinline__ void route_token(const RouteParams& p, int64_t row, double* by_e) {
-    const int lane = threadIdx.x & 63, E = p.n_experts, G = p.n_groups, size = p.group_size;
-    const bool plain = G > 1 && p.group_score == GROUP_TOP2 && !p.bias;  // groups by s, then experts by the logits
-    auto logits_of = [&] {
-        for (int e = lane; e < E; e += 64) by_e[e] = double(logit(p, row, e));
-    };
+// What few tokens come to, by a whole wave: the fp64 values that a token's experts are chosen by (groups: that its groups
+// are) go to LDS, by_e, and the softmax's largest logit and sum come back.
+__device__ __forceinline__ Softmax choices64(const RouteParams& p, int64_t row, bool groups, double* by_e) {
+    const int lane = threadIdx.x & 63, E = p.n_experts;
+    const bool plain = groups && p.group_score == GROUP_TOP2 && !p.bias;  // by s, where experts go by their logits
     Softmax m{0.0f, 1.0};
     wave_sync();
-    logits_of();
+#pragma unroll 4
+    for (int e = lane; e < E; e += 64) by_e[e] = double(logit(p, row, e));
     if (p.score == SCORE_SOFTMAX) {
         float most = NONE;
         for (int e = lane; e < E; e += 64) most = __builtin_fmaxf(most, float(by_e[e]));
@@ -326,38 +306,53 @@ __device__ __forceinline__ void route_token(const RouteParams& p, int64_t row, d
         m.sum = sum > 0.0 ? sum : 1.0;
     }
     if (p.bias || plain) {
+#pragma unroll 2
         for (int e = lane; e < E; e += 64) {
             const float l = float(by_e[e]);
             by_e[e] = plain ? (l > NONE ? score(l, p.score, m) : -HUGE_VAL) : choice(p, l, e, m);
         }
     }
     wave_sync();
-    if (G > 1) {
-        double a = -HUGE_VAL, b = -HUGE_VAL;
-        if (lane < G) {
-            int at = lane % size;  // lanes start at different banks
-            for (int i = 0; i < size; ++i) {
-                const double c = by_e[lane * size + at];
-                at = at + 1 == size ? 0 : at + 1;
-                b = fmax(b, fmin(a, c));
-                a = fmax(a, c);
-            }
+    return m;
+}
+
+// A token's groups (at most 64) by their fp64 values: a bit every 1 << shift for each that is kept.
+__device__ __forceinline__ uint64_t kept_groups(const RouteParams& p, int64_t row, int shift, double* by_e) {
+    const int lane = threadIdx.x & 63, G = p.n_groups, size = p.group_size, g = lane >> shift;
+    choices64(p, row, true, by_e);
+    double a = -HUGE_VAL, b = -HUGE_VAL;
+    if (g < G) {
+        int at = g % size;  // groups start at different banks
+#pragma unroll 4
+        for (int i = 0; i < size; ++i) {
+            const double c = by_e[g * size + at];
+            at = at + 1 == size ? 0 : at + 1;
+            b = fmax(b, fmin(a, c));
+            a = fmax(a, c);
         }
-        const double value = p.group_score == GROUP_TOP2 && b > -HUGE_VAL ? a + b : a;
-        int before = 0;
-        for (int h = 0; h < G; ++h) {
-            const double v = __shfl(value, h);
-            before += v > value || (v == value && h < lane);
-        }
-        const uint64_t kept = __ballot(lane < G && value > -HUGE_VAL && before < p.top_groups);
-        if (plain) logits_of();
-        wave_sync();
+    }
+    const double value = p.group_score == GROUP_TOP2 && b > -HUGE_VAL ? a + b : a;
+    int before = 0;
+    for (int h = 0; h < G; ++h) {
+        const double v = __shfl(value, h << shift);
+        before += v > value || (v == value && h < g);
+    }
+    wave_sync();
+    return __ballot(g < G && value > -HUGE_VAL && before < p.top_groups);
+}
+
+// A token with more candidates than route_kernel has room for: each pick is the best that is left of all.
+__device__ __forceinline__ void route_token(const RouteParams& p, int64_t row, uint64_t kept, int shift, double* by_e) {
+    const int lane = threadIdx.x & 63, E = p.n_experts, size = p.group_size;
+    const Softmax m = choices64(p, row, false, by_e);
+    if (p.n_groups > 1) {
         for (int e = lane; e < E; e += 64)
-            if (!(kept >> (e / size & 63) & 1)) by_e[e] = -HUGE_VAL;
+            if (!(kept >> (e / size << shift & 63) & 1)) by_e[e] = -HUGE_VAL;
     }
     auto mine_best = [&](double& v, int& i) {
         v = -HUGE_VAL;
         i = E;
+#pragma unroll 4
         for (int e = lane; e < E; e += 64) {
             const double c = by_e[e];
             if (c > v) {
@@ -398,19 +393,15 @@ __device__ __forceinline__ void route_token(const RouteParams& p, int64_t row, d
     wave_sync();
 }
 
-// What one wave holds in LDS: the choices by expert (or groups' scores before), a list of its tokens' candidates, and
-// in place of both the fp64 choices of a token that is done again.
+// What one wave holds in LDS: the choices by expert, a list of its tokens' candidates, and what one token's experts are
+// chosen by in fp64.
 template <int LPT, int V>
 struct RouteLds {
     static constexpr int CAP = V >= 8 ? 4 * LPT : 2 * LPT;  // candidates of a token: their fp64 choices fit in the place of c
-    union {
-        struct {
-            float c[64 * V];
-            uint16_t e[64 / LPT][CAP];       // candidates
-            uint16_t chosen[64 / LPT][CAP];  // in order
-        };
-        double by_e[LPT * V];
-    };
+    float c[64 * V];
+    double by_e[LPT * V];
+    uint16_t e[64 / LPT][CAP];       // candidates
+    uint16_t chosen[64 / LPT][CAP];  // in order
 };
 
 // How many of the values w that the 16 lanes of the row hold come before v: larger ones, and equal ones of a lower
@@ -454,7 +445,25 @@ __global__ __launch_bounds__(256, 5) void route_kernel(RouteParams p, int64_t ro
     if (r0 >= p.n_tokens) return;
     const bool in = r0 + tok < p.n_tokens;
     const int64_t row = in ? r0 + tok : p.n_tokens - 1;  // lanes behind the last token do it again
+    constexpr uint64_t TOKEN = LPT == 64 ? ~0ull : (1ull << LPT % 64) - 1;
+    const float* bias = p.bias;
+    const bool in_lanes = LPT == 16 && G <= 16 && groups_in_lanes(size);
+    const int turn = in_lanes ? __builtin_ctz(size / 4) : 0;  // 1 << turn lanes hold a group of a vector of experts
+    uint64_t kept = ~0ull;  // G > 1: a token's groups, one every 1 << shift bits
+    int shift = 0;
+    if (!in_lanes)
+        while (shift < 4 && (G << (shift + 1)) <= LPT) ++shift;
+    auto lane_max = [](const float (&x)[V]) {
+        float m = x[0];
+#pragma unroll
+        for (int v = 1; v < V; ++v) m = __builtin_fmaxf(m, x[v]);
+        return m;
+    };
     float l[V], c[V];
+    float* const all = lds.c + tok * (LPT * V);
+    auto put4 = [&](float* to, int q, const float (&x)[V]) {
+        *reinterpret_cast<float4*>(to + (q * LPT + sl) * 4) = make_float4(x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]);
+    };
     if (E == LPT * V) {
 #pragma unroll
         for (int q = 0; q < N; ++q)
@@ -470,12 +479,6 @@ __global__ __launch_bounds__(256, 5) void route_kernel(RouteParams p, int64_t ro
     }
 #pragma unroll
     for (int v = 0; v < V; ++v) l[v] = clean_logit(l[v]);
-    auto lane_max = [](const float (&x)[V]) {
-        float m = x[0];
-#pragma unroll
-        for (int v = 1; v < V; ++v) m = __builtin_fmaxf(m, x[v]);
-        return m;
-    };
     Softmax soft{0.0f, 1.0};
     float z = 1.0f;
     if (!sigmoid) {
@@ -493,7 +496,6 @@ __global__ __launch_bounds__(256, 5) void route_kernel(RouteParams p, int64_t ro
         z = z > 0.0f ? z : 1.0f;
         soft.sum = double(z);
     }
-    bool redo = false;  // left to route_token
     const float share = sigmoid ? 1.0f : 1.0f / z;  // no score is larger
     if (by_score) {
 #pragma unroll
@@ -502,7 +504,6 @@ __global__ __launch_bounds__(256, 5) void route_kernel(RouteParams p, int64_t ro
             else c[v] *= share;
         }
     }
-    const float* bias = p.bias;
     auto choices = [&] {
         if (!bias) {
             // bf16 logits are often equal: the lower half of their bits takes the expert's place in the order.  -0 becomes
@@ -526,35 +527,27 @@ __global__ __launch_bounds__(256, 5) void route_kernel(RouteParams p, int64_t ro
                 c[4 * q + j] = __builtin_fmaxf(__builtin_fmaf(l[4 * q + j], 0.0f, c[4 * q + j] + b[j]), NONE);
         }
     };
-    // Twice the error of a choice c in fp32, but for the 2^-24 |c| of its last addition.  Sigmoid: the exponent's product
-    // (|l| s (1 - s) 1.5 2^-24, at most 0.4 2^-24), exp2, the sum and the reciprocal: 3.5 2^-24 at most, 2^-20 is twice
-    // that.  Softmax: the exponential's own (2 + |l - most|) 2^-24 and its sum's of up to 22 additions and 9 2^-24 of its
-    // terms, each of a score: 36 2^-24 of the largest at most.
-    const float slack = by_score ? (sigmoid ? 9.5367431640625e-07f : 7.62939453125e-06f * share) : 0.0f;  // 2^-20, 2^-17
+    // Twice the error of a choice c in fp32, but for the 2^-24 |c| of its last addition.  Sigmoid: the exponent
+    // s (1 - s) (1.3 |l| + 2) 2^-24, the sum and the reciprocal 3 s 2^-24: 3.2 2^-24 at most.  Softmax, of the largest score:
+    // the exponential (2.3 |l - most| + 2) 2^-24, its sum 21 additions and the terms' own, 20 on average, and two roundings:
+    // 47 2^-24.
+    const float slack = by_score ? (sigmoid ? 4.76837158203125e-07f : 7.62939453125e-06f * share) : 0.0f;  // 2^-21, 2^-17
 
     if (G > 1) {
         const bool plain = top2 && !bias;  // groups by s, not by c
         if (!plain) {
             choices();
+#pragma unroll
+            for (int q = 0; q < N; ++q) put4(all, q, c);
         } else {
 #pragma unroll
             for (int v = 0; v < V; ++v) c[v] = l[v] > NONE ? c[v] : NONE;
         }
-        // -value of the worst group kept, value of the best other; how many are kept: those without an expert (none)
-        // count for nothing, and are kept or not.  More than top_groups where some are equal: left open
-        float worst = NONE, next = NONE;
-        int count = 0;
-        auto note = [&](float value, bool keep, bool none) {
-            worst = keep && !none ? __builtin_fmaxf(worst, -value) : worst;
-            next = keep || none ? next : __builtin_fmaxf(next, value);
-            count += keep && !none;
-        };
-        if (LPT == 16 && groups_in_lanes(size)) {
-            // m lanes hold a group of every vector: pairs of the larger two meet over DPP
-            const int m = size / 4;
-            float value[N];
-            bool none[N];
-            uint32_t larger[N] = {};
+        // lanes sl >> shift = g come to hold the two largest of group g, best and second
+        float best = NONE, second = NONE;
+        if (in_lanes) {
+            // pairs of the larger two meet over DPP, then in LDS (where the candidates come to be listed)
+            float2* const pairs = reinterpret_cast<float2*>(lds.e) + tok * 16;
 #pragma unroll
             for (int q = 0; q < N; ++q) {
                 const float* s = c + 4 * q;
@@ -562,71 +555,96 @@ __global__ __launch_bounds__(256, 5) void route_kernel(RouteParams p, int64_t ro
                 const float low2 = __builtin_fminf(s[2], s[3]), high2 = __builtin_fmaxf(s[2], s[3]);
                 float a = __builtin_fmaxf(high, high2);
                 float b = __builtin_fmaxf(__builtin_fmaxf(low, low2), __builtin_fminf(high, high2));
-                if (m >= 2) top2_step<0xb1>(a, b);    // quad_perm 1 0 3 2
-                if (m >= 4) top2_step<0x4e>(a, b);    // quad_perm 2 3 0 1
-                if (m >= 8) top2_step<0x141>(a, b);   // row_half_mirror
-                if (m >= 16) top2_step<0x140>(a, b);  // row_mirror
-                value[q] = finite_value(top2 && b > NONE ? a + b : a);
-                none[q] = a == NONE;
+                if (turn >= 1) top2_step<0xb1>(a, b);   // quad_perm 1 0 3 2
+                if (turn >= 2) top2_step<0x4e>(a, b);   // quad_perm 2 3 0 1
+                if (turn >= 3) top2_step<0x141>(a, b);  // row_half_mirror
+                if (turn >= 4) top2_step<0x140>(a, b);  // row_mirror
+                if ((sl & ((1 << turn) - 1)) == 0)
+                    pairs[(q * 16 + sl) >> turn] = make_float2(a, b);
             }
-            larger_groups(value, larger, m);
-            if (plain) choices();
-#pragma unroll
-            for (int q = 0; q < N; ++q) {
-                const bool keep = __builtin_popcount(larger[q]) < p.top_groups;
-                note(value[q], keep, none[q]);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) c[4 * q + j] = keep ? c[4 * q + j] : NONE;
-            }
-            redo = int(group_sum<LPT>(float(count))) > p.top_groups * m;
-        } else {
-            // h lanes, a power of two, share a group of any size: every h-th score each, from a place of its own on; pairs
-            // of the larger two meet over DPP (rows of 16 at most: 16 lanes)
-            const uint32_t inverse = ((1u << 20) + size - 1) / size;  // e / size = e inverse >> 20 for e < 1024
-            int shift = 0;
-            while (shift < 4 && (G << (shift + 1)) <= LPT) ++shift;
-            const int h = 1 << shift, group = sl >> shift, part = sl & (h - 1);
-#pragma unroll
-            for (int v = 0; v < V; ++v)
-                lds.c[tok * (LPT * V) + (v / 4 * LPT + sl) * 4 + v % 4] = c[v];
             wave_sync();
-            float a = NONE, b = NONE;
+            if (sl < G) {
+                best = pairs[sl].x;
+                second = pairs[sl].y;
+            }
+        } else {
+            // 1 << shift lanes share a group of any size: every so many of its scores each, from a place of its own on
+            const int h = 1 << shift, group = sl >> shift;
+            if (plain) {
+                // by s here, which leaves LDS to the choices behind
+#pragma unroll
+                for (int q = 0; q < N; ++q) put4(all, q, c);
+            }
+            wave_sync();
             if (group < G) {
-                const float* scores = lds.c + tok * (LPT * V) + group * size;
+                const float* of = all + group * size;
 #pragma unroll 4
-                for (int i = part; i < size; i += h) {
-                    const float v = scores[i];
-                    b = __builtin_fmaxf(b, __builtin_fminf(a, v));
-                    a = __builtin_fmaxf(a, v);
+                for (int i = sl & (h - 1); i < size; i += h) {
+                    const float v = of[i];
+                    second = __builtin_fmaxf(second, __builtin_fminf(best, v));
+                    best = __builtin_fmaxf(best, v);
                 }
             }
-            if (h >= 2) top2_step<0xb1>(a, b);
-            if (h >= 4) top2_step<0x4e>(a, b);
-            if (h >= 8) top2_step<0x141>(a, b);
-            if (h >= 16) top2_step<0x140>(a, b);
-            const float value = finite_value(top2 && b > NONE ? a + b : a);
-            const bool keep = group_larger<LPT>(value) < p.top_groups * h && group < G;
-            note(value, keep, a == NONE);  // lanes behind the groups' have none
-            const uint64_t kept = __ballot(keep) >> first;  // h bits a group; other tokens' behind
-            redo = int(group_sum<LPT>(float(count))) > p.top_groups * h;
-            if (plain) choices();
+            if (h >= 2) top2_step<0xb1>(best, second);
+            if (h >= 4) top2_step<0x4e>(best, second);
+            if (h >= 8) top2_step<0x141>(best, second);
+            if (h >= 16) top2_step<0x140>(best, second);
+        }
+        // A group without an expert (none) counts for nothing, whether it is kept or not.  Groups are left open where equal
+        // ones make more than top_groups, and where the worst kept and the best other lie within their errors: each
+        // the slack, 2^-24 of its terms' sizes and of itself
+        const bool two = top2 && second > NONE, none = best == NONE;
+        const float value = finite_value(two ? best + second : best);
+        const bool keep = (group_larger<LPT>(value) >> shift) < p.top_groups && sl >> shift < G;
+        kept = __ballot(keep) >> first;  // other tokens' behind
+        bool open = (int(group_sum<LPT>(keep && !none ? 1.0f : 0.0f)) >> shift) > p.top_groups;
+        if (by_score) {
+            const float worst = -group_max<LPT>(keep && !none ? -value : NONE);
+            const float next = group_max<LPT>(keep || none ? NONE : value);
+            const float sizes = group_max<LPT>(none ? 0.0f : __builtin_fabsf(best) + (two ? __builtin_fabsf(second) : 0.0f));
+            const float near = (top2 ? 2.0f : 1.0f) * (slack + 1.1920928955078125e-07f * sizes);
+            open |= next > NONE && !(worst - next > near);
+        }
+        if (plain) {
+            choices();
+#pragma unroll
+            for (int q = 0; q < N; ++q) put4(all, q, c);
+        }
+        for (uint64_t left = __ballot(open && in); left; left &= ~(TOKEN << (__builtin_ctzll(left) / LPT * LPT))) {
+            const int t = __builtin_ctzll(left) / LPT;
+            const uint64_t exact = kept_groups(p, r0 + t, shift, lds.by_e);
+            if (tok == t) kept = exact;
+        }
+        // the choices come back from LDS: in registers they would be held beside what fp64 needs
+        wave_sync();
+#pragma unroll
+        for (int q = 0; q < N; ++q) {
+            const float4 r = *reinterpret_cast<const float4*>(all + (q * LPT + sl) * 4);
+            c[4 * q] = r.x;
+            c[4 * q + 1] = r.y;
+            c[4 * q + 2] = r.z;
+            c[4 * q + 3] = r.w;
+        }
+        if (in_lanes) {
+#pragma unroll
+            for (int q = 0; q < N; ++q) {
+                const bool k = uint32_t(kept) >> ((q * 16 + sl) >> turn) & 1;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) c[4 * q + j] = k ? c[4 * q + j] : NONE;
+            }
+        } else {
+            const uint32_t inverse = ((1u << 20) + size - 1) / size;  // e / size = e inverse >> 20 for e < 1024
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 const uint32_t g = uint32_t((v / 4 * LPT + sl) * 4 + v % 4) * inverse >> 20;
                 c[v] = kept >> (g << shift & 63) & 1 ? c[v] : NONE;
             }
-            wave_sync();
-        }
-        if (by_score) {
-            worst = -group_max<LPT>(worst);
-            next = group_max<LPT>(next);
-            const float near = 2.0f * slack + 4.76837158203125e-07f * (__builtin_fabsf(worst) + __builtin_fabsf(next));
-            redo |= next > NONE && !(worst - next > near);
         }
     } else {
         choices();
+#pragma unroll
+        for (int q = 0; q < N; ++q) put4(all, q, c);
     }
-
     // candidates: not below the top_k-th largest of the lanes' largest, less the slack
     const float most = finite_value(lane_max(c));
     float bar = -group_max<LPT>(group_larger<LPT>(most) < K ? -most : NONE);
@@ -636,14 +654,10 @@ __global__ __launch_bounds__(256, 5) void route_kernel(RouteParams p, int64_t ro
 #pragma unroll
     for (int v = 0; v < V; ++v) live = push_sign(live, c[v] - bar);
     live = ~live & ((1u << V) - 1);  // bit V - 1 - v: of c[v]
-    float* const all = lds.c + tok * (LPT * V);
-#pragma unroll
-    for (int q = 0; q < N; ++q)
-        *reinterpret_cast<float4*>(all + (q * LPT + sl) * 4) = make_float4(c[4 * q], c[4 * q + 1], c[4 * q + 2], c[4 * q + 3]);
     int n = __builtin_popcount(live);
     int at = group_before<LPT>(n, sl);
     n = __shfl(at + n, first + LPT - 1);  // of the token
-    redo |= n > CAP;
+    const bool redo = n > CAP;  // left to route_token
     if (!redo)
         for (; live; live &= live - 1) {
             const int v = V - 1 - __builtin_ctz(live);
@@ -741,14 +755,16 @@ __global__ __launch_bounds__(256, 5) void route_kernel(RouteParams p, int64_t ro
         const float total = p.renormalise ? group_sum<LPT>(w) : z;
         w = sl < got ? w / total : 0.0f;
     }
-    constexpr uint64_t TOKEN = LPT == 64 ? ~0ull : (1ull << LPT % 64) - 1;
     uint64_t left = __ballot(redo && in);
     if (in && sl < K && !(left >> first & TOKEN)) {
         p.weights[row * K + sl] = p.scale * w;
         p.ids[row * K + sl] = pick;
     }
-    for (int t = 0; left; ++t, left = LPT == 64 ? 0 : left >> LPT % 64)
-        if (left & TOKEN) route_token(p, r0 + t, lds.by_e);
+    for (; left; left &= ~(TOKEN << (__builtin_ctzll(left) / LPT * LPT))) {
+        const int src = __builtin_ctzll(left);
+        const uint64_t of = uint64_t(uint32_t(__shfl(int(kept >> 32), src))) << 32 | uint32_t(__shfl(int(kept), src));
+        route_token(p, r0 + src / LPT, of, shift, lds.by_e);
+    }
 }
 
 // v of lane J of every row of 16 (of the LPT lanes of a token).
@@ -965,10 +981,8 @@ void launch_tokens(K kernel, const P& p, int per, hipStream_t stream) {
 }  // namespace
 
 hipError_t run_route(const RouteParams& p, const DeviceInfo& dev, hipStream_t stream) {
-    // lanes a token: twice as many as it chooses experts (fewer candidates), one at least a group that is not found in
-    // registers
-    const bool in_lanes = p.n_experts <= 256 && groups_in_lanes(p.group_size);
-    const int need = std::max(2 * p.top_k, in_lanes ? 1 : p.n_groups);
+    // lanes a token: twice as many as it chooses experts (fewer candidates), one at least a group
+    const int need = std::max(2 * p.top_k, p.n_groups);
     const int lanes = p.top_k > 32 && need <= 128 && p.n_groups <= 64 ? 64 : need;
     if (token_shape(p.n_experts, lanes, [&](auto lpt, auto v) {
             launch_tokens(route_kernel<lpt.value, v.value>, p, 256 / lpt.value, stream);
