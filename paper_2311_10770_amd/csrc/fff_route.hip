@@ -225,6 +225,17 @@ __device__ __forceinline__ int group_larger(float v) {
         n += __builtin_popcount(row_larger(v, __shfl_xor(v, 32))) + __builtin_popcount(row_larger(v, __shfl_xor(v, 48)));
     return n;
 }
+// The bits of all of the token's lanes.
+template <int LPT>
+__device__ __forceinline__ uint32_t group_or(uint32_t v) {
+    v |= __builtin_amdgcn_mov_dpp(int(v), ROR + 8, 0xf, 0xf, true);
+    v |= __builtin_amdgcn_mov_dpp(int(v), ROR + 4, 0xf, 0xf, true);
+    v |= __builtin_amdgcn_mov_dpp(int(v), ROR + 2, 0xf, 0xf, true);
+    v |= __builtin_amdgcn_mov_dpp(int(v), ROR + 1, 0xf, 0xf, true);
+    if constexpr (LPT >= 32) v |= __shfl_xor(v, 16);
+    if constexpr (LPT == 64) v |= __shfl_xor(v, 32);
+    return v;
+}
 // Sum of v over the token's lanes before this one.
 template <int LPT>
 __device__ __forceinline__ int group_before(int v, int sl) {
@@ -403,22 +414,6 @@ struct RouteLds {
     uint16_t e[64 / LPT][CAP];       // candidates
     uint16_t chosen[64 / LPT][CAP];  // in order
 };
-
-// How many of the values w that the 16 lanes of the row hold come before v: larger ones, and equal ones of a lower
-// expert.  w and f: this row's lanes' or another row's, OWN: whether this lane's is among them.
-template <bool OWN, int R = 0>
-__device__ __forceinline__ int row_before(float v, int e, float w, int f) {
-    if constexpr (R == 16) {
-        return 0;
-    } else if constexpr (OWN && R == 0) {
-        return row_before<OWN, 1>(v, e, w, f);
-    } else {
-        constexpr int CTRL = ROR + (R == 0 ? 1 : R);
-        const float x = R == 0 ? w : dpp<CTRL>(w);
-        const int g = R == 0 ? f : __builtin_amdgcn_mov_dpp(f, CTRL, 0xf, 0xf, true);
-        return (x > v || (x == v && g < e)) + row_before<OWN, R + 1>(v, e, w, f);
-    }
-}
 
 // LPT lanes a token, four neighbouring experts a vector, V experts a lane.
 //
@@ -669,26 +664,29 @@ __global__ __launch_bounds__(256, 5) void route_kernel(RouteParams p, int64_t ro
     for (int d = LPT; d < 64; d *= 2) longest = max(longest, __shfl_xor(longest, d));
     longest = __builtin_amdgcn_readfirstlane(longest);
     wave_sync();
-    // their order, in fp32 first: a candidate a lane where there are no more
+    // Their order, in fp32 first: a lane has one or two of them where there are no more, and finds its places by counting;
+    // where equal ones meet in a place, and where there are more, each counts those before it out of LDS.
+    bool counted = false;
     if (LPT < 64 && longest <= LPT) {
-        const int e = sl < got ? list[sl] : E + sl;
+        const int e = sl < got ? list[sl] : 0;
         const float x = sl < got ? finite_value(all[e]) : NONE;
         int before = __builtin_popcount(row_larger(x, x));
         if constexpr (LPT == 32) before += __builtin_popcount(row_larger(x, __shfl_xor(x, 16)));
-        // a place each, but for equal ones
-        uint32_t places = sl < got ? 1u << before : 0;
-        places |= uint32_t(__float_as_int(dpp<ROR + 8>(__uint_as_float(places))));
-        places |= uint32_t(__float_as_int(dpp<ROR + 4>(__uint_as_float(places))));
-        places |= uint32_t(__float_as_int(dpp<ROR + 2>(__uint_as_float(places))));
-        places |= uint32_t(__float_as_int(dpp<ROR + 1>(__uint_as_float(places))));
-        if constexpr (LPT == 32) places |= __shfl_xor(places, 16);
-        if (__any(__builtin_popcount(places) != got)) {
-            const float y = sl < got ? all[e] : NONE;
-            before = row_before<true>(y, e, y, e);
-            if constexpr (LPT == 32) before += row_before<false>(y, e, __shfl_xor(y, 16), __shfl_xor(e, 16));
-        }
-        if (sl < got) order[before] = uint16_t(e);
-    } else {
+        const uint32_t places = group_or<LPT>(sl < got ? 1u << before : 0);
+        counted = !__any(__builtin_popcount(places) != got);
+        if (counted && sl < got) order[before] = uint16_t(e);
+    } else if (LPT == 16 && longest <= 32) {
+        const bool two = sl + 16 < got;
+        const int e = sl < got ? list[sl] : 0, f = two ? list[sl + 16] : 0;
+        const float x = sl < got ? finite_value(all[e]) : NONE, y = two ? finite_value(all[f]) : NONE;
+        const int before = __builtin_popcount(row_larger(x, x)) + __builtin_popcount(row_larger(x, y));
+        const int behind = __builtin_popcount(row_larger(y, x)) + __builtin_popcount(row_larger(y, y));
+        const uint32_t places = group_or<LPT>((sl < got ? 1u << before : 0) | (two ? 1u << behind : 0));
+        counted = !__any(__builtin_popcount(places) != got);
+        if (counted && sl < got) order[before] = uint16_t(e);
+        if (counted && two) order[behind] = uint16_t(f);
+    }
+    if (!counted) {
         for (int i = sl; i < got; i += LPT) {
             const int e = list[i];
             const float x = all[e];
