@@ -67,6 +67,7 @@ __global__ __launch_bounds__(256) void combine_kernel(CombineParams p, int vecs,
 template <int LPE, bool SHORT>
 __global__ __launch_bounds__(256) void combine_bwd_kernel(CombineBwdParams p) {
     constexpr int EPB = 256 / LPE, STEP = LPE * 8;
+    __shared__ float red[LPE == 256 ? 4 : 1];
     const int sl = threadIdx.x % LPE;
     const uint32_t H = p.hidden;
     const int64_t entries = p.n_tokens * p.top_k;
@@ -121,7 +122,13 @@ __global__ __launch_bounds__(256) void combine_bwd_kernel(CombineBwdParams p) {
             }
         }
         if (p.dweights) {
-            acc = group_sum<LPE>(acc);
+            acc = group_sum<LPE < 64 ? LPE : 64>(acc);
+            if constexpr (LPE == 256) {
+                __syncthreads();  // a turn's sums are read before the next one's are written
+                if (sl % 64 == 0) red[sl / 64] = acc;
+                __syncthreads();
+                acc = (red[0] + red[1]) + (red[2] + red[3]);
+            }
             if (sl == 0) p.dweights[e] = acc;
         }
     }
@@ -147,6 +154,8 @@ hipError_t run_combine_backward(const CombineBwdParams& p, const DeviceInfo& dev
     if (p.hidden < 8) launch(combine_bwd_kernel<16, true>, 16);
     else if (p.hidden <= 256) launch(combine_bwd_kernel<16, false>, 16);
     else if (p.hidden <= 512) launch(combine_bwd_kernel<32, false>, 32);
+    // few entries of long rows: a workgroup each (one row of 16384: 18 us with a wave, 10.6 so, which is the host's)
+    else if (p.hidden > 2048 && entries <= 2 * std::max(dev.cu_count, 1)) launch(combine_bwd_kernel<256, false>, 256);
     else launch(combine_bwd_kernel<64, false>, 64);
     return hipGetLastError();
 }

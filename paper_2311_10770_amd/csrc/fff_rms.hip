@@ -58,24 +58,57 @@ __device__ __forceinline__ void put_packed(uint8_t* q, uint8_t* scale, int col, 
     if (left > 0 && col % PACK_BLOCK == 0) scale[col / PACK_BLOCK] = uint8_t(code);
 }
 
-template <bool FULL>
+// How a row fits its lanes' vectors of four: exactly, in whole vectors, or with a part of one at its end.
+enum { ROW_FULL = 0, ROW_WHOLE = 1, ROW_RAGGED = 2 };
+
+// Four values of a row from element e on, `left` of them in the row, of a matrix of `all` elements; zeros behind the
+// row, but that a ragged row's last vector may run on into the next one, and clear4 takes those values out (element by
+// element such ends cost a row more than all its vectors: 65536 rows of 250 bf16, backward: 69 us, 33 so).  Only
+// the matrix's last ones are read one by one.
+template <int FIT>
+__device__ __forceinline__ Raw4 row4(const void* base, int bf, int64_t e, int left, int64_t all) {
+    if (FIT == ROW_FULL) return load4<true>(base, bf, e, 4);
+    if (FIT == ROW_RAGGED && left > 0 && e + 4 > all) return load4<false>(base, bf, e, left);
+    Raw4 r = {0, 0, 0, 0};
+    if (left > 0) r = load4<true>(base, bf, e, 4);
+    return r;
+}
+template <int FIT>
+__device__ __forceinline__ void clear4(float* f, int left) {
+    if (FIT != ROW_RAGGED) return;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) f[j] = j < left ? f[j] : 0.0f;
+}
+template <int FIT>
+__device__ __forceinline__ void put4(void* base, int bf, int64_t e, int left, const float* f) {
+    if (FIT == ROW_FULL || (FIT == ROW_WHOLE && left > 0)) store4<true>(base, bf, e, 4, f);
+    else if (FIT == ROW_RAGGED) store4<false>(base, bf, e, left, f);
+}
+
+template <int FIT>
 __device__ __forceinline__ void gain4(float* f, const float* g, int col, int left) {
     if (g) {
-        unpack4(f, load4<FULL>(g, 0, col, left), 0);
+        unpack4(f, load4<FIT == ROW_FULL>(g, 0, col, left), 0);
     } else {
         f[0] = f[1] = f[2] = f[3] = 1.0f;
     }
 }
 
 // Rows held in registers: LPR lanes a row, lane sl holding the NV vectors of four columns
-// c LPR + sl.  One read and one write of every byte.  FULL: the row is exactly LPR NV vectors long.
-template <int LPR, int NV, bool FULL>
+// c LPR + sl.  One read and one write of every byte.
+template <int LPR, int NV, int FIT>
 __global__ __launch_bounds__(row_threads(LPR)) void rms_kernel(RmsParams p) {
     constexpr int NT = row_threads(LPR), RPB = NT / LPR;
     __shared__ float red[2][LPR / 64 + 1];
     const int sl = threadIdx.x % LPR, H = p.hidden;
-    const int64_t blocks = pack_blocks(H);
+    const int64_t blocks = pack_blocks(H), total = p.n_tokens * H;
     const float width = float(H);
+    float gain[NV][4];
+#pragma unroll
+    for (int c = 0; c < NV; ++c) {
+        const int col = (c * LPR + sl) * 4;
+        gain4<FIT>(gain[c], p.gamma, col, H - col);
+    }
     int turn = 0;
     for (int64_t r0 = int64_t(blockIdx.x) * RPB; r0 < p.n_tokens; r0 += int64_t(gridDim.x) * RPB) {
         const int64_t row = r0 + threadIdx.x / LPR;
@@ -84,13 +117,13 @@ __global__ __launch_bounds__(row_threads(LPR)) void rms_kernel(RmsParams p) {
 #pragma unroll
         for (int c = 0; c < NV; ++c) {
             const int col = (c * LPR + sl) * 4;
-            rx[c] = load4<FULL>(p.x, p.x_bf16, row * H + col, H - col);
+            rx[c] = row4<FIT>(p.x, p.x_bf16, row * H + col, H - col, total);
         }
         if (p.residual) {
 #pragma unroll
             for (int c = 0; c < NV; ++c) {
                 const int col = (c * LPR + sl) * 4;
-                rr[c] = load4<FULL>(p.residual, p.s_bf16, row * H + col, H - col);
+                rr[c] = row4<FIT>(p.residual, p.s_bf16, row * H + col, H - col, total);
             }
         }
         float f[NV][4], sq = 0.0f;
@@ -109,24 +142,24 @@ __global__ __launch_bounds__(row_threads(LPR)) void rms_kernel(RmsParams p) {
 #pragma unroll
             for (int c = 0; c < NV; ++c) {
                 const int col = (c * LPR + sl) * 4;
-                store4<FULL>(p.s, p.s_bf16, row * H + col, H - col, f[c]);
+                put4<FIT>(p.s, p.s_bf16, row * H + col, H - col, f[c]);
             }
         }
 #pragma unroll
-        for (int c = 0; c < NV; ++c)
+        for (int c = 0; c < NV; ++c) {
+            clear4<FIT>(f[c], H - (c * LPR + sl) * 4);
 #pragma unroll
             for (int j = 0; j < 4; ++j) sq = __builtin_fmaf(f[c][j], f[c][j], sq);
+        }
         sq = row_sum<LPR>(sq, red[turn]);
         turn ^= 1;
         const float rstd = 1.0f / sqrtf(sq / width + p.eps);
 #pragma unroll
         for (int c = 0; c < NV; ++c) {
             const int col = (c * LPR + sl) * 4;
-            float g[4];
-            gain4<FULL>(g, p.gamma, col, H - col);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) f[c][j] = f[c][j] * rstd * g[j];
-            if (p.y) store4<FULL>(p.y, p.y_bf16, row * H + col, H - col, f[c]);
+            for (int j = 0; j < 4; ++j) f[c][j] = f[c][j] * rstd * gain[c][j];
+            if (p.y) put4<FIT>(p.y, p.y_bf16, row * H + col, H - col, f[c]);
             if (p.q) put_packed(p.q + row * H, p.q_scale + row * blocks, col, H - col, f[c]);
         }
         if (sl == 0 && p.rstd) p.rstd[row] = rstd;
@@ -135,19 +168,20 @@ __global__ __launch_bounds__(row_threads(LPR)) void rms_kernel(RmsParams p) {
 
 // The gradients of rows held in registers, as rms_kernel holds them.  Every workgroup sums dgamma over its
 // rows in registers and leaves one partial row.
-template <int LPR, int NV, bool FULL>
+template <int LPR, int NV, int FIT>
 __global__ __launch_bounds__(row_threads(LPR)) void rms_bwd_kernel(RmsBwdParams p) {
     constexpr int NT = row_threads(LPR), RPB = NT / LPR, W = LPR * NV * 4;
     __shared__ float red[2][LPR / 64 + 1];
     __shared__ float cols[RPB > 1 ? W : 1];
     const int sl = threadIdx.x % LPR, H = p.hidden;
     const float width = float(H);
+    const int64_t total = p.n_tokens * H;
     const bool rows_out = p.ds || p.dx;
     float gain[NV][4], dg[NV][4] = {};
 #pragma unroll
     for (int c = 0; c < NV; ++c) {
         const int col = (c * LPR + sl) * 4;
-        gain4<FULL>(gain[c], p.gamma, col, H - col);
+        gain4<FIT>(gain[c], p.gamma, col, H - col);
     }
     int turn = 0;
     for (int64_t r0 = int64_t(blockIdx.x) * RPB; r0 < p.n_tokens; r0 += int64_t(gridDim.x) * RPB) {
@@ -157,18 +191,18 @@ __global__ __launch_bounds__(row_threads(LPR)) void rms_bwd_kernel(RmsBwdParams 
 #pragma unroll
         for (int c = 0; c < NV; ++c) {
             const int col = (c * LPR + sl) * 4;
-            ry[c] = load4<FULL>(p.dy, p.y_bf16, row * H + col, H - col);
+            ry[c] = row4<FIT>(p.dy, p.y_bf16, row * H + col, H - col, total);
         }
 #pragma unroll
         for (int c = 0; c < NV; ++c) {
             const int col = (c * LPR + sl) * 4;
-            rs[c] = load4<FULL>(p.s, p.s_bf16, row * H + col, H - col);
+            rs[c] = row4<FIT>(p.s, p.s_bf16, row * H + col, H - col, total);
         }
         if (p.ds_in && rows_out) {
 #pragma unroll
             for (int c = 0; c < NV; ++c) {
                 const int col = (c * LPR + sl) * 4;
-                ru[c] = load4<FULL>(p.ds_in, p.s_bf16, row * H + col, H - col);
+                ru[c] = row4<FIT>(p.ds_in, p.s_bf16, row * H + col, H - col, total);
             }
         }
         const float rstd = p.rstd[row];
@@ -177,10 +211,12 @@ __global__ __launch_bounds__(row_threads(LPR)) void rms_bwd_kernel(RmsBwdParams 
         for (int c = 0; c < NV; ++c) {
             unpack4(g[c], ry[c], p.y_bf16);
             unpack4(xh[c], rs[c], p.s_bf16);
-            const int left = H - (c * LPR + sl) * 4;  // columns behind the row hold zeros (0 rstd may be NaN)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) xh[c][j] *= rstd;
+            clear4<FIT>(xh[c], H - (c * LPR + sl) * 4);
+            clear4<FIT>(g[c], H - (c * LPR + sl) * 4);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                xh[c][j] = FULL || j < left ? xh[c][j] * rstd : 0.0f;
                 dg[c][j] = __builtin_fmaf(g[c][j], xh[c][j], dg[c][j]);
                 g[c][j] *= gain[c][j];
                 b = __builtin_fmaf(g[c][j], xh[c][j], b);
@@ -205,8 +241,8 @@ __global__ __launch_bounds__(row_threads(LPR)) void rms_bwd_kernel(RmsBwdParams 
 #pragma unroll
         for (int c = 0; c < NV; ++c) {
             const int col = (c * LPR + sl) * 4;
-            if (p.ds) store4<FULL>(p.ds, p.s_bf16, row * H + col, H - col, g[c]);
-            if (p.dx) store4<FULL>(p.dx, p.x_bf16, row * H + col, H - col, g[c]);
+            if (p.ds) put4<FIT>(p.ds, p.s_bf16, row * H + col, H - col, g[c]);
+            if (p.dx) put4<FIT>(p.dx, p.x_bf16, row * H + col, H - col, g[c]);
         }
     }
     if (!p.dgamma) return;
@@ -231,7 +267,7 @@ __global__ __launch_bounds__(row_threads(LPR)) void rms_bwd_kernel(RmsBwdParams 
 #pragma unroll
         for (int c = 0; c < NV; ++c) {
             const int col = (c * LPR + sl) * 4;
-            store4<FULL>(part, 0, col, H - col, dg[c]);
+            put4<FIT>(part, 0, col, H - col, dg[c]);
         }
     }
 }
@@ -256,6 +292,7 @@ __global__ __launch_bounds__(LONG) void rms_any_kernel(RmsParams p) {
             return left;
         };
         float f[4], sq = 0.0f;
+#pragma unroll 4
         for (int64_t i = 0; i < turns; ++i) {
             sum4((i * LONG + threadIdx.x) * 4, f);
 #pragma unroll
@@ -385,30 +422,33 @@ int rows_per_group(int32_t hidden) {
     return i < 0 ? 8 : row_threads(ROW_SHAPES[i].lanes) / ROW_SHAPES[i].lanes;
 }
 
-template <int I, bool FULL>
+template <int I, int FIT>
 void launch_rms(const RmsParams& p, unsigned grid, hipStream_t stream) {
-    hipLaunchKernelGGL((rms_kernel<ROW_SHAPES[I].lanes, ROW_SHAPES[I].nv, FULL>), dim3(grid),
+    hipLaunchKernelGGL((rms_kernel<ROW_SHAPES[I].lanes, ROW_SHAPES[I].nv, FIT>), dim3(grid),
                        dim3(row_threads(ROW_SHAPES[I].lanes)), 0, stream, p);
 }
-template <int I, bool FULL>
+template <int I, int FIT>
 void launch_rms(const RmsBwdParams& p, unsigned grid, hipStream_t stream) {
-    hipLaunchKernelGGL((rms_bwd_kernel<ROW_SHAPES[I].lanes, ROW_SHAPES[I].nv, FULL>), dim3(grid),
+    hipLaunchKernelGGL((rms_bwd_kernel<ROW_SHAPES[I].lanes, ROW_SHAPES[I].nv, FIT>), dim3(grid),
                        dim3(row_threads(ROW_SHAPES[I].lanes)), 0, stream, p);
 }
 template <int I, class P>
 void launch_rows(int shape, const P& p, unsigned grid, hipStream_t stream) {
     if constexpr (I < N_ROW_SHAPES) {
         if (shape != I) return launch_rows<I + 1>(shape, p, grid, stream);
-        const bool full = p.hidden == ROW_SHAPES[I].lanes * ROW_SHAPES[I].nv * 4;
-        full ? launch_rms<I, true>(p, grid, stream) : launch_rms<I, false>(p, grid, stream);
+        if (p.hidden == ROW_SHAPES[I].lanes * ROW_SHAPES[I].nv * 4) launch_rms<I, ROW_FULL>(p, grid, stream);
+        else if (p.hidden % 4 == 0) launch_rms<I, ROW_WHOLE>(p, grid, stream);
+        else launch_rms<I, ROW_RAGGED>(p, grid, stream);
     }
 }
 
-// Workgroups of the backward, each leaving one partial row: two a CU at most, four where one works on a row at a time
-// with four waves.
+// Workgroups of the backward, each leaving one partial row: more of them for short rows, whose partial rows are short
+// too, and where one works on a row at a time with four waves (us: 65536 rows of 100 fp32, 512 and 2048: 37.9, 24.8; 9069 of
+// 1522, 512 and 1024: 60, 43).
 int rms_parts(int64_t n_tokens, int32_t hidden) {
     const int per = rows_per_group(hidden), shape = row_shape(hidden);
-    const int64_t most = shape >= 0 && ROW_SHAPES[shape].lanes == 256 ? 1024 : 512;
+    int64_t most = std::min<int64_t>(2048, std::max<int64_t>(512, (int64_t(1) << 18) / hidden));
+    if (shape >= 0 && ROW_SHAPES[shape].lanes == 256) most = 1024;
     return int(std::min<int64_t>(most, (n_tokens + per - 1) / per));
 }
 
