@@ -243,6 +243,24 @@ def test_combine_backward(fff_lib, T, k, H):
             assert again[0] is inside and torch.equal(inside, got[0]) and torch.equal(again[1], got[1])
 
 
+@pytest.mark.parametrize("T,k,H", [(3, 2, 2563), (5, 1, 4099), (2, 4, 8191), (1, 1, 2049)])
+def test_combine_backward_long_rows_in_place(fff_lib, T, k, H):
+    """Rows that several waves share, with a part of a vector at their end: the gradient written over them changes no
+    sum that another wave is still forming."""
+    for dt in ("bf16", "f32"):
+        flush_print(f"[gpu] combine_backward in place {T}x{k}x{H} {dt}")
+        gen = _gen(T + 10 * k + 100 * H)
+        dy, rows, weights = _randn(gen, T, H, dtype=dt), _randn(gen, T * k, H, dtype=dt), _randn(gen, T, k)
+        want, err = ref.combine_backward(dy, k, rows, weights, None)
+        got = fff_lib.combine_backward(dy, k, rows, weights)
+        for _ in range(8):
+            inside = rows.clone()
+            again = fff_lib.combine_backward(dy, k, inside, weights, drows=inside)
+            for v, o, w, e, what in zip(again, got, want, err, ("drows", "dweights")):
+                ops_ref.check(v, w, e, f"{what} {T}x{k}x{H}")
+                assert torch.equal(v, o)
+
+
 def test_combine_rows_apart(fff_lib):
     """NaN in a row that takes part spoils its own token's column alone; a weight of 0 does not hide it."""
     for H in (40, 77, 512):
