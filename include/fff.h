@@ -715,7 +715,8 @@ int fff_combine_backward(const fff_combine_backward_args* a);
  * fff_rms_norm -- s = residual + x (residual optional), then
  *   y = s / sqrt(mean(s^2) + eps) * gamma
  * per row, y in y_dtype and, with q, in 8 bits too (from the fp32 y).  y, q and rstd
- * come from the fp32 s, before it is rounded to s_dtype for the stream.  Any
+ * come from the fp32 s, before it is rounded to s_dtype for the stream; the squares
+ * are fp32 too (values past 1.8e19 overflow them).  Any
  * hidden >= 1; n_tokens < 2^32.
  */
 typedef struct {

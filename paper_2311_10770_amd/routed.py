@@ -207,7 +207,8 @@ def route_backward(dweights, logits, ids, *, score="softmax", renormalise=False,
         raise ValueError("ids are needed")
     dlogits, dlogits_at = _out(dlogits, "dlogits", at, logits, None, new=dlogits_dtype or logits.dtype)
     _run(_lib().fff_route_backward, FffRouteBackwardArgs(
-        dweights.data_ptr(), logits.data_ptr(), _like(ids, "ids", at, (B, K), torch.int32), dlogits_at, B, shape[1], K, _dt(logits, "logits"), _dt(dlogits, "dlogits"),
+        dweights.data_ptr(), logits.data_ptr(), _like(ids, "ids", at, (B, K), torch.int32), dlogits_at, B, shape[1], K,
+        _dt(logits, "logits"), _dt(dlogits, "dlogits"),
         _choice(SCORES, score, "score"), int(bool(renormalise)), scale, _raw_stream(device, stream)))
     return dlogits
 
