@@ -218,25 +218,14 @@ __device__ __forceinline__ uint32_t row_larger(float v, float w, uint32_t bits =
         return row_larger<R + 1>(v, w, push_sign(bits, v - x));
     }
 }
-// How many of the LPT lanes' (finite) values are larger than v.
+// How many of the LPT lanes' (finite) values w are larger than v.
 template <int LPT>
-__device__ __forceinline__ int group_larger(float v) {
-    int n = __builtin_popcount(row_larger(v, v));
-    if constexpr (LPT >= 32) n += __builtin_popcount(row_larger(v, __shfl_xor(v, 16)));
+__device__ __forceinline__ int group_larger(float v, float w) {
+    int n = __builtin_popcount(row_larger(v, w));
+    if constexpr (LPT >= 32) n += __builtin_popcount(row_larger(v, __shfl_xor(w, 16)));
     if constexpr (LPT == 64)
-        n += __builtin_popcount(row_larger(v, __shfl_xor(v, 32))) + __builtin_popcount(row_larger(v, __shfl_xor(v, 48)));
+        n += __builtin_popcount(row_larger(v, __shfl_xor(w, 32))) + __builtin_popcount(row_larger(v, __shfl_xor(w, 48)));
     return n;
-}
-// The bits of all of the token's lanes.
-template <int LPT>
-__device__ __forceinline__ uint32_t group_or(uint32_t v) {
-    v |= __builtin_amdgcn_mov_dpp(int(v), ROR + 8, 0xf, 0xf, true);
-    v |= __builtin_amdgcn_mov_dpp(int(v), ROR + 4, 0xf, 0xf, true);
-    v |= __builtin_amdgcn_mov_dpp(int(v), ROR + 2, 0xf, 0xf, true);
-    v |= __builtin_amdgcn_mov_dpp(int(v), ROR + 1, 0xf, 0xf, true);
-    if constexpr (LPT >= 32) v |= __shfl_xor(v, 16);
-    if constexpr (LPT == 64) v |= __shfl_xor(v, 32);
-    return v;
 }
 // Sum of v over the token's lanes before this one.
 template <int LPT>
@@ -262,7 +251,7 @@ __device__ __forceinline__ void top2_step(float& a, float& b) {
     a = __builtin_fmaxf(a, x);
 }
 
-// Whether route_kernel<16> finds groups of `size` experts in its lanes' registers: a power of two of whole vectors.
+// Whether route_kernel finds groups of `size` experts in its lanes' registers: a power of two of whole vectors.
 __host__ __device__ __forceinline__ bool groups_in_lanes(int size) { return size >= 4 && size <= 64 && (size & (size - 1)) == 0; }
 
 // The best (v, then the lowest i) of the wave's lanes, for each of them.
@@ -410,15 +399,18 @@ __device__ __forceinline__ void route_token(const RouteParams& p, int64_t row, u
 // chosen by in fp64.
 template <int LPT, int V>
 struct RouteLds {
-    static constexpr int CAP = V >= 8 ? 4 * LPT : 2 * LPT;  // candidates of a token: their fp64 choices fit in the place of c
-    float c[64 * V];
+    static constexpr int CAP = 4 * LPT;  // candidates of a token, whose fp64 choices lie in the place of c
+    static constexpr int AREA = V >= 8 ? LPT * V : 2 * CAP;  // of a token in c
+    float c[64 / LPT * AREA];
     double by_e[LPT * V];
     uint16_t e[64 / LPT][CAP];       // candidates
     uint16_t chosen[64 / LPT][CAP];  // in order
 };
 
 // LPT lanes a token (16, 32 or 64), four neighbouring experts a vector, V experts a lane: lanes hold few experts each, in
-// registers, and a wave 64 / LPT tokens.  Two lanes a pick at least, as the largest of each lane's own bound the choice.
+// registers, and a wave 64 / LPT tokens.  One lane a pick at least: the largest of each lane's own bound the choice, where
+// there are less than two a pick the largest two (33530 tokens, top 14 of 64 in groups: 45 us with 32 lanes and
+// their largest alone, 16.7 with 16 lanes).  64 lanes keep to the largest alone: their two need registers that spill.
 //
 // Bound by vector instructions, but for the plain choice by logits: 65536 tokens, top 8 of 256 fp32 (71 MB: 14 us at a
 // copy's rate): by the logits 16.9 us, sigmoid and bias 23.6, softmax and bias 27.6; sigmoid, bias and the best 4 of 8
@@ -428,9 +420,10 @@ struct RouteLds {
 // copy's rate).
 //
 // Choices are first formed in fp32 (c, whose error is below `slack` / 2).  Of the LPT lanes' largest, the
-// top_k-th is no more than the top_k-th largest of all, so only experts within the slack of it
-// can be chosen: a dozen of 256.  These candidates alone are ordered, each by counting those before it; where two
-// neighbours in that order lie within the slack, the token's candidates are evaluated and ordered in fp64.
+// top_k-th is no more than the top_k-th largest of all, and the same holds for the largest two of each, so only
+// experts within the slack of it can be chosen: a dozen of 256.  These candidates alone are ordered, each by counting
+// those before it; where two neighbours in that order lie within the slack, the token's candidates are evaluated and ordered
+// in fp64.
 // Groups whose values leave their choice open are resolved by kept_groups, and tokens that have more candidates
 // than there is room for (as where all logits are equal) are left to route_token: whole waves, in fp64 (65536 tokens of 256
 // equal logits: 150 to 237 us).
@@ -453,7 +446,7 @@ __global__ __launch_bounds__(256, 5) void route_kernel(RouteParams p, int64_t ro
     const int64_t row = in ? r0 + tok : p.n_tokens - 1;  // lanes behind the last token do it again
     constexpr uint64_t TOKEN = LPT == 64 ? ~0ull : (1ull << LPT % 64) - 1;
     const float* bias = p.bias;
-    const bool in_lanes = LPT == 16 && G <= 16 && groups_in_lanes(size);
+    const bool in_lanes = G <= LPT && groups_in_lanes(size);
     const int turn = in_lanes ? __builtin_ctz(size / 4) : 0;  // 1 << turn lanes hold a group of a vector of experts
     uint64_t kept = ~0ull;  // G > 1: a token's groups, one every 1 << shift bits
     int shift = 0;
@@ -466,7 +459,7 @@ __global__ __launch_bounds__(256, 5) void route_kernel(RouteParams p, int64_t ro
         return m;
     };
     float l[V], c[V];
-    float* const all = lds.c + tok * (LPT * V);
+    float* const all = lds.c + tok * Lds::AREA;
     auto put4 = [&](float* to, int q, const float (&x)[V]) {
         *reinterpret_cast<float4*>(to + (q * LPT + sl) * 4) = make_float4(x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]);
     };
@@ -553,7 +546,7 @@ __global__ __launch_bounds__(256, 5) void route_kernel(RouteParams p, int64_t ro
         float best = NONE, second = NONE;
         if (in_lanes) {
             // pairs of the larger two meet over DPP, then in LDS (where the candidates come to be listed)
-            float2* const pairs = reinterpret_cast<float2*>(lds.e) + tok * 16;
+            float2* const pairs = reinterpret_cast<float2*>(lds.e) + tok * LPT;
 #pragma unroll
             for (int q = 0; q < N; ++q) {
                 const float* s = c + 4 * q;
@@ -566,7 +559,7 @@ __global__ __launch_bounds__(256, 5) void route_kernel(RouteParams p, int64_t ro
                 if (turn >= 3) top2_step<0x141>(a, b);  // row_half_mirror
                 if (turn >= 4) top2_step<0x140>(a, b);  // row_mirror
                 if ((sl & ((1 << turn) - 1)) == 0)
-                    pairs[(q * 16 + sl) >> turn] = make_float2(a, b);
+                    pairs[(q * LPT + sl) >> turn] = make_float2(a, b);
             }
             wave_sync();
             if (sl < G) {
@@ -601,7 +594,7 @@ __global__ __launch_bounds__(256, 5) void route_kernel(RouteParams p, int64_t ro
         // the slack, 2^-24 of its terms' sizes and of itself
         const bool two = top2 && second > NONE, none = best == NONE;
         const float value = finite_value(two ? best + second : best);
-        const bool keep = (group_larger<LPT>(value) >> shift) < p.top_groups && sl >> shift < G;
+        const bool keep = (group_larger<LPT>(value, value) >> shift) < p.top_groups && sl >> shift < G;
         kept = __ballot(keep) >> first;  // other tokens' behind
         bool open = (int(group_sum<LPT>(keep && !none ? 1.0f : 0.0f)) >> shift) > p.top_groups;
         if (by_score) {
@@ -634,7 +627,8 @@ __global__ __launch_bounds__(256, 5) void route_kernel(RouteParams p, int64_t ro
         if (in_lanes) {
 #pragma unroll
             for (int q = 0; q < N; ++q) {
-                const bool k = uint32_t(kept) >> ((q * 16 + sl) >> turn) & 1;
+                const int g = (q * LPT + sl) >> turn;
+                const bool k = (LPT == 64 ? uint32_t(kept >> g) : uint32_t(kept) >> g) & 1;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) c[4 * q + j] = k ? c[4 * q + j] : NONE;
             }
@@ -651,9 +645,23 @@ __global__ __launch_bounds__(256, 5) void route_kernel(RouteParams p, int64_t ro
 #pragma unroll
         for (int q = 0; q < N; ++q) put4(all, q, c);
     }
-    // candidates: not below the top_k-th largest of the lanes' largest, less the slack
+    // candidates: not below the top_k-th largest of the lanes' largest (or largest two), less the slack
     const float most = finite_value(lane_max(c));
-    float bar = -group_max<LPT>(group_larger<LPT>(most) < K ? -most : NONE);
+    int larger = group_larger<LPT>(most, most);
+    float bar = larger < K ? -most : NONE;
+    if (LPT < 64 && 2 * K > LPT) {
+        float a = c[0], b = NONE;  // the largest, the second
+#pragma unroll
+        for (int v = 1; v < V; ++v) {
+            b = __builtin_amdgcn_fmed3f(a, b, c[v]);
+            a = __builtin_fmaxf(a, c[v]);
+        }
+        b = finite_value(b);
+        larger += group_larger<LPT>(most, b);
+        bar = larger < K ? -most : NONE;
+        if (group_larger<LPT>(b, most) + group_larger<LPT>(b, b) < K) bar = -b;  // no more than most
+    }
+    bar = -group_max<LPT>(bar);
     if (bias) bar -= slack + 4.76837158203125e-07f * __builtin_fabsf(bar);
     bar = __builtin_fmaxf(bar, -3.4028234663852886e38f);  // every expert there is
     uint32_t live = 0;
@@ -676,25 +684,25 @@ __global__ __launch_bounds__(256, 5) void route_kernel(RouteParams p, int64_t ro
     longest = __builtin_amdgcn_readfirstlane(longest);
     wave_sync();
     // Their order, in fp32 first: a lane has one or two of them where there are no more, and finds its places by counting;
-    // where equal ones meet in a place, and where there are more, each counts those before it out of LDS.
+    // where equal ones meet in a place (the counts' sum is short of 0 + 1 + ...), and where there are more, each counts
+    // those before it out of LDS.
     bool counted = false;
+    const float in_order = 0.5f * float(got) * float(got - 1);
     if (LPT < 64 && longest <= LPT) {
         const int e = sl < got ? list[sl] : 0;
         const float x = sl < got ? finite_value(all[e]) : NONE;
-        int before = __builtin_popcount(row_larger(x, x));
-        if constexpr (LPT == 32) before += __builtin_popcount(row_larger(x, __shfl_xor(x, 16)));
-        const uint32_t places = group_or<LPT>(sl < got ? 1u << before : 0);
-        counted = !__any(__builtin_popcount(places) != got);
+        const int before = group_larger<LPT>(x, x);
+        counted = !__any(group_sum<LPT>(sl < got ? float(before) : 0.0f) != in_order);
         if (counted && sl < got) order[before] = uint16_t(e);
-    } else if (LPT == 16 && longest <= 32) {
-        const bool two = sl + 16 < got;
-        const int e = sl < got ? list[sl] : 0, f = two ? list[sl + 16] : 0;
-        const float x = sl < got ? finite_value(all[e]) : NONE, y = two ? finite_value(all[f]) : NONE;
-        const int before = __builtin_popcount(row_larger(x, x)) + __builtin_popcount(row_larger(x, y));
-        const int behind = __builtin_popcount(row_larger(y, x)) + __builtin_popcount(row_larger(y, y));
-        const uint32_t places = group_or<LPT>((sl < got ? 1u << before : 0) | (two ? 1u << behind : 0));
-        counted = !__any(__builtin_popcount(places) != got);
-        if (counted && sl < got) order[before] = uint16_t(e);
+    } else if (LPT < 64 && longest <= 2 * LPT) {
+        const bool one = sl < got, two = sl + LPT < got;
+        const int e = one ? list[sl] : 0, f = two ? list[sl + LPT] : 0;
+        const float x = one ? finite_value(all[e]) : NONE, y = two ? finite_value(all[f]) : NONE;
+        const int before = group_larger<LPT>(x, x) + group_larger<LPT>(x, y);
+        const int behind = group_larger<LPT>(y, x) + group_larger<LPT>(y, y);
+        const float places = (one ? float(before) : 0.0f) + (two ? float(behind) : 0.0f);
+        counted = !__any(group_sum<LPT>(places) != in_order);
+        if (counted && one) order[before] = uint16_t(e);
         if (counted && two) order[behind] = uint16_t(f);
     }
     if (!counted) {
@@ -711,13 +719,17 @@ __global__ __launch_bounds__(256, 5) void route_kernel(RouteParams p, int64_t ro
     }
     wave_sync();
     if (bias) {
-        // two neighbours in the order that lie within the slack, and are not of equal logits and biases
+        // two neighbours in the order that lie within the slack, and are not of equal logits and biases.  The errors of
+        // a softmax's sum and its reciprocal, 43 2^-24, are the same factor in both: of the difference of their scores,
+        // which is that of the biases where the choices are close; beside it are 3 2^-24 of the largest score in each.
         bool near = false;
         for (int i = sl; i + 1 < got; i += LPT) {
             const int e = order[i], f = order[i + 1];
             const float x = all[e], y = all[f];
             if (x - y < slack + 2.384185791015625e-07f * __builtin_fabsf(x))
-                near |= logit(p, row, e) != logit(p, row, f) || bias[e] != bias[f];
+                near |= (logit(p, row, e) != logit(p, row, f) || bias[e] != bias[f]) &&
+                        (sigmoid || x - y < 4.76837158203125e-07f * share + 2.384185791015625e-07f * __builtin_fabsf(x) +
+                                                7.62939453125e-06f * __builtin_fabsf(bias[e] - bias[f]));  // 2^-21, 2^-22, 2^-17
         }
         if (__any(near)) {
             // in fp64, in the place of the fp32 choices, with the softmax's sum formed in fp64 too
@@ -992,11 +1004,14 @@ void launch_tokens(K kernel, const P& p, int per, hipStream_t stream) {
 
 }  // namespace
 
-hipError_t run_route(const RouteParams& p, const DeviceInfo& dev, hipStream_t stream) {
-    // lanes a token: twice as many as it chooses experts (fewer candidates), one at least a group
-    const int need = std::max(2 * p.top_k, p.n_groups);
-    const int lanes = p.top_k > 32 && need <= 128 && p.n_groups <= 64 ? 64 : need;
-    if (token_shape(p.n_experts, lanes, [&](auto lpt, auto v) {
+hipError_t run_route(const RouteParams& args, const DeviceInfo& dev, hipStream_t stream) {
+    RouteParams p = args;
+    if (p.top_groups == p.n_groups) {  // every group is kept
+        p.n_groups = p.top_groups = 1;
+        p.group_size = p.n_experts;
+    }
+    // lanes a token: one at least a pick and a group
+    if (token_shape(p.n_experts, std::max(p.top_k, p.n_groups), [&](auto lpt, auto v) {
             launch_tokens(route_kernel<lpt.value, v.value>, p, 256 / lpt.value, stream);
         }))
         return hipGetLastError();

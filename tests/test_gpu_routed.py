@@ -72,6 +72,29 @@ def test_route_groups(fff_lib, T, E, k, G, keep, group_score):
                      group_score=group_score, renormalise=n % 2 == 0)
 
 
+@pytest.mark.parametrize("T,E,k,G,keep", [
+    (70, 64, 14, 8, 5), (67, 256, 16, 16, 9), (66, 100, 11, 1, 1), (65, 33, 16, 1, 1), (65, 17, 9, 1, 1), (69, 64, 16, 4, 1),
+    (40, 256, 24, 1, 1), (37, 64, 30, 1, 1), (33, 512, 32, 32, 20), (35, 500, 17, 1, 1), (34, 128, 20, 32, 12), (38, 256, 8, 32, 5),
+    (21, 1024, 6, 64, 9), (20, 256, 40, 64, 30), (19, 128, 64, 32, 32), (36, 96, 32, 1, 1), (39, 72, 25, 18, 9), (45, 50, 8, 5, 5)])
+def test_route_many_picks(fff_lib, T, E, k, G, keep):
+    """Less than two lanes a pick, and groups over 16, 32 and 64 lanes; some tokens with few experts, some with equal ones."""
+    for n, (t, score, with_bias, group_score) in enumerate([
+            ("f32", "sigmoid", True, "top2"), ("bf16", "softmax", False, "max"), ("f32", "softmax", True, "max"),
+            ("bf16", "sigmoid", True, "top2")]):
+        flush_print(f"[gpu] route {T}x{E} top {k}, {keep} of {G} groups by {group_score}, {score} {t} bias={with_bias}")
+        gen = _gen(11 * T + E + n)
+        logits = _randn(gen, T, E, dtype=t, scale=1.5)
+        logits[2::5] = torch.randint(-2, 3, logits[2::5].shape, generator=gen, device=DEV).to(logits.dtype)
+        logits[3::5, : E - k // 2] = -INF  # less than k
+        logits[4::5, ::2] = NAN
+        bias = _randn(gen, E, scale=0.1) if with_bias else None
+        _check_route(fff_lib, logits, k, f"{T}x{E}", score=score, bias=bias, n_groups=G, top_groups=keep,
+                     group_score=group_score, renormalise=n % 2 == 0)
+        if with_bias:  # equal and nearly equal sums
+            _check_route(fff_lib, logits, k, f"{T}x{E}", score=score, bias=torch.zeros_like(bias), n_groups=G, top_groups=keep,
+                         group_score=group_score)
+
+
 @pytest.mark.parametrize("E", [6, 64, 200, 256, 1000, 3000])
 def test_route_ties_go_to_the_lowest_index(fff_lib, E):
     """Equal logits under equal biases, many of them: integers in bf16, all equal, and equal sums in 64 bits."""
