@@ -46,140 +46,6 @@ __device__ __forceinline__ double choice(const RouteParams& p, float l, int e, c
     return c > -HUGE_VAL ? c : -HUGE_VAL;
 }
 
-// The value of a token's group g in fp64.
-__device__ __forceinline__ double group_value(const RouteParams& p, int64_t row, int g, Softmax m) {
-    const int size = p.group_size;
-    double a = -HUGE_VAL, b = -HUGE_VAL;
-    for (int e = g * size; e < (g + 1) * size; ++e) {
-        const float l = logit(p, row, e);
-        double c = choice(p, l, e, m);
-        if (!p.bias && p.group_score == GROUP_TOP2 && c > -HUGE_VAL) c = score(l, p.score, m);
-        b = fmax(b, fmin(a, c));
-        a = fmax(a, c);
-    }
-    return p.group_score == GROUP_TOP2 && b > -HUGE_VAL ? a + b : a;
-}
-
-constexpr int ANY = 256;  // threads of the kernel for any size
-
-// Largest v (lowest i among equals) of the workgroup, for every thread.
-__device__ __forceinline__ void block_best(double& v, int& i, double* sv, int* si) {
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const double w = __shfl_xor(v, d);
-        const int j = __shfl_xor(i, d);
-        if (w > v || (w == v && j < i)) {
-            v = w;
-            i = j;
-        }
-    }
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) {
-        sv[threadIdx.x >> 6] = v;
-        si[threadIdx.x >> 6] = i;
-    }
-    __syncthreads();
-    v = sv[0];
-    i = si[0];
-#pragma unroll
-    for (int w = 1; w < ANY / 64; ++w)
-        if (sv[w] > v || (sv[w] == v && si[w] < i)) {
-            v = sv[w];
-            i = si[w];
-        }
-}
-__device__ __forceinline__ double block_add(double v, double* sv) {
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) sv[threadIdx.x >> 6] = v;
-    __syncthreads();
-    return (sv[0] + sv[1]) + (sv[2] + sv[3]);
-}
-
-// Any number of experts, groups and picks: a workgroup a token, all of it in fp64.  Nothing is kept of the row but its
-// groups' values: each pick reads the row again (out of the caches) for the best expert that comes behind the one before
-// it in the order, so its time is top_k passes of fp64: 4096 tokens, top 8 of 2048 bf16: 143 us, 377 with a bias
-// and groups.  It is left simple: a thousand experts and less, which the kernel below takes, are what models have.
-__global__ __launch_bounds__(ANY) void route_any_kernel(RouteParams p) {
-    __shared__ double sv[ANY / 64], s_group[MAX_ROUTE_GROUPS];
-    __shared__ int si[ANY / 64];
-    __shared__ uint8_t s_kept[MAX_ROUTE_GROUPS];
-    __shared__ float s_logit[MAX_TOP_K];
-    const int E = p.n_experts, G = p.n_groups, size = p.group_size, tid = threadIdx.x;
-    for (int64_t row = blockIdx.x; row < p.n_tokens; row += gridDim.x) {
-        Softmax m{0.0f, 1.0};
-        if (p.score == SCORE_SOFTMAX) {
-            double most = -HUGE_VAL;
-            int at = 0;
-            for (int e = tid; e < E; e += ANY) most = fmax(most, double(logit(p, row, e)));
-            block_best(most, at, sv, si);
-            m.most = float(most);
-            double sum = 0.0;
-            for (int e = tid; e < E; e += ANY) {
-                const float l = logit(p, row, e);
-                if (l > NONE) sum += exp(double(l) - most);
-            }
-            m.sum = block_add(sum, sv);
-        }
-        if (G > 1) {
-            __syncthreads();
-            for (int g = tid; g < G; g += ANY) {
-                s_group[g] = group_value(p, row, g, m);
-            }
-            __syncthreads();
-            for (int g = tid; g < G; g += ANY) {
-                const double v = s_group[g];
-                int before = 0;
-                for (int h = 0; h < G; ++h) before += s_group[h] > v || (s_group[h] == v && h < g);
-                s_kept[g] = v > -HUGE_VAL && before < p.top_groups;
-            }
-            __syncthreads();
-        }
-        double last = HUGE_VAL;
-        int last_at = -1, got = 0;
-        for (; got < p.top_k; ++got) {
-            double best = -HUGE_VAL;
-            int at = E;
-            for (int e = tid; e < E; e += ANY) {
-                if (G > 1 && !s_kept[e / size]) continue;
-                const double c = choice(p, logit(p, row, e), e, m);
-                if (c > best && (c < last || (c == last && e > last_at))) {
-                    best = c;
-                    at = e;
-                }
-            }
-            block_best(best, at, sv, si);
-            if (best == -HUGE_VAL) break;
-            last = best;
-            last_at = at;
-            if (tid == 0) {
-                p.ids[row * p.top_k + got] = at;
-                s_logit[got] = logit(p, row, at);
-            }
-        }
-        __syncthreads();
-        if (tid < p.top_k) {
-            // renormalised sums start from the largest chosen logit: scores that underflow keep their shares
-            float most = NONE;
-            for (int j = 0; j < got; ++j) most = __builtin_fmaxf(most, s_logit[j]);
-            const bool small = p.renormalise && (p.score == SCORE_SOFTMAX || most < -300.0f);
-            auto weight = [&](int j) {
-                return small ? exp(double(s_logit[j]) - double(most)) : score(s_logit[j], p.score, m);
-            };
-            double w = tid < got ? weight(tid) : 0.0;
-            if (p.renormalise && tid < got) {
-                double sum = 0.0;
-                for (int j = 0; j < got; ++j) sum += weight(j);
-                w /= sum;
-            }
-            p.weights[row * p.top_k + tid] = float(double(p.scale) * w);
-            if (tid >= got) p.ids[row * p.top_k + tid] = -1;
-        }
-        __syncthreads();
-    }
-}
-
 // ---- up to 1024 experts: LPT lanes a token ---------------------------------
 
 // v of the lane that a DPP control names (one that has a lane for each, as the rotations of a row of 16 do).
@@ -285,6 +151,157 @@ __device__ __forceinline__ void wave_best(double& v, int& i) {
     };
     swap(std::false_type{});
     swap(std::true_type{});
+}
+
+constexpr int ANY = 256;  // threads of the kernel for any size
+
+// Largest v (lowest i among equals) of the workgroup, for every thread.  Calls alternate between two of sv and si, so one
+// barrier a call is enough.
+__device__ __forceinline__ void block_best(double& v, int& i, double* sv, int* si) {
+    wave_best(v, i);
+    if ((threadIdx.x & 63) == 0) {
+        sv[threadIdx.x >> 6] = v;
+        si[threadIdx.x >> 6] = i;
+    }
+    __syncthreads();
+    v = sv[0];
+    i = si[0];
+#pragma unroll
+    for (int w = 1; w < ANY / 64; ++w)
+        if (sv[w] > v || (sv[w] == v && si[w] < i)) {
+            v = sv[w];
+            i = si[w];
+        }
+}
+__device__ __forceinline__ double block_add(double v, double* sv) {
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) sv[threadIdx.x >> 6] = v;
+    __syncthreads();
+    return (sv[0] + sv[1]) + (sv[2] + sv[3]);
+}
+
+// ---- any number of experts, groups and picks: a workgroup a token ------------
+//
+// All of it in fp64.  Nothing is kept of the row but its groups' values and each thread's best expert: a pick is a
+// reduction over the workgroup, behind which one wave looks through the winner's experts again.  4096 tokens, top 8 of 2048
+// bf16: 71 us, 123 with softmax, bias and groups (a pass over the row for each pick took 143 and 377).
+__global__ __launch_bounds__(ANY) void route_any_kernel(RouteParams p) {
+    __shared__ double sv[2][ANY / 64], s_add[ANY / 64], s_group[MAX_ROUTE_GROUPS];
+    __shared__ int si[2][ANY / 64];
+    __shared__ uint8_t s_kept[MAX_ROUTE_GROUPS];
+    __shared__ float s_logit[MAX_TOP_K];
+    const int E = p.n_experts, G = p.n_groups, size = p.group_size, tid = threadIdx.x;
+    int turn = 0;
+    for (int64_t row = blockIdx.x; row < p.n_tokens; row += gridDim.x) {
+        Softmax m{0.0f, 1.0};
+        if (p.score == SCORE_SOFTMAX && (p.bias || !p.renormalise || (G > 1 && p.group_score == GROUP_TOP2))) {
+            double most = -HUGE_VAL;
+            int at = 0;
+            for (int e = tid; e < E; e += ANY) most = fmax(most, double(logit(p, row, e)));
+            block_best(most, at, sv[turn], si[turn]);
+            turn ^= 1;
+            m.most = float(most);
+            double sum = 0.0;
+            for (int e = tid; e < E; e += ANY) {
+                const float l = logit(p, row, e);
+                if (l > NONE) sum += exp(double(l) - most);
+            }
+            m.sum = block_add(sum, s_add);
+        }
+        if (G > 1) {
+            __syncthreads();
+            // h threads a group, that many experts apart
+            int h = 1;
+            while (h < 64 && 2 * h * G <= ANY) h *= 2;
+            for (int g0 = 0; g0 < G; g0 += ANY / h) {
+                const int g = g0 + tid / h;
+                double a = -HUGE_VAL, b = -HUGE_VAL;  // the group's largest, and the second
+                auto take = [&](double c) {
+                    b = fmax(b, fmin(a, c));
+                    a = fmax(a, c);
+                };
+                for (int e = g * size + tid % h; g < G && e < (g + 1) * size; e += h) {
+                    const float l = logit(p, row, e);
+                    double c = choice(p, l, e, m);
+                    if (!p.bias && p.group_score == GROUP_TOP2 && c > -HUGE_VAL) c = score(l, p.score, m);
+                    take(c);
+                }
+                for (int d = 1; d < h; d *= 2) {
+                    const double x = __shfl_xor(a, d), y = __shfl_xor(b, d);
+                    take(x);
+                    b = fmax(b, y);
+                }
+                if (g < G && tid % h == 0) s_group[g] = p.group_score == GROUP_TOP2 && b > -HUGE_VAL ? a + b : a;
+            }
+            __syncthreads();
+            for (int g = tid; g < G; g += ANY) {
+                const double v = s_group[g];
+                int before = 0;
+                for (int h = 0; h < G; ++h) before += s_group[h] > v || (s_group[h] == v && h < g);
+                s_kept[g] = v > -HUGE_VAL && before < p.top_groups;
+            }
+            __syncthreads();
+        }
+        // a thread has the best of the experts tid, tid + ANY, ...; when it is picked, the lanes of its wave look for the next
+        double last = HUGE_VAL, v = -HUGE_VAL;
+        int last_at = -1, mine = E, got = 0;
+        auto look = [&](int e0, int step, double& best, int& at) {
+            for (int e = e0; e < E; e += step) {
+                if (G > 1 && !s_kept[e / size]) continue;
+                const double c = choice(p, logit(p, row, e), e, m);
+                if (c > best && (c < last || (c == last && e > last_at))) {
+                    best = c;
+                    at = e;
+                }
+            }
+        };
+        look(tid, ANY, v, mine);
+        for (; got < p.top_k; ++got) {
+            double best = v;
+            int at = mine;
+            block_best(best, at, sv[turn], si[turn]);
+            turn ^= 1;
+            if (best == -HUGE_VAL) break;
+            last = best;
+            last_at = at;
+            const int owner = at % ANY;
+            if (owner >> 6 == tid >> 6) {
+                double next = -HUGE_VAL;
+                int next_at = E;
+                look(owner + ANY * (tid & 63), ANY * 64, next, next_at);
+                wave_best(next, next_at);
+                if (tid == owner) {
+                    v = next;
+                    mine = next_at;
+                }
+            }
+            if (tid == 0) {
+                p.ids[row * p.top_k + got] = at;
+                s_logit[got] = logit(p, row, at);
+            }
+        }
+        __syncthreads();
+        if (tid < p.top_k) {
+            // renormalised sums start from the largest chosen logit: scores that underflow keep their shares
+            float most = NONE;
+            for (int j = 0; j < got; ++j) most = __builtin_fmaxf(most, s_logit[j]);
+            const bool small = p.renormalise && (p.score == SCORE_SOFTMAX || most < -300.0f);
+            auto weight = [&](int j) {
+                return small ? exp(double(s_logit[j]) - double(most)) : score(s_logit[j], p.score, m);
+            };
+            double w = tid < got ? weight(tid) : 0.0;
+            if (p.renormalise && tid < got) {
+                double sum = 0.0;
+                for (int j = 0; j < got; ++j) sum += weight(j);
+                w /= sum;
+            }
+            p.weights[row * p.top_k + tid] = float(double(p.scale) * w);
+            if (tid >= got) p.ids[row * p.top_k + tid] = -1;
+        }
+        __syncthreads();
+    }
 }
 
 // What few tokens come to, by a whole wave: the fp64 values that a token's experts are chosen by (groups: that its groups
@@ -906,8 +923,8 @@ __global__ __launch_bounds__(256) void route_bwd_kernel(RouteBwdParams p, int64_
     }
 }
 
-// The gradient for any number of experts: a wave a token, each expert looks through the entries (4096 x 2048 bf16, top 8:
-// 50 us, 37 renormalised; 34 MB are 7 at a copy's rate).
+// The gradient for any number of experts: a wave a token, whose experts look through the entries where any is one of their
+// 64 (4096 x 2048 bf16, top 8: 40 us, 15 renormalised; 34 MB are 7 at a copy's rate).
 __global__ __launch_bounds__(256) void route_bwd_any_kernel(RouteBwdParams p) {
     const int lane = threadIdx.x & 63, E = p.n_experts, K = p.top_k;
     const bool sigmoid = p.score != SCORE_SOFTMAX;
@@ -951,14 +968,19 @@ __global__ __launch_bounds__(256) void route_bwd_any_kernel(RouteBwdParams p) {
         }
         for (int e = lane; e - lane < E; e += 64) {
             float own = 0.0f;
-            for (int j = 0; j < K; ++j) {
+            const bool any = __any(id >= 0 && id >> 6 == e >> 6);  // an entry of these 64 experts
+            for (int j = 0; any && j < K; ++j) {
                 const int i = __shfl(id, j);
                 const float v = __shfl(d, j);
                 if (i == e) own += v;
             }
             if (e >= E) continue;
-            const float v = at(e);
             float g = 0.0f;
+            if (!any && (sigmoid || p.renormalise)) {
+                store_elem(p.dlogits, p.d_bf16, row * E + e, 0.0f);
+                continue;
+            }
+            const float v = at(e);
             if (v > NONE) {
                 if (sigmoid) {
                     const float rest = 1.0f / (1.0f + expf(v));  // 1 - s
