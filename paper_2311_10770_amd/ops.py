@@ -93,6 +93,7 @@ class FffGroupedWeightGradArgs(ctypes.Structure):
     ]
 
 
+_Tensor = torch.Tensor
 _get_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 _LIB = None
 
@@ -116,7 +117,7 @@ def _sizes(*named):
 
 def _gpu(t, what: str, index=None):
     """``t`` as a contiguous GPU tensor (on GPU ``index``)."""
-    if not isinstance(t, torch.Tensor):
+    if not isinstance(t, _Tensor):
         raise ValueError(f"{what} must be a torch.Tensor")
     if not t.is_cuda:
         raise ValueError(f"{what} must be a GPU tensor")
@@ -131,6 +132,10 @@ def _like(t, what, index, shape, dtype=None):
     """Pointer of an optional tensor of exactly ``shape`` (and ``dtype``), or None."""
     if t is None:
         return None
+    # as nearly always, in one condition: the checks below, one by one, are for their messages
+    if (isinstance(t, _Tensor) and t.is_cuda and t.get_device() == index and t.shape == shape
+            and (dtype is None or t.dtype is dtype) and t.is_contiguous()):
+        return t.data_ptr()
     _gpu(t, what, index)
     if t.shape != shape:
         raise ValueError(f"{what} must be {list(shape)}, got {tuple(t.shape)}")
@@ -165,13 +170,13 @@ def _on_call(fn):
     @functools.wraps(fn)
     def call(*args, stream=None, **kw):
         t = args[0] if args else kw.get(name)
-        if not (isinstance(t, torch.Tensor) and t.is_cuda):
-            return fn(*args, stream=None, **kw)  # refused there
+        if not (isinstance(t, _Tensor) and t.is_cuda):
+            return fn(*args, **kw)  # refused there
         if stream is None:
             if t.get_device() == _get_device():
-                return fn(*args, stream=None, **kw)
+                return fn(*args, **kw)
             with torch.cuda.device(t.device):
-                return fn(*args, stream=None, **kw)
+                return fn(*args, **kw)
         if stream.device != t.device:
             raise ValueError(f"stream is on {stream.device}, the tensors on {t.device}")
         with torch.cuda.stream(stream):
@@ -200,11 +205,12 @@ def _rng(p, seed, offset, rng_offset, index):
 
 def _rows(x, what: str):
     _gpu(x, what)
-    if x.dim() != 2:
+    shape = x.shape
+    if len(shape) != 2:
         raise ValueError(f"{what} must be a 2-D tensor [n_tokens, hidden]")
-    if x.shape[1] > _INT32:
-        raise ValueError(f"{what} has rows of {x.shape[1]}: hidden must fit 32 bits")
-    return x.shape
+    if shape[1] > _INT32:
+        raise ValueError(f"{what} has rows of {shape[1]}: hidden must fit 32 bits")
+    return shape
 
 
 def _run(fn, args):

@@ -110,10 +110,11 @@ class Packed(NamedTuple):
 
 
 def _choice(names, v, what):
-    try:
-        return names[v] if isinstance(v, str) else int(v)
-    except KeyError:
-        raise ValueError(f"{what} must be one of {', '.join(names)}, got {v!r}") from None
+    if v in names:
+        return names[v]
+    if isinstance(v, str):
+        raise ValueError(f"{what} must be one of {', '.join(names)}, got {v!r}")
+    return int(v)
 
 
 def _top_k(top_k, n_tokens):
@@ -175,14 +176,14 @@ def route(logits, top_k: int, *, bias=None, score="softmax", n_groups=1, top_gro
     device, at, top_k = logits.device, logits.get_device(), _top_k(top_k, B)
     n_groups = int(n_groups)
     top_groups = n_groups if top_groups is None else int(top_groups)
-    if max(abs(n_groups), abs(top_groups)) > _INT32:
+    if not 0 < top_groups <= n_groups <= _INT32:
         _sizes((n_groups, "n_groups"), (top_groups, "top_groups"))
     ids, ids_at = _out(ids, "ids", at, logits, (B, top_k), torch.int32)
     weights, weights_at = _out(weights, "weights", at, logits, (B, top_k), torch.float32)
     _run(_lib().fff_route, FffRouteArgs(
         logits.data_ptr(), _like(bias, "bias", at, (E,), torch.float32), ids_at, weights_at, B, E, top_k, n_groups, top_groups,
         _dt(logits, "logits"), _choice(SCORES, score, "score"), _choice(GROUP_SCORES, group_score, "group_score"),
-        int(bool(renormalise)), scale, _raw_stream(device, stream)))
+        1 if renormalise else 0, scale, _raw_stream(device, stream)))
     return ids, weights
 
 
