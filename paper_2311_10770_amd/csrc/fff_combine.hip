@@ -60,6 +60,18 @@ __global__ __launch_bounds__(256) void combine_kernel(CombineParams p, int vecs,
     }
 }
 
+// Eight columns from element e on, with OWN those alone that lie behind the first `skip`.
+template <bool OWN>
+__device__ __forceinline__ void store_own(void* base, int bf, int64_t e, int skip, const float* f) {
+    if (OWN && skip) {
+#pragma unroll
+        for (int c = 1; c < 8; ++c)
+            if (c >= skip) store_elem(base, bf, e + c, f[c]);
+    } else {
+        store8(base, bf, e, 8, f);
+    }
+}
+
 // LPE lanes an entry, two vectors of eight columns a lane in flight.  A vector that would end behind its row starts
 // earlier instead, so that all of it lies in the row: its first columns are another lane's, and left out of the sum
 // (16384 x 4 rows of 1001 bf16 with both gradients: 72 -> 68 us, of 1024: 62, 4.8 TB/s; 22085 x 5 rows of 133
@@ -121,13 +133,7 @@ __global__ __launch_bounds__(256) void combine_bwd_kernel(CombineBwdParams p) {
 #pragma unroll
                         for (int c = 0; c < 8; ++c) f[c] *= w;
                     }
-                    if (LPE > 64 && skip[u]) {
-#pragma unroll
-                        for (int c = 1; c < 8; ++c)
-                            if (c >= skip[u]) store_elem(p.drows, p.drows_bf16, e * H + col[u] + c, f[c]);
-                    } else {
-                        store8(p.drows, p.drows_bf16, e * H + col[u], 8, f);
-                    }
+                    store_own<(LPE > 64)>(p.drows, p.drows_bf16, e * H + col[u], skip[u], f);
                 }
             }
         }
@@ -144,12 +150,87 @@ __global__ __launch_bounds__(256) void combine_bwd_kernel(CombineBwdParams p) {
     }
 }
 
+// The gradients of many tokens' rows: LPT lanes a token, U of its rows in flight, for which its dy is read once.  Vectors
+// as above.  us, beside the kernel above: 16384 x 4 rows of 1001 bf16, both gradients 52 (5.5 TB/s) and 68; 65536 x 4 of 768
+// with weights 165 and 214; 65536 x 8 of 64 29 and 54; 16384 x 8 of 4096 431 and 455.  A row takes one or two turns of its
+// lanes: with four (2048 columns and a wave) 238, with 256 lanes 205.  Fewer tokens than fill the chip leave it to the
+// kernel above (256 x 8 rows of 4096 with a wave a token: 26 and 12).
+template <int LPT>
+__global__ __launch_bounds__(256) void combine_bwd_token_kernel(CombineBwdParams p) {
+    __shared__ float red[2][U][4];
+    const int sl = threadIdx.x % LPT;
+    const uint32_t H = p.hidden;
+    const int in_group = threadIdx.x / LPT;
+    int turn = 0;
+    for (int64_t t0 = int64_t(blockIdx.x) * (256 / LPT); t0 < p.n_tokens; t0 += int64_t(gridDim.x) * (256 / LPT)) {
+        const int64_t t = t0 + (LPT >= 64 ? __builtin_amdgcn_readfirstlane(in_group) : in_group);
+        if (t >= p.n_tokens) break;
+        const int64_t e0 = t * p.top_k;
+        for (int j0 = 0; j0 < p.top_k; j0 += U) {
+            float w[U], acc[U] = {};
+            bool in[U], live[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                in[u] = j0 + u < p.top_k;
+                live[u] = in[u] && (!p.ids || p.ids[e0 + j0 + u] >= 0);
+                w[u] = live[u] && p.weights ? p.weights[e0 + j0 + u] : 1.0f;
+            }
+            for (uint32_t c = sl * 8; c < H; c += LPT * 8) {
+                const uint32_t col = c + 8 <= H ? c : H - 8;
+                const int skip = int(c - col);
+                Raw8 row[U];
+                float dy[8];
+                const Raw8 d = load8<true>(p.dy, p.y_bf16, t * H + col, 0);
+                if (p.dweights) {
+#pragma unroll
+                    for (int u = 0; u < U; ++u)
+                        if (live[u]) row[u] = load8<true>(p.rows, p.rows_bf16, (e0 + j0 + u) * H + col, 0);
+                }
+                unpack8(dy, d, p.y_bf16);
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    if (!in[u]) continue;
+                    float f[8];
+                    if (live[u] && p.dweights) {
+                        unpack8(f, row[u], p.rows_bf16);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) acc[u] = i >= skip ? __builtin_fmaf(dy[i], f[i], acc[u]) : acc[u];
+                    }
+                    if (!p.drows) continue;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) f[i] = live[u] ? w[u] * dy[i] : 0.0f;
+                    store_own<(LPT > 64)>(p.drows, p.drows_bf16, (e0 + j0 + u) * H + col, skip, f);
+                }
+            }
+            if (p.dweights) {
+#pragma unroll
+                for (int u = 0; u < U; ++u) acc[u] = group_sum<LPT < 64 ? LPT : 64>(acc[u]);
+                if constexpr (LPT == 256) {
+                    if (sl % 64 == 0) {
+#pragma unroll
+                        for (int u = 0; u < U; ++u) red[turn][u][sl / 64] = acc[u];
+                    }
+                    __syncthreads();
+#pragma unroll
+                    for (int u = 0; u < U; ++u) acc[u] = (red[turn][u][0] + red[turn][u][1]) + (red[turn][u][2] + red[turn][u][3]);
+                    turn ^= 1;
+                }
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    if (sl == 0 && in[u]) p.dweights[e0 + j0 + u] = acc[u];
+            }
+        }
+    }
+}
+
+constexpr int64_t MOST = int64_t(1) << 23;  // workgroups: a launch holds less than 2^32 threads
+
 }  // namespace
 
 hipError_t run_combine(const CombineParams& p, const DeviceInfo& dev, hipStream_t stream) {
     const int vecs = int((int64_t(p.hidden) + 7) / 8);
     const int64_t all = p.n_tokens * vecs;
-    const unsigned grid = unsigned(std::min<int64_t>((all + 255) / 256, 64 * std::max(dev.cu_count, 1)));
+    const unsigned grid = unsigned(std::min<int64_t>((all + 255) / 256, MOST));
     hipLaunchKernelGGL(combine_kernel, dim3(grid), dim3(256), 0, stream, p, vecs, all);
     return hipGetLastError();
 }
@@ -161,7 +242,17 @@ hipError_t run_combine_backward(const CombineBwdParams& p, const DeviceInfo& dev
         const unsigned grid = unsigned(std::min<int64_t>((entries + per - 1) / per, 64 * std::max(dev.cu_count, 1)));
         hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, stream, p);
     };
+    auto tokens = [&](auto kernel, int lanes) {
+        const int per = 256 / lanes;
+        const unsigned grid = unsigned(std::min<int64_t>((p.n_tokens + per - 1) / per, MOST));
+        hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, stream, p);
+    };
     if (p.hidden < 8) launch(combine_bwd_kernel<16, true>, 16);
+    // two thousand waves: eight a CU
+    else if (p.n_tokens >= 8192 && p.hidden <= 128) tokens(combine_bwd_token_kernel<16>, 16);
+    else if (p.n_tokens >= 4096 && p.hidden <= 256) tokens(combine_bwd_token_kernel<32>, 32);
+    else if (p.n_tokens >= 2048 && p.hidden <= 1024) tokens(combine_bwd_token_kernel<64>, 64);
+    else if (p.n_tokens >= 512 && p.hidden > 1024) tokens(combine_bwd_token_kernel<256>, 256);
     else if (p.hidden <= 256) launch(combine_bwd_kernel<16, false>, 16);
     else if (p.hidden <= 512) launch(combine_bwd_kernel<32, false>, 32);
     // few entries of long rows: a workgroup each (one row of 16384: 18 us with a wave, 10.6 so, which is the host's)

@@ -214,7 +214,10 @@ def test_route_backward_any_ids(fff_lib, E):
 
 COMBINE_SIZES = [(1, 1, 1), (2, 3, 5), (7, 2, 8), (5, 4, 31), (33, 1, 64), (9, 8, 100), (4, 5, 129), (6, 6, 256), (3, 2, 257),
                  (17, 3, 519), (11, 8, 768), (3, 16, 1001), (5, 2, 1024), (2, 9, 2056), (8, 8, 4096), (1, 4, 8200), (2, 70, 40),
-                 (1, 1, 16384), (300, 4, 96)]
+                 (1, 1, 16384), (300, 4, 96),
+                 # many tokens: lanes a token
+                 (8200, 3, 20), (8193, 1, 127), (4099, 5, 200), (4096, 2, 129), (2050, 5, 520), (2049, 6, 1001), (515, 6, 1100),
+                 (513, 4, 2051), (600, 1, 4099), (512, 3, 2048)]
 
 
 @pytest.mark.parametrize("T,k,H", COMBINE_SIZES)
@@ -486,6 +489,19 @@ def test_pack_extremes(fff_lib):
     back = fff_lib.unpack_rows(type(packed)(ones.to(DEV), every.to(DEV).view(torch.float8_e8m0fnu)), dtype=torch.float32)
     want = ref.unpack(ones, every)
     assert torch.equal(back.cpu().double().nan_to_num(), want.nan_to_num()) and torch.isnan(back[:, -32:]).all()
+
+
+def test_unpack_every_byte_at_every_scale(fff_lib):
+    """All 256 values at all 256 scales, as other programs may write them: exact, to infinity where fp32 ends."""
+    values = torch.arange(256, dtype=torch.uint8).repeat(256, 1).view(torch.float8_e4m3fn)
+    codes = torch.arange(256, dtype=torch.uint8)[:, None].repeat(1, 8)
+    flush_print("[gpu] unpack every byte at every scale")
+    packed = fff_lib.Packed(values.to(DEV), codes.to(DEV).view(torch.float8_e8m0fnu))
+    want = ref.unpack(values, codes).float()
+    for dt in (torch.float32, torch.bfloat16):
+        got = fff_lib.unpack_rows(packed, dtype=dt).cpu()
+        assert torch.equal(torch.isnan(got), torch.isnan(want))
+        assert torch.equal(got.nan_to_num(7.0), want.to(dt).nan_to_num(7.0))
 
 
 @pytest.mark.parametrize("B,H", PACK_SHAPES)
