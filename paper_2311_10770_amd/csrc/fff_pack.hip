@@ -54,7 +54,7 @@ struct Units {
 
 constexpr int PACK_U = 2, UNPACK_U = 4;
 
-// 65536 x 4096 bf16: 155 us for 814 MB, 5.2 TB/s, a copy's rate, with two units in flight a thread.  Rows of whole blocks need
+// 65536 x 4096 bf16: 144 us for 814 MB, 5.7 TB/s, past a copy's rate, with two units in flight a thread.  Rows of whole blocks need
 // neither the division nor the checks behind a row's end.
 template <bool FLAT>
 __global__ __launch_bounds__(256) void pack_kernel(PackParams p, int upr, int64_t all) {
@@ -94,10 +94,23 @@ __global__ __launch_bounds__(256) void pack_kernel(PackParams p, int upr, int64_
     }
 }
 
+// act(z) of a finite z or NaN.  GELU to be stored in bf16: z Phi(z) as max(z, 0) - |z| Phi(-|z|), two instructions less than
+// the choice between Phi(-|z|) and 1 - Phi(-|z|), at a rounding less.
+template <int ACT, bool FINE>
+__device__ __forceinline__ float packed_act(float z) {
+    if constexpr (ACT == ACT_GELU_ERF && !FINE) {
+        float e;
+        return __builtin_fmaf(-__builtin_fabsf(z), normal_tail(z, e), __builtin_fmaxf(z, 0.0f));
+    } else {
+        return act_value<ACT, FINE>(z);
+    }
+}
+
 // FINE: an output is stored in fp32, and the activation as exact as that shows.
 //
-// 65536 x 4096 bf16: the identity 137 us for 814 MB, 5.9 TB/s, GELU's output 170, 4.8 (its instructions, not all of them
-// behind the four units' loads), and its gradient and output in one pass 346 for 1.89 GB, 5.5.
+// 65536 x 4096 bf16: the identity 138 us for 814 MB, 5.9 TB/s, GELU's output 163, 5.0 (its instructions, 21 a value, not all
+// of them behind the loads), and its gradient and output in one pass 342 for 1.89 GB, 5.5.  Four units in flight: with two
+// 10 us more for GELU, with eight 5.
 template <int ACT, bool FLAT, bool FINE>
 __global__ __launch_bounds__(256) void unpack_kernel(UnpackParams p, int upr, int64_t all) {
     constexpr int U = UNPACK_U;
@@ -129,10 +142,8 @@ __global__ __launch_bounds__(256) void unpack_kernel(UnpackParams p, int upr, in
             if (left <= 0) continue;
             const float scale = scale_value(code[u]);
             float z[8], f[8];
-            unpack_e4m3(z, w[u][0]);
-            unpack_e4m3(z + 4, w[u][1]);
-#pragma unroll
-            for (int c = 0; c < 8; ++c) z[c] *= scale;
+            unpack_e4m3(z, w[u][0], scale);
+            unpack_e4m3(z + 4, w[u][1], scale);
             if (p.dx) {
                 unpack8(f, raw[u], p.dy_bf16);
 #pragma unroll
@@ -141,7 +152,7 @@ __global__ __launch_bounds__(256) void unpack_kernel(UnpackParams p, int upr, in
             }
             if (p.y) {
 #pragma unroll
-                for (int c = 0; c < 8; ++c) f[c] = act_value<ACT, FINE>(z[c]);
+                for (int c = 0; c < 8; ++c) f[c] = packed_act<ACT, FINE>(z[c]);
                 store8(p.y, p.y_bf16, at.e[u], FLAT ? 8 : left, f);
             }
         }
@@ -150,8 +161,10 @@ __global__ __launch_bounds__(256) void unpack_kernel(UnpackParams p, int upr, in
 
 int units_of(int32_t hidden) { return int(pack_blocks(hidden)) * 4; }
 
-unsigned grid_of(int64_t all, int per, const DeviceInfo& dev) {
-    return unsigned(std::min<int64_t>((all + per - 1) / per, 64 * std::max(dev.cu_count, 1)));
+// A turn a workgroup: with loops over a capped grid packing 65536 x 4096 bf16 took 155 us, 144 so (a launch holds less than
+// 2^32 threads).
+unsigned grid_of(int64_t all, int per) {
+    return unsigned(std::min<int64_t>((all + per - 1) / per, int64_t(1) << 23));
 }
 
 }  // namespace
@@ -159,7 +172,7 @@ unsigned grid_of(int64_t all, int per, const DeviceInfo& dev) {
 hipError_t run_pack_rows(const PackParams& p, const DeviceInfo& dev, hipStream_t stream) {
     const int upr = units_of(p.hidden);
     const int64_t all = p.n_rows * upr;
-    const unsigned grid = grid_of(all, 256 * PACK_U, dev);
+    const unsigned grid = grid_of(all, 256 * PACK_U);
     if (p.hidden % PACK_BLOCK == 0) hipLaunchKernelGGL(pack_kernel<true>, dim3(grid), dim3(256), 0, stream, p, upr, all);
     else hipLaunchKernelGGL(pack_kernel<false>, dim3(grid), dim3(256), 0, stream, p, upr, all);
     return hipGetLastError();
@@ -168,7 +181,7 @@ hipError_t run_pack_rows(const PackParams& p, const DeviceInfo& dev, hipStream_t
 hipError_t run_unpack_rows(const UnpackParams& p, const DeviceInfo& dev, hipStream_t stream) {
     const int upr = units_of(p.hidden);
     const int64_t all = p.n_rows * upr;
-    const unsigned grid = grid_of(all, 256 * UNPACK_U, dev);
+    const unsigned grid = grid_of(all, 256 * UNPACK_U);
     const bool flat = p.hidden % PACK_BLOCK == 0, fine = (p.dx && !p.dx_bf16) || (p.y && !p.y_bf16);
     auto launch = [&](auto act) {
         constexpr int ACT = act.value;

@@ -48,8 +48,10 @@ __device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d
     w = __builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
     return uint32_t(w);
 }
-__device__ __forceinline__ void unpack_e4m3(float* f, uint32_t w) {
-    const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(int(w), false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(int(w), true);
+// Four values times their scale, which is a power of two (the conversion adds its exponent) or NaN.
+__device__ __forceinline__ void unpack_e4m3(float* f, uint32_t w, float scale) {
+    const auto lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, scale, false);
+    const auto hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, scale, true);
     f[0] = lo[0];
     f[1] = lo[1];
     f[2] = hi[0];

@@ -97,8 +97,8 @@ __device__ __forceinline__ void gain4(float* f, const float* g, int col, int lef
 
 // Rows held in registers: LPR lanes a row, lane sl holding the NV vectors of four columns
 // c LPR + sl.  One read and one write of every byte.  Rows of up to 1024 columns take a wave or less, whose sum needs no LDS;
-// longer ones a workgroup.  65536 x 1024, bf16 x on an fp32 stream, with bf16 and 8-bit y: 164 us for 873 MB,
-// 5.3 TB/s; one row of 4096: 2.8 us, and the host 11.
+// longer ones a workgroup.  65536 x 1024, bf16 x on an fp32 stream, with bf16 and 8-bit y: 158 us for 873 MB,
+// 5.5 TB/s; one row of 4096: 2.8 us, and the host 11.
 template <int LPR, int NV, int FIT>
 __global__ __launch_bounds__(row_threads(LPR)) void rms_kernel(RmsParams p) {
     constexpr int NT = row_threads(LPR), RPB = NT / LPR;
@@ -467,8 +467,12 @@ hipError_t run_rms_norm(const RmsParams& p, const DeviceInfo& dev, hipStream_t s
         hipLaunchKernelGGL(rms_any_kernel, dim3(grid), dim3(LONG), 0, stream, p);
         return hipGetLastError();
     }
+    // a wave a row of more than 512 columns: a row a wave, else 16 workgroups a CU that keep gamma (bf16 with a residual, us:
+    // 65536 x 768 69 and 75, x 320 34 and 30, x 512 the same; 8192 x 8192 107 and 102)
+    const bool once = ROW_SHAPES[shape].lanes == 64 && ROW_SHAPES[shape].nv > 2;
+    const int64_t most = once ? int64_t(1) << 23 : 16 * cus;
     const int per = rows_per_group(p.hidden);
-    launch_rows<0>(shape, p, unsigned(std::min<int64_t>((p.n_tokens + per - 1) / per, 16 * cus)), stream);
+    launch_rows<0>(shape, p, unsigned(std::min<int64_t>((p.n_tokens + per - 1) / per, most)), stream);
     return hipGetLastError();
 }
 
