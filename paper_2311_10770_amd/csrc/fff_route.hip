@@ -93,6 +93,16 @@ __device__ __forceinline__ int group_larger(float v, float w) {
         n += __builtin_popcount(row_larger(v, __shfl_xor(w, 32))) + __builtin_popcount(row_larger(v, __shfl_xor(w, 48)));
     return n;
 }
+// The bits of all of the token's lanes.
+template <int LPT>
+__device__ __forceinline__ uint32_t group_or(uint32_t v) {
+    v |= __builtin_amdgcn_mov_dpp(int(v), ROR + 8, 0xf, 0xf, true);
+    v |= __builtin_amdgcn_mov_dpp(int(v), ROR + 4, 0xf, 0xf, true);
+    v |= __builtin_amdgcn_mov_dpp(int(v), ROR + 2, 0xf, 0xf, true);
+    v |= __builtin_amdgcn_mov_dpp(int(v), ROR + 1, 0xf, 0xf, true);
+    if constexpr (LPT >= 32) v |= __shfl_xor(v, 16);
+    return v;
+}
 // Sum of v over the token's lanes before this one.
 template <int LPT>
 __device__ __forceinline__ int group_before(int v, int sl) {
@@ -667,11 +677,13 @@ __global__ __launch_bounds__(256, 5) void route_kernel(RouteParams p, int64_t ro
     int larger = group_larger<LPT>(most, most);
     float bar = larger < K ? -most : NONE;
     if (LPT < 64 && 2 * K > LPT) {
-        float a = c[0], b = NONE;  // the largest, the second
+        float a = NONE, b = NONE;  // the largest, the second
 #pragma unroll
-        for (int v = 1; v < V; ++v) {
-            b = __builtin_amdgcn_fmed3f(a, b, c[v]);
-            a = __builtin_fmaxf(a, c[v]);
+        for (int v = 0; v < V; ++v) {
+            float x = c[v];
+            asm volatile("" : "+v"(x));  // of this branch alone: else the compiler takes part of it into the maximum above
+            b = __builtin_amdgcn_fmed3f(a, b, x);
+            a = __builtin_fmaxf(a, x);
         }
         b = finite_value(b);
         larger += group_larger<LPT>(most, b);
@@ -701,15 +713,13 @@ __global__ __launch_bounds__(256, 5) void route_kernel(RouteParams p, int64_t ro
     longest = __builtin_amdgcn_readfirstlane(longest);
     wave_sync();
     // Their order, in fp32 first: a lane has one or two of them where there are no more, and finds its places by counting;
-    // where equal ones meet in a place (the counts' sum is short of 0 + 1 + ...), and where there are more, each counts
-    // those before it out of LDS.
+    // where equal ones meet in a place, and where there are more, each counts those before it out of LDS.
     bool counted = false;
-    const float in_order = 0.5f * float(got) * float(got - 1);
     if (LPT < 64 && longest <= LPT) {
         const int e = sl < got ? list[sl] : 0;
         const float x = sl < got ? finite_value(all[e]) : NONE;
         const int before = group_larger<LPT>(x, x);
-        counted = !__any(group_sum<LPT>(sl < got ? float(before) : 0.0f) != in_order);
+        counted = !__any(__builtin_popcount(group_or<LPT>(sl < got ? 1u << before : 0)) != got);
         if (counted && sl < got) order[before] = uint16_t(e);
     } else if (LPT < 64 && longest <= 2 * LPT) {
         const bool one = sl < got, two = sl + LPT < got;
@@ -717,8 +727,14 @@ __global__ __launch_bounds__(256, 5) void route_kernel(RouteParams p, int64_t ro
         const float x = one ? finite_value(all[e]) : NONE, y = two ? finite_value(all[f]) : NONE;
         const int before = group_larger<LPT>(x, x) + group_larger<LPT>(x, y);
         const int behind = group_larger<LPT>(y, x) + group_larger<LPT>(y, y);
-        const float places = (one ? float(before) : 0.0f) + (two ? float(behind) : 0.0f);
-        counted = !__any(group_sum<LPT>(places) != in_order);
+        if constexpr (LPT == 16) {
+            const uint32_t places = group_or<LPT>((one ? 1u << before : 0) | (two ? 1u << behind : 0));
+            counted = !__any(__builtin_popcount(places) != got);
+        } else {
+            // more places than bits: their sum is short of 0 + 1 + ... where two meet
+            const float places = (one ? float(before) : 0.0f) + (two ? float(behind) : 0.0f);
+            counted = !__any(group_sum<LPT>(places) != 0.5f * float(got) * float(got - 1));
+        }
         if (counted && one) order[before] = uint16_t(e);
         if (counted && two) order[behind] = uint16_t(f);
     }
@@ -743,10 +759,13 @@ __global__ __launch_bounds__(256, 5) void route_kernel(RouteParams p, int64_t ro
         for (int i = sl; i + 1 < got; i += LPT) {
             const int e = order[i], f = order[i + 1];
             const float x = all[e], y = all[f];
-            if (x - y < slack + 2.384185791015625e-07f * __builtin_fabsf(x))
-                near |= (logit(p, row, e) != logit(p, row, f) || bias[e] != bias[f]) &&
-                        (sigmoid || x - y < 4.76837158203125e-07f * share + 2.384185791015625e-07f * __builtin_fabsf(x) +
-                                                7.62939453125e-06f * __builtin_fabsf(bias[e] - bias[f]));  // 2^-21, 2^-22, 2^-17
+            if (x - y < slack + 2.384185791015625e-07f * __builtin_fabsf(x)) {
+                bool open = logit(p, row, e) != logit(p, row, f) || bias[e] != bias[f];
+                if (!sigmoid)  // 2^-21, 2^-22, 2^-17
+                    open &= x - y < 4.76837158203125e-07f * share + 2.384185791015625e-07f * __builtin_fabsf(x) +
+                                        7.62939453125e-06f * __builtin_fabsf(bias[e] - bias[f]);
+                near |= open;
+            }
         }
         if (__any(near)) {
             // in fp64, in the place of the fp32 choices, with the softmax's sum formed in fp64 too
