@@ -441,7 +441,7 @@ struct RouteLds {
 //
 // Bound by vector instructions, but for the plain choice by logits: 65536 tokens, top 8 of 256 fp32 (71 MB: 14 us at a
 // copy's rate): by the logits 16.9 us, sigmoid and bias 23.6, softmax and bias 27.6; sigmoid, bias and the best 4 of 8
-// groups 34, 900 instructions a wave, of which the groups are a third.  Each pick by a reduction over the lanes, in
+// groups 35, 955 instructions a wave, of which the groups are a third.  Each pick by a reduction over the lanes, in
 // fp64, cost 1988 there.  One token of 64 experts: 3.0 us, the launch, behind the host's 9.  A wave holds c, by_e
 // and the lists in LDS, 2 to 13 KB: at 1024 experts that leaves 3 workgroups a CU (65536 tokens, bf16: 96 us, 27 at a
 // copy's rate).
