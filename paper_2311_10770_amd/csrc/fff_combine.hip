@@ -151,9 +151,10 @@ __global__ __launch_bounds__(256) void combine_bwd_kernel(CombineBwdParams p) {
 }
 
 // The gradients of many tokens' rows: LPT lanes a token, U of its rows in flight, for which its dy is read once.  Vectors
-// as above.  us, beside the kernel above: 16384 x 4 rows of 1001 bf16, both gradients 52 (5.5 TB/s) and 68; 65536 x 4 of 768
-// with weights 165 and 214; 65536 x 8 of 64 29 and 54; 16384 x 8 of 4096 431 and 455.  A row takes one or two turns of its
-// lanes: with four (2048 columns and a wave) 238, with 256 lanes 205.  Fewer tokens than fill the chip leave it to the
+// as above.  us, into buffers in turn, beside the kernel above: 16384 x 4 rows of 1001 bf16, both gradients 64 (4.5 TB/s; of
+// 1024 columns, whole lines of memory, 56, 5.3) and 72; 65536 x 4 of 768 with weights 163 and 214; 16384 x 8 of 4096 430
+// and 451; 65536 x 8 of 64, into one buffer, 29 and 54; but 9000 x 5 of 1024 fp32 86 and 83.  A row takes one or two turns of its
+// lanes (16384 x 8 of 2048: four of a wave 238, one of 256 lanes 205).  Fewer tokens than fill the chip leave it to the
 // kernel above (256 x 8 rows of 4096 with a wave a token: 26 and 12).
 template <int LPT>
 __global__ __launch_bounds__(256) void combine_bwd_token_kernel(CombineBwdParams p) {
