@@ -802,9 +802,10 @@ __global__ __launch_bounds__(256, 5) void route_kernel(RouteParams p, int64_t ro
         const uint32_t u = __float_as_uint(all[pick]);  // without a bias: the logit, with its place if it has one
         lg = bias ? logit(p, row, pick) : __uint_as_float(p.bf16 && (u & 0xffffu) != 0xffffu ? u & 0xffff0000u : u);
     }
-    // renormalised from the largest chosen logit where scores underflow: they keep their shares
+    // renormalised from the largest chosen logit where all scores are small (from -20 on 1 + exp(l) is 1 in fp32): they keep
+    // their shares where they underflow
     const float top = p.renormalise ? group_max<LPT>(lg) : soft.most;
-    const bool shifted = !sigmoid || (p.renormalise && top < -60.0f);
+    const bool shifted = !sigmoid || (p.renormalise && top < -20.0f);
     float w = expf(shifted ? lg - top : -lg);
     if (!shifted) w = 1.0f / (1.0f + w);
     w = sl < got ? w : 0.0f;
@@ -908,7 +909,7 @@ __global__ __launch_bounds__(256) void route_bwd_kernel(RouteBwdParams p, int64_
         most = group_max<LPT>(lg);
     }
     // this entry's share of d; all: what the softmax takes from every expert's
-    const bool shifted = !sigmoid || (p.renormalise && most < -60.0f);
+    const bool shifted = !sigmoid || (p.renormalise && most < -20.0f);
     const float x = expf(shifted ? lg - most : -lg);
     float s = id < 0 ? 0.0f : shifted ? x : 1.0f / (1.0f + x), all = 0.0f;
     const float rest = sigmoid ? 1.0f / (1.0f + expf(lg)) : 1.0f;  // 1 - s
@@ -975,7 +976,7 @@ __global__ __launch_bounds__(256) void route_bwd_any_kernel(RouteBwdParams p) {
             }
             sum = group_sum<64>(sum);
         }
-        const bool shifted = !sigmoid || (p.renormalise && most < -60.0f);
+        const bool shifted = !sigmoid || (p.renormalise && most < -20.0f);
         // this entry's part of d, and what is taken from every expert's
         float s = id < 0 ? 0.0f : shifted ? expf(l - most) : 1.0f / (1.0f + expf(-l)), all = 0.0f;
         if (p.renormalise) {

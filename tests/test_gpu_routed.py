@@ -131,6 +131,22 @@ def test_route_zeros_and_infinities_of_either_type(fff_lib, E):
                 assert torch.isfinite(w).all()
 
 
+@pytest.mark.parametrize("E", [4, 100, 600, 2000])
+def test_route_small_scores_keep_their_shares(fff_lib, E):
+    """Renormalised sigmoids that fp32 holds no more beside one that it does, far below 0."""
+    for top in (-21.0, -50.0, -59.0, -70.0, -200.0):
+        logits = torch.full((3, E), -1e4, device=DEV)
+        logits[:, 1], logits[:, 2] = top, torch.tensor([top - 1.0, top - 40.0, top - 60.0], device=DEV)
+        flush_print(f"[gpu] route small scores {E} from {top}")
+        _, w = _check_route(fff_lib, logits, 2, f"{E} from {top}", score="sigmoid", renormalise=True)
+        assert (w > 0).all()
+        dw = torch.tensor([[0.0, 1.0]] * 3, device=DEV)
+        ids = torch.tensor([[1, 2]] * 3, dtype=torch.int32, device=DEV)
+        got = fff_lib.route_backward(dw, logits, ids, score="sigmoid", renormalise=True)
+        want, err = ref.route_backward(dw, logits, ids, score="sigmoid", renormalise=True)
+        ops_ref.check(got, want, err, f"gradient {E} from {top}")
+
+
 @pytest.mark.parametrize("E,G", [(64, 1), (256, 8), (100, 5), (3000, 1)])
 def test_route_order_of_close_choices(fff_lib, E, G):
     """Choices closer to each other than fp32 resolves: a bias that takes back what the score differs by, to 1e-9."""
