@@ -443,7 +443,7 @@ struct RouteLds {
 // copy's rate): by the logits 16.9 us, sigmoid and bias 23.6, softmax and bias 27.6; sigmoid, bias and the best 4 of 8
 // groups 35, 955 instructions a wave, of which the groups are a third.  Each pick by a reduction over the lanes, in
 // fp64, cost 1988 there.  One token of 64 experts: 3.0 us, the launch, behind the host's 9.  A wave holds c, by_e
-// and the lists in LDS, 2 to 13 KB: at 1024 experts that leaves 3 workgroups a CU (65536 tokens, bf16: 96 us, 27 at a
+// and the lists in LDS, 4 to 13 KB: at 1024 experts that leaves 3 workgroups a CU (65536 tokens, bf16: 96 us, 27 at a
 // copy's rate).
 //
 // Choices are first formed in fp32 (c, whose error is below `slack` / 2).  Of the LPT lanes' largest, the
