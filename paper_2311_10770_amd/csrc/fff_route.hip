@@ -127,9 +127,6 @@ __device__ __forceinline__ void top2_step(float& a, float& b) {
     a = __builtin_fmaxf(a, x);
 }
 
-// Whether route_kernel finds groups of `size` experts in its lanes' registers: a power of two of whole vectors.
-__host__ __device__ __forceinline__ bool groups_in_lanes(int size) { return size >= 4 && size <= 64 && (size & (size - 1)) == 0; }
-
 // The best (v, then the lowest i) of the wave's lanes, for each of them.
 __device__ __forceinline__ void wave_best(double& v, int& i) {
     auto meet = [&](double w, int j) {
@@ -473,11 +470,15 @@ __global__ __launch_bounds__(256, 5) void route_kernel(RouteParams p, int64_t ro
     const int64_t row = in ? r0 + tok : p.n_tokens - 1;  // lanes behind the last token do it again
     constexpr uint64_t TOKEN = LPT == 64 ? ~0ull : (1ull << LPT % 64) - 1;
     const float* bias = p.bias;
-    const bool in_lanes = G <= LPT && groups_in_lanes(size);
-    const int turn = in_lanes ? __builtin_ctz(size / 4) : 0;  // 1 << turn lanes hold a group of a vector of experts
+    // groups of V, 2 V .. 16 V experts: lane sl takes V neighbouring experts out of LDS, all of one group, for its value (the
+    // registers' own vectors lie in N groups, whose pairs took 16 us of 36 where this takes 14 of 34).  The choice keeps
+    // to the registers' layout: there the experts of few groups lie in more lanes, and bound it better (34 us, 53 else)
+    const int part = size / V;
+    const bool whole = G > 1 && size % V == 0 && part <= 16 && (part & (part - 1)) == 0;
     uint64_t kept = ~0ull;  // G > 1: a token's groups, one every 1 << shift bits
     int shift = 0;
-    if (!in_lanes)
+    if (whole) shift = __builtin_ctz(part);
+    else
         while (shift < 4 && (G << (shift + 1)) <= LPT) ++shift;
     auto lane_max = [](const float (&x)[V]) {
         float m = x[0];
@@ -571,51 +572,38 @@ __global__ __launch_bounds__(256, 5) void route_kernel(RouteParams p, int64_t ro
         }
         // lanes sl >> shift = g come to hold the two largest of group g, best and second
         float best = NONE, second = NONE;
-        if (in_lanes) {
-            // pairs of the larger two meet over DPP, then in LDS (where the candidates come to be listed)
-            float2* const pairs = reinterpret_cast<float2*>(lds.e) + tok * LPT;
+        if (plain) {
+            // by s here, which leaves LDS to the choices behind
+#pragma unroll
+            for (int q = 0; q < N; ++q) put4(all, q, c);
+        }
+        wave_sync();
+        const int h = 1 << shift, group = sl >> shift;
+        if (whole) {
 #pragma unroll
             for (int q = 0; q < N; ++q) {
-                const float* s = c + 4 * q;
-                const float low = __builtin_fminf(s[0], s[1]), high = __builtin_fmaxf(s[0], s[1]);
-                const float low2 = __builtin_fminf(s[2], s[3]), high2 = __builtin_fmaxf(s[2], s[3]);
-                float a = __builtin_fmaxf(high, high2);
-                float b = __builtin_fmaxf(__builtin_fmaxf(low, low2), __builtin_fminf(high, high2));
-                if (turn >= 1) top2_step<0xb1>(a, b);   // quad_perm 1 0 3 2
-                if (turn >= 2) top2_step<0x4e>(a, b);   // quad_perm 2 3 0 1
-                if (turn >= 3) top2_step<0x141>(a, b);  // row_half_mirror
-                if (turn >= 4) top2_step<0x140>(a, b);  // row_mirror
-                if ((sl & ((1 << turn) - 1)) == 0)
-                    pairs[(q * LPT + sl) >> turn] = make_float2(a, b);
-            }
-            wave_sync();
-            if (sl < G) {
-                best = pairs[sl].x;
-                second = pairs[sl].y;
-            }
-        } else {
-            // 1 << shift lanes share a group of any size: every so many of its scores each, from a place of its own on
-            const int h = 1 << shift, group = sl >> shift;
-            if (plain) {
-                // by s here, which leaves LDS to the choices behind
+                const float4 r = *reinterpret_cast<const float4*>(all + sl * V + (q + sl) % N * 4);  // other banks than its neighbours
+                const float x[4] = {r.x, r.y, r.z, r.w};
 #pragma unroll
-                for (int q = 0; q < N; ++q) put4(all, q, c);
-            }
-            wave_sync();
-            if (group < G) {
-                const float* of = all + group * size;
-#pragma unroll 4
-                for (int i = sl & (h - 1); i < size; i += h) {
-                    const float v = of[i];
-                    second = __builtin_fmaxf(second, __builtin_fminf(best, v));
-                    best = __builtin_fmaxf(best, v);
+                for (int j = 0; j < 4; ++j) {
+                    second = __builtin_amdgcn_fmed3f(best, second, x[j]);
+                    best = __builtin_fmaxf(best, x[j]);
                 }
             }
-            if (h >= 2) top2_step<0xb1>(best, second);
-            if (h >= 4) top2_step<0x4e>(best, second);
-            if (h >= 8) top2_step<0x141>(best, second);
-            if (h >= 16) top2_step<0x140>(best, second);
+        } else if (group < G) {
+            // 1 << shift lanes share a group of any size: every so many of its scores each, from a place of its own on
+            const float* of = all + group * size;
+#pragma unroll 4
+            for (int i = sl & (h - 1); i < size; i += h) {
+                const float v = of[i];
+                second = __builtin_fmaxf(second, __builtin_fminf(best, v));
+                best = __builtin_fmaxf(best, v);
+            }
         }
+        if (h >= 2) top2_step<0xb1>(best, second);   // quad_perm 1 0 3 2
+        if (h >= 4) top2_step<0x4e>(best, second);   // quad_perm 2 3 0 1
+        if (h >= 8) top2_step<0x141>(best, second);  // row_half_mirror
+        if (h >= 16) top2_step<0x140>(best, second);  // row_mirror
         // A group without an expert (none) counts for nothing, whether it is kept or not.  Groups are left open where equal
         // ones make more than top_groups, and where the worst kept and the best other lie within their errors: each
         // the slack, 2^-24 of its terms' sizes and of itself
@@ -651,10 +639,11 @@ __global__ __launch_bounds__(256, 5) void route_kernel(RouteParams p, int64_t ro
             c[4 * q + 2] = r.z;
             c[4 * q + 3] = r.w;
         }
-        if (in_lanes) {
+        if (whole) {
+            const int to = __builtin_ctz(size / 4);  // 4 << to experts a group: of a vector's
 #pragma unroll
             for (int q = 0; q < N; ++q) {
-                const int g = (q * LPT + sl) >> turn;
+                const int g = (q * LPT + sl) >> to << shift;
                 const bool k = (LPT == 64 ? uint32_t(kept >> g) : uint32_t(kept) >> g) & 1;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) c[4 * q + j] = k ? c[4 * q + j] : NONE;
