@@ -438,7 +438,7 @@ struct RouteLds {
 //
 // Bound by vector instructions, but for the plain choice by logits: 65536 tokens, top 8 of 256 fp32 (71 MB: 14 us at a
 // copy's rate): by the logits 16.9 us, sigmoid and bias 23.6, softmax and bias 27.6; sigmoid, bias and the best 4 of 8
-// groups 35, 955 instructions a wave, of which the groups are a third.  Each pick by a reduction over the lanes, in
+// groups 31 (4 of 16: 33), of which the groups are a quarter.  Each pick by a reduction over the lanes, in
 // fp64, cost 1988 there.  One token of 64 experts: 3.0 us, the launch, behind the host's 9.  A wave holds c, by_e
 // and the lists in LDS, 4 to 13 KB: at 1024 experts that leaves 3 workgroups a CU (65536 tokens, bf16: 96 us, 27 at a
 // copy's rate).
@@ -661,34 +661,42 @@ __global__ __launch_bounds__(256, 5) void route_kernel(RouteParams p, int64_t ro
 #pragma unroll
         for (int q = 0; q < N; ++q) put4(all, q, c);
     }
-    // candidates: not below the top_k-th largest of the lanes' largest (or largest two), less the slack
+    // candidates: not below the top_k-th largest of the lanes' largest, less the slack; or of their largest two, where lanes
+    // are few, or hold the experts of few groups, so that too many are left to be ordered over the lanes (us, 65536 tokens over
+    // 256 experts, 4 of 8 groups 34 -> 31, 4 of 16 48 -> 33; where the largest leave less, their two cost 2 to 3 more)
     const float most = finite_value(lane_max(c));
-    int larger = group_larger<LPT>(most, most);
-    float bar = larger < K ? -most : NONE;
-    if (LPT < 64 && 2 * K > LPT) {
-        float a = NONE, b = NONE;  // the largest, the second
+    const int larger = group_larger<LPT>(most, most);
+    bool two = LPT < 64 && 2 * K > LPT;
+    uint32_t live;
+    int n, at;
+    for (;;) {
+        float bar = larger < K ? -most : NONE;
+        if (LPT < 64 && two) {
+            float a = NONE, b = NONE;  // the largest, the second
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            float x = c[v];
-            asm volatile("" : "+v"(x));  // of this branch alone: else the compiler takes part of it into the maximum above
-            b = __builtin_amdgcn_fmed3f(a, b, x);
-            a = __builtin_fmaxf(a, x);
+            for (int v = 0; v < V; ++v) {
+                float x = c[v];
+                asm volatile("" : "+v"(x));  // of this branch alone: else the compiler takes part of it into the maximum above
+                b = __builtin_amdgcn_fmed3f(a, b, x);
+                a = __builtin_fmaxf(a, x);
+            }
+            b = finite_value(b);
+            bar = larger + group_larger<LPT>(most, b) < K ? -most : NONE;
+            if (group_larger<LPT>(b, most) + group_larger<LPT>(b, b) < K) bar = -b;  // no more than most
         }
-        b = finite_value(b);
-        larger += group_larger<LPT>(most, b);
-        bar = larger < K ? -most : NONE;
-        if (group_larger<LPT>(b, most) + group_larger<LPT>(b, b) < K) bar = -b;  // no more than most
-    }
-    bar = -group_max<LPT>(bar);
-    if (bias) bar -= slack + 4.76837158203125e-07f * __builtin_fabsf(bar);
-    bar = __builtin_fmaxf(bar, -3.4028234663852886e38f);  // every expert there is
-    uint32_t live = 0;
+        bar = -group_max<LPT>(bar);
+        if (bias) bar -= slack + 4.76837158203125e-07f * __builtin_fabsf(bar);
+        bar = __builtin_fmaxf(bar, -3.4028234663852886e38f);  // every expert there is
+        live = 0;
 #pragma unroll
-    for (int v = 0; v < V; ++v) live = push_sign(live, c[v] - bar);
-    live = ~live & ((1u << V) - 1);  // bit V - 1 - v: of c[v]
-    int n = __builtin_popcount(live);
-    int at = group_before<LPT>(n, sl);
-    n = __shfl(at + n, first + LPT - 1);  // of the token
+        for (int v = 0; v < V; ++v) live = push_sign(live, c[v] - bar);
+        live = ~live & ((1u << V) - 1);  // bit V - 1 - v: of c[v]
+        n = __builtin_popcount(live);
+        at = group_before<LPT>(n, sl);
+        n = __shfl(at + n, first + LPT - 1);  // of the token
+        if (LPT == 64 || two || !__any(n > 2 * LPT)) break;
+        two = true;
+    }
     const bool redo = n > CAP;  // left to route_token
     if (!redo)
         for (; live; live &= live - 1) {
