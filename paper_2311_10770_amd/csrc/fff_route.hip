@@ -21,6 +21,13 @@ namespace {
 
 constexpr float NONE = -__builtin_inff();
 
+// A sigmoid times exp(-shift), for shift = 0 or the largest of a token's chosen logits where that is below 0: the common factor
+// cancels from their shares, which so keep their bits where the sigmoids themselves leave fp32 (1 / (1 + exp(-l)) is 0 from
+// -88.8 on; its share beside one at -19 is 1e-30).  No step overflows.
+__device__ __forceinline__ float sigmoid_part(float l, float shift) {
+    return expf(__builtin_fminf(l, 0.0f) - shift) / (1.0f + expf(-__builtin_fabsf(l)));
+}
+
 // A logit: -inf where it is NaN (no expert), the largest fp32 value where it is infinite.
 __device__ __forceinline__ float clean_logit(float l) {
     return __builtin_fminf(__builtin_fmaxf(l, NONE), 3.4028234663852886e38f);  // the larger of NaN and a number is that
@@ -799,12 +806,9 @@ __global__ __launch_bounds__(256, 5) void route_kernel(RouteParams p, int64_t ro
         const uint32_t u = __float_as_uint(all[pick]);  // without a bias: the logit, with its place if it has one
         lg = bias ? logit(p, row, pick) : __uint_as_float(p.bf16 && (u & 0xffffu) != 0xffffu ? u & 0xffff0000u : u);
     }
-    // renormalised from the largest chosen logit where all scores are small (from -20 on 1 + exp(l) is 1 in fp32): they keep
-    // their shares where they underflow
+    // renormalised from the largest chosen logit, below 0 for sigmoids: shares keep their bits where scores underflow
     const float top = p.renormalise ? group_max<LPT>(lg) : soft.most;
-    const bool shifted = !sigmoid || (p.renormalise && top < -20.0f);
-    float w = expf(shifted ? lg - top : -lg);
-    if (!shifted) w = 1.0f / (1.0f + w);
+    float w = sigmoid ? sigmoid_part(lg, __builtin_fminf(top, 0.0f)) : expf(lg - top);
     w = sl < got ? w : 0.0f;
     if (p.renormalise || !sigmoid) {
         const float total = p.renormalise ? group_sum<LPT>(w) : z;
@@ -906,9 +910,8 @@ __global__ __launch_bounds__(256) void route_bwd_kernel(RouteBwdParams p, int64_
         most = group_max<LPT>(lg);
     }
     // this entry's share of d; all: what the softmax takes from every expert's
-    const bool shifted = !sigmoid || (p.renormalise && most < -20.0f);
-    const float x = expf(shifted ? lg - most : -lg);
-    float s = id < 0 ? 0.0f : shifted ? x : 1.0f / (1.0f + x), all = 0.0f;
+    float s = sigmoid ? sigmoid_part(lg, p.renormalise ? __builtin_fminf(most, 0.0f) : 0.0f) : expf(lg - most), all = 0.0f;
+    s = id < 0 ? 0.0f : s;
     const float rest = sigmoid ? 1.0f / (1.0f + expf(lg)) : 1.0f;  // 1 - s
     if (p.renormalise) {
         const float total = group_sum<LPT>(s);
@@ -973,9 +976,9 @@ __global__ __launch_bounds__(256) void route_bwd_any_kernel(RouteBwdParams p) {
             }
             sum = group_sum<64>(sum);
         }
-        const bool shifted = !sigmoid || (p.renormalise && most < -20.0f);
         // this entry's part of d, and what is taken from every expert's
-        float s = id < 0 ? 0.0f : shifted ? expf(l - most) : 1.0f / (1.0f + expf(-l)), all = 0.0f;
+        float s = sigmoid ? sigmoid_part(l, p.renormalise ? __builtin_fminf(most, 0.0f) : 0.0f) : expf(l - most), all = 0.0f;
+        s = id < 0 ? 0.0f : s;
         if (p.renormalise) {
             const float total = group_sum<64>(s);
             s = id < 0 ? 0.0f : s / total;
