@@ -787,6 +787,9 @@ int fff_pack_rows(const fff_pack_rows_args* a);
  *   y = act(z)         (the next product's input, for its weight gradient)
  *   dx = dy act'(z)    (the gradient through the activation)
  * either part optional.  dx may be the buffer dy, of its type.  n_rows < 2^32.
+ * An infinite z, which fff_pack_rows does not write but other programs' scales can hold, gives
+ * with either GELU what the formulas give, whatever the types: act(+inf) = +inf; NaN for
+ * act(-inf) and for act' of both.
  */
 typedef struct {
     const uint8_t* q;      /* [n_rows, hidden] */

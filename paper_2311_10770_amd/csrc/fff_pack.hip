@@ -94,13 +94,15 @@ __global__ __launch_bounds__(256) void pack_kernel(PackParams p, int upr, int64_
     }
 }
 
-// act(z) of a finite z or NaN.  GELU to be stored in bf16: z Phi(z) as max(z, 0) - |z| Phi(-|z|), two instructions less than
-// the choice between Phi(-|z|) and 1 - Phi(-|z|), at a rounding less.
-template <int ACT, bool FINE>
+// act(z).  GELU to be stored in bf16: z Phi(z) as max(z, 0) - |z| Phi(-|z|), two instructions less than the choice between
+// Phi(-|z|) and 1 - Phi(-|z|), at a rounding less.  FAR: z may be +inf, which stays finite beside Phi(-inf) = 0; the same bits
+// for every other z.
+template <int ACT, bool FINE, bool FAR>
 __device__ __forceinline__ float packed_act(float z) {
     if constexpr (ACT == ACT_GELU_ERF && !FINE) {
         float e;
-        return __builtin_fmaf(-__builtin_fabsf(z), normal_tail(z, e), __builtin_fmaxf(z, 0.0f));
+        const float m = __builtin_fabsf(FAR ? __builtin_fminf(z, 3.4028234663852886e38f) : z);
+        return __builtin_fmaf(-m, normal_tail(z, e), __builtin_fmaxf(z, 0.0f));
     } else {
         return act_value<ACT, FINE>(z);
     }
@@ -136,25 +138,35 @@ __global__ __launch_bounds__(256) void unpack_kernel(UnpackParams p, int upr, in
 #pragma unroll
             for (int u = 0; u < U; ++u) raw[u] = load8<FLAT>(p.dy, p.dy_bf16, at.e[u], total);
         }
+        auto units = [&](auto far) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int left = at.left[u];
-            if (left <= 0) continue;
-            const float scale = scale_value(code[u]);
-            float z[8], f[8];
-            unpack_e4m3(z, w[u][0], scale);
-            unpack_e4m3(z + 4, w[u][1], scale);
-            if (p.dx) {
-                unpack8(f, raw[u], p.dy_bf16);
+            for (int u = 0; u < U; ++u) {
+                const int left = at.left[u];
+                if (left <= 0) continue;
+                const float scale = scale_value(code[u]);
+                float z[8], f[8];
+                unpack_e4m3(z, w[u][0], scale);
+                unpack_e4m3(z + 4, w[u][1], scale);
+                if (p.dx) {
+                    unpack8(f, raw[u], p.dy_bf16);
 #pragma unroll
-                for (int c = 0; c < 8; ++c) f[c] *= act_slope<ACT, FINE>(z[c]);
-                store8(p.dx, p.dx_bf16, at.e[u], FLAT ? 8 : left, f);
+                    for (int c = 0; c < 8; ++c) f[c] *= act_slope<ACT, FINE>(z[c]);
+                    store8(p.dx, p.dx_bf16, at.e[u], FLAT ? 8 : left, f);
+                }
+                if (p.y) {
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) f[c] = packed_act<ACT, FINE, far.value>(z[c]);
+                    store8(p.y, p.y_bf16, at.e[u], FLAT ? 8 : left, f);
+                }
             }
-            if (p.y) {
-#pragma unroll
-                for (int c = 0; c < 8; ++c) f[c] = packed_act<ACT, FINE>(z[c]);
-                store8(p.y, p.y_bf16, at.e[u], FLAT ? 8 : left, f);
-            }
+        };
+        if constexpr (ACT == ACT_GELU_ERF && !FINE) {
+            // a wave's own form where a scale of its units reaches past fp32: 65536 x 4096, GELU's output 160 us, its gradient
+            // and output 334, and 159 and 339 without it (a minimum for each value: 169 and 356)
+            if (__any(max(max(code[0], code[1]), max(code[2], code[3])) >= INFINITE_CODE)) units(std::true_type{});
+            else units(std::false_type{});
+        } else {
+            units(std::true_type{});
         }
     }
 }

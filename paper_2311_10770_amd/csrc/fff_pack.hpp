@@ -32,6 +32,7 @@ __device__ __forceinline__ uint32_t scale_code(uint32_t most) {
 }
 // 1 / scale (codes that scale_code gives: at most 247), and the scale of any code.
 __device__ __forceinline__ float scale_inverse(uint32_t code) { return __uint_as_float((254 - code) << 23); }
+constexpr uint32_t INFINITE_CODE = 247;  // 448 times 2^120 is past fp32: values of this scale and of larger ones may be infinite
 __device__ __forceinline__ float scale_value(uint32_t code) {
     return __uint_as_float(code == 255 ? 0x7fc00000u : code ? code << 23 : 0x00400000u);
 }

@@ -34,3 +34,50 @@ def test_route_shares_of_sigmoids_far_apart(fff_lib, E, t):
         got = fff_lib.route_backward(dw, logits, ids, score="sigmoid", renormalise=True, scale=2.0, dlogits_dtype=torch.float32)
         d, derr = ref.route_backward(dw, logits, ids, score="sigmoid", renormalise=True, scale=2.0)
         ops_ref.check(got, d, derr, f"{E} from {top}: gradient")
+
+
+@pytest.mark.parametrize("act", ["gelu", "gelu_tanh", "identity"])
+def test_activation_of_every_byte_at_every_scale(fff_lib, act):
+    """All 256 values at all 256 scales, as other programs may write them, infinities among them: what the formulas give
+    in IEEE arithmetic (+inf from +inf; NaN from NaN, from -inf and for the derivative of either), the same in each type."""
+    values = torch.arange(256, dtype=torch.uint8).repeat(256, 1).view(torch.float8_e4m3fn)
+    codes = torch.arange(256, dtype=torch.uint8)[:, None].repeat(1, 8)
+    packed = fff_lib.Packed(values.to(DEV), codes.to(DEV).view(torch.float8_e8m0fnu))
+    flush_print(f"[gpu] {act} of every byte at every scale")
+    z = ref.unpack(values, codes).float()  # infinite where fp32 ends
+    finite, up = torch.isfinite(z), z == math.inf
+    assert up.sum() > 100 and (z == -math.inf).sum() > 100
+    y, ey, dx, edx = ref.activations(torch.where(finite, z, 0.0).double(), act, torch.ones(z.shape, dtype=torch.float64))
+    # |y| = |z| Phi(z) for z < 0 is below 0.4 exp(-z^2 / 2) (Phi(z) < phi(z) / |z|): where that exponential leaves the normal
+    # numbers of fp32, from -13.3 on, and is lost, y is off by 0.4 times 2^-126 at most
+    ey = ey + 0.4 * ref.TINY
+    for dt in (torch.float32, torch.bfloat16):
+        got = fff_lib.unpack_rows(packed, act=act, dtype=dt).cpu()
+        slope, again = (v.cpu() for v in fff_lib.activation_backward(torch.ones(z.shape, dtype=dt, device=DEV), packed, act, keep_y=True))
+        assert torch.equal(torch.isnan(got), torch.isnan(again)) and torch.equal(got.nan_to_num(7.0), again.nan_to_num(7.0))
+        assert (got[up] == math.inf).all()
+        if act == "identity":
+            assert torch.equal(got[~torch.isnan(z)], z.to(dt)[~torch.isnan(z)]) and (slope == 1).all()
+        else:
+            assert torch.isnan(got[~finite & ~up]).all() and torch.isnan(slope[~finite]).all()
+        assert torch.isnan(got[torch.isnan(z)]).all()
+        ops_ref.check(torch.where(finite, got, 0.0), y, ey, f"{act} {dt}")
+        ops_ref.check(torch.where(finite, slope, dx.to(dt)), dx, edx, f"slope of {act} {dt}")
+
+
+def test_activation_beside_a_far_block(fff_lib):
+    """A block's activations have the same bits whatever its neighbours' scales."""
+    gen = torch.Generator(device=DEV).manual_seed(3)
+    for H in (96, 100, 1024):
+        z = torch.randn((40, H), generator=gen, device=DEV) * 3
+        far = z.clone()
+        far[::3] = 3e38
+        flush_print(f"[gpu] activation beside a far block {H}")
+        a, b = fff_lib.pack_rows(z), fff_lib.pack_rows(far)
+        near = torch.arange(40, device=DEV) % 3 != 0
+        for act in ("gelu", "gelu_tanh"):
+            for dt in (torch.float32, torch.bfloat16):
+                dy = torch.ones((40, H), dtype=dt, device=DEV)
+                for u, v in zip(fff_lib.activation_backward(dy, a, act, keep_y=True), fff_lib.activation_backward(dy, b, act, keep_y=True)):
+                    assert torch.equal(u[near], v[near])
+                assert torch.equal(v[~near], fff_lib.unpack_rows(b, dtype=dt)[~near])
