@@ -361,16 +361,12 @@ def pack_rows(x, *, packed=None, stream=None):
     return packed
 
 
-def _act(act):
-    return ACTS[act] if isinstance(act, str) else int(act)
-
-
 @_on_call
 def _unpack_rows(values, packed, act, y, dtype, *, stream=None):
     q, q_scale, shape = _packed(packed, None)
     y, y_at = _out(y, "y", values.get_device(), values, None, new=dtype)
     _run(_lib().fff_unpack_rows, FffUnpackRowsArgs(
-        q, q_scale, None, y_at, None, shape[0], shape[1], FFF_F32, _dt(y, "y"), FFF_F32, _act(act),
+        q, q_scale, None, y_at, None, shape[0], shape[1], FFF_F32, _dt(y, "y"), FFF_F32, _choice(ACTS, act, "act"),
         _raw_stream(values.device, stream)))
     return y
 
@@ -403,5 +399,5 @@ def activation_backward(dy, packed, act="gelu", *, dx=None, dx_dtype=None, y=Non
         y, y_at = _out(y, "y", at, dy, None, new=y_dtype or dy.dtype)
     _run(_lib().fff_unpack_rows, FffUnpackRowsArgs(
         q, q_scale, dy.data_ptr(), y_at, dx_at, shape[0], shape[1], _dt(dy, "dy"),
-        _dt(y, "y") if y is not None else FFF_F32, _dt(dx, "dx"), _act(act), _raw_stream(device, stream)))
+        _dt(y, "y") if y is not None else FFF_F32, _dt(dx, "dx"), _choice(ACTS, act, "act"), _raw_stream(device, stream)))
     return (dx, y) if keep_y else dx

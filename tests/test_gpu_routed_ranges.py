@@ -81,3 +81,14 @@ def test_activation_beside_a_far_block(fff_lib):
                 for u, v in zip(fff_lib.activation_backward(dy, a, act, keep_y=True), fff_lib.activation_backward(dy, b, act, keep_y=True)):
                     assert torch.equal(u[near], v[near])
                 assert torch.equal(v[~near], fff_lib.unpack_rows(b, dtype=dt)[~near])
+
+
+def test_an_unknown_activation_is_refused(fff_lib):
+    """By the error type and the list of names that an unknown score is refused with."""
+    x = torch.zeros((3, 40), device=DEV)
+    packed = fff_lib.pack_rows(x)
+    for call in (lambda: fff_lib.unpack_rows(packed, act="relu"), lambda: fff_lib.activation_backward(x, packed, "relu")):
+        with pytest.raises(ValueError, match="act must be one of gelu.*relu"):
+            call()
+    for act in ("gelu", "gelu_erf", "gelu_tanh", "identity", 0, 1, 2):
+        assert (fff_lib.unpack_rows(packed, act=act) == 0).all()
