@@ -92,3 +92,101 @@ def test_an_unknown_activation_is_refused(fff_lib):
             call()
     for act in ("gelu", "gelu_erf", "gelu_tanh", "identity", 0, 1, 2):
         assert (fff_lib.unpack_rows(packed, act=act) == 0).all()
+
+
+def _tokens_alone(fff, logits, tail, k, what, **kw):
+    """route and route_backward of `logits`, whose last rows are `tail`, against `tail` alone."""
+    n = tail.shape[0]
+    flush_print(f"[gpu] {what}: route")
+    ids, w = fff.route(logits, k, **kw)
+    one, v = fff.route(tail, k, **kw)
+    assert torch.equal(ids[-n:], one) and torch.equal(w[-n:], v)
+    assert torch.equal(ids[:4], fff.route(logits[:4].contiguous(), k, **kw)[0])
+    del w
+    kw = {key: kw[key] for key in ("score", "renormalise") if key in kw}
+    dw = torch.zeros(ids.shape, device=DEV)
+    dw[-n:] = torch.arange(n * k, device=DEV).view(n, k) % 5 - 1.5
+    flush_print(f"[gpu] {what}: route_backward")
+    d = fff.route_backward(dw, logits, ids, **kw)
+    assert torch.equal(d[-n:], fff.route_backward(dw[-n:].contiguous(), tail, one, **kw)) and (d[:4] == 0).all()
+    assert (d[-n:] != 0).any()
+
+
+def test_route_past_a_launch(fff_lib):
+    """More tokens than a launch holds at 16 lanes each: 2^23 workgroups of 16."""
+    T, gen = (1 << 27) + 37, torch.Generator(device=DEV).manual_seed(5)
+    tail = torch.randn((41, 2), generator=gen, device=DEV).bfloat16()
+    logits = torch.zeros((T, 2), dtype=torch.bfloat16, device=DEV)
+    logits[-41:] = tail
+    _tokens_alone(fff_lib, logits, tail, 2, "past a launch", score="softmax")
+
+
+@pytest.mark.parametrize("E", [1024, 2048])
+def test_route_past_four_billion_logits(fff_lib, E):
+    T, gen = (1 << 32) // E + 5, torch.Generator(device=DEV).manual_seed(E)
+    tail = torch.randn((7, E), generator=gen, device=DEV).bfloat16()
+    logits = torch.zeros((T, E), dtype=torch.bfloat16, device=DEV)
+    logits[:, E // 3] = 1.0
+    logits[-7:] = tail
+    _tokens_alone(fff_lib, logits, tail, 3, f"past 2^32 logits of {E}", score="sigmoid", renormalise=True)
+    _tokens_alone(fff_lib, logits, tail, 1, f"past 2^32 logits of {E}", score="softmax")
+
+
+@pytest.mark.parametrize("H", [1024, 1001, 16400])
+def test_rms_norm_past_four_billion_elements(fff_lib, H):
+    """Rows held in registers and longer ones, both directions: as the same rows alone."""
+    B, gen = (1 << 32) // H + 6, torch.Generator(device=DEV).manual_seed(H)
+    x = torch.zeros((B, H), dtype=torch.bfloat16, device=DEV)
+    tail = torch.randn((5, H), generator=gen, device=DEV).bfloat16()
+    gamma = torch.rand(H, generator=gen, device=DEV) + 0.5
+    x[-5:] = tail
+    flush_print(f"[gpu] past 2^32 elements of {H}: rms_norm")
+    y, s, rstd, packed = fff_lib.rms_norm(x, gamma, pack=True)
+    want = fff_lib.rms_norm(tail, gamma, pack=True)
+    assert torch.equal(y[-5:], want[0]) and torch.equal(rstd[-5:], want[2]) and (y[:4] == 0).all()
+    for a, b in zip(packed, want[3]):
+        assert torch.equal(a.view(torch.uint8)[-5:], b.view(torch.uint8))
+    del packed
+    dy = y  # zeros but for the last rows
+    flush_print(f"[gpu] past 2^32 elements of {H}: rms_norm_backward")
+    ds, _, dgamma = fff_lib.rms_norm_backward(dy, x, rstd, gamma, ds_in=x)
+    alone = fff_lib.rms_norm_backward(want[0], tail, want[2], gamma, ds_in=tail)
+    assert torch.equal(ds[-5:], alone[0]) and (ds[:4] == 0).all()
+    # five products and sums of them in some order, each of fp32, on both sides
+    xh = tail.double() * want[2].double()[:, None]
+    assert ((dgamma - alone[2]).double().abs() <= 2 * (5 + 6) * ops_ref.U * (want[0].double() * xh).abs().sum(0)).all()
+
+
+def test_activation_gradient_past_four_billion_elements(fff_lib):
+    for H in (1024, 1001):
+        B, gen = (1 << 32) // H + 6, torch.Generator(device=DEV).manual_seed(H)
+        z = torch.zeros((B, H), dtype=torch.bfloat16, device=DEV)
+        tail = torch.randn((5, H), generator=gen, device=DEV).bfloat16()
+        z[-5:] = tail
+        flush_print(f"[gpu] past 2^32 elements of {H}: activation_backward")
+        packed, alone = fff_lib.pack_rows(z), fff_lib.pack_rows(tail)
+        dx, y = fff_lib.activation_backward(z, packed, "gelu", keep_y=True)
+        want = fff_lib.activation_backward(tail, alone, "gelu", keep_y=True)
+        assert torch.equal(dx[-5:], want[0]) and torch.equal(y[-5:], want[1])
+        assert (dx[:4] == 0).all() and (y[:4] == 0).all()
+
+
+@pytest.mark.parametrize("k,H", [(2, 1024), (3, 1001), (1, 4096)])
+def test_combine_gradient_past_four_billion_elements(fff_lib, k, H):
+    """The kernel of many tokens, at the lanes of each row length."""
+    T, gen = (1 << 32) // (H * k) + 5, torch.Generator(device=DEV).manual_seed(H)
+    rows = torch.zeros((T * k, H), dtype=torch.bfloat16, device=DEV)
+    tail = torch.randn((3 * k, H), generator=gen, device=DEV).bfloat16()
+    rows[-3 * k:] = tail
+    w = torch.rand((T, k), generator=gen, device=DEV)
+    flush_print(f"[gpu] past 2^32 elements of {k} x {H}: combine")
+    dy = fff_lib.combine(rows, k, w)
+    assert torch.equal(dy[-3:], fff_lib.combine(tail, k, w[-3:].contiguous()))
+    flush_print(f"[gpu] past 2^32 elements of {k} x {H}: combine_backward")
+    drows, dw = fff_lib.combine_backward(dy, k, rows, w)
+    d = dy[-3:].double()
+    want = (w[-3:].double()[:, :, None] * d[:, None]).view(3 * k, H)
+    ops_ref.check(drows[-3 * k:], want.cpu(), (ops_ref.U * want.abs()).cpu(), "drows")
+    terms = d[:, None] * tail.double().view(3, k, H)
+    ops_ref.check(dw[-3:], terms.sum(2).cpu(), ((H + 4) * ops_ref.U * terms.abs().sum(2)).cpu(), "dweights")
+    assert (drows[:4] == 0).all() and (dw[:4] == 0).all()
