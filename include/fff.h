@@ -597,7 +597,9 @@ typedef enum { FFF_GROUP_MAX = 0, FFF_GROUP_TOP2 = 1 } fff_group_score;
  * index where two are equal), and with `scale`
  *   weights = scale s, or with renormalise  scale s / sum of s over the chosen.
  * A bias (to balance the experts' loads) moves the choice and no weight.  c is
- * compared in fp64, so that a choice does not hang on fp32 roundings.
+ * compared in fp64, so that a choice does not hang on fp32 roundings (a softmax's sum
+ * has fp64's own: values of c within those of each other may come in either order, for
+ * n_experts, top_k and n_groups always the same).
  * With n_groups > 1 the experts form n_groups runs of equal length, and a token
  * chooses only among the top_groups groups of the largest
  *   max c (FFF_GROUP_MAX), or the sum of the group's two largest c (FFF_GROUP_TOP2;
@@ -708,7 +710,8 @@ int fff_combine_backward(const fff_combine_backward_args* a);
  * nearest, even at ties, and none is cut off, but that what would round to 2^128
  * becomes 240 x 2^120, the largest finite number of the format that fp32 holds.
  * Infinite and NaN values become NaN and leave the others' scale alone.  Such
- * values are exact in bf16. */
+ * values are exact in fp32, and in bf16 where the scale is 2^-124 (byte 3) or more:
+ * e4m3's smallest value is 2^-9, bf16's 2^-133. */
 #define FFF_PACK_BLOCK 32
 
 /*
@@ -716,7 +719,8 @@ int fff_combine_backward(const fff_combine_backward_args* a);
  *   y = s / sqrt(mean(s^2) + eps) * gamma
  * per row, y in y_dtype and, with q, in 8 bits too (from the fp32 y).  y, q and rstd
  * come from the fp32 s, before it is rounded to s_dtype for the stream; the squares
- * are fp32 too (values past 1.8e19 overflow them).  Any
+ * are fp32 too (values past 1.8e19 overflow them, and values below 1e-19 lose bits in
+ * them, which shows where eps is no larger).  Any
  * hidden >= 1; n_tokens < 2^32.
  */
 typedef struct {

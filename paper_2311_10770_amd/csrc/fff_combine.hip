@@ -150,10 +150,10 @@ __global__ __launch_bounds__(256) void combine_bwd_kernel(CombineBwdParams p) {
     }
 }
 
-// The gradients of many tokens' rows: LPT lanes a token, U of its rows in flight, for which its dy is read once.  Vectors
-// as above.  us, into buffers in turn, beside the kernel above: 16384 x 4 rows of 1001 bf16, both gradients 64 (4.5 TB/s; of
+// The gradients of many tokens' rows: LPT lanes a token, U of its rows in flight, for which its dy is read once (by the next U
+// again, out of the caches).  Vectors as above.  us, into buffers in turn, beside the kernel above: 16384 x 4 rows of 1001 bf16, both gradients 64 (4.5 TB/s; of
 // 1024 columns, whole lines of memory, 56, 5.3) and 72; 65536 x 4 of 768 with weights 163 and 214; 16384 x 8 of 4096 430
-// and 451; 65536 x 8 of 64, into one buffer, 29 and 54; but 9000 x 5 of 1024 fp32 86 and 83.  A row takes one or two turns of its
+// and 451; 65536 x 8 of 64, into one buffer, 29 and 54; but 9000 x 5 of 1024 fp32 87 and 82 (bf16 42 and 45).  A row takes one or two turns of its
 // lanes (16384 x 8 of 2048: four of a wave 238, one of 256 lanes 205).  Fewer tokens than fill the chip leave it to the
 // kernel above (256 x 8 rows of 4096 with a wave a token: 26 and 12).
 template <int LPT>
@@ -249,7 +249,11 @@ hipError_t run_combine_backward(const CombineBwdParams& p, const DeviceInfo& dev
         hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, stream, p);
     };
     if (p.hidden < 8) launch(combine_bwd_kernel<16, true>, 16);
-    // two thousand waves: eight a CU
+    // two thousand waves: eight a CU.  us, lanes a token and lanes an entry, at half of a bound, at it and at twice as many
+    // tokens, 8 bf16 rows each, both gradients: 64 columns 5.6 and 4.6, 7.1 8.2, 9.6 12.5; 128 6.9 6.1, 9.1 8.9, 13.9 14.0; 256
+    // 7.0 5.6, 9.4 9.6, 13.8 14.7; 1024 10.6 10.0, 13.9 15.2, 29.0 33.7; 4096 11.7 11.8, 15.0 14.7, 29.1 42.2.  Of two rows
+    // a token the same within 0.2 at the bounds (4096 columns 6.9 10.9).  fp32 rows of up to 1024 columns gain nothing, which
+    // the rule leaves out: 8 of 128 18.4 14.4, at four times the bound 67 58; 8 of 1024 35.6 35.6 and 119 112
     else if (p.n_tokens >= 8192 && p.hidden <= 128) tokens(combine_bwd_token_kernel<16>, 16);
     else if (p.n_tokens >= 4096 && p.hidden <= 256) tokens(combine_bwd_token_kernel<32>, 32);
     else if (p.n_tokens >= 2048 && p.hidden <= 1024) tokens(combine_bwd_token_kernel<64>, 64);

@@ -110,8 +110,8 @@ __device__ __forceinline__ float packed_act(float z) {
 
 // FINE: an output is stored in fp32, and the activation as exact as that shows.
 //
-// 65536 x 4096 bf16: the identity 138 us for 814 MB, 5.9 TB/s, GELU's output 163, 5.0 (its instructions, 21 a value, not all
-// of them behind the loads), and its gradient and output in one pass 342 for 1.89 GB, 5.5.  Four units in flight: with two
+// 65536 x 4096 bf16: the identity 133 us for 814 MB, 6.1 TB/s, GELU's output 160, 5.1 (its instructions, 21 a value, not all
+// of them behind the loads), and its gradient and output in one pass 334 for 1.89 GB, 5.7.  Four units in flight: with two
 // 10 us more for GELU, with eight 5.
 template <int ACT, bool FLAT, bool FINE>
 __global__ __launch_bounds__(256) void unpack_kernel(UnpackParams p, int upr, int64_t all) {

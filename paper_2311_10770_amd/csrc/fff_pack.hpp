@@ -5,7 +5,8 @@
 // The scale of a block is the smallest power of two that brings its largest finite value to
 // at most 448, so no value is cut off; a power of two, since it moves no mantissa bit: what a block holds
 // are e4m3's own roundings (half a step, 2^-4 of a value; below 2^-15 of the block's largest at worst,
-// where e4m3 has no more exponents, 2^-10 of the scale), and every packed value is exact in bf16.
+// where e4m3 has no more exponents, 2^-10 of the scale).  Packed values are exact in fp32, and in bf16 from scale code 3 on:
+// e4m3's smallest value is 2^-9, bf16's 2^-133.
 #pragma once
 
 #include "fff_rows.hpp"

@@ -441,14 +441,19 @@ struct RouteLds {
 // LPT lanes a token (16, 32 or 64), four neighbouring experts a vector, V experts a lane: lanes hold few experts each, in
 // registers, and a wave 64 / LPT tokens.  One lane a pick at least: the largest of each lane's own bound the choice, where
 // there are less than two a pick the largest two (33530 tokens, top 14 of 64 in groups: 45 us with 32 lanes and
-// their largest alone, 16.7 with 16 lanes).  64 lanes keep to the largest alone: their two need registers that spill.
+// their largest alone, 16.7 with 16 lanes).  64 lanes keep to the largest alone: with the two 40 of 64 experts take 38 us
+// for 24 (at five waves a SIMD they spill 16 to 22 registers up to 512 experts) and 8 of 1024 98 for 96, but 40 of 1024
+// 187 for 228.
 //
-// Bound by vector instructions, but for the plain choice by logits: 65536 tokens, top 8 of 256 fp32 (71 MB: 14 us at a
-// copy's rate): by the logits 16.9 us, sigmoid and bias 23.6, softmax and bias 27.6; sigmoid, bias and the best 4 of 8
-// groups 31 (4 of 16: 33), of which the groups are a quarter.  Each pick by a reduction over the lanes, in
-// fp64, cost 1988 there.  One token of 64 experts: 3.0 us, the launch, behind the host's 9.  A wave holds c, by_e
-// and the lists in LDS, 4 to 13 KB: at 1024 experts that leaves 3 workgroups a CU (65536 tokens, bf16: 96 us, 27 at a
-// copy's rate).
+// Bound by vector instructions, which issue in 0.8 to 1.0 of a SIMD's cycles throughout: 65536 tokens, top 8 of 256 fp32
+// (71 MB: 14 us at a copy's rate): by the logits 16.9 us (494 instructions a wave), sigmoid and bias 24 (626), softmax and
+// bias 27.6 (641); sigmoid, bias and the best 4 of 8 groups 31 (4 of 16: 33), of which the groups are a quarter.  Each pick
+// by a reduction over the lanes, in fp64, cost 1988 there.  One token of 64 experts: 3.0 us, the launch, behind the host's
+// 9.  Few experts leave most of a token's lanes without any, at the same instructions: 2 of 8 and 4 of 32 12.4 us (403), for
+// 0.6 and 2.1 at a copy's rate.  A wave of 64 lanes has one token for as many (65536 x 1024 bf16, top 8: 96 us, 729 a wave;
+// 28 at a copy's rate); of its 13 KB of LDS there three workgroups fit a CU.  Five waves a SIMD: at 32 lanes up to
+// 256 experts 13 registers are kept in scratch for them, which costs nothing that shows (24 of 256 with sigmoid and bias
+// 52.6 us, 52.2 at four waves without scratch; 24 of 128 36.4 and 36.4).
 //
 // Choices are first formed in fp32 (c, whose error is below `slack` / 2).  Of the LPT lanes' largest, the
 // top_k-th is no more than the top_k-th largest of all, and the same holds for the largest two of each, so only
@@ -849,7 +854,9 @@ __device__ __forceinline__ float of_expert(int id, float d, int top_k, int first
 // j; what the entries give their experts passes through LDS, summed in the entries' order first, so that no atomics
 // are needed and an expert may be there twice.  Only the plain softmax reads the other experts' logits: else theirs is
 // 0.  65536 x 64 bf16, plain softmax: 8.1 us for 19 MB, 2.3 TB/s, of which the launch and its ends are half
-// (a wave a token that looks through its entries for each expert: 88).
+// (a wave a token that looks through its entries for each expert: 88).  65536 x 256 fp32, top 8: plain softmax 28.7 for
+// 138 MB, 4.8 TB/s; renormalised, and the sigmoid both ways, 24.4 for 73 MB (the chosen logits alone are read, each in a line
+// of its own).  65536 x 8 takes 7.6, x 32 8.1, the instructions of lanes that hold no expert.
 template <int LPT, int V>
 __global__ __launch_bounds__(256) void route_bwd_kernel(RouteBwdParams p, int64_t row0) {
     constexpr int TPW = 64 / LPT, N = V / 4;

@@ -374,7 +374,7 @@ def _unpack_rows(values, packed, act, y, dtype, *, stream=None):
 def unpack_rows(packed, *, act="identity", y=None, dtype=torch.bfloat16, stream=None):
     """``act`` of the rows that ``packed`` holds, through ``fff_unpack_rows``; returns y (allocated of ``dtype``).
 
-    With the identity the packed values themselves, exact in bfloat16 and float32: an input of
+    With the identity the packed values themselves, exact in float32 (in bfloat16 for scales of 2^-124 and more): an input of
     ``grouped_weight_grad``.  With "gelu" or "gelu_tanh" the activation of a packed pre-activation."""
     try:
         values = packed[0]
