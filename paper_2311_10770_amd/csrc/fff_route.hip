@@ -23,7 +23,7 @@ constexpr float NONE = -__builtin_inff();
 
 // A sigmoid times exp(-shift), for shift = 0 or the largest of a token's chosen logits where that is below 0: the common factor
 // cancels from their shares, which so keep their bits where the sigmoids themselves leave fp32 (1 / (1 + exp(-l)) is 0 from
-// -88.8 on; its share beside one at -19 is 1e-30).  No step overflows.
+// -88.8 on; its share beside one at -19 is 1e-30).  No step overflows: of -l it is 1 - s down to fp32's smallest step.
 __device__ __forceinline__ float sigmoid_part(float l, float shift) {
     return expf(__builtin_fminf(l, 0.0f) - shift) / (1.0f + expf(-__builtin_fabsf(l)));
 }
@@ -919,7 +919,7 @@ __global__ __launch_bounds__(256) void route_bwd_kernel(RouteBwdParams p, int64_
     // this entry's share of d; all: what the softmax takes from every expert's
     float s = sigmoid ? sigmoid_part(lg, p.renormalise ? __builtin_fminf(most, 0.0f) : 0.0f) : expf(lg - most), all = 0.0f;
     s = id < 0 ? 0.0f : s;
-    const float rest = sigmoid ? 1.0f / (1.0f + expf(lg)) : 1.0f;  // 1 - s
+    const float rest = sigmoid ? sigmoid_part(-lg, 0.0f) : 1.0f;  // 1 - s
     if (p.renormalise) {
         const float total = group_sum<LPT>(s);
         s = id < 0 ? 0.0f : s / total;
@@ -1010,8 +1010,8 @@ __global__ __launch_bounds__(256) void route_bwd_any_kernel(RouteBwdParams p) {
             const float v = at(e);
             if (v > NONE) {
                 if (sigmoid) {
-                    const float rest = 1.0f / (1.0f + expf(v));  // 1 - s
-                    g = own == 0.0f ? 0.0f : p.renormalise ? own * rest : own * (1.0f / (1.0f + expf(-v))) * rest;
+                    const float rest = sigmoid_part(-v, 0.0f);  // 1 - s
+                    g = own == 0.0f ? 0.0f : p.renormalise ? own * rest : own * sigmoid_part(v, 0.0f) * rest;
                 } else {
                     g = p.renormalise ? own : expf(v - most) / sum * (own - all);
                 }

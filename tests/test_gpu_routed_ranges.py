@@ -190,3 +190,24 @@ def test_combine_gradient_past_four_billion_elements(fff_lib, k, H):
     terms = d[:, None] * tail.double().view(3, k, H)
     ops_ref.check(dw[-3:], terms.sum(2).cpu(), ((H + 4) * ops_ref.U * terms.abs().sum(2)).cpu(), "dweights")
     assert (drows[:4] == 0).all() and (dw[:4] == 0).all()
+
+
+@pytest.mark.parametrize("E", [5, 100, 600, 2000])
+@pytest.mark.parametrize("renormalise", [False, True])
+def test_route_gradient_of_saturated_sigmoids(fff_lib, E, renormalise):
+    """1 - s of logits whose exponential leaves fp32: large gradients of the weights make normal numbers of it."""
+    logits = torch.full((6, E), -1e4, device=DEV)
+    logits[:, 3] = torch.tensor([80.0, 87.0, 88.5, 89.0, 90.0, 92.0], device=DEV)
+    logits[:, 1] = logits[:, 3] - 1
+    ids = torch.tensor([[3, 1]] * 6, dtype=torch.int32, device=DEV)
+    dw = torch.tensor([[1.0, -1.0]] * 6, device=DEV)
+    flush_print(f"[gpu] gradient of saturated sigmoids {E} renormalise={renormalise}")
+    got = fff_lib.route_backward(dw, logits, ids, score="sigmoid", renormalise=renormalise, scale=1e9)
+    want, err = ref.route_backward(dw, logits, ids, score="sigmoid", renormalise=renormalise, scale=1e9)
+    # 1 - s is off by its own roundings, which the references' bounds count relative to it, and by two halves of fp32's
+    # smallest step, 2^-149, where it has fewer bits: a factor of what the weights' gradients come to, 1e9 at most
+    if not renormalise:
+        err = err - ref.TINY * 1e9 * (want != 0)
+        assert (err >= 0).all()
+    ops_ref.check(got, want, err + 1e9 * 2.0 ** -149 * (want != 0), f"{E}")
+    assert (got[:, [1, 3]] != 0).all()
